@@ -387,6 +387,121 @@ int flexmoe_layer_forward_bucketed(const flexmoe_layer_desc *desc, int32_t T, co
                                    void *y, void *workspace, size_t workspace_bytes,
                                    const flexmoe_route_out *dbg, void *stream);
 
+/* ---- The experts' products for training ----------------------------------
+ * Matrix products over ragged groups of rows, one weight matrix W_e [N][K] per
+ * group (expert), with both gradients:
+ *   forward       y_r[n]   = sum_k x_r[k] W_e[n][k]
+ *   input grad    dx_r[k]  = sum_n dy_r[n] W_e[n][k]
+ *   weight grad   dW_e[n][k] (+)= sum_r dy_r[n] x_r[k]
+ * for the rows r in [offsets[e], offsets[e + 1]) of group e.  Any group may be
+ * empty: its dW_e is 0 (or unchanged when added to).
+ *   x, dx [R][ldx], y, dy [R][ldy] (dtype), w [groups][N][ldw] (dtype),
+ *   dw [groups][N][lddw] (dw_dtype), offsets [groups + 1] int32 on the device,
+ *   ascending, within [0, R]; rows outside [offsets[0], offsets[groups]) are
+ *   neither read nor written.
+ * keep [groups] int32 (device; with keep_axis other than FLEXMOE_KEEP_NONE,
+ * NULL otherwise) limits W_e to its first k_e rows (FLEXMOE_KEEP_N, as gate and
+ * up) or columns (FLEXMOE_KEEP_K, as down): what lies past it is read into no
+ * sum, whatever it holds, and is written as zeros in y, dx and dW (left as it
+ * is when dW is added to).  Counts are clamped to [0, N] or [0, K].
+ * Arithmetic: products and sums in fp32 (bf16 products are exact there),
+ * rounded once to the output's type; added gradients are rounded after each
+ * call.  Deterministic.
+ * Shapes (FLEXMOE_ESHAPE otherwise): 1 <= groups <= 256; N and K from 1 to 2^21,
+ * multiples of nothing; row strides (elements, 0 = packed) at least the row's
+ * length, at most 2^21 and whole 16-byte units; 0 <= R <= max_rows <= 2^30.
+ * Matrices start on 16-byte boundaries, and a row may be read up to the 16-byte
+ * unit that its last element lies in; no element past the row is written.
+ * Workspace: flexmoe_grouped_workspace_bytes(desc, R), 256-byte aligned; one
+ * sized for max_rows serves every smaller R and all three products.  R = 0 is a
+ * no-op for forward and input grad; weight grad writes its zeros. */
+enum { FLEXMOE_KEEP_NONE = 0, FLEXMOE_KEEP_N = 1, FLEXMOE_KEEP_K = 2 };
+typedef struct flexmoe_grouped_desc {
+    int32_t groups;
+    int32_t N, K;
+    int32_t dtype;      /* flexmoe_dtype of x, w, y, dy and dx (int8: of y)      */
+    int32_t dw_dtype;   /* flexmoe_dtype of dw                                   */
+    int32_t keep_axis;  /* FLEXMOE_KEEP_*                                        */
+    int32_t max_rows;
+    int32_t ldx, ldw, ldy, lddw;
+} flexmoe_grouped_desc;
+size_t flexmoe_grouped_workspace_bytes(const flexmoe_grouped_desc *desc, int32_t R);
+int flexmoe_grouped_forward(const flexmoe_grouped_desc *desc, int32_t R, const void *x,
+                            const void *w, const int32_t *offsets, const int32_t *keep, void *y,
+                            void *workspace, size_t workspace_bytes, void *stream);
+int flexmoe_grouped_input_grad(const flexmoe_grouped_desc *desc, int32_t R, const void *dy,
+                               const void *w, const int32_t *offsets, const int32_t *keep, void *dx,
+                               void *workspace, size_t workspace_bytes, void *stream);
+int flexmoe_grouped_weight_grad(const flexmoe_grouped_desc *desc, int32_t R, const void *dy,
+                                const void *x, const int32_t *offsets, const int32_t *keep, void *dw,
+                                int32_t accumulate, void *workspace, size_t workspace_bytes,
+                                void *stream);
+
+/* ---- Products in 8-bit integers ------------------------------------------
+ * flexmoe_quantize_rows: row r of v [rows][cols] as whole numbers
+ *   q_r = round(v_r * (127 / m)), ties to even, and scale[r] = m / 127 for m =
+ *   max |v_r|; v = x, or silu(x_gate) * x with x_gate (NULL otherwise; same
+ *   shape, stride and type).  A row of zeros has scale 0; a row with a NaN or an
+ *   infinity has the scale NaN and zeros.  x [rows][ldx] (dtype; rows of
+ *   whole 16-byte units), q [rows][ldq] int8 (ldq a multiple of 16; up to 7 values past the
+ *   row are written as 0, inside its stride), strides of 0 = packed.  The rows
+ *   of a weight matrix give its channels' scales.
+ * flexmoe_quantized_forward: y_r[n] = q_scale[r] w_scale[e][n] sum_k q_r[k] W_e[n][k],
+ *   the sum exact in 32-bit integers (K <= 131071).  q [R][ldx] and
+ *   w [groups][N][ldw] int8, w_scale [groups][N]; y [R][ldy] of desc->dtype.
+ *   Groups, offsets, keep, strides, errors and workspace
+ *   (flexmoe_quantized_workspace_bytes) as above; one group is a plain product. */
+int flexmoe_quantize_rows(int32_t rows, int32_t cols, int32_t dtype, const void *x,
+                          const void *x_gate, int64_t ldx, void *q, int64_t ldq, float *scale,
+                          void *stream);
+size_t flexmoe_quantized_workspace_bytes(const flexmoe_grouped_desc *desc, int32_t R);
+int flexmoe_quantized_forward(const flexmoe_grouped_desc *desc, int32_t R, const void *q,
+                         const float *q_scale, const void *w, const float *w_scale,
+                         const int32_t *offsets, const int32_t *keep, void *y, void *workspace,
+                         size_t workspace_bytes, void *stream);
+
+/* ---- AdamW ----------------------------------------------------------------
+ * One step over `count` tensors (a host array, read before the call returns):
+ *   g = grad * grad_scale
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay)
+ *       - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
+ * in fp32.  param is read, stepped and rounded (to nearest even); a tensor with
+ * a master copy (fp32, bf16 parameters only) is stepped there and param gets
+ * its rounded value.
+ * state_bits 32: m, v [n] fp32, scales NULL.  state_bits 8: m, v [n] bytes and
+ * m_scale, v_scale [ceil(n / 256)] fp32, one for each 256 consecutive values;
+ * all zeros at the start.  m's byte: sign bit and k = 0 .. 127, which stands for
+ * m_scale times 0 (k = 0) or the float with the bits (896 + k) << 20; v's byte k
+ * stands for (k v_scale)^2.  Both are rounded up or down at random so that
+ * their mean is kept (a v above 0 never becomes 0), from bits that depend on
+ * seed, step, the tensor's place in the list and the value's index alone: the
+ * same call gives the same bits.  A block that gets a NaN or an infinity stands
+ * for NaN from then on.  flexmoe_adamw_read_state writes what 8-bit states of
+ * one tensor stand for as dtype (checkpoints, inspection).
+ * Any n >= 0 and any alignment to the elements (16-byte alignment is fastest;
+ * scales, fp32 arrays: 4 bytes).  step >= 1, betas in [0, 1), eps >= 1e-30. */
+typedef struct flexmoe_adamw_tensor {
+    void *param;        /* param_dtype                                           */
+    const void *grad;   /* grad_dtype                                            */
+    void *m, *v;
+    float *m_scale, *v_scale;
+    float *master;      /* fp32 copy of a bf16 parameter, or NULL                */
+    int64_t n;
+} flexmoe_adamw_tensor;
+typedef struct flexmoe_adamw_desc {
+    int32_t param_dtype, grad_dtype;  /* flexmoe_dtype                           */
+    int32_t state_bits;               /* 8 or 32                                 */
+    uint32_t seed;
+    int64_t step;                     /* 1 for the first step                    */
+    double lr, beta1, beta2, eps, weight_decay, grad_scale;
+} flexmoe_adamw_desc;
+int flexmoe_adamw_step(const flexmoe_adamw_desc *desc, const flexmoe_adamw_tensor *tensors,
+                       int32_t count, void *stream);
+int flexmoe_adamw_read_state(int64_t n, const void *m, const void *v, const float *m_scale,
+                             const float *v_scale, int32_t dtype, void *m_out, void *v_out,
+                             void *stream);
+
 /* k = ceil(r * I) for a retention ratio r in [0, 1] (Sec. 3.1).  A slack of
  * 1e-9 absorbs the binary representation error of decimal ratios (0.7 * 1000
  * gives 700).  Returns -1 for r outside [0, 1], NaN, or I < 1. */

@@ -10,8 +10,6 @@
 // reads routing results back: tile counts live on the device and the routed
 // GEMM grids are sized by an upper bound computed from (T, E, I); surplus
 // workgroups exit at once.
-#include <stdarg.h>
-#include <stdio.h>
 #include <string.h>
 
 #include <algorithm>
@@ -19,6 +17,7 @@
 #include <mutex>
 #include <vector>
 
+#include "error.h"
 #include "flexmoe.h"
 #include "kernels.h"
 #include "saliency.h"
@@ -27,20 +26,6 @@
 using namespace flexmoe;
 
 namespace {
-
-thread_local char g_err[512] = "";
-
-int fail(int code, const char* fmt, ...) {
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(g_err, sizeof g_err, fmt, ap);
-    va_end(ap);
-    return code;
-}
-
-int hip_fail(hipError_t e, const char* what) {
-    return fail(FLEXMOE_EHIP, "%s: %s", what, hipGetErrorString(e));
-}
 
 size_t align256(size_t b) { return (b + 255) & ~size_t(255); }
 

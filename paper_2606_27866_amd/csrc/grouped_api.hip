@@ -1,0 +1,197 @@
+// Host side of the experts' products (include/flexmoe.h): argument checks, the
+// choice of kernel and of the parts of the reduction, launches.
+#include <algorithm>
+
+#include "error.h"
+#include "flexmoe.h"
+#include "grouped.h"
+
+using namespace flexmoe;
+
+namespace {
+
+constexpr long long kMaxStride = 1 << 21;  // elements: a tile's rows stay below 2^31 bytes apart
+constexpr int kMaxInt8Depth = 131071;      // 128 * 128 * K stays below 2^31
+
+bool misaligned(const void* p, uintptr_t mask) { return ((uintptr_t)p & mask) != 0; }
+
+int elem_bytes(int dtype) { return dtype == FLEXMOE_BF16 ? 2 : 4; }
+
+// D's strides with 0 replaced by the packed ones.
+struct Strides {
+    long long x, w, y, dw;
+};
+
+int check(const flexmoe_grouped_desc* D, bool int8, const char* who, Strides* st) {
+    if (!D) return fail(FLEXMOE_EINVAL, "%s: desc is NULL", who);
+    for (int dt : {D->dtype, D->dw_dtype})
+        if (dt != FLEXMOE_F32 && dt != FLEXMOE_BF16)
+            return fail(FLEXMOE_EDTYPE, "%s: dtype %d is neither FLEXMOE_F32 nor FLEXMOE_BF16", who, dt);
+    if (D->groups < 1 || D->groups > kMaxExperts)
+        return fail(FLEXMOE_ESHAPE, "%s: groups = %d outside [1, %d]", who, D->groups, kMaxExperts);
+    if (D->N < 1 || D->K < 1 || D->N > kMaxStride || D->K > kMaxStride)
+        return fail(FLEXMOE_ESHAPE, "%s: N = %d, K = %d outside [1, 2^21]", who, D->N, D->K);
+    if (int8 && D->K > kMaxInt8Depth) return fail(FLEXMOE_ESHAPE, "%s: K = %d above %d", who, D->K, kMaxInt8Depth);
+    if (D->keep_axis < FLEXMOE_KEEP_NONE || D->keep_axis > FLEXMOE_KEEP_K)
+        return fail(FLEXMOE_EINVAL, "%s: keep_axis = %d outside [0, 2]", who, D->keep_axis);
+    if (D->max_rows < 0 || D->max_rows > (1 << 30)) return fail(FLEXMOE_ESHAPE, "%s: max_rows = %d outside [0, 2^30]", who, D->max_rows);
+    const int ein = int8 ? 16 : 16 / elem_bytes(D->dtype), eout = 16 / elem_bytes(D->dtype), edw = 16 / elem_bytes(D->dw_dtype);
+    *st = Strides{D->ldx ? D->ldx : D->K, D->ldw ? D->ldw : D->K, D->ldy ? D->ldy : D->N, D->lddw ? D->lddw : D->K};
+    const struct { long long ld, least; int unit; const char* name; } all[] = {
+        {st->x, D->K, ein, "ldx"}, {st->w, D->K, ein, "ldw"}, {st->y, D->N, eout, "ldy"}, {st->dw, D->K, edw, "lddw"}};
+    for (const auto& s : all) {
+        if (int8 && s.name[2] == 'd') continue;
+        if (s.ld < s.least || s.ld > kMaxStride || s.ld % s.unit)
+            return fail(FLEXMOE_ESHAPE, "%s: %s = %lld must be a multiple of %d in [%lld, 2^21]", who, s.name, s.ld, s.unit, s.least);
+    }
+    return FLEXMOE_OK;
+}
+
+int check_rows(const flexmoe_grouped_desc* D, int R, const char* who) {
+    if (R < 0) return fail(FLEXMOE_EINVAL, "%s: R = %d is negative", who, R);
+    if (R > D->max_rows) return fail(FLEXMOE_ESHAPE, "%s: R = %d above max_rows = %d", who, R, D->max_rows);
+    return FLEXMOE_OK;
+}
+
+// Row tiles of `bm` rows over all groups at most: sum ceil(n_e / bm) <=
+// ceil(R / bm) + E - 1, and every tile holds a row.
+long long row_tiles_bound(int R, int E, int bm) { return std::min<long long>((long long)(R + bm - 1) / bm + E - 1, R); }
+
+struct Plan {
+    GroupedForm form;
+    GroupedElem elem;
+    int splits;
+    size_t workspace;
+};
+
+Plan plan(const flexmoe_grouped_desc& D, GroupedForm form, bool int8, int R) {
+    Plan pl{form, int8 ? kElemI8 : D.dtype == FLEXMOE_BF16 ? kElemBf16 : kElemF32, 1, 0};
+    (void)R;
+    return pl;
+}
+
+int launch(const flexmoe_grouped_desc* D, const Strides& st, GroupedForm form, bool int8, int R, const void* a, const void* b, void* c,
+           const float* sa, const float* sb, const int32_t* offsets, const int32_t* keep, int accumulate, void* ws, size_t ws_bytes,
+           hipStream_t s, const char* who) {
+    int rc = check_rows(D, R, who);
+    if (rc) return rc;
+    if (R == 0 && form != kWeightGrad) return FLEXMOE_OK;
+    if ((R > 0 && (!a || !b)) || !c || !offsets) return fail(FLEXMOE_EINVAL, "%s: a pointer is NULL", who);
+    if ((D->keep_axis != FLEXMOE_KEEP_NONE) != (keep != nullptr))
+        return fail(FLEXMOE_EINVAL, "%s: keep goes with keep_axis (%d)", who, D->keep_axis);
+    if (misaligned(a, 15) || misaligned(b, 15) || misaligned(c, 15)) return fail(FLEXMOE_EINVAL, "%s: matrices must be 16-byte aligned", who);
+    if (misaligned(offsets, 3) || misaligned(keep, 3) || misaligned(sa, 3) || misaligned(sb, 3))
+        return fail(FLEXMOE_EINVAL, "%s: offsets, keep and scales must be 4-byte aligned", who);
+    const Plan pl = plan(*D, form, int8, R);
+    if (pl.workspace) {
+        if (!ws || ws_bytes < pl.workspace) return fail(FLEXMOE_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, ws ? ws_bytes : 0, pl.workspace);
+        if (misaligned(ws, 255)) return fail(FLEXMOE_EWORKSPACE, "%s: workspace must be 256-byte aligned", who);
+    }
+    GroupedParams p{};
+    p.a = a, p.b = b, p.c = c, p.sa = sa, p.sb = sb, p.offsets = offsets, p.keep = keep, p.partial = ws;
+    p.E = D->groups, p.R = R, p.N = D->N, p.K = D->K, p.keep_axis = D->keep_axis;
+    p.splits = pl.splits, p.accumulate = accumulate;
+    p.out_bf16 = (form == kWeightGrad ? D->dw_dtype : D->dtype) == FLEXMOE_BF16;
+    if (form == kForward) p.lda = st.x, p.ldb = st.w, p.ldc = st.y;
+    else if (form == kInputGrad) p.lda = st.y, p.ldb = st.w, p.ldc = st.x;
+    else p.lda = st.y, p.ldb = st.x, p.ldc = st.dw;
+    const int cols = form == kForward ? D->N : D->K;
+    p.tiles_c = ceil_div(cols, kGroupTile);
+    p.tiles_r = ceil_div(D->N, kGroupTile);
+    const long long row_tiles = form == kWeightGrad ? (long long)D->groups * p.tiles_r : row_tiles_bound(R, D->groups, kGroupTile);
+    const long long tiles = row_tiles * p.tiles_c * p.splits;
+    if (tiles > (1LL << 30)) return fail(FLEXMOE_ESHAPE, "%s: %lld tiles are too many for one launch", who, tiles);
+    hipError_t err = launch_grouped_mid(p, form, pl.elem, tiles, s);
+    if (err == hipSuccess && p.splits > 1) err = launch_grouped_join(p, form, pl.elem, s);
+    if (err != hipSuccess) return hip_fail(err, who);
+    return FLEXMOE_OK;
+}
+
+size_t workspace_bytes(const flexmoe_grouped_desc* D, int R, bool int8, const char* who) {
+    Strides st;
+    if (check(D, int8, who, &st) || check_rows(D, R, who)) return 0;
+    size_t most = 256;  // 0 stands for an error
+    // what fewer rows need may be more: their reductions are split further
+    for (int form = kForward; form <= (int8 ? kForward : kWeightGrad); ++form)
+        for (int r = R; r > 0; r = r > 64 ? r * 15 / 16 : r - 1) most = std::max(most, plan(*D, (GroupedForm)form, int8, r).workspace);
+    return most;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t flexmoe_grouped_workspace_bytes(const flexmoe_grouped_desc* desc, int32_t R) {
+    return workspace_bytes(desc, R, false, "grouped_workspace_bytes");
+}
+
+int flexmoe_grouped_forward(const flexmoe_grouped_desc* desc, int32_t R, const void* x, const void* w, const int32_t* offsets,
+                            const int32_t* keep, void* y, void* workspace, size_t workspace_bytes, void* stream) {
+    Strides st;
+    const int rc = check(desc, false, "grouped_forward", &st);
+    return rc ? rc
+              : launch(desc, st, kForward, false, R, x, w, y, nullptr, nullptr, offsets, keep, 0, workspace, workspace_bytes,
+                       (hipStream_t)stream, "grouped_forward");
+}
+
+int flexmoe_grouped_input_grad(const flexmoe_grouped_desc* desc, int32_t R, const void* dy, const void* w, const int32_t* offsets,
+                               const int32_t* keep, void* dx, void* workspace, size_t workspace_bytes, void* stream) {
+    Strides st;
+    const int rc = check(desc, false, "grouped_input_grad", &st);
+    return rc ? rc
+              : launch(desc, st, kInputGrad, false, R, dy, w, dx, nullptr, nullptr, offsets, keep, 0, workspace, workspace_bytes,
+                       (hipStream_t)stream, "grouped_input_grad");
+}
+
+int flexmoe_grouped_weight_grad(const flexmoe_grouped_desc* desc, int32_t R, const void* dy, const void* x, const int32_t* offsets,
+                                const int32_t* keep, void* dw, int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream) {
+    Strides st;
+    const int rc = check(desc, false, "grouped_weight_grad", &st);
+    if (rc) return rc;
+    if (accumulate != 0 && accumulate != 1) return fail(FLEXMOE_EINVAL, "grouped_weight_grad: accumulate = %d must be 0 or 1", accumulate);
+    return launch(desc, st, kWeightGrad, false, R, dy, x, dw, nullptr, nullptr, offsets, keep, accumulate, workspace, workspace_bytes,
+                  (hipStream_t)stream, "grouped_weight_grad");
+}
+
+int flexmoe_quantize_rows(int32_t rows, int32_t cols, int32_t dtype, const void* x, const void* x_gate, int64_t ldx, void* q, int64_t ldq,
+                          float* scale, void* stream) {
+    const char* who = "quantize_rows";
+    if (dtype != FLEXMOE_F32 && dtype != FLEXMOE_BF16)
+        return fail(FLEXMOE_EDTYPE, "%s: dtype %d is neither FLEXMOE_F32 nor FLEXMOE_BF16", who, dtype);
+    if (rows < 0) return fail(FLEXMOE_EINVAL, "%s: rows = %d is negative", who, rows);
+    if (cols < 1 || cols > kMaxStride) return fail(FLEXMOE_ESHAPE, "%s: cols = %d outside [1, 2^21]", who, cols);
+    const int unit = 16 / elem_bytes(dtype);
+    if (!ldx) ldx = cols;
+    if (!ldq) ldq = cols;
+    if (ldx < cols || ldx > kMaxStride || ldx % unit)
+        return fail(FLEXMOE_ESHAPE, "%s: ldx = %lld must be a multiple of %d in [%d, 2^21]", who, (long long)ldx, unit, cols);
+    if (ldq < cols || ldq > kMaxStride || ldq % 16)
+        return fail(FLEXMOE_ESHAPE, "%s: ldq = %lld must be a multiple of 16 in [%d, 2^21]", who, (long long)ldq, cols);
+    if (rows == 0) return FLEXMOE_OK;
+    if (!x || !q || !scale) return fail(FLEXMOE_EINVAL, "%s: a pointer is NULL", who);
+    if (misaligned(x, 15) || misaligned(x_gate, 15) || misaligned(q, 15) || misaligned(scale, 3))
+        return fail(FLEXMOE_EINVAL, "%s: matrices must be 16-byte aligned, scales 4-byte", who);
+    const hipError_t err = x_gate ? launch_quantize_rows(x_gate, x, (size_t)ldx, (int8_t*)q, (size_t)ldq, scale, rows, cols,
+                                                         dtype == FLEXMOE_BF16, (hipStream_t)stream)
+                                  : launch_quantize_rows(x, nullptr, (size_t)ldx, (int8_t*)q, (size_t)ldq, scale, rows, cols,
+                                                         dtype == FLEXMOE_BF16, (hipStream_t)stream);
+    if (err != hipSuccess) return hip_fail(err, who);
+    return FLEXMOE_OK;
+}
+
+size_t flexmoe_quantized_workspace_bytes(const flexmoe_grouped_desc* desc, int32_t R) {
+    return workspace_bytes(desc, R, true, "quantized_workspace_bytes");
+}
+
+int flexmoe_quantized_forward(const flexmoe_grouped_desc* desc, int32_t R, const void* q, const float* q_scale, const void* w,
+                         const float* w_scale, const int32_t* offsets, const int32_t* keep, void* y, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+    Strides st;
+    const int rc = check(desc, true, "quantized_forward", &st);
+    if (rc) return rc;
+    if (R > 0 && (!q_scale || !w_scale)) return fail(FLEXMOE_EINVAL, "quantized_forward: a scale pointer is NULL");
+    return launch(desc, st, kForward, true, R, q, w, y, q_scale, w_scale, offsets, keep, 0, workspace, workspace_bytes, (hipStream_t)stream,
+                  "quantized_forward");
+}
+
+}  // extern "C"

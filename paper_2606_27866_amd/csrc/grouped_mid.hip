@@ -1,0 +1,308 @@
+// Grouped products on 128 x 128 tiles (gfx950): every form and element type.
+//
+// A workgroup of 4 waves (2 x 2, each up to 64 x 64 of C as 16 x 16 MFMA
+// accumulators) multiplies K tiles of 128 bytes depth.  Operands go from
+// memory to LDS by buffer_load ... lds, 16 KB per operand and K tile, A one K
+// tile ahead in two stages and B two ahead in three: 80 KB, so that two
+// workgroups share a compute unit and one's MFMAs cover the other's waits.  An
+// operand that is contiguous in the reduction is laid out as 128 rows of 128
+// bytes, one that is not as K-tile rows of 128 values, which the fragment
+// reads transpose (across_frag).
+//
+// What lies outside a group, a width or a matrix reads as zeros: whole rows
+// and 16-byte chunks by offsets past the descriptor, the elements of a chunk
+// that straddles the end of the reduction by clearing both fragments, C's
+// rows and columns past the width at the store.
+#include <algorithm>
+
+#include "grouped.h"
+
+namespace flexmoe {
+
+namespace {
+using namespace mfma;
+
+constexpr int GT = 256;                   // threads
+constexpr int STAGE = 16384;              // bytes of an operand's K tile
+constexpr int SMEM = 5 * STAGE;           // A0 A1 B0 B1 B2
+constexpr int NI = STAGE / 1024 / 4;      // requests per wave and operand: 4
+
+// Requests of one operand for this lane: instruction i of wave w fills LDS
+// bytes (w * NI + i) * 1024 + lane * 16.
+template <typename E, bool kAcross, int N>
+struct Loader {
+    const char* base;       // first element of the operand's part
+    size_t step;            // bytes a K tile advances (across: 0 in the lane offsets)
+    uint32_t off[N];        // lane offset, kOOB if its row or column does not exist
+    int col[N];             // along: the chunk's first depth inside a K tile
+    size_t ldb;             // across: bytes per depth
+    uint32_t tail;          // across: bytes of the last depth that may be read
+    __amdgpu_buffer_rsrc_t r;
+    int depth;
+
+    // `own`: rows (along) or columns (across) that exist from the tile's first
+    // on; `wave0`: this wave's first instruction
+    __device__ __forceinline__ void init(const void* p, size_t ld, int own, int d, int wave0) {
+        const int lane = threadIdx.x & 63;
+        base = reinterpret_cast<const char*>(p);
+        depth = d;
+        if constexpr (!kAcross) {
+            r = make_rsrc_bytes(base, 0x7ffffff0u);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int row = (wave0 + i) * 8 + lane / CHUNKS, c = swz(row, lane % CHUNKS);
+                col[i] = c * E::kPer;
+                off[i] = row < own ? (uint32_t)((size_t)row * ld * E::kBytes) + c * 16 : kOOB;
+            }
+        } else {
+            constexpr int kChunks = 128 * E::kBytes / 16;  // of an LDS row
+            ldb = ld * E::kBytes;
+            step = ldb * E::kDepth;
+            tail = (uint32_t)((min(own, 128) * E::kBytes + 15) & ~15);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int dep = (wave0 + i) * (64 / kChunks) + lane / kChunks;
+                const int c = across_chunk<E>(dep, lane % kChunks);
+                col[i] = 0;
+                off[i] = c * E::kPer < own ? (uint32_t)(dep * ldb) + c * 16 : kOOB;
+            }
+        }
+    }
+    // K tile kt to `lds` (this wave's first instruction's place); past the end zeros
+    __device__ __forceinline__ void request(int kt, unsigned char* lds) {
+        const int lim = depth - kt * E::kDepth;
+        if constexpr (!kAcross) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) load_lds16(r, col[i] < lim ? off[i] : kOOB, (uint32_t)kt * ROWB, lds + i * 1024);
+        } else {
+            // the descriptor covers the depths that exist
+            const int n = min(lim, E::kDepth);
+            r = make_rsrc_bytes(base + (size_t)kt * step, n > 0 ? (uint32_t)((n - 1) * ldb) + tail : 0u);
+#pragma unroll
+            for (int i = 0; i < N; ++i) load_lds16(r, off[i], 0, lds + i * 1024);
+        }
+    }
+};
+
+// F fragments from own index `first` on, at both K steps.
+template <typename E, bool kAcross, int F>
+__device__ __forceinline__ void read_frags(const unsigned char* tile, int first, typename E::Frag (&f)[2][F]) {
+    const int lane = threadIdx.x & 63;
+    if constexpr (kAcross && E::kBytes == 2) {
+        static_assert(F == 4, "read four at a time");
+        uint32_t addr[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) addr[i] = across_addr<128>(tile, first + i * 16);
+        across_read4<128, 0>(addr, f[0]);
+        across_read4<128, 1>(addr, f[1]);
+    } else {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+                if constexpr (kAcross) f[s][i] = across_frag_f32<128>(tile, first + i * 16, s);
+                else f[s][i] = __builtin_bit_cast(typename E::Frag, lds_frag(tile, first + i * 16 + (lane & 15), s * 4 + (lane >> 4)));
+            }
+    }
+}
+
+template <typename E, int kForm, bool kBf16Out>
+__global__ __launch_bounds__(GT, 2) void grouped_mid_kernel(GroupedParams p) {
+    constexpr bool kAcrossA = kForm == kWeightGrad, kAcrossB = kForm != kForward;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[SMEM];
+    GroupedTile t;
+    if (!grouped_tile<kForm>(p, xcd_tile(8), kGroupTile, kGroupTile, E::kDepth, t)) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int wm = wave >> 1, wn = wave & 1, lr = lane & 15, lc = lane >> 4;
+    const int nr = t.r1 - t.r0, depth = t.d1 - t.d0;
+    typedef typename E::T T;
+    const T *a = reinterpret_cast<const T*>(p.a), *b = reinterpret_cast<const T*>(p.b);
+    int own_a, own_b;
+    if constexpr (kForm == kWeightGrad) {
+        a += (size_t)(t.row0 + t.d0) * p.lda + t.r0;
+        b += (size_t)(t.row0 + t.d0) * p.ldb + t.c0;
+        own_a = nr, own_b = p.K - t.c0;
+    } else {
+        a += (size_t)(t.row0 + t.r0) * p.lda + t.d0;
+        b += (size_t)t.e * p.N * p.ldb;
+        b += kForm == kForward ? (size_t)t.c0 * p.ldb + t.d0 : (size_t)t.d0 * p.ldb + t.c0;
+        own_a = nr, own_b = (kForm == kForward ? p.N : p.K) - t.c0;
+    }
+    const int nk = ceil_div(depth, E::kDepth);
+
+    auto run = [&](auto mf_c) {
+        constexpr int MF = decltype(mf_c)::value;
+        constexpr int NA = kAcrossA ? NI : MF;  // along: 32 * MF rows of A
+        Loader<E, kAcrossA, NA> la;
+        Loader<E, kAcrossB, NI> lb;
+        la.init(a, p.lda, own_a, depth, wave * NA);
+        lb.init(b, p.ldb, own_b, depth, wave * NI);
+        unsigned char* const sa = smem;
+        unsigned char* const sb = smem + 2 * STAGE;
+        auto request_a = [&](int kt, int stage) { la.request(kt, sa + stage * STAGE + wave * (NA * 1024)); };
+        auto request_b = [&](int kt, int stage) { lb.request(kt, sb + stage * STAGE + wave * (NI * 1024)); };
+        typename E::Acc acc[4][MF];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < MF; ++i) acc[j][i] = typename E::Acc{0, 0, 0, 0};
+        request_a(0, 0);
+        request_b(0, 0);
+        request_b(1, 1);
+        int st_b = 0;
+        for (int kt = 0; kt < nk; ++kt) {
+            // tile kt is in when only B of tile kt + 1 is outstanding; this
+            // wave's LDS reads of tile kt - 1 are done, so that its stages may
+            // be refilled after the barrier
+            __builtin_amdgcn_s_waitcnt(waitcnt_vm(NI) & kWaitLgkm0);
+            barrier_no_fence();
+            request_a(kt + 1, (kt + 1) & 1);
+            request_b(kt + 2, st_b == 0 ? 2 : st_b - 1);
+            const unsigned char* at = sa + (kt & 1) * STAGE;
+            const unsigned char* bt = sb + st_b * STAGE;
+            st_b = st_b == 2 ? 0 : st_b + 1;
+            typename E::Frag fa[2][MF], fb[2][4];
+            read_frags<E, kAcrossB, 4>(bt, wn * 64, fb);
+            read_frags<E, kAcrossA, MF>(at, wm * 16 * MF, fa);
+            if constexpr (!kAcrossA)
+                if (kt == nk - 1 && depth % E::kPer) {
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        const int valid = depth - kt * E::kDepth - (s * 4 + lc) * E::kPer;
+#pragma unroll
+                        for (int i = 0; i < MF; ++i) fa[s][i] = head<E>(fa[s][i], valid);
+                        if constexpr (!kAcrossB)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) fb[s][j] = head<E>(fb[s][j], valid);
+                    }
+                }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int i = 0; i < MF; ++i) acc[j][i] = E::mma(fb[s][j], fa[s][i], acc[j][i]);
+        }
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));  // no request may outlive the workgroup's LDS
+
+        // lane -> C row lane % 16 of a fragment, 4 consecutive columns from
+        // 4 * (lane / 16)
+        const int cols = kForm == kForward ? p.N : p.K;
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+            const int r = t.r0 + wm * 16 * MF + i * 16 + lr;
+            if (r >= t.r1) continue;
+            const int clim = r < t.rlim ? t.clim : 0;
+            const size_t crow = kForm == kWeightGrad ? (size_t)t.e * p.N + r : (size_t)t.row0 + r;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int c = t.c0 + wn * 64 + j * 16 + lc * 4;
+                if (c >= cols) continue;
+                if (p.splits > 1) {
+                    const size_t rows = kForm == kWeightGrad ? (size_t)p.E * p.N : (size_t)p.R;
+                    const size_t ldp = (cols + 3) & ~3;
+                    typename E::Acc v = acc[j][i];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = c + k < clim ? v[k] : 0;
+                    *reinterpret_cast<typename E::Acc*>(reinterpret_cast<char*>(p.partial) +
+                                                        ((t.split * rows + crow) * ldp + c) * 4) = v;
+                    continue;
+                }
+                floatx4 v;
+                if constexpr (E::kBytes == 1) {
+                    const float s = p.sa[crow];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        v[k] = c + k < clim ? (float)acc[j][i][k] * (s * p.sb[(size_t)t.e * p.N + c + k]) : 0.f;
+                } else {
+                    v = acc[j][i];
+                }
+                store_run<kBf16Out>(reinterpret_cast<char*>(p.c) + crow * p.ldc * (kBf16Out ? 2 : 4), c, cols, clim, v,
+                                    kForm == kWeightGrad ? p.accumulate : 0);
+            }
+        }
+    };
+    if constexpr (kAcrossA) run(std::integral_constant<int, 4>{});
+    else if (nr > 96) run(std::integral_constant<int, 4>{});
+    else if (nr > 64) run(std::integral_constant<int, 3>{});
+    else if (nr > 32) run(std::integral_constant<int, 2>{});
+    else run(std::integral_constant<int, 1>{});
+}
+
+// The parts of a split reduction added in their order: one thread per run of 4
+// columns of C.
+template <bool kI8, bool kBf16Out, bool kRowGroups>
+__global__ __launch_bounds__(256) void grouped_join_kernel(GroupedParams p, int cols, size_t rows) {
+    const size_t runs = (cols + 3) / 4, ldp = runs * 4;
+    const int first = kRowGroups ? group_begin(p, 0) : 0, end = kRowGroups ? group_begin(p, p.E) : 0;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < rows * runs; i += (size_t)gridDim.x * 256) {
+        const size_t r = i / runs;
+        const int c = (int)(i - r * runs) * 4;
+        if (kRowGroups && ((int)r < first || (int)r >= end)) continue;
+        const char* src = reinterpret_cast<const char*>(p.partial) + (r * ldp + c) * 4;
+        floatx4 v{0.f, 0.f, 0.f, 0.f};
+        if constexpr (kI8) {
+            mfma::intx4 s{0, 0, 0, 0};
+            for (int k = 0; k < p.splits; ++k) s += *reinterpret_cast<const mfma::intx4*>(src + (size_t)k * rows * ldp * 4);
+            int e = 0;  // the group of row r
+            for (int lo = 0, hi = p.E; lo < hi;) {
+                const int m = (lo + hi) / 2;
+                if (group_begin(p, m + 1) <= (int)r) lo = m + 1;
+                else hi = m;
+                e = lo;
+            }
+            e = min(e, p.E - 1);
+            const float sr = p.sa[r];
+            const int clim = p.keep_axis == 1 ? group_width(p, e, p.N) : p.N;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = c + k < clim ? (float)s[k] * (sr * p.sb[(size_t)e * p.N + c + k]) : 0.f;
+        } else {
+            for (int k = 0; k < p.splits; ++k) v += *reinterpret_cast<const floatx4*>(src + (size_t)k * rows * ldp * 4);
+        }
+        store_run<kBf16Out>(reinterpret_cast<char*>(p.c) + r * p.ldc * (kBf16Out ? 2 : 4), c, cols, cols, v,
+                            kRowGroups ? 0 : p.accumulate);
+    }
+}
+
+template <typename E, int kForm>
+void launch_mid(const GroupedParams& p, unsigned grid, hipStream_t s) {
+    if (p.out_bf16) grouped_mid_kernel<E, kForm, true><<<grid, GT, 0, s>>>(p);
+    else grouped_mid_kernel<E, kForm, false><<<grid, GT, 0, s>>>(p);
+}
+
+}  // namespace
+
+hipError_t launch_grouped_mid(const GroupedParams& p, GroupedForm form, GroupedElem elem, long long tiles, hipStream_t s) {
+    if (tiles <= 0) return hipSuccess;
+    const unsigned grid = (unsigned)((tiles + 63) / 64 * 64);
+    if (elem == kElemI8) launch_mid<I8, kForward>(p, grid, s);
+    else if (elem == kElemBf16 && form == kForward) launch_mid<Bf16, kForward>(p, grid, s);
+    else if (elem == kElemBf16 && form == kInputGrad) launch_mid<Bf16, kInputGrad>(p, grid, s);
+    else if (elem == kElemBf16) launch_mid<Bf16, kWeightGrad>(p, grid, s);
+    else if (form == kForward) launch_mid<F32, kForward>(p, grid, s);
+    else if (form == kInputGrad) launch_mid<F32, kInputGrad>(p, grid, s);
+    else launch_mid<F32, kWeightGrad>(p, grid, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_grouped_join(const GroupedParams& p, GroupedForm form, GroupedElem elem, hipStream_t s) {
+    const int cols = form == kForward ? p.N : p.K;
+    const size_t rows = form == kWeightGrad ? (size_t)p.E * p.N : (size_t)p.R;
+    const size_t runs = rows * ((cols + 3) / 4);
+    if (!runs) return hipSuccess;
+    const unsigned grid = (unsigned)std::min<size_t>((runs + 255) / 256, 4096);
+    if (elem == kElemI8) {
+        if (p.out_bf16) grouped_join_kernel<true, true, true><<<grid, 256, 0, s>>>(p, cols, rows);
+        else grouped_join_kernel<true, false, true><<<grid, 256, 0, s>>>(p, cols, rows);
+    } else if (form == kWeightGrad) {
+        if (p.out_bf16) grouped_join_kernel<false, true, false><<<grid, 256, 0, s>>>(p, cols, rows);
+        else grouped_join_kernel<false, false, false><<<grid, 256, 0, s>>>(p, cols, rows);
+    } else {
+        if (p.out_bf16) grouped_join_kernel<false, true, true><<<grid, 256, 0, s>>>(p, cols, rows);
+        else grouped_join_kernel<false, false, true><<<grid, 256, 0, s>>>(p, cols, rows);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace flexmoe

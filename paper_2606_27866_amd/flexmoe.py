@@ -35,13 +35,18 @@ EXPORTED = ("flexmoe_workspace_bytes", "flexmoe_rank_reorder", "flexmoe_set_budg
             "flexmoe_layer_forward_bucketed", "flexmoe_saliency_workspace_bytes",
             "flexmoe_channel_saliency", "flexmoe_transpose_weights", "flexmoe_sample_actions",
             "flexmoe_train_workspace_bytes", "flexmoe_train_forward", "flexmoe_train_backward",
-            "flexmoe_action_grad", "flexmoe_layer_forward_noalloc")
+            "flexmoe_action_grad", "flexmoe_layer_forward_noalloc",
+            "flexmoe_grouped_workspace_bytes", "flexmoe_grouped_forward", "flexmoe_grouped_input_grad",
+            "flexmoe_grouped_weight_grad", "flexmoe_quantize_rows", "flexmoe_quantized_workspace_bytes",
+            "flexmoe_quantized_forward", "flexmoe_adamw_step", "flexmoe_adamw_read_state")
 
 # kernel indices of flexmoe_kernel_times
 KERNELS = ("route", "dispatch_scan", "dispatch_scatter", "gate_up", "down", "combine",
            "gate_up_shared", "down_shared", "sal_transpose", "sal_prep", "sal_dgrad", "sal_wgrad",
            "sal_reduce", "act_dgrad", "act_dx", "act_other")
 MAX_ACTIONS = 16
+KEEP_AXES = {"none": 0, "N": 1, "K": 2}  # FLEXMOE_KEEP_*
+STATE_BLOCK = 256                        # values that share a scale in 8-bit optimizer states
 
 
 class FlexMoEError(RuntimeError):
@@ -57,6 +62,22 @@ class flexmoe_layer_desc(ctypes.Structure):
 
 class flexmoe_kernel_times(ctypes.Structure):
     _fields_ = [("ms", ctypes.c_double * len(KERNELS)), ("launches", ctypes.c_int64 * len(KERNELS))]
+
+
+class flexmoe_grouped_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("groups", "N", "K", "dtype", "dw_dtype", "keep_axis", "max_rows", "ldx", "ldw", "ldy", "lddw")]
+
+
+class flexmoe_adamw_tensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "m", "v", "m_scale", "v_scale", "master")] + \
+               [("n", ctypes.c_int64)]
+
+
+class flexmoe_adamw_desc(ctypes.Structure):
+    _fields_ = [("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("state_bits", ctypes.c_int32),
+                ("seed", ctypes.c_uint32), ("step", ctypes.c_int64)] + \
+               [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay", "grad_scale")]
 
 
 class flexmoe_action_set(ctypes.Structure):
@@ -133,6 +154,24 @@ def lib():
         L.flexmoe_train_backward.restype = ctypes.c_int
         L.flexmoe_action_grad.argtypes = [D, i32, AS, vp, vp, f32, f32, f32, vp, vp, vp, vp, sz, vp]
         L.flexmoe_action_grad.restype = ctypes.c_int
+        G, i64 = ctypes.POINTER(flexmoe_grouped_desc), ctypes.c_int64
+        for name in ("grouped", "quantized"):
+            f = getattr(L, "flexmoe_%s_workspace_bytes" % name)
+            f.argtypes, f.restype = [G, i32], sz
+        L.flexmoe_grouped_forward.argtypes = [G, i32] + [vp] * 6 + [sz, vp]
+        L.flexmoe_grouped_forward.restype = ctypes.c_int
+        L.flexmoe_grouped_input_grad.argtypes = [G, i32] + [vp] * 6 + [sz, vp]
+        L.flexmoe_grouped_input_grad.restype = ctypes.c_int
+        L.flexmoe_grouped_weight_grad.argtypes = [G, i32] + [vp] * 5 + [i32, vp, sz, vp]
+        L.flexmoe_grouped_weight_grad.restype = ctypes.c_int
+        L.flexmoe_quantize_rows.argtypes = [i32, i32, i32, vp, vp, i64, vp, i64, vp, vp]
+        L.flexmoe_quantize_rows.restype = ctypes.c_int
+        L.flexmoe_quantized_forward.argtypes = [G, i32] + [vp] * 8 + [sz, vp]
+        L.flexmoe_quantized_forward.restype = ctypes.c_int
+        L.flexmoe_adamw_step.argtypes = [ctypes.POINTER(flexmoe_adamw_desc), vp, i32, vp]
+        L.flexmoe_adamw_step.restype = ctypes.c_int
+        L.flexmoe_adamw_read_state.argtypes = [i64] + [vp] * 4 + [i32] + [vp] * 3
+        L.flexmoe_adamw_read_state.restype = ctypes.c_int
         L.flexmoe_keep_from_ratio.argtypes = [ctypes.c_double, i32]
         L.flexmoe_keep_from_ratio.restype = ctypes.c_int
         L.flexmoe_timing_enable.argtypes = [ctypes.c_int]
@@ -343,6 +382,328 @@ def flexmoe_action_grad(desc, T, actions, alpha, gumbel, tau, lambda_cost, beta,
                                      float(tau), float(lambda_cost), float(beta), _p(dmask), _p(dalpha),
                                      _p(stats), _p(workspace), _nbytes(workspace, workspace_bytes),
                                      _stream(stream)))
+
+
+# ---- the experts' products, 8-bit products, AdamW ---------------------------
+def make_grouped_desc(groups, N, K, dtype=FLEXMOE_BF16, dw_dtype=FLEXMOE_F32, keep_axis="none", max_rows=0, ldx=0, ldw=0,
+                      ldy=0, lddw=0):
+    return flexmoe_grouped_desc(groups, N, K, dtype, dw_dtype, KEEP_AXES[keep_axis], max_rows, ldx, ldw, ldy, lddw)
+
+
+def flexmoe_grouped_workspace_bytes(desc, R: int) -> int:
+    n = lib().flexmoe_grouped_workspace_bytes(ctypes.byref(desc), int(R))
+    if n == 0:
+        raise FlexMoEError(-2, flexmoe_last_error())
+    return int(n)
+
+
+def flexmoe_grouped_forward(desc, R, x, w, offsets, keep, y, workspace, workspace_bytes=None, stream=None):
+    _check(lib().flexmoe_grouped_forward(ctypes.byref(desc), int(R), _p(x), _p(w), _p(offsets), _p(keep), _p(y),
+                                         _p(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)))
+
+
+def flexmoe_grouped_input_grad(desc, R, dy, w, offsets, keep, dx, workspace, workspace_bytes=None, stream=None):
+    _check(lib().flexmoe_grouped_input_grad(ctypes.byref(desc), int(R), _p(dy), _p(w), _p(offsets), _p(keep), _p(dx),
+                                            _p(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)))
+
+
+def flexmoe_grouped_weight_grad(desc, R, dy, x, offsets, keep, dw, accumulate, workspace, workspace_bytes=None,
+                                stream=None):
+    _check(lib().flexmoe_grouped_weight_grad(ctypes.byref(desc), int(R), _p(dy), _p(x), _p(offsets), _p(keep), _p(dw),
+                                             int(accumulate), _p(workspace), _nbytes(workspace, workspace_bytes),
+                                             _stream(stream)))
+
+
+def flexmoe_quantize_rows(rows, cols, dtype, x, x_gate, ldx, q, ldq, scale, stream=None):
+    _check(lib().flexmoe_quantize_rows(int(rows), int(cols), int(dtype), _p(x), _p(x_gate), int(ldx), _p(q), int(ldq),
+                                       _p(scale), _stream(stream)))
+
+
+def flexmoe_quantized_workspace_bytes(desc, R: int) -> int:
+    n = lib().flexmoe_quantized_workspace_bytes(ctypes.byref(desc), int(R))
+    if n == 0:
+        raise FlexMoEError(-2, flexmoe_last_error())
+    return int(n)
+
+
+def flexmoe_quantized_forward(desc, R, q, q_scale, w, w_scale, offsets, keep, y, workspace, workspace_bytes=None, stream=None):
+    _check(lib().flexmoe_quantized_forward(ctypes.byref(desc), int(R), _p(q), _p(q_scale), _p(w), _p(w_scale), _p(offsets),
+                                           _p(keep), _p(y), _p(workspace), _nbytes(workspace, workspace_bytes),
+                                           _stream(stream)))
+
+
+def flexmoe_adamw_step(desc, tensors, count=None, stream=None):
+    """tensors: a ctypes array of flexmoe_adamw_tensor, or the address of one with `count` entries."""
+    if count is None:
+        count = len(tensors)
+    _check(lib().flexmoe_adamw_step(ctypes.byref(desc), tensors if isinstance(tensors, int) else ctypes.addressof(tensors),
+                                    int(count), _stream(stream)))
+
+
+def flexmoe_adamw_read_state(n, m, v, m_scale, v_scale, dtype, m_out, v_out, stream=None):
+    _check(lib().flexmoe_adamw_read_state(int(n), _p(m), _p(v), _p(m_scale), _p(v_scale), int(dtype), _p(m_out), _p(v_out),
+                                          _stream(stream)))
+
+
+def _dtype_code(dtype) -> int:
+    import torch
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("dtype must be torch.bfloat16 or torch.float32, got %s" % dtype)
+    return FLEXMOE_BF16 if dtype == torch.bfloat16 else FLEXMOE_F32
+
+
+def _matrix(t, shape, dtype, name):
+    """Row stride of a [rows, cols] or [groups, rows, cols] tensor whose rows are contiguous."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be %s %s, got %s %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+    if not t.is_cuda:
+        raise ValueError("%s must be on the GPU" % name)
+    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError("%s must be contiguous in its last dimension" % name)
+    ld = t.stride(-2) if t.shape[-2] > 1 else _pitch(t.shape[-1], t)
+    if len(shape) == 3 and t.shape[0] > 1:
+        if t.shape[1] == 1:
+            ld = t.stride(0)
+        elif t.stride(0) != t.shape[1] * ld:
+            raise ValueError("%s must hold its groups one after another (strides %s)" % (name, t.stride()))
+    return ld
+
+
+def _pitch(cols, t_or_bytes) -> int:
+    """Row length in elements rounded up to whole 16-byte units."""
+    unit = 16 // (t_or_bytes if isinstance(t_or_bytes, int) else t_or_bytes.element_size())
+    return -(-cols // unit) * unit
+
+
+def _padded(shape, dtype, device, zero=False):
+    """A new tensor of `shape` whose rows start on 16-byte boundaries (a view of wider rows where they must)."""
+    import torch
+    cols = _pitch(shape[-1], torch.empty((), dtype=dtype).element_size())
+    make = torch.zeros if zero else torch.empty
+    t = make((*shape[:-1], cols), dtype=dtype, device=device)
+    return t if cols == shape[-1] else t[..., :shape[-1]]
+
+
+def _vector(t, n, dtype, name):
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError("%s must be %d contiguous %s values on the GPU, got %s %s" % (name, n, dtype, t.dtype, tuple(t.shape)))
+    return t
+
+
+class GroupedProduct:
+    """The products of `groups` experts' matrices W_e [N][K] with their rows, and both gradients.
+
+    A holder around the C calls (no arithmetic): it keeps the workspace for up to max_rows rows and allocates outputs.
+    offsets [groups + 1] int32 on the device are the groups' row ranges (the forward's routing copies hold them); keep
+    [groups] int32 limits W_e's rows (keep_axis "N") or columns ("K").  Calls on different streams need holders of their
+    own: they share the workspace.
+    """
+
+    def __init__(self, groups, N, K, max_rows, dtype=None, keep_axis="none", device="cuda"):
+        import torch
+        self.groups, self.N, self.K, self.max_rows, self.keep_axis = groups, N, K, max_rows, keep_axis
+        self.dtype = torch.bfloat16 if dtype is None else dtype
+        self.device = device
+        code = _dtype_code(self.dtype)
+        self.desc = make_grouped_desc(groups, N, K, code, FLEXMOE_F32, keep_axis, max_rows, _pitch(K, self._es()),
+                                      _pitch(K, self._es()), _pitch(N, self._es()), _pitch(K, 2))
+        nbytes = flexmoe_grouped_workspace_bytes(self.desc, max_rows)
+        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+    def _es(self):
+        return 2 if _dtype_code(self.dtype) == FLEXMOE_BF16 else 4
+
+    def _groups(self, offsets, keep):
+        import torch
+        _vector(offsets, self.groups + 1, torch.int32, "offsets")
+        if keep is not None:
+            _vector(keep, self.groups, torch.int32, "keep")
+
+    def forward(self, x, w, offsets, keep=None, y=None, stream=None):
+        """y_r = x_r W_e^T for x [R, K], w [groups, N, K]."""
+        self._groups(offsets, keep)
+        R, d = x.shape[0], self.desc
+        if y is None:
+            y = _padded((R, self.N), self.dtype, x.device)
+        d.ldx, d.ldw = _matrix(x, (R, self.K), self.dtype, "x"), _matrix(w, (self.groups, self.N, self.K), self.dtype, "w")
+        d.ldy = _matrix(y, (R, self.N), self.dtype, "y")
+        flexmoe_grouped_forward(d, R, x, w, offsets, keep, y, self.workspace, stream=stream)
+        return y
+
+    def input_grad(self, dy, w, offsets, keep=None, dx=None, stream=None):
+        """dx_r = dy_r W_e for dy [R, N]."""
+        self._groups(offsets, keep)
+        R, d = dy.shape[0], self.desc
+        if dx is None:
+            dx = _padded((R, self.K), self.dtype, dy.device)
+        d.ldy, d.ldw = _matrix(dy, (R, self.N), self.dtype, "dy"), _matrix(w, (self.groups, self.N, self.K), self.dtype, "w")
+        d.ldx = _matrix(dx, (R, self.K), self.dtype, "dx")
+        flexmoe_grouped_input_grad(d, R, dy, w, offsets, keep, dx, self.workspace, stream=stream)
+        return dx
+
+    def weight_grad(self, dy, x, offsets, keep=None, dw=None, accumulate=False, dw_dtype=None, stream=None):
+        """dW_e = dy^T x over e's rows, written to (or with accumulate added to) dw [groups, N, K]."""
+        import torch
+        self._groups(offsets, keep)
+        R, d = dy.shape[0], self.desc
+        if dw is None:
+            if accumulate:
+                raise ValueError("accumulate needs dw")
+            dw = _padded((self.groups, self.N, self.K), torch.float32 if dw_dtype is None else dw_dtype, dy.device)
+        elif dw_dtype is not None and dw.dtype != dw_dtype:
+            raise ValueError("dw is %s, not %s" % (dw.dtype, dw_dtype))
+        d.dw_dtype = _dtype_code(dw.dtype)
+        d.ldy, d.ldx = _matrix(dy, (R, self.N), self.dtype, "dy"), _matrix(x, (R, self.K), self.dtype, "x")
+        d.lddw = _matrix(dw, (self.groups, self.N, self.K), dw.dtype, "dw")
+        flexmoe_grouped_weight_grad(d, R, dy, x, offsets, keep, dw, accumulate, self.workspace, stream=stream)
+        return dw
+
+
+def quantize_rows(x, gate=None, q=None, scale=None, stream=None):
+    """Rows of x (or silu(gate) * x) as whole numbers up to 127 and a scale each: (q int8 like x, scale)."""
+    import torch
+    lead, cols = x.shape[:-1], x.shape[-1]
+    rows = int(np.prod(lead, dtype=np.int64))
+    ldx = _matrix(x, x.shape, x.dtype, "x")
+    if gate is not None and _matrix(gate, x.shape, x.dtype, "gate") != ldx:
+        raise ValueError("x and gate must have the same strides")
+    if q is None:
+        q = _padded(x.shape, torch.int8, x.device)
+    if scale is None:
+        scale = torch.empty(lead, dtype=torch.float32, device=x.device)
+    flexmoe_quantize_rows(rows, cols, _dtype_code(x.dtype), x, gate, ldx, q, _matrix(q, x.shape, torch.int8, "q"),
+                          _vector(scale, rows, torch.float32, "scale"), stream)
+    return q, scale
+
+
+class Int8Product:
+    """8-bit experts (one group: a plain matrix): y_r = x_r W_e^T with W_e in whole numbers and a scale per channel.
+
+    w [groups, N, K] int8 and w_scale [groups, N] (quantize_rows of the weights).  Calling it rounds the rows of x and
+    multiplies; `product` takes rows that are rounded already.  It keeps the workspace and the rounded rows' buffers for
+    up to max_rows rows: calls on different streams need holders of their own.
+    """
+
+    def __init__(self, w, w_scale, max_rows, keep_axis="none", out_dtype=None):
+        import torch
+        self.groups, self.N, self.K = w.shape
+        self.w, self.w_scale, self.max_rows = w, _vector(w_scale, self.groups * self.N, torch.float32, "w_scale"), max_rows
+        self.out_dtype = torch.bfloat16 if out_dtype is None else out_dtype
+        self.desc = make_grouped_desc(self.groups, self.N, self.K, _dtype_code(self.out_dtype), FLEXMOE_F32, keep_axis, max_rows,
+                                      _pitch(self.K, 1), _matrix(w, w.shape, torch.int8, "w"),
+                                      _pitch(self.N, 2 if self.out_dtype == torch.bfloat16 else 4))
+        self.workspace = torch.empty(flexmoe_quantized_workspace_bytes(self.desc, max_rows), dtype=torch.uint8, device=w.device)
+        self.q = _padded((max_rows, self.K), torch.int8, w.device)
+        self.q_scale = torch.empty(max_rows, dtype=torch.float32, device=w.device)
+        self.offsets = None
+
+    @classmethod
+    def from_weights(cls, w, max_rows, keep_axis="none", out_dtype=None):
+        """From bf16 or fp32 weights [groups, N, K]."""
+        return cls(*quantize_rows(w), max_rows, keep_axis, out_dtype)
+
+    def __call__(self, x, offsets=None, keep=None, gate=None, y=None, stream=None):
+        """x [R, K] bf16 or fp32 (with gate: silu(gate) * x); offsets may be left out for one group."""
+        R = x.shape[0]
+        if R > self.max_rows:
+            raise ValueError("%d rows, max_rows is %d" % (R, self.max_rows))
+        q, scale = quantize_rows(x, gate, self.q[:R], self.q_scale[:R], stream)
+        return self.product(q, scale, offsets, keep, y, stream)
+
+    def product(self, q, q_scale, offsets=None, keep=None, y=None, stream=None):
+        import torch
+        R, d = q.shape[0], self.desc
+        if offsets is None:
+            if self.groups != 1:
+                raise ValueError("offsets are needed for %d groups" % self.groups)
+            offsets = torch.tensor([0, R], dtype=torch.int32, device=q.device)
+        _vector(offsets, self.groups + 1, torch.int32, "offsets")
+        if keep is not None:
+            _vector(keep, self.groups, torch.int32, "keep")
+        if y is None:
+            y = _padded((R, self.N), self.out_dtype, q.device)
+        d.ldx, d.ldy = _matrix(q, (R, self.K), torch.int8, "q"), _matrix(y, (R, self.N), self.out_dtype, "y")
+        flexmoe_quantized_forward(d, R, q, _vector(q_scale, R, torch.float32, "q_scale"), self.w, self.w_scale, offsets, keep, y,
+                                  self.workspace, stream=stream)
+        return y
+
+
+class AdamW:
+    """AdamW over a list of contiguous tensors, states in 32 or in 8 bits (one launch per 56 tensors).
+
+    params: bf16 or fp32, all alike.  masters: fp32 copies that the step works on (bf16 parameters).  states: (m, v) or,
+    with 8 bits, (m, v, m_scale, v_scale) lists to continue from; zeros otherwise.  step(grads) takes one gradient per
+    parameter.
+    """
+
+    def __init__(self, params, masters=None, states=None, state_bits=32, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0,
+                 step=0, seed=0):
+        import torch
+        self.params, self.masters, self.state_bits = list(params), masters, state_bits
+        self.betas, self.eps, self.weight_decay, self.t, self.seed = betas, eps, weight_decay, step, seed
+        if not self.params:
+            raise ValueError("no parameters")
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32, got %s" % (state_bits,))
+        dt = self.params[0].dtype
+        for p in self.params:
+            self._like(p, p.numel(), dt, "params")
+        sizes = [p.numel() for p in self.params]
+        if states is None:
+            def zeros(n, dtype):
+                return torch.zeros(n, dtype=dtype, device=self.params[0].device)
+
+            st = torch.uint8 if state_bits == 8 else torch.float32
+            states = ([zeros(n, st) for n in sizes], [zeros(n, st) for n in sizes])
+            if state_bits == 8:
+                blocks = [-(-n // STATE_BLOCK) for n in sizes]
+                states += ([zeros(n, torch.float32) for n in blocks], [zeros(n, torch.float32) for n in blocks])
+        self.m, self.v = states[:2]
+        self.m_scale, self.v_scale = states[2:] if state_bits == 8 else (None, None)
+        st = torch.uint8 if state_bits == 8 else torch.float32
+        self._table = (flexmoe_adamw_tensor * len(sizes))()
+        for i, n in enumerate(sizes):
+            e = self._table[i]
+            e.param, e.n = self.params[i].data_ptr(), n
+            e.m, e.v = (self._like(s[i], n, st, "states") for s in (self.m, self.v))
+            if state_bits == 8:
+                e.m_scale, e.v_scale = (self._like(s[i], -(-n // STATE_BLOCK), torch.float32, "scales")
+                                        for s in (self.m_scale, self.v_scale))
+            if masters is not None:
+                e.master = self._like(masters[i], n, torch.float32, "masters")
+        # the table's gradient column, filled by every step
+        stride = ctypes.sizeof(flexmoe_adamw_tensor) // 8
+        self._grads = np.frombuffer(self._table, dtype=np.uint64)[flexmoe_adamw_tensor.grad.offset // 8::stride]
+        self.sizes, self._param_code = sizes, _dtype_code(dt)
+
+    @staticmethod
+    def _like(t, n, dtype, name):
+        if t.dtype != dtype or t.numel() < n or not t.is_contiguous() or not t.is_cuda:
+            raise ValueError("%s: need %d contiguous %s values on the GPU, got %s %s" % (name, n, dtype, t.dtype, tuple(t.shape)))
+        return t.data_ptr()
+
+    def step(self, grads, lr, grad_scale=1.0, stream=None):
+        """One step with the gradients `grads` (bf16 or fp32, all alike, contiguous)."""
+        if len(grads) != len(self.sizes):
+            raise ValueError("%d gradients for %d parameters" % (len(grads), len(self.sizes)))
+        dt = grads[0].dtype
+        self._grads[:] = [self._like(g, n, dt, "grads") for g, n in zip(grads, self.sizes)]
+        d = flexmoe_adamw_desc(self._param_code, _dtype_code(dt), self.state_bits, self.seed & 0xffffffff, self.t + 1, lr,
+                               self.betas[0], self.betas[1], self.eps, self.weight_decay, grad_scale)
+        flexmoe_adamw_step(d, self._table, stream=stream)
+        self.t += 1
+
+
+def adamw_state_values(m, v, m_scale, v_scale, dtype=None, stream=None):
+    """What 8-bit states stand for: (m, v) as fp32 or bf16."""
+    import torch
+    dtype = torch.float32 if dtype is None else dtype
+    mo, vo = torch.empty(m.numel(), dtype=dtype, device=m.device), torch.empty(m.numel(), dtype=dtype, device=m.device)
+    blocks = -(-m.numel() // STATE_BLOCK)
+    flexmoe_adamw_read_state(m.numel(), _vector(m, m.numel(), torch.uint8, "m"), _vector(v, m.numel(), torch.uint8, "v"),
+                             _vector(m_scale, blocks, torch.float32, "m_scale"), _vector(v_scale, blocks, torch.float32, "v_scale"),
+                             _dtype_code(dtype), mo, vo, stream)
+    return mo, vo
 
 
 class ClippedWeights:
