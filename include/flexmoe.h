@@ -439,8 +439,8 @@ int flexmoe_grouped_weight_grad(const flexmoe_grouped_desc *desc, int32_t R, con
 
 /* ---- Products in 8-bit integers ------------------------------------------
  * flexmoe_quantize_rows: row r of v [rows][cols] as whole numbers
- *   q_r = round(v_r * (127 / m)), ties to even, and scale[r] = m / 127 for m =
- *   max |v_r|; v = x, or silu(x_gate) * x with x_gate (NULL otherwise; same
+ *   q_r = round(v_r * ((1 / m) * 127)) in fp32, ties to even, and scale[r] =
+ *   m / 127 for m = max |v_r|; v = x, or silu(x_gate) * x with x_gate (NULL otherwise; same
  *   shape, stride and type).  A row of zeros has scale 0; a row with a NaN or an
  *   infinity has the scale NaN and zeros.  x [rows][ldx] (dtype; rows of
  *   whole 16-byte units), q [rows][ldq] int8 (ldq a multiple of 16; up to 7 values past the

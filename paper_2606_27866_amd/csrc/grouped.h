@@ -33,6 +33,7 @@ struct GroupedParams {
     int tiles_r;              // weight gradient: row tiles of C
     int splits;               // parts of the reduction, each a workgroup's
     int out_bf16;             // C is bf16 (else fp32)
+    int slim;                 // 128 x 128 tiles: one LDS stage, four workgroups per compute unit
     int accumulate;           // weight gradient: C += instead of C =
 };
 
@@ -52,60 +53,76 @@ __device__ __forceinline__ int group_width(const GroupedParams& p, int e, int fu
     return p.keep ? min(max(p.keep[e], 0), full) : full;
 }
 
-// Row tiles of `bm` rows of every group, counted before a wave's eyes: lane l
-// holds groups 4l .. 4l + 3.  Finds the group whose tiles hold number q.
-// Returns false past the last tile.  All 64 lanes must be active and q uniform.
-__device__ __forceinline__ bool find_group(const GroupedParams& p, int bm, int q, int& e, int& row0, int& rows, int& first,
-                                           int& tiles) {
+// The group whose row tiles (of bm rows) hold number q, its rows, the number of
+// its first row tile and how many it has; false past the last tile.  Lane l
+// counts groups 4l .. 4l + 3.  Groups are taken in their order, or, where their
+// widths set the length of the reduction, in four classes of width, the widest
+// first, so that a launch ends on short tiles (60 groups of 1408 x 2048, 16384
+// rows, input gradient 105 -> 96 us; 8 of 4096 x 14336, forward 992 -> 1010).  All 64 lanes must be active and q uniform.
+__device__ __forceinline__ bool find_group(const GroupedParams& p, int bm, int q, bool by_width, int full, int& e, int& row0,
+                                           int& rows, int& first, int& tiles) {
     static_assert(kMaxExperts <= 4 * kWave, "four groups per lane");
     const int lane = threadIdx.x & 63;
-    int b[5], t[4], sum = 0;
+    int b[5], t[4], cls[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < 5; ++j) b[j] = group_begin(p, min(4 * lane + j, p.E));
+    if (by_width)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        t[j] = (max(b[j + 1] - b[j], 0) + bm - 1) / bm;
-        sum += t[j];
-    }
-    const int incl = wave_incl_scan(sum);
-    const unsigned long long owner = __ballot(incl - sum <= q && q < incl);
-    if (!owner) return false;
-    int base = incl - sum, f = 0, my = 0;
-    bool found = false;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if (!found && q < base + t[j]) {
-            found = true;
-            my = j;
-            f = base;
+        for (int j = 0; j < 4; ++j) {
+            const int w = group_width(p, min(4 * lane + j, p.E - 1), full);
+            cls[j] = w >= full - full / 4 ? 0 : w >= full / 2 ? 1 : w >= full / 4 ? 2 : 3;
         }
-        if (!found) base += t[j];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) t[j] = (max(b[j + 1] - b[j], 0) + bm - 1) / bm;
+    int before = 0;  // tiles of the classes done
+    for (int k = 0; k < (by_width ? 4 : 1); ++k) {
+        int u[4], sum = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            u[j] = cls[j] == k ? t[j] : 0;
+            sum += u[j];
+        }
+        const int incl = before + wave_incl_scan(sum);
+        const unsigned long long owner = __ballot(incl - sum <= q && q < incl);
+        if (!owner) {
+            before = lane63(incl);
+            continue;
+        }
+        int f = incl - sum, my = 0;
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+            if (my == j && q >= f + u[j]) {
+                f += u[j];
+                my = j + 1;
+            }
+        const int lb = my == 0 ? b[0] : my == 1 ? b[1] : my == 2 ? b[2] : b[3];
+        const int le = my == 0 ? b[1] : my == 1 ? b[2] : my == 2 ? b[3] : b[4];
+        const int lt = my == 0 ? u[0] : my == 1 ? u[1] : my == 2 ? u[2] : u[3];
+        const int src = __builtin_ctzll(owner);
+        e = 4 * src + __builtin_amdgcn_readlane(my, src);
+        row0 = __builtin_amdgcn_readlane(lb, src);
+        rows = __builtin_amdgcn_readlane(le, src) - row0;
+        first = __builtin_amdgcn_readlane(f, src);
+        tiles = __builtin_amdgcn_readlane(lt, src);
+        return true;
     }
-    const int lb = my == 0 ? b[0] : my == 1 ? b[1] : my == 2 ? b[2] : b[3];
-    const int le = my == 0 ? b[1] : my == 1 ? b[2] : my == 2 ? b[3] : b[4];
-    const int lt = my == 0 ? t[0] : my == 1 ? t[1] : my == 2 ? t[2] : t[3];
-    const int src = __builtin_ctzll(owner);
-    e = 4 * src + __builtin_amdgcn_readlane(my, src);
-    row0 = __builtin_amdgcn_readlane(lb, src);
-    rows = __builtin_amdgcn_readlane(le, src) - row0;
-    first = __builtin_amdgcn_readlane(f, src);
-    tiles = __builtin_amdgcn_readlane(lt, src);
-    return true;
+    return false;
 }
 
 // Tile number L (row tiles of a group fastest, then column tiles, then parts
-// of the reduction: neighbours share a weight tile).  kD is the depth of a K
-// tile: parts of the reduction are whole K tiles.
+// of the reduction: neighbours share a weight tile).  A group's row tiles take
+// equal shares of its rows, in steps of `unit`; kd is the depth of a K tile:
+// parts of the reduction are whole K tiles.
 template <int kForm>
-__device__ __forceinline__ bool grouped_tile(const GroupedParams& p, int L, int bm, int bn, int kd, GroupedTile& t) {
+__device__ __forceinline__ bool grouped_tile(const GroupedParams& p, int L, int bm, int bn, int unit, int kd, GroupedTile& t) {
     int mt, ct, depth;
     if constexpr (kForm == kWeightGrad) {
         const int per = p.tiles_r * p.tiles_c * p.splits;
         t.e = L / per;
         if (t.e >= p.E) return false;
         const int local = L - t.e * per;
-        mt = local % p.tiles_r;
-        ct = local / p.tiles_r % p.tiles_c;
+        ct = local % p.tiles_c;
+        mt = local / p.tiles_c % p.tiles_r;
         t.split = local / (p.tiles_r * p.tiles_c);
         t.row0 = group_begin(p, t.e);
         t.rows = max(group_begin(p, t.e + 1) - t.row0, 0);
@@ -115,13 +132,13 @@ __device__ __forceinline__ bool grouped_tile(const GroupedParams& p, int L, int 
     } else {
         const int per = p.tiles_c * p.splits;
         int first, tiles;
-        if (!find_group(p, bm, L / per, t.e, t.row0, t.rows, first, tiles)) return false;
+        const bool by_width = p.keep_axis == (kForm == kForward ? 2 : 1);
+        if (!find_group(p, bm, L / per, by_width, kForm == kForward ? p.K : p.N, t.e, t.row0, t.rows, first, tiles)) return false;
         const int local = L - first * per;
         mt = local % tiles;
         ct = local / tiles % p.tiles_c;
         t.split = local / (tiles * p.tiles_c);
-        // equal shares of the rows, in steps of 16
-        const int step = ceil_div(ceil_div(t.rows, tiles), 16) * 16;
+        const int step = ceil_div(ceil_div(t.rows, tiles), unit) * unit;
         t.r0 = mt * step;
         t.r1 = min(t.r0 + step, t.rows);
         depth = kForm == kForward ? p.K : p.N;
@@ -252,6 +269,29 @@ __device__ __forceinline__ void across_read4(const uint32_t (&a)[4], bf16x8 (&f)
         f[j] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(l[j], h[j], 0, 1, 2, 3));
 }
 
+// Two bf16 fragments at both K steps: f[2 * step + fragment].
+template <int W>
+__device__ __forceinline__ void across_read2x2(uint32_t a0, uint32_t a1, bf16x8 (&f)[4]) {
+    typedef int int2_t __attribute__((ext_vector_type(2)));
+    int2_t l[4], h[4];
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8 offset:%10\n\t"
+        "ds_read_b64_tr_b16 %4, %8 offset:%11\n\t"
+        "ds_read_b64_tr_b16 %1, %9 offset:%10\n\t"
+        "ds_read_b64_tr_b16 %5, %9 offset:%11\n\t"
+        "ds_read_b64_tr_b16 %2, %8 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %6, %8 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %7, %9 offset:%13\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(l[0]), "=&v"(l[1]), "=&v"(l[2]), "=&v"(l[3]), "=&v"(h[0]), "=&v"(h[1]), "=&v"(h[2]), "=&v"(h[3])
+        : "v"(a0), "v"(a1), "n"(0), "n"(4 * W * 2), "n"(32 * W * 2), "n"(36 * W * 2)
+        : "memory");
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        f[j] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(l[j], h[j], 0, 1, 2, 3));
+}
+
 // One fp32 fragment of an across tile, at K step s: lane group g takes depths
 // 16s + 4g + j, index lane % 16.
 template <int W>
@@ -271,48 +311,229 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc_bytes(const void* ba
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, (int)bytes, 0x00020000);
 }
 
-// v as C's type; a lane's 4 consecutive columns col .. col + 3 of C row `c`
-// (16-byte aligned rows), of which those below `cols` exist in C and those
-// below `clim` are not zero.
-template <bool kBf16>
-__device__ __forceinline__ void store_run(void* crow, int col, int cols, int clim, floatx4 v, int accumulate) {
+constexpr int STAGE = 16384;  // bytes of 128 rows' K tile
+
+// Requests of N instructions of 1 KB for 128 own indices of an operand:
+// instruction i fills the tile's LDS bytes (wave0 + i) * 1024 + lane * 16.
+template <typename E, bool kAcross, int N>
+struct Loader {
+    const char* base;       // first element of the operand's part
+    size_t step;            // bytes a K tile advances (across: 0 in the lane offsets)
+    uint32_t off[N];        // lane offset, kOOB if its row or column does not exist
+    int col[N];             // along: the chunk's first depth inside a K tile
+    size_t ldb;             // across: bytes per depth
+    uint32_t tail;          // across: bytes of the last depth that may be read
+    __amdgpu_buffer_rsrc_t r;
+    int depth;
+
+    // `own`: rows (along) or columns (across) that exist from the tile's first
+    // on; `wave0`: this wave's first instruction
+    __device__ __forceinline__ void init(const void* p, size_t ld, int own, int d, int wave0) {
+        const int lane = threadIdx.x & 63;
+        base = reinterpret_cast<const char*>(p);
+        depth = d;
+        if constexpr (!kAcross) {
+            r = make_rsrc_bytes(base, 0x7ffffff0u);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = col + k < clim ? v[k] : 0.f;
+            for (int i = 0; i < N; ++i) {
+                const int row = (wave0 + i) * 8 + lane / CHUNKS, c = swz(row, lane % CHUNKS);
+                col[i] = c * E::kPer;
+                off[i] = row < own ? (uint32_t)((size_t)row * ld * E::kBytes) + c * 16 : kOOB;
+            }
+        } else {
+            constexpr int kChunks = 128 * E::kBytes / 16;  // of an LDS row
+            ldb = ld * E::kBytes;
+            step = ldb * E::kDepth;
+            tail = (uint32_t)((min(own, 128) * E::kBytes + 15) & ~15);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int dep = (wave0 + i) * (64 / kChunks) + lane / kChunks;
+                const int c = across_chunk<E>(dep, lane % kChunks);
+                col[i] = 0;
+                off[i] = c * E::kPer < own ? (uint32_t)(dep * ldb) + c * 16 : kOOB;
+            }
+        }
+    }
+    // K tile kt to `lds` (this wave's first instruction's place); past the end zeros
+    __device__ __forceinline__ void request(int kt, unsigned char* lds) {
+        const int lim = depth - kt * E::kDepth;
+        if constexpr (!kAcross) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) load_lds16(r, col[i] < lim ? off[i] : kOOB, (uint32_t)kt * ROWB, lds + i * 1024);
+        } else {
+            // the descriptor covers the depths that exist
+            const int n = max(min(lim, E::kDepth), 0);
+            r = make_rsrc_bytes(base + (size_t)kt * step, max((n - 1) * (int)ldb + (int)tail, 0) & -(int)(n > 0));
+#pragma unroll
+            for (int i = 0; i < N; ++i) load_lds16(r, off[i], 0, lds + i * 1024);
+        }
+    }
+};
+
+// A lane's 4 consecutive columns col .. col + 3 of C row `crow` (16-byte
+// aligned rows), of which those below `cols` exist: what is there, and v as C's
+// type.
+template <bool kBf16>
+__device__ __forceinline__ floatx4 load_run(const void* crow, int col, int cols) {
+    floatx4 v{0.f, 0.f, 0.f, 0.f};
+    if constexpr (kBf16) {
+        const bf16_t* o = reinterpret_cast<const bf16_t*>(crow) + col;
+        if (col + 3 < cols) {
+            const uint2 w = *reinterpret_cast<const uint2*>(o);
+            v = floatx4{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                        __uint_as_float(w.y & 0xffff0000u)};
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (col + k < cols) v[k] = bf16_to_f32(o[k]);
+        }
+    } else {
+        const float* o = reinterpret_cast<const float*>(crow) + col;
+        if (col + 3 < cols) {
+            v = *reinterpret_cast<const floatx4*>(o);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (col + k < cols) v[k] = o[k];
+        }
+    }
+    return v;
+}
+template <bool kBf16>
+__device__ __forceinline__ void store_run(void* crow, int col, int cols, floatx4 v) {
     if constexpr (kBf16) {
         bf16_t* o = reinterpret_cast<bf16_t*>(crow) + col;
         if (col + 3 < cols) {
-            if (accumulate) {
-                const uint2 w = *reinterpret_cast<const uint2*>(o);
-                v[0] += __uint_as_float(w.x << 16), v[1] += __uint_as_float(w.x & 0xffff0000u);
-                v[2] += __uint_as_float(w.y << 16), v[3] += __uint_as_float(w.y & 0xffff0000u);
-            }
             *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
         } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (col + k < cols) o[k] = f32_to_bf16(accumulate ? v[k] + bf16_to_f32(o[k]) : v[k]);
+                if (col + k < cols) o[k] = f32_to_bf16(v[k]);
         }
     } else {
         float* o = reinterpret_cast<float*>(crow) + col;
         if (col + 3 < cols) {
-            if (accumulate) v += *reinterpret_cast<const floatx4*>(o);
             *reinterpret_cast<floatx4*>(o) = v;
         } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (col + k < cols) o[k] = accumulate ? v[k] + o[k] : v[k];
+                if (col + k < cols) o[k] = v[k];
+        }
+    }
+}
+
+// First elements of a tile's operands, and how many of their own indices exist
+// from there on.
+template <typename E, int kForm>
+struct Operands {
+    const typename E::T *a, *b;
+    int own_a, own_b;
+    __device__ __forceinline__ Operands(const GroupedParams& p, const GroupedTile& t)
+        : a(reinterpret_cast<const typename E::T*>(p.a)), b(reinterpret_cast<const typename E::T*>(p.b)), own_a(t.r1 - t.r0) {
+        if constexpr (kForm == kWeightGrad) {
+            a += (size_t)(t.row0 + t.d0) * p.lda + t.r0;
+            b += (size_t)(t.row0 + t.d0) * p.ldb + t.c0;
+        } else {
+            a += (size_t)(t.row0 + t.r0) * p.lda + t.d0;
+            b += (size_t)t.e * p.N * p.ldb;
+            b += kForm == kForward ? (size_t)t.c0 * p.ldb + t.d0 : (size_t)t.d0 * p.ldb + t.c0;
+        }
+        own_b = (kForm == kForward ? p.N : p.K) - t.c0;
+    }
+};
+
+// C's part of a tile that a wave holds: kRows fragments of 16 rows from C row
+// `first` on and 16 runs of 4 columns, run q at column(q), to C or to this
+// part's place among the partial sums.  value(i, j) is the accumulator of row
+// fragment i and runs 4j .. 4j + 3 (lane -> row lane % 16, run 4j + lane / 16).
+// Each row fragment goes through 4 KB of LDS that are the wave's own, so that a
+// store covers 4 rows of 16 consecutive runs, whole cache lines, where straight
+// from the accumulators it covers 16 rows of 4 runs (stores alone of 692 MB of
+// fp32 with four 128 x 128 tiles per compute unit: 190 -> 123 us).
+template <typename E, int kForm, bool kBf16Out, int kRows, typename Column, typename Value>
+__device__ __forceinline__ void store_tile(const GroupedParams& p, const GroupedTile& t, int first, unsigned char* scratch,
+                                           Column&& column, Value&& value) {
+    const int lane = threadIdx.x & 63, lr = lane & 15, lc = lane >> 4;
+    const int cols = kForm == kForward ? p.N : p.K;
+    const bool add = kForm == kWeightGrad && p.accumulate && p.splits == 1 && !p.slim;
+    const int c = column(lr);
+    auto crow_of = [&](int r) { return kForm == kWeightGrad ? (size_t)t.e * p.N + r : (size_t)t.row0 + r; };
+    auto address = [&](int r) { return reinterpret_cast<char*>(p.c) + crow_of(r) * p.ldc * (kBf16Out ? 2 : 4); };
+    // old values are read a fragment ahead: the compiler keeps a read behind
+    // the stores before it
+    floatx4 old[kForm == kWeightGrad ? 2 : 1][4];
+    auto load_old = [&](int i) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int r = first + i * 16 + 4 * s + lc;
+            if (r < t.r1 && c < cols) old[i & 1][s] = load_run<kBf16Out>(address(r), c, cols);
+        }
+    };
+    if constexpr (kForm == kWeightGrad)
+        if (add) load_old(0);
+    // int8: this lane's columns' and rows' scales, read before any store for
+    // the same reason
+    float sb[4], sa[kRows][4];
+    if constexpr (E::kBytes == 1)
+        if (p.splits == 1) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sb[k] = c + k < cols ? p.sb[(size_t)t.e * p.N + c + k] : 0.f;
+#pragma unroll
+            for (int i = 0; i < kRows; ++i)
+#pragma unroll
+                for (int s = 0; s < 4; ++s) sa[i][s] = p.sa[crow_of(min(first + i * 16 + 4 * s + lc, t.r1 - 1))];
+        }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        if constexpr (kForm == kWeightGrad)
+            if (add && i + 1 < kRows) load_old(i + 1);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<typename E::Acc*>(scratch + lr * 256 + ((4 * j + lc) ^ lr) * 16) = value(i, j);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int row = 4 * s + lc, r = first + i * 16 + row;
+            typename E::Acc v = *reinterpret_cast<const typename E::Acc*>(scratch + row * 256 + (lr ^ row) * 16);
+            const int clim = r < t.rlim ? t.clim : 0;
+            // what lies past a width is left as it is when C is added to
+            const int end = kForm == kWeightGrad && p.accumulate && p.splits == 1 ? min(clim, cols) : cols;
+            if (r >= t.r1 || c >= end) continue;
+            const size_t crow = crow_of(r);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = c + k < clim ? v[k] : 0;
+            if (p.splits > 1) {
+                const size_t rows = kForm == kWeightGrad ? (size_t)p.E * p.N : (size_t)p.R;
+                const size_t ldp = (cols + 3) & ~3;
+                *reinterpret_cast<typename E::Acc*>(reinterpret_cast<char*>(p.partial) + ((t.split * rows + crow) * ldp + c) * 4) = v;
+                continue;
+            }
+            floatx4 f;
+            if constexpr (E::kBytes == 1) {
+                // past the width the factor may be anything: not multiplied
+#pragma unroll
+                for (int k = 0; k < 4; ++k) f[k] = c + k < clim ? (float)v[k] * (sa[i][s] * sb[k]) : 0.f;
+            } else {
+                f = v;
+            }
+            if constexpr (kForm == kWeightGrad)
+                if (add) f += old[i & 1][s];
+            store_run<kBf16Out>(address(r), c, end, f);
         }
     }
 }
 
 }  // namespace mfma
 
+// 128 x 128 tiles: every form and type
 hipError_t launch_grouped_mid(const GroupedParams& p, GroupedForm form, GroupedElem elem, long long grid, hipStream_t s);
+// 256 x 256 tiles: bf16 (every form) and int8
+hipError_t launch_grouped_big(const GroupedParams& p, GroupedForm form, GroupedElem elem, long long grid, hipStream_t s);
 hipError_t launch_grouped_join(const GroupedParams& p, GroupedForm form, GroupedElem elem, hipStream_t s);
 // rows [rows][cols] of x (or silu(x) * x2) as whole numbers up to 127 and a scale each
 hipError_t launch_quantize_rows(const void* x, const void* x2, size_t ldx, int8_t* q, size_t ldq, float* scale, int rows, int cols,
                                 bool bf16, hipStream_t s);
 
-constexpr int kGroupTile = 128;  // rows and columns of a launch_grouped_mid tile
+constexpr int kGroupTile = 128;     // rows and columns of a launch_grouped_mid tile
+constexpr int kGroupBigTile = 256;  // of a launch_grouped_big tile
 
 }  // namespace flexmoe

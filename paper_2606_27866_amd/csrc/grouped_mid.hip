@@ -23,66 +23,26 @@ namespace {
 using namespace mfma;
 
 constexpr int GT = 256;                   // threads
-constexpr int STAGE = 16384;              // bytes of an operand's K tile
 constexpr int SMEM = 5 * STAGE;           // A0 A1 B0 B1 B2
 constexpr int NI = STAGE / 1024 / 4;      // requests per wave and operand: 4
 
-// Requests of one operand for this lane: instruction i of wave w fills LDS
-// bytes (w * NI + i) * 1024 + lane * 16.
-template <typename E, bool kAcross, int N>
-struct Loader {
-    const char* base;       // first element of the operand's part
-    size_t step;            // bytes a K tile advances (across: 0 in the lane offsets)
-    uint32_t off[N];        // lane offset, kOOB if its row or column does not exist
-    int col[N];             // along: the chunk's first depth inside a K tile
-    size_t ldb;             // across: bytes per depth
-    uint32_t tail;          // across: bytes of the last depth that may be read
-    __amdgpu_buffer_rsrc_t r;
-    int depth;
-
-    // `own`: rows (along) or columns (across) that exist from the tile's first
-    // on; `wave0`: this wave's first instruction
-    __device__ __forceinline__ void init(const void* p, size_t ld, int own, int d, int wave0) {
-        const int lane = threadIdx.x & 63;
-        base = reinterpret_cast<const char*>(p);
-        depth = d;
-        if constexpr (!kAcross) {
-            r = make_rsrc_bytes(base, 0x7ffffff0u);
+// F fragments from own index `first` on, at K step s.
+template <typename E, bool kAcross, int F>
+__device__ __forceinline__ void read_step(const unsigned char* tile, int first, int s, typename E::Frag (&f)[F]) {
+    const int lane = threadIdx.x & 63;
+    if constexpr (kAcross && E::kBytes == 2) {
+        uint32_t addr[4];
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int row = (wave0 + i) * 8 + lane / CHUNKS, c = swz(row, lane % CHUNKS);
-                col[i] = c * E::kPer;
-                off[i] = row < own ? (uint32_t)((size_t)row * ld * E::kBytes) + c * 16 : kOOB;
-            }
-        } else {
-            constexpr int kChunks = 128 * E::kBytes / 16;  // of an LDS row
-            ldb = ld * E::kBytes;
-            step = ldb * E::kDepth;
-            tail = (uint32_t)((min(own, 128) * E::kBytes + 15) & ~15);
+        for (int i = 0; i < 4; ++i) addr[i] = across_addr<128>(tile, first + i * 16) + s * (32 * 256);
+        across_read4<128, 0>(addr, f);
+    } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int dep = (wave0 + i) * (64 / kChunks) + lane / kChunks;
-                const int c = across_chunk<E>(dep, lane % kChunks);
-                col[i] = 0;
-                off[i] = c * E::kPer < own ? (uint32_t)(dep * ldb) + c * 16 : kOOB;
-            }
+        for (int i = 0; i < F; ++i) {
+            if constexpr (kAcross) f[i] = across_frag_f32<128>(tile, first + i * 16, s);
+            else f[i] = __builtin_bit_cast(typename E::Frag, lds_frag(tile, first + i * 16 + (lane & 15), s * 4 + (lane >> 4)));
         }
     }
-    // K tile kt to `lds` (this wave's first instruction's place); past the end zeros
-    __device__ __forceinline__ void request(int kt, unsigned char* lds) {
-        const int lim = depth - kt * E::kDepth;
-        if constexpr (!kAcross) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) load_lds16(r, col[i] < lim ? off[i] : kOOB, (uint32_t)kt * ROWB, lds + i * 1024);
-        } else {
-            // the descriptor covers the depths that exist
-            const int n = min(lim, E::kDepth);
-            r = make_rsrc_bytes(base + (size_t)kt * step, n > 0 ? (uint32_t)((n - 1) * ldb) + tail : 0u);
-#pragma unroll
-            for (int i = 0; i < N; ++i) load_lds16(r, off[i], 0, lds + i * 1024);
-        }
-    }
-};
+}
 
 // F fragments from own index `first` on, at both K steps.
 template <typename E, bool kAcross, int F>
@@ -106,28 +66,16 @@ __device__ __forceinline__ void read_frags(const unsigned char* tile, int first,
     }
 }
 
-template <typename E, int kForm, bool kBf16Out>
-__global__ __launch_bounds__(GT, 2) void grouped_mid_kernel(GroupedParams p) {
+template <typename E, int kForm, bool kBf16Out, bool kSlim>
+__global__ __launch_bounds__(GT, kSlim ? 4 : 2) void grouped_mid_kernel(GroupedParams p) {
     constexpr bool kAcrossA = kForm == kWeightGrad, kAcrossB = kForm != kForward;
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[SMEM];
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[kSlim ? 2 * STAGE : SMEM];
     GroupedTile t;
-    if (!grouped_tile<kForm>(p, xcd_tile(8), kGroupTile, kGroupTile, E::kDepth, t)) return;
+    if (!grouped_tile<kForm>(p, xcd_tile(8), kGroupTile, kGroupTile, 16, E::kDepth, t)) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int wm = wave >> 1, wn = wave & 1, lr = lane & 15, lc = lane >> 4;
+    const int wm = wave >> 1, wn = wave & 1, lc = lane >> 4;
     const int nr = t.r1 - t.r0, depth = t.d1 - t.d0;
-    typedef typename E::T T;
-    const T *a = reinterpret_cast<const T*>(p.a), *b = reinterpret_cast<const T*>(p.b);
-    int own_a, own_b;
-    if constexpr (kForm == kWeightGrad) {
-        a += (size_t)(t.row0 + t.d0) * p.lda + t.r0;
-        b += (size_t)(t.row0 + t.d0) * p.ldb + t.c0;
-        own_a = nr, own_b = p.K - t.c0;
-    } else {
-        a += (size_t)(t.row0 + t.r0) * p.lda + t.d0;
-        b += (size_t)t.e * p.N * p.ldb;
-        b += kForm == kForward ? (size_t)t.c0 * p.ldb + t.d0 : (size_t)t.d0 * p.ldb + t.c0;
-        own_a = nr, own_b = (kForm == kForward ? p.N : p.K) - t.c0;
-    }
+    const Operands<E, kForm> op(p, t);
     const int nk = ceil_div(depth, E::kDepth);
 
     auto run = [&](auto mf_c) {
@@ -135,8 +83,8 @@ __global__ __launch_bounds__(GT, 2) void grouped_mid_kernel(GroupedParams p) {
         constexpr int NA = kAcrossA ? NI : MF;  // along: 32 * MF rows of A
         Loader<E, kAcrossA, NA> la;
         Loader<E, kAcrossB, NI> lb;
-        la.init(a, p.lda, own_a, depth, wave * NA);
-        lb.init(b, p.ldb, own_b, depth, wave * NI);
+        la.init(op.a, p.lda, op.own_a, depth, wave * NA);
+        lb.init(op.b, p.ldb, op.own_b, depth, wave * NI);
         unsigned char* const sa = smem;
         unsigned char* const sb = smem + 2 * STAGE;
         auto request_a = [&](int kt, int stage) { la.request(kt, sa + stage * STAGE + wave * (NA * 1024)); };
@@ -146,6 +94,40 @@ __global__ __launch_bounds__(GT, 2) void grouped_mid_kernel(GroupedParams p) {
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int i = 0; i < MF; ++i) acc[j][i] = typename E::Acc{0, 0, 0, 0};
+        if constexpr (kForm == kWeightGrad && kSlim)
+            if (p.accumulate && p.splits == 1) {
+#pragma unroll
+                for (int i = 0; i < MF; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int r = t.r0 + wm * 16 * MF + i * 16 + (lane & 15), c = t.c0 + wn * 64 + j * 16 + lc * 4;
+                        if (r < t.r1 && c < p.K)
+                            acc[j][i] = load_run<kBf16Out>(reinterpret_cast<const char*>(p.c) + ((size_t)t.e * p.N + r) * p.ldc * (kBf16Out ? 2 : 4), c, p.K);
+                    }
+            }
+        if constexpr (kSlim) {
+            // one stage: four workgroups share a compute unit and cover each
+            // other's waits
+            unsigned char* const sb1 = smem + STAGE;
+            for (int kt = 0; kt < nk; ++kt) {
+                la.request(kt, smem + wave * (NA * 1024));
+                lb.request(kt, sb1 + wave * (NI * 1024));
+                __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+                barrier_no_fence();
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    typename E::Frag fa[MF], fb[4];
+                    read_step<E, kAcrossB, 4>(sb1, wn * 64, s, fb);
+                    read_step<E, kAcrossA, MF>(smem, wm * 16 * MF, s, fa);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int i = 0; i < MF; ++i) acc[j][i] = E::mma(fb[j], fa[i], acc[j][i]);
+                }
+                __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+                if (kt + 1 < nk) barrier_no_fence();
+            }
+        } else {
         request_a(0, 0);
         request_b(0, 0);
         request_b(1, 1);
@@ -184,44 +166,13 @@ __global__ __launch_bounds__(GT, 2) void grouped_mid_kernel(GroupedParams p) {
 #pragma unroll
                     for (int i = 0; i < MF; ++i) acc[j][i] = E::mma(fb[s][j], fa[s][i], acc[j][i]);
         }
-        __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));  // no request may outlive the workgroup's LDS
-
-        // lane -> C row lane % 16 of a fragment, 4 consecutive columns from
-        // 4 * (lane / 16)
-        const int cols = kForm == kForward ? p.N : p.K;
-#pragma unroll
-        for (int i = 0; i < MF; ++i) {
-            const int r = t.r0 + wm * 16 * MF + i * 16 + lr;
-            if (r >= t.r1) continue;
-            const int clim = r < t.rlim ? t.clim : 0;
-            const size_t crow = kForm == kWeightGrad ? (size_t)t.e * p.N + r : (size_t)t.row0 + r;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int c = t.c0 + wn * 64 + j * 16 + lc * 4;
-                if (c >= cols) continue;
-                if (p.splits > 1) {
-                    const size_t rows = kForm == kWeightGrad ? (size_t)p.E * p.N : (size_t)p.R;
-                    const size_t ldp = (cols + 3) & ~3;
-                    typename E::Acc v = acc[j][i];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] = c + k < clim ? v[k] : 0;
-                    *reinterpret_cast<typename E::Acc*>(reinterpret_cast<char*>(p.partial) +
-                                                        ((t.split * rows + crow) * ldp + c) * 4) = v;
-                    continue;
-                }
-                floatx4 v;
-                if constexpr (E::kBytes == 1) {
-                    const float s = p.sa[crow];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        v[k] = c + k < clim ? (float)acc[j][i][k] * (s * p.sb[(size_t)t.e * p.N + c + k]) : 0.f;
-                } else {
-                    v = acc[j][i];
-                }
-                store_run<kBf16Out>(reinterpret_cast<char*>(p.c) + crow * p.ldc * (kBf16Out ? 2 : 4), c, cols, clim, v,
-                                    kForm == kWeightGrad ? p.accumulate : 0);
-            }
         }
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(0) & kWaitLgkm0);  // no request may outlive the loop
+
+        barrier_no_fence();  // every wave has read its fragments: LDS becomes the stores' scratch
+        store_tile<E, kForm, kBf16Out, MF>(
+            p, t, t.r0 + wm * 16 * MF, smem + wave * 4096, [&](int q) { return t.c0 + wn * 64 + q * 4; },
+            [&](int i, int j) { return acc[j][i]; });
     };
     if constexpr (kAcrossA) run(std::integral_constant<int, 4>{});
     else if (nr > 96) run(std::integral_constant<int, 4>{});
@@ -260,15 +211,22 @@ __global__ __launch_bounds__(256) void grouped_join_kernel(GroupedParams p, int 
         } else {
             for (int k = 0; k < p.splits; ++k) v += *reinterpret_cast<const floatx4*>(src + (size_t)k * rows * ldp * 4);
         }
-        store_run<kBf16Out>(reinterpret_cast<char*>(p.c) + r * p.ldc * (kBf16Out ? 2 : 4), c, cols, cols, v,
-                            kRowGroups ? 0 : p.accumulate);
+        char* const crow = reinterpret_cast<char*>(p.c) + r * p.ldc * (kBf16Out ? 2 : 4);
+        if (!kRowGroups && p.accumulate) v += load_run<kBf16Out>(crow, c, cols);
+        store_run<kBf16Out>(crow, c, cols, v);
     }
 }
 
 template <typename E, int kForm>
 void launch_mid(const GroupedParams& p, unsigned grid, hipStream_t s) {
-    if (p.out_bf16) grouped_mid_kernel<E, kForm, true><<<grid, GT, 0, s>>>(p);
-    else grouped_mid_kernel<E, kForm, false><<<grid, GT, 0, s>>>(p);
+    if constexpr (kForm == kWeightGrad)
+        if (p.slim) {
+            if (p.out_bf16) grouped_mid_kernel<E, kForm, true, true><<<grid, GT, 0, s>>>(p);
+            else grouped_mid_kernel<E, kForm, false, true><<<grid, GT, 0, s>>>(p);
+            return;
+        }
+    if (p.out_bf16) grouped_mid_kernel<E, kForm, true, false><<<grid, GT, 0, s>>>(p);
+    else grouped_mid_kernel<E, kForm, false, false><<<grid, GT, 0, s>>>(p);
 }
 
 }  // namespace

@@ -1,5 +1,6 @@
 // Rows rounded to 8 bits with a scale each (gfx950): s = max|v| / 127 over the
-// row, q = round(v * (127 / max|v|)), ties to even, for v = x or silu(x) * x2.
+// row, q = round(v * ((1 / max|v|) * 127)) in fp32, ties to even, for v = x or
+// silu(x) * x2.
 // A row that holds a NaN or an infinity gets the scale NaN and zeros, so that
 // what is computed from it is NaN; a row of zeros the scale 0.
 //
@@ -101,7 +102,7 @@ __global__ __launch_bounds__(QT) void quantize_kernel(const void* x, const void*
     }
     const float top = __uint_as_float(m);
     const bool finite = m < 0x7f800000u;
-    const float inv = finite && m ? fminf(127.f / top, 3.4028234e38f) : 0.f;
+    const float inv = finite && m ? fminf(1.f / top * 127.f, 3.4028234e38f) : 0.f;
     if (t == 0) scale[row] = finite ? top / 127.f : __uint_as_float(0x7fc00000u);
     if constexpr (kChunks > 0) {
 #pragma unroll

@@ -202,7 +202,8 @@ def _stream(stream) -> Optional[int]:
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
     import torch
-    return torch.cuda.current_stream().cuda_stream
+    # the raw handle of torch's current stream (torch.cuda.current_stream builds objects around it: 2.8 us against 0.1)
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def make_desc(d, E, I, top_k, I_shared=0, dtype=FLEXMOE_BF16, norm_topk=1, max_tokens=0):
@@ -454,13 +455,21 @@ def _dtype_code(dtype) -> int:
 
 def _matrix(t, shape, dtype, name):
     """Row stride of a [rows, cols] or [groups, rows, cols] tensor whose rows are contiguous."""
+    if t.dtype is dtype and t.shape == shape and t.is_cuda and shape[-2] > 1:
+        st = t.stride()
+        if st[-1] == 1 and (len(st) == 2 or st[0] == shape[1] * st[1]):
+            return st[-2]
+    return _matrix_checked(t, shape, dtype, name)
+
+
+def _matrix_checked(t, shape, dtype, name):
     if t.dtype != dtype or tuple(t.shape) != tuple(shape):
         raise ValueError("%s must be %s %s, got %s %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
     if not t.is_cuda:
         raise ValueError("%s must be on the GPU" % name)
     if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError("%s must be contiguous in its last dimension" % name)
-    ld = t.stride(-2) if t.shape[-2] > 1 else _pitch(t.shape[-1], t)
+    ld = t.stride(-2) if t.shape[-2] > 1 else _pitch(t.shape[-1], t.element_size())
     if len(shape) == 3 and t.shape[0] > 1:
         if t.shape[1] == 1:
             ld = t.stride(0)
@@ -469,25 +478,25 @@ def _matrix(t, shape, dtype, name):
     return ld
 
 
-def _pitch(cols, t_or_bytes) -> int:
+def _pitch(cols, element_size) -> int:
     """Row length in elements rounded up to whole 16-byte units."""
-    unit = 16 // (t_or_bytes if isinstance(t_or_bytes, int) else t_or_bytes.element_size())
+    unit = 16 // element_size
     return -(-cols // unit) * unit
 
 
-def _padded(shape, dtype, device, zero=False):
+def _padded(shape, dtype, device):
     """A new tensor of `shape` whose rows start on 16-byte boundaries (a view of wider rows where they must)."""
     import torch
-    cols = _pitch(shape[-1], torch.empty((), dtype=dtype).element_size())
-    make = torch.zeros if zero else torch.empty
-    t = make((*shape[:-1], cols), dtype=dtype, device=device)
-    return t if cols == shape[-1] else t[..., :shape[-1]]
+    cols = _pitch(shape[-1], dtype.itemsize)
+    if cols == shape[-1]:
+        return torch.empty(shape, dtype=dtype, device=device)
+    return torch.empty((*shape[:-1], cols), dtype=dtype, device=device)[..., :shape[-1]]
 
 
 def _vector(t, n, dtype, name):
-    if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
         raise ValueError("%s must be %d contiguous %s values on the GPU, got %s %s" % (name, n, dtype, t.dtype, tuple(t.shape)))
-    return t
+    return t.data_ptr()
 
 
 class GroupedProduct:
@@ -503,76 +512,74 @@ class GroupedProduct:
         import torch
         self.groups, self.N, self.K, self.max_rows, self.keep_axis = groups, N, K, max_rows, keep_axis
         self.dtype = torch.bfloat16 if dtype is None else dtype
-        self.device = device
+        self._i32, self._f32, self._w_shape = torch.int32, torch.float32, (groups, N, K)
         code = _dtype_code(self.dtype)
-        self.desc = make_grouped_desc(groups, N, K, code, FLEXMOE_F32, keep_axis, max_rows, _pitch(K, self._es()),
-                                      _pitch(K, self._es()), _pitch(N, self._es()), _pitch(K, 2))
-        nbytes = flexmoe_grouped_workspace_bytes(self.desc, max_rows)
-        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-
-    def _es(self):
-        return 2 if _dtype_code(self.dtype) == FLEXMOE_BF16 else 4
+        es = self.dtype.itemsize
+        self.desc = make_grouped_desc(groups, N, K, code, FLEXMOE_F32, keep_axis, max_rows, _pitch(K, es), _pitch(K, es),
+                                      _pitch(N, es), _pitch(K, 2))
+        self._desc = ctypes.byref(self.desc)
+        self.workspace = torch.empty(flexmoe_grouped_workspace_bytes(self.desc, max_rows), dtype=torch.uint8, device=device)
+        self._ws = (self.workspace.data_ptr(), self.workspace.numel())
 
     def _groups(self, offsets, keep):
-        import torch
-        _vector(offsets, self.groups + 1, torch.int32, "offsets")
-        if keep is not None:
-            _vector(keep, self.groups, torch.int32, "keep")
+        return (_vector(offsets, self.groups + 1, self._i32, "offsets"),
+                None if keep is None else _vector(keep, self.groups, self._i32, "keep"))
 
     def forward(self, x, w, offsets, keep=None, y=None, stream=None):
         """y_r = x_r W_e^T for x [R, K], w [groups, N, K]."""
-        self._groups(offsets, keep)
-        R, d = x.shape[0], self.desc
+        R, d, dt = x.shape[0], self.desc, self.dtype
         if y is None:
-            y = _padded((R, self.N), self.dtype, x.device)
-        d.ldx, d.ldw = _matrix(x, (R, self.K), self.dtype, "x"), _matrix(w, (self.groups, self.N, self.K), self.dtype, "w")
-        d.ldy = _matrix(y, (R, self.N), self.dtype, "y")
-        flexmoe_grouped_forward(d, R, x, w, offsets, keep, y, self.workspace, stream=stream)
+            y = _padded((R, self.N), dt, x.device)
+        d.ldx, d.ldw = _matrix(x, (R, self.K), dt, "x"), _matrix(w, self._w_shape, dt, "w")
+        d.ldy = _matrix(y, (R, self.N), dt, "y")
+        _check(lib().flexmoe_grouped_forward(self._desc, R, x.data_ptr(), w.data_ptr(), *self._groups(offsets, keep),
+                                             y.data_ptr(), *self._ws, _stream(stream)))
         return y
 
     def input_grad(self, dy, w, offsets, keep=None, dx=None, stream=None):
         """dx_r = dy_r W_e for dy [R, N]."""
-        self._groups(offsets, keep)
-        R, d = dy.shape[0], self.desc
+        R, d, dt = dy.shape[0], self.desc, self.dtype
         if dx is None:
-            dx = _padded((R, self.K), self.dtype, dy.device)
-        d.ldy, d.ldw = _matrix(dy, (R, self.N), self.dtype, "dy"), _matrix(w, (self.groups, self.N, self.K), self.dtype, "w")
-        d.ldx = _matrix(dx, (R, self.K), self.dtype, "dx")
-        flexmoe_grouped_input_grad(d, R, dy, w, offsets, keep, dx, self.workspace, stream=stream)
+            dx = _padded((R, self.K), dt, dy.device)
+        d.ldy, d.ldw = _matrix(dy, (R, self.N), dt, "dy"), _matrix(w, self._w_shape, dt, "w")
+        d.ldx = _matrix(dx, (R, self.K), dt, "dx")
+        _check(lib().flexmoe_grouped_input_grad(self._desc, R, dy.data_ptr(), w.data_ptr(), *self._groups(offsets, keep),
+                                                dx.data_ptr(), *self._ws, _stream(stream)))
         return dx
 
     def weight_grad(self, dy, x, offsets, keep=None, dw=None, accumulate=False, dw_dtype=None, stream=None):
         """dW_e = dy^T x over e's rows, written to (or with accumulate added to) dw [groups, N, K]."""
-        import torch
-        self._groups(offsets, keep)
-        R, d = dy.shape[0], self.desc
+        R, d, dt = dy.shape[0], self.desc, self.dtype
         if dw is None:
             if accumulate:
                 raise ValueError("accumulate needs dw")
-            dw = _padded((self.groups, self.N, self.K), torch.float32 if dw_dtype is None else dw_dtype, dy.device)
+            dw = _padded(self._w_shape, self._f32 if dw_dtype is None else dw_dtype, dy.device)
         elif dw_dtype is not None and dw.dtype != dw_dtype:
             raise ValueError("dw is %s, not %s" % (dw.dtype, dw_dtype))
         d.dw_dtype = _dtype_code(dw.dtype)
-        d.ldy, d.ldx = _matrix(dy, (R, self.N), self.dtype, "dy"), _matrix(x, (R, self.K), self.dtype, "x")
-        d.lddw = _matrix(dw, (self.groups, self.N, self.K), dw.dtype, "dw")
-        flexmoe_grouped_weight_grad(d, R, dy, x, offsets, keep, dw, accumulate, self.workspace, stream=stream)
+        d.ldy, d.ldx = _matrix(dy, (R, self.N), dt, "dy"), _matrix(x, (R, self.K), dt, "x")
+        d.lddw = _matrix(dw, self._w_shape, dw.dtype, "dw")
+        _check(lib().flexmoe_grouped_weight_grad(self._desc, R, dy.data_ptr(), x.data_ptr(), *self._groups(offsets, keep),
+                                                 dw.data_ptr(), int(accumulate), *self._ws, _stream(stream)))
         return dw
 
 
 def quantize_rows(x, gate=None, q=None, scale=None, stream=None):
     """Rows of x (or silu(gate) * x) as whole numbers up to 127 and a scale each: (q int8 like x, scale)."""
     import torch
-    lead, cols = x.shape[:-1], x.shape[-1]
-    rows = int(np.prod(lead, dtype=np.int64))
-    ldx = _matrix(x, x.shape, x.dtype, "x")
-    if gate is not None and _matrix(gate, x.shape, x.dtype, "gate") != ldx:
+    shape = x.shape
+    cols = shape[-1]
+    rows = shape[0] if len(shape) == 2 else x.numel() // cols
+    ldx = _matrix(x, shape, x.dtype, "x")
+    if gate is not None and _matrix(gate, shape, x.dtype, "gate") != ldx:
         raise ValueError("x and gate must have the same strides")
     if q is None:
-        q = _padded(x.shape, torch.int8, x.device)
+        q = _padded(shape, torch.int8, x.device)
     if scale is None:
-        scale = torch.empty(lead, dtype=torch.float32, device=x.device)
-    flexmoe_quantize_rows(rows, cols, _dtype_code(x.dtype), x, gate, ldx, q, _matrix(q, x.shape, torch.int8, "q"),
-                          _vector(scale, rows, torch.float32, "scale"), stream)
+        scale = torch.empty(shape[:-1], dtype=torch.float32, device=x.device)
+    _check(lib().flexmoe_quantize_rows(rows, cols, _dtype_code(x.dtype), x.data_ptr(), None if gate is None else gate.data_ptr(), ldx,
+                                       q.data_ptr(), _matrix(q, shape, torch.int8, "q"), _vector(scale, rows, torch.float32, "scale"),
+                                       _stream(stream)))
     return q, scale
 
 
@@ -587,15 +594,17 @@ class Int8Product:
     def __init__(self, w, w_scale, max_rows, keep_axis="none", out_dtype=None):
         import torch
         self.groups, self.N, self.K = w.shape
-        self.w, self.w_scale, self.max_rows = w, _vector(w_scale, self.groups * self.N, torch.float32, "w_scale"), max_rows
+        self.w, self.w_scale, self.max_rows = w, w_scale, max_rows
+        self._i8, self._i32, self._f32 = torch.int8, torch.int32, torch.float32
+        _vector(w_scale, self.groups * self.N, torch.float32, "w_scale")
         self.out_dtype = torch.bfloat16 if out_dtype is None else out_dtype
         self.desc = make_grouped_desc(self.groups, self.N, self.K, _dtype_code(self.out_dtype), FLEXMOE_F32, keep_axis, max_rows,
-                                      _pitch(self.K, 1), _matrix(w, w.shape, torch.int8, "w"),
-                                      _pitch(self.N, 2 if self.out_dtype == torch.bfloat16 else 4))
+                                      _pitch(self.K, 1), _matrix(w, w.shape, torch.int8, "w"), _pitch(self.N, self.out_dtype.itemsize))
+        self._desc = ctypes.byref(self.desc)
         self.workspace = torch.empty(flexmoe_quantized_workspace_bytes(self.desc, max_rows), dtype=torch.uint8, device=w.device)
+        self._ws = (self.workspace.data_ptr(), self.workspace.numel())
         self.q = _padded((max_rows, self.K), torch.int8, w.device)
         self.q_scale = torch.empty(max_rows, dtype=torch.float32, device=w.device)
-        self.offsets = None
 
     @classmethod
     def from_weights(cls, w, max_rows, keep_axis="none", out_dtype=None):
@@ -605,26 +614,37 @@ class Int8Product:
     def __call__(self, x, offsets=None, keep=None, gate=None, y=None, stream=None):
         """x [R, K] bf16 or fp32 (with gate: silu(gate) * x); offsets may be left out for one group."""
         R = x.shape[0]
-        if R > self.max_rows:
-            raise ValueError("%d rows, max_rows is %d" % (R, self.max_rows))
-        q, scale = quantize_rows(x, gate, self.q[:R], self.q_scale[:R], stream)
-        return self.product(q, scale, offsets, keep, y, stream)
+        if x.shape != (R, self.K) or R > self.max_rows:
+            raise ValueError("x must be [R, %d] with at most %d rows, got %s" % (self.K, self.max_rows, tuple(x.shape)))
+        stream = _stream(stream)
+        ldx = _matrix(x, x.shape, x.dtype, "x")
+        if gate is not None and _matrix(gate, x.shape, x.dtype, "gate") != ldx:
+            raise ValueError("x and gate must have the same strides")
+        q, scale, d = self.q.data_ptr(), self.q_scale.data_ptr(), self.desc
+        ldq = self.q.stride(0) if self.max_rows > 1 else _pitch(self.K, 1)
+        _check(lib().flexmoe_quantize_rows(R, self.K, _dtype_code(x.dtype), x.data_ptr(), None if gate is None else gate.data_ptr(), ldx,
+                                           q, ldq, scale, stream))
+        d.ldx = ldq
+        return self._product(R, q, scale, offsets, keep, y, x.device, stream)
 
     def product(self, q, q_scale, offsets=None, keep=None, y=None, stream=None):
-        import torch
-        R, d = q.shape[0], self.desc
+        R = q.shape[0]
+        self.desc.ldx = _matrix(q, (R, self.K), self._i8, "q")
+        return self._product(R, q.data_ptr(), _vector(q_scale, R, self._f32, "q_scale"), offsets, keep, y, q.device, _stream(stream))
+
+    def _product(self, R, q, q_scale, offsets, keep, y, device, stream):
         if offsets is None:
+            import torch
             if self.groups != 1:
                 raise ValueError("offsets are needed for %d groups" % self.groups)
-            offsets = torch.tensor([0, R], dtype=torch.int32, device=q.device)
-        _vector(offsets, self.groups + 1, torch.int32, "offsets")
-        if keep is not None:
-            _vector(keep, self.groups, torch.int32, "keep")
+            offsets = torch.tensor([0, R], dtype=torch.int32, device=device)
         if y is None:
-            y = _padded((R, self.N), self.out_dtype, q.device)
-        d.ldx, d.ldy = _matrix(q, (R, self.K), torch.int8, "q"), _matrix(y, (R, self.N), self.out_dtype, "y")
-        flexmoe_quantized_forward(d, R, q, _vector(q_scale, R, torch.float32, "q_scale"), self.w, self.w_scale, offsets, keep, y,
-                                  self.workspace, stream=stream)
+            y = _padded((R, self.N), self.out_dtype, device)
+        self.desc.ldy = _matrix(y, (R, self.N), self.out_dtype, "y")
+        _check(lib().flexmoe_quantized_forward(self._desc, R, q, q_scale, self.w.data_ptr(), self.w_scale.data_ptr(),
+                                               _vector(offsets, self.groups + 1, self._i32, "offsets"),
+                                               None if keep is None else _vector(keep, self.groups, self._i32, "keep"),
+                                               y.data_ptr(), *self._ws, stream))
         return y
 
 
@@ -675,6 +695,7 @@ class AdamW:
         stride = ctypes.sizeof(flexmoe_adamw_tensor) // 8
         self._grads = np.frombuffer(self._table, dtype=np.uint64)[flexmoe_adamw_tensor.grad.offset // 8::stride]
         self.sizes, self._param_code = sizes, _dtype_code(dt)
+        self._tensor = torch.Tensor
 
     @staticmethod
     def _like(t, n, dtype, name):
@@ -684,10 +705,16 @@ class AdamW:
 
     def step(self, grads, lr, grad_scale=1.0, stream=None):
         """One step with the gradients `grads` (bf16 or fp32, all alike, contiguous)."""
+        T = self._tensor
         if len(grads) != len(self.sizes):
             raise ValueError("%d gradients for %d parameters" % (len(grads), len(self.sizes)))
+        # unbound methods over the list: a third of the time of a Python function per tensor
+        if list(map(T.numel, grads)) != self.sizes or not all(map(T.is_contiguous, grads)):
+            raise ValueError("every gradient must be contiguous and as long as its parameter")
         dt = grads[0].dtype
-        self._grads[:] = [self._like(g, n, dt, "grads") for g, n in zip(grads, self.sizes)]
+        if not all(g.dtype is dt and g.is_cuda for g in grads):
+            raise ValueError("the gradients must be of one dtype and on the GPU")
+        self._grads[:] = list(map(T.data_ptr, grads))
         d = flexmoe_adamw_desc(self._param_code, _dtype_code(dt), self.state_bits, self.seed & 0xffffffff, self.t + 1, lr,
                                self.betas[0], self.betas[1], self.eps, self.weight_decay, grad_scale)
         flexmoe_adamw_step(d, self._table, stream=stream)

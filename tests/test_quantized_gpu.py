@@ -15,7 +15,7 @@ def reference_rows(v):
     v = np.asarray(v, np.float32)
     top = np.abs(v).max(-1, keepdims=True)
     with np.errstate(divide="ignore", invalid="ignore"):
-        q = np.rint(v * np.where(top > 0, np.float32(127) / top, np.float32(0)).astype(np.float32))
+        q = np.rint(v * np.where(top > 0, np.float32(1) / top * np.float32(127), np.float32(0)).astype(np.float32))
     return np.clip(q, -127, 127).astype(np.int8), (top / np.float32(127))[..., 0]
 
 
