@@ -154,7 +154,9 @@ Plan plan(const flexmoe_grouped_desc& D, GroupedForm form, bool int8, int R) {
     // 2048 at 34 / 136 / 273 / 546 rows each: 130 to 159, 189 to 209, 247 to
     // 253, 340 to 336 us; 8 of 14336 x 4096 at 32 / 256 / 512: 349 to 385, 589
     // to 543, 795 to 724.
-    if (form == kWeightGrad && pl.splits == 1 && R < 256LL * D.groups) pl.tiles = kSlim;
+    // (fp32 only up to 1024 rows: those workgroups have no registers for a second
+    // level of sums.)
+    if (form == kWeightGrad && pl.splits == 1 && R < 256LL * D.groups && (pl.elem == kElemBf16 || R <= 1024)) pl.tiles = kSlim;
     if (pl.splits > 1) pl.workspace = (size_t)(out * pl.splits);
     return pl;
 }

@@ -90,6 +90,16 @@ __global__ __launch_bounds__(GT, kSlim ? 4 : 2) void grouped_mid_kernel(GroupedP
         auto request_a = [&](int kt, int stage) { la.request(kt, sa + stage * STAGE + wave * (NA * 1024)); };
         auto request_b = [&](int kt, int stage) { lb.request(kt, sb + stage * STAGE + wave * (NI * 1024)); };
         typename E::Acc acc[4][MF];
+        // fp32: sums of 256 products are added to a second set, so that an
+        // error grows with the number of those sums, not of products
+        constexpr bool kTwoLevels = E::kBytes == 4 && !kSlim;
+        constexpr int kFlush = 8;
+        typename E::Acc total[kTwoLevels ? 4 : 1][kTwoLevels ? MF : 1];
+        if constexpr (kTwoLevels)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < MF; ++i) total[j][i] = typename E::Acc{0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -143,6 +153,37 @@ __global__ __launch_bounds__(GT, kSlim ? 4 : 2) void grouped_mid_kernel(GroupedP
             const unsigned char* at = sa + (kt & 1) * STAGE;
             const unsigned char* bt = sb + st_b * STAGE;
             st_b = st_b == 2 ? 0 : st_b + 1;
+            if constexpr (kTwoLevels) {
+                // one K step at a time: the fragments of both would not fit
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    typename E::Frag fa[MF], fb[4];
+                    read_step<E, kAcrossB, 4>(bt, wn * 64, s, fb);
+                    read_step<E, kAcrossA, MF>(at, wm * 16 * MF, s, fa);
+                    if constexpr (!kAcrossA)
+                        if (kt == nk - 1 && depth % E::kPer) {
+                            const int valid = depth - kt * E::kDepth - (s * 4 + lc) * E::kPer;
+#pragma unroll
+                            for (int i = 0; i < MF; ++i) fa[i] = head<E>(fa[i], valid);
+                            if constexpr (!kAcrossB)
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) fb[j] = head<E>(fb[j], valid);
+                        }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int i = 0; i < MF; ++i) acc[j][i] = E::mma(fb[j], fa[i], acc[j][i]);
+                }
+                if (kt % kFlush == kFlush - 1)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int i = 0; i < MF; ++i) {
+                            total[j][i] += acc[j][i];
+                            acc[j][i] = typename E::Acc{0, 0, 0, 0};
+                        }
+                continue;
+            } else {
             typename E::Frag fa[2][MF], fb[2][4];
             read_frags<E, kAcrossB, 4>(bt, wn * 64, fb);
             read_frags<E, kAcrossA, MF>(at, wm * 16 * MF, fa);
@@ -165,10 +206,16 @@ __global__ __launch_bounds__(GT, kSlim ? 4 : 2) void grouped_mid_kernel(GroupedP
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int i = 0; i < MF; ++i) acc[j][i] = E::mma(fb[s][j], fa[s][i], acc[j][i]);
+            }
         }
         }
         __builtin_amdgcn_s_waitcnt(waitcnt_vm(0) & kWaitLgkm0);  // no request may outlive the loop
 
+        if constexpr (kTwoLevels)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < MF; ++i) acc[j][i] += total[j][i];
         barrier_no_fence();  // every wave has read its fragments: LDS becomes the stores' scratch
         store_tile<E, kForm, kBf16Out, MF>(
             p, t, t.r0 + wm * 16 * MF, smem + wave * 4096, [&](int q) { return t.c0 + wn * 64 + q * 4; },
