@@ -1,11 +1,12 @@
-"""Build libflexmoe.so (HIP, gfx950) in-tree with hipcc.
+"""Build libflexmoe.so (HIP, gfx950) and the _tensors module in-tree.
 
     python -m paper_2606_27866_amd.build
 
 The library is one shared object holding every kernel and the C ABI of
 include/flexmoe.h.  All device code is compiled with packed-fp32 arithmetic
 disabled (-packed-fp32-ops); hipcc's host pass warns that it does not know
-the feature, which is harmless.
+the feature, which is harmless.  _tensors.so (host code, g++) reads lists of
+tensors for the binding.
 """
 from __future__ import annotations
 
@@ -18,6 +19,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libflexmoe.so")
+TENSORS = os.path.join(HERE, "_tensors.so")
+TENSORS_SRC = os.path.join(CSRC, "tensor_table.cpp")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
@@ -37,7 +40,26 @@ def compile_command(out: str, extra=()):
             "-I", os.path.join(ROOT, "include"), "-o", out, *extra, *sources()]
 
 
+def tensors_command(out: str):
+    import sysconfig
+
+    import torch
+    from torch.utils.cpp_extension import include_paths
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    inc = [*include_paths(), sysconfig.get_path("include")]
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-o", out, TENSORS_SRC, *["-I" + p for p in inc], "-L" + lib,
+            "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"]
+
+
+def build_tensors() -> str:
+    tmp = TENSORS + ".tmp%d" % os.getpid()
+    subprocess.run(tensors_command(tmp), check=True)
+    os.replace(tmp, TENSORS)
+    return TENSORS
+
+
 def build(verbose: bool = False) -> str:
+    build_tensors()
     tmp = LIB + ".tmp%d" % os.getpid()
     cmd = compile_command(tmp)
     if verbose:
@@ -55,10 +77,11 @@ def build(verbose: bool = False) -> str:
 
 
 def is_stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(TENSORS):
         return True
     t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(f) > t for f in sources() + headers())
+    return (any(os.path.getmtime(f) > t for f in sources() + headers())
+            or os.path.getmtime(TENSORS_SRC) > os.path.getmtime(TENSORS))
 
 
 if __name__ == "__main__":

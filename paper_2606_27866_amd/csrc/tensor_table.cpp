@@ -1,0 +1,53 @@
+// Python module _tensors: the addresses of a list of tensors, checked, in one
+// call.  An optimizer step takes a list of hundreds of gradients; reading four
+// attributes of each through Python costs 0.3 us a tensor, this 0.01.
+#include <Python.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+namespace {
+
+// column(tensors: list, sizes: address of int64[len], code: 0 fp32 / 1 bf16 / 2 uint8, dst: address, stride: bytes)
+// writes tensor i's address to dst + i * stride.  Returns -1, or the index of the
+// first tensor that is not contiguous on the GPU, of that type and of sizes[i]
+// values (nothing after it is written).
+PyObject* column(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 5 || !PyList_Check(args[0])) {
+        PyErr_SetString(PyExc_TypeError, "column(list, sizes, code, dst, stride)");
+        return nullptr;
+    }
+    const int64_t* sizes = static_cast<const int64_t*>(PyLong_AsVoidPtr(args[1]));
+    const long code = PyLong_AsLong(args[2]);
+    char* dst = static_cast<char*>(PyLong_AsVoidPtr(args[3]));
+    const long stride = PyLong_AsLong(args[4]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::ScalarType want = code == 0 ? at::kFloat : code == 1 ? at::kBFloat16 : at::kByte;
+    const Py_ssize_t count = PyList_GET_SIZE(args[0]);
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        PyObject* o = PyList_GET_ITEM(args[0], i);
+        if (!THPVariable_Check(o)) return PyLong_FromSsize_t(i);
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || t.scalar_type() != want || t.numel() != sizes[i] ||
+            !t.is_contiguous())
+            return PyLong_FromSsize_t(i);
+        *reinterpret_cast<void**>(dst + i * stride) = t.data_ptr();
+    }
+    return PyLong_FromLong(-1);
+}
+
+PyObject* guarded_column(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    try {
+        return column(self, args, n);
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
+PyMethodDef methods[] = {{"column", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(guarded_column)), METH_FASTCALL,
+                          "addresses of a list of tensors into a table"},
+                         {nullptr, nullptr, 0, nullptr}};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__tensors() { return PyModule_Create(&module); }

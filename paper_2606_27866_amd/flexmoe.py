@@ -14,7 +14,7 @@ from typing import Optional, Sequence
 
 import numpy as np
 
-from .build import LIB
+from .build import LIB, TENSORS
 
 FLEXMOE_F32 = 0
 FLEXMOE_BF16 = 1
@@ -182,6 +182,21 @@ def lib():
         L.flexmoe_last_error.restype = ctypes.c_char_p
         _lib = L
     return _lib
+
+
+_tensors = None
+
+
+def tensors():
+    """The _tensors module (built in-tree by build.py); raise if it is absent."""
+    global _tensors
+    if _tensors is None:
+        if not os.path.exists(TENSORS):
+            raise RuntimeError("_tensors.so is not built (%s); run `python -m paper_2606_27866_amd.build`" % TENSORS)
+        import torch  # noqa: F401  (its libraries are loaded first)
+        from . import _tensors as module
+        _tensors = module
+    return _tensors
 
 
 def _check(rc: int):
@@ -691,11 +706,11 @@ class AdamW:
                                         for s in (self.m_scale, self.v_scale))
             if masters is not None:
                 e.master = self._like(masters[i], n, torch.float32, "masters")
-        # the table's gradient column, filled by every step
-        stride = ctypes.sizeof(flexmoe_adamw_tensor) // 8
-        self._grads = np.frombuffer(self._table, dtype=np.uint64)[flexmoe_adamw_tensor.grad.offset // 8::stride]
+        # the table's gradient column is filled by every step
+        self._n = np.array(sizes, dtype=np.int64)
+        self._column = (self._n.ctypes.data, ctypes.addressof(self._table) + flexmoe_adamw_tensor.grad.offset,
+                        ctypes.sizeof(flexmoe_adamw_tensor))
         self.sizes, self._param_code = sizes, _dtype_code(dt)
-        self._tensor = torch.Tensor
 
     @staticmethod
     def _like(t, n, dtype, name):
@@ -705,17 +720,17 @@ class AdamW:
 
     def step(self, grads, lr, grad_scale=1.0, stream=None):
         """One step with the gradients `grads` (bf16 or fp32, all alike, contiguous)."""
-        T = self._tensor
+        grads = grads if type(grads) is list else list(grads)
         if len(grads) != len(self.sizes):
             raise ValueError("%d gradients for %d parameters" % (len(grads), len(self.sizes)))
-        # unbound methods over the list: a third of the time of a Python function per tensor
-        if list(map(T.numel, grads)) != self.sizes or not all(map(T.is_contiguous, grads)):
-            raise ValueError("every gradient must be contiguous and as long as its parameter")
-        dt = grads[0].dtype
-        if not all(g.dtype is dt and g.is_cuda for g in grads):
-            raise ValueError("the gradients must be of one dtype and on the GPU")
-        self._grads[:] = list(map(T.data_ptr, grads))
-        d = flexmoe_adamw_desc(self._param_code, _dtype_code(dt), self.state_bits, self.seed & 0xffffffff, self.t + 1, lr,
+        code = _dtype_code(grads[0].dtype)
+        sizes, dst, stride = self._column
+        bad = tensors().column(grads, sizes, code, dst, stride)
+        if bad >= 0:
+            g = grads[bad]
+            raise ValueError("gradient %d: need %d contiguous %s values on the GPU, got %s %s"
+                             % (bad, self.sizes[bad], grads[0].dtype, g.dtype, tuple(g.shape)))
+        d = flexmoe_adamw_desc(self._param_code, code, self.state_bits, self.seed & 0xffffffff, self.t + 1, lr,
                                self.betas[0], self.betas[1], self.eps, self.weight_decay, grad_scale)
         flexmoe_adamw_step(d, self._table, stream=stream)
         self.t += 1
