@@ -24,9 +24,13 @@
 //
 // Bound by memory: 28 bytes per value with 32-bit states (bf16 parameter,
 // master copy, bf16 gradient), 16 with 8-bit ones.  A wave takes 256
-// consecutive values at a time (4 per lane: 16-byte accesses of fp32), four of
-// those in flight.  The list travels in the kernel's arguments, 56 tensors a
-// launch; workgroups are dealt to tensors by 4096 values.
+// consecutive values at a time (4 per lane: 16-byte accesses of fp32), with 8-bit
+// states one of those, with 32-bit ones four, or two in lists of less than 2^24
+// values (100 M values, bf16 with master: 8 bits 267 us for one, 276 for two, 279
+// for four: 6.0 TB/s; 32 bits 483, 481, 468: 6.0 TB/s; 1.5 M values in 192
+// tensors, 32 bits: 19, 17, 22 us).  Every value is read once and written once,
+// with the non-temporal hint (8 bits 307 -> 279 us, 32 bits 525 -> 468).  The
+// list travels in the kernel's arguments, 56 tensors a launch.
 #include <algorithm>
 #include <cmath>
 
@@ -39,8 +43,9 @@ namespace {
 
 constexpr int AT = 256;            // threads
 constexpr int kBlock = 256;        // values of a block of states
-constexpr int kUnroll = 4;         // blocks per wave
-constexpr int kChunk = AT / 64 * kUnroll * kBlock;  // values per workgroup: 4096
+
+// Values of a workgroup whose waves take `unroll` blocks each.
+constexpr int chunk(int unroll) { return AT / 64 * unroll * kBlock; }
 constexpr int kTensors = 56;       // per launch: the arguments stay below 4 KB
 
 struct AdamwArgs {
@@ -83,11 +88,13 @@ __device__ __forceinline__ float v_value(uint32_t code, float scale) {
     return s * s;
 }
 
+typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
+
 // 4 values of lane-contiguous memory; n of them exist (kFull: all, and aligned).
 template <bool kFull>
 __device__ __forceinline__ void load4(const float* p, int n, float (&v)[4]) {
     if constexpr (kFull) {
-        const floatx4 w = *reinterpret_cast<const floatx4*>(p);
+        const floatx4 w = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(p));
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[k] = w[k];
     } else {
@@ -98,7 +105,7 @@ __device__ __forceinline__ void load4(const float* p, int n, float (&v)[4]) {
 template <bool kFull>
 __device__ __forceinline__ void load4(const bf16_t* p, int n, float (&v)[4]) {
     if constexpr (kFull) {
-        const uint2 w = *reinterpret_cast<const uint2*>(p);
+        const uintx2 w = __builtin_nontemporal_load(reinterpret_cast<const uintx2*>(p));
         v[0] = __uint_as_float(w.x << 16), v[1] = __uint_as_float(w.x & 0xffff0000u);
         v[2] = __uint_as_float(w.y << 16), v[3] = __uint_as_float(w.y & 0xffff0000u);
     } else {
@@ -109,7 +116,7 @@ __device__ __forceinline__ void load4(const bf16_t* p, int n, float (&v)[4]) {
 template <bool kFull>
 __device__ __forceinline__ void load4(const uint8_t* p, int n, uint32_t& v) {
     if constexpr (kFull) {
-        v = *reinterpret_cast<const uint32_t*>(p);
+        v = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p));
     } else {
         v = 0;
 #pragma unroll
@@ -120,7 +127,7 @@ __device__ __forceinline__ void load4(const uint8_t* p, int n, uint32_t& v) {
 template <bool kFull>
 __device__ __forceinline__ void store4(float* p, int n, const float (&v)[4]) {
     if constexpr (kFull) {
-        *reinterpret_cast<floatx4*>(p) = floatx4{v[0], v[1], v[2], v[3]};
+        __builtin_nontemporal_store(floatx4{v[0], v[1], v[2], v[3]}, reinterpret_cast<floatx4*>(p));
     } else {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
@@ -131,7 +138,7 @@ template <bool kFull>
 __device__ __forceinline__ void store4(bf16_t* p, int n, const float (&v)[4]) {
     if constexpr (kFull) {
         const bf16x2_t a = __builtin_convertvector(float2_t{v[0], v[1]}, bf16x2_t), b = __builtin_convertvector(float2_t{v[2], v[3]}, bf16x2_t);
-        *reinterpret_cast<uint2*>(p) = make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+        __builtin_nontemporal_store(uintx2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)}, reinterpret_cast<uintx2*>(p));
     } else {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
@@ -141,7 +148,7 @@ __device__ __forceinline__ void store4(bf16_t* p, int n, const float (&v)[4]) {
 template <bool kFull>
 __device__ __forceinline__ void store4(uint8_t* p, int n, uint32_t v) {
     if constexpr (kFull) {
-        *reinterpret_cast<uint32_t*>(p) = v;
+        __builtin_nontemporal_store(v, reinterpret_cast<uint32_t*>(p));
     } else {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
@@ -233,7 +240,7 @@ __device__ __forceinline__ void step_values(const AdamwArgs& a, const flexmoe_ad
     }
 }
 
-template <typename P, typename G, int kBits, bool kMaster>
+template <typename P, typename G, int kBits, int kUnroll, bool kMaster>
 __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const flexmoe_adamw_tensor& t, size_t at, uint32_t key) {
     const int lane = threadIdx.x & 63;
     const size_t left = (size_t)t.n - at;  // from this wave's first value on
@@ -255,18 +262,18 @@ __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const flexmoe_ada
     }
 }
 
-template <typename P, typename G, int kBits>
+template <typename P, typename G, int kBits, int kUnroll>
 __global__ __launch_bounds__(AT) void adamw_kernel(AdamwArgs a) {
     static_assert(kTensors < 64, "one lane per tensor");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t f = a.first[min(lane, kTensors)];
     const int j = __popcll(__ballot(lane < kTensors && f <= blockIdx.x)) - 1;  // tensors without values share their start
     const flexmoe_adamw_tensor& t = a.t[j];
-    const size_t at = (size_t)(blockIdx.x - a.first[j]) * kChunk + wave * (kUnroll * kBlock);
+    const size_t at = (size_t)(blockIdx.x - a.first[j]) * chunk(kUnroll) + wave * (kUnroll * kBlock);
     if (at >= (size_t)t.n) return;
     const uint32_t key = a.key + (uint32_t)(a.tensor0 + j) * kTensorStep;
-    if (sizeof(P) == 2 && t.master) step_chunk<P, G, kBits, true>(a, t, at, key);
-    else step_chunk<P, G, kBits, false>(a, t, at, key);
+    if (sizeof(P) == 2 && t.master) step_chunk<P, G, kBits, kUnroll, true>(a, t, at, key);
+    else step_chunk<P, G, kBits, kUnroll, false>(a, t, at, key);
 }
 
 template <typename O>
@@ -285,6 +292,14 @@ __global__ __launch_bounds__(AT) void adamw_read_kernel(const uint8_t* m, const 
     for (int k = 0; k < 4; ++k) x[k] = m_value((a >> (8 * k)) & 255u, sm), y[k] = v_value((b >> (8 * k)) & 255u, sv);
     if (full) store4<true>(om + i, 4, x), store4<true>(ov + i, 4, y);
     else store4<false>(om + i, c, x), store4<false>(ov + i, c, y);
+}
+
+template <int kBits, int kUnroll>
+void launch(const AdamwArgs& a, bool param_bf16, bool grad_bf16, unsigned grid, hipStream_t s) {
+    if (param_bf16 && grad_bf16) adamw_kernel<bf16_t, bf16_t, kBits, kUnroll><<<grid, AT, 0, s>>>(a);
+    else if (param_bf16) adamw_kernel<bf16_t, float, kBits, kUnroll><<<grid, AT, 0, s>>>(a);
+    else if (grad_bf16) adamw_kernel<float, bf16_t, kBits, kUnroll><<<grid, AT, 0, s>>>(a);
+    else adamw_kernel<float, float, kBits, kUnroll><<<grid, AT, 0, s>>>(a);
 }
 
 bool misaligned(const void* p, uintptr_t mask) { return ((uintptr_t)p & mask) != 0; }
@@ -337,14 +352,18 @@ int flexmoe_adamw_step(const flexmoe_adamw_desc* D, const flexmoe_adamw_tensor* 
     a.eps = (float)D->eps;
     a.key = D->seed * kSeedStep + (uint32_t)D->step * kTimeStep;
     const hipStream_t s = (hipStream_t)stream;
+    uint64_t total = 0;
+    for (int i = 0; i < count; ++i) total += (uint64_t)tensors[i].n;
+    const int unroll = D->state_bits == 8 ? 1 : total < (1u << 24) ? 2 : 4;
+    const uint64_t per = (uint64_t)chunk(unroll);
     for (int i = 0; i < count;) {
-        // as many tensors as the arguments and a grid hold; a tensor longer
-        // than a grid goes alone in 2^31 workgroups (2^40 values are 2^28)
+        // as many tensors as the arguments and a grid hold (2^40 values alone
+        // are 2^30 workgroups)
         uint64_t groups = 0;
         int n = 0;
         a.tensor0 = i;
         for (; i + n < count && n < kTensors; ++n) {
-            const uint64_t g = ((uint64_t)tensors[i + n].n + kChunk - 1) / kChunk;
+            const uint64_t g = ((uint64_t)tensors[i + n].n + per - 1) / per;
             if (n > 0 && groups + g > (1u << 30)) break;
             a.t[n] = tensors[i + n];
             a.first[n] = (uint32_t)groups;
@@ -354,15 +373,10 @@ int flexmoe_adamw_step(const flexmoe_adamw_desc* D, const flexmoe_adamw_tensor* 
         for (int k = n; k <= kTensors; ++k) a.first[k] = 0xffffffffu;
         if (!groups) continue;
         const unsigned grid = (unsigned)groups;
-        const bool pb = D->param_dtype == FLEXMOE_BF16, gb = D->grad_dtype == FLEXMOE_BF16, eight = D->state_bits == 8;
-        if (pb && gb && eight) adamw_kernel<bf16_t, bf16_t, 8><<<grid, AT, 0, s>>>(a);
-        else if (pb && gb) adamw_kernel<bf16_t, bf16_t, 32><<<grid, AT, 0, s>>>(a);
-        else if (pb && eight) adamw_kernel<bf16_t, float, 8><<<grid, AT, 0, s>>>(a);
-        else if (pb) adamw_kernel<bf16_t, float, 32><<<grid, AT, 0, s>>>(a);
-        else if (gb && eight) adamw_kernel<float, bf16_t, 8><<<grid, AT, 0, s>>>(a);
-        else if (gb) adamw_kernel<float, bf16_t, 32><<<grid, AT, 0, s>>>(a);
-        else if (eight) adamw_kernel<float, float, 8><<<grid, AT, 0, s>>>(a);
-        else adamw_kernel<float, float, 32><<<grid, AT, 0, s>>>(a);
+        const bool pb = D->param_dtype == FLEXMOE_BF16, gb = D->grad_dtype == FLEXMOE_BF16;
+        if (unroll == 1) launch<8, 1>(a, pb, gb, grid, s);
+        else if (unroll == 2) launch<32, 2>(a, pb, gb, grid, s);
+        else launch<32, 4>(a, pb, gb, grid, s);
         const hipError_t err = hipGetLastError();
         if (err != hipSuccess) return hip_fail(err, "adamw_step launch");
     }
