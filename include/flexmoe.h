@@ -479,7 +479,7 @@ int flexmoe_quantized_forward(const flexmoe_grouped_desc *desc, int32_t R, const
  * same call gives the same bits.  A block that gets a NaN or an infinity stands
  * for NaN from then on.  flexmoe_adamw_read_state writes what 8-bit states of
  * one tensor stand for as dtype (checkpoints, inspection).
- * Any n >= 0 and any alignment to the elements (16-byte alignment is fastest;
+ * n from 0 to 2^33 and any alignment to the elements (16-byte alignment is fastest;
  * scales, fp32 arrays: 4 bytes).  step >= 1, betas in [0, 1), eps >= 1e-30. */
 typedef struct flexmoe_adamw_tensor {
     void *param;        /* param_dtype                                           */

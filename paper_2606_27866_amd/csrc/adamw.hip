@@ -46,6 +46,8 @@ constexpr int kBlock = 256;        // values of a block of states
 
 // Values of a workgroup whose waves take `unroll` blocks each.
 constexpr int chunk(int unroll) { return AT / 64 * unroll * kBlock; }
+constexpr int64_t kMaxValues = 1LL << 33;   // of a tensor: its workgroups' threads are fewer than 2^32
+constexpr uint64_t kMaxGroups = 1u << 24;  // of a launch, for the same reason
 constexpr int kTensors = 56;       // per launch: the arguments stay below 4 KB
 
 struct AdamwArgs {
@@ -329,7 +331,7 @@ int flexmoe_adamw_step(const flexmoe_adamw_desc* D, const flexmoe_adamw_tensor* 
     for (int i = 0; i < count; ++i) {
         const flexmoe_adamw_tensor& t = tensors[i];
         if (t.n < 0) return fail(FLEXMOE_EINVAL, "adamw_step: tensor %d has n = %lld", i, (long long)t.n);
-        if (t.n > (1LL << 40)) return fail(FLEXMOE_ESHAPE, "adamw_step: tensor %d has n = %lld above 2^40", i, (long long)t.n);
+        if (t.n > kMaxValues) return fail(FLEXMOE_ESHAPE, "adamw_step: tensor %d has n = %lld above 2^33", i, (long long)t.n);
         if (t.n == 0) continue;
         if (!t.param || !t.grad || !t.m || !t.v) return fail(FLEXMOE_EINVAL, "adamw_step: tensor %d has a NULL pointer", i);
         if ((D->state_bits == 8) != (t.m_scale && t.v_scale) || (D->state_bits == 32 && (t.m_scale || t.v_scale)))
@@ -357,14 +359,13 @@ int flexmoe_adamw_step(const flexmoe_adamw_desc* D, const flexmoe_adamw_tensor* 
     const int unroll = D->state_bits == 8 ? 1 : total < (1u << 24) ? 2 : 4;
     const uint64_t per = (uint64_t)chunk(unroll);
     for (int i = 0; i < count;) {
-        // as many tensors as the arguments and a grid hold (2^40 values alone
-        // are 2^30 workgroups)
+        // as many tensors as the arguments and a grid hold
         uint64_t groups = 0;
         int n = 0;
         a.tensor0 = i;
         for (; i + n < count && n < kTensors; ++n) {
             const uint64_t g = ((uint64_t)tensors[i + n].n + per - 1) / per;
-            if (n > 0 && groups + g > (1u << 30)) break;
+            if (n > 0 && groups + g >= kMaxGroups) break;
             a.t[n] = tensors[i + n];
             a.first[n] = (uint32_t)groups;
             groups += g;
@@ -388,7 +389,7 @@ int flexmoe_adamw_read_state(int64_t n, const void* m, const void* v, const floa
     if (dtype != FLEXMOE_F32 && dtype != FLEXMOE_BF16)
         return fail(FLEXMOE_EDTYPE, "adamw_read_state: dtype %d is neither FLEXMOE_F32 nor FLEXMOE_BF16", dtype);
     if (n < 0) return fail(FLEXMOE_EINVAL, "adamw_read_state: n = %lld is negative", (long long)n);
-    if (n > (1LL << 40)) return fail(FLEXMOE_ESHAPE, "adamw_read_state: n = %lld above 2^40", (long long)n);
+    if (n > kMaxValues) return fail(FLEXMOE_ESHAPE, "adamw_read_state: n = %lld above 2^33", (long long)n);
     if (n == 0) return FLEXMOE_OK;
     if (!m || !v || !m_scale || !v_scale || !m_out || !v_out) return fail(FLEXMOE_EINVAL, "adamw_read_state: a pointer is NULL");
     const uintptr_t om = dtype == FLEXMOE_BF16 ? 1 : 3;

@@ -34,6 +34,7 @@ struct GroupedParams {
     int splits;               // parts of the reduction, each a workgroup's
     int out_bf16;             // C is bf16 (else fp32)
     int slim;                 // 128 x 128 tiles: one LDS stage, four workgroups per compute unit
+    int once;                 // weights of groups with one row tile carry the non-temporal hint
     int accumulate;           // weight gradient: C += instead of C =
 };
 
@@ -46,6 +47,7 @@ struct GroupedTile {
     int rlim, clim;           // C rows and columns that exist; the rest are zeros
     int d0, d1;               // the part of the reduction
     int split;
+    int row_tiles;            // row tiles of the group (weight gradient: of C)
 };
 
 __device__ __forceinline__ int group_begin(const GroupedParams& p, int e) { return min(max(p.offsets[e], 0), p.R); }
@@ -121,6 +123,7 @@ __device__ __forceinline__ bool grouped_tile(const GroupedParams& p, int L, int 
         t.e = L / per;
         if (t.e >= p.E) return false;
         const int local = L - t.e * per;
+        t.row_tiles = p.tiles_r;
         ct = local % p.tiles_c;
         mt = local / p.tiles_c % p.tiles_r;
         t.split = local / (p.tiles_r * p.tiles_c);
@@ -134,6 +137,7 @@ __device__ __forceinline__ bool grouped_tile(const GroupedParams& p, int L, int 
         int first, tiles;
         const bool by_width = p.keep_axis == (kForm == kForward ? 2 : 1);
         if (!find_group(p, bm, L / per, by_width, kForm == kForward ? p.K : p.N, t.e, t.row0, t.rows, first, tiles)) return false;
+        t.row_tiles = tiles;
         const int local = L - first * per;
         mt = local % tiles;
         ct = local / tiles % p.tiles_c;
@@ -306,6 +310,58 @@ __device__ __forceinline__ floatx4 across_frag_f32(const unsigned char* base, in
     return v;
 }
 
+// F fragments from own index `first` on, at K step s.
+template <typename E, bool kAcross, int F>
+__device__ __forceinline__ void read_step(const unsigned char* tile, int first, int s, typename E::Frag (&f)[F]) {
+    const int lane = threadIdx.x & 63;
+    if constexpr (kAcross && E::kBytes == 2) {
+        uint32_t addr[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) addr[i] = across_addr<128>(tile, first + i * 16) + s * (32 * 256);
+        across_read4<128, 0>(addr, f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            if constexpr (kAcross) f[i] = across_frag_f32<128>(tile, first + i * 16, s);
+            else f[i] = __builtin_bit_cast(typename E::Frag, lds_frag(tile, first + i * 16 + (lane & 15), s * 4 + (lane >> 4)));
+        }
+    }
+}
+
+// F fragments from own index `first` on, at both K steps.
+template <typename E, bool kAcross, int F>
+__device__ __forceinline__ void read_frags(const unsigned char* tile, int first, typename E::Frag (&f)[2][F]) {
+    const int lane = threadIdx.x & 63;
+    if constexpr (kAcross && E::kBytes == 2) {
+        static_assert(F == 4, "read four at a time (two: read_pair)");
+        uint32_t addr[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) addr[i] = across_addr<128>(tile, first + i * 16);
+        across_read4<128, 0>(addr, f[0]);
+        across_read4<128, 1>(addr, f[1]);
+    } else {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+                if constexpr (kAcross) f[s][i] = across_frag_f32<128>(tile, first + i * 16, s);
+                else f[s][i] = __builtin_bit_cast(typename E::Frag, lds_frag(tile, first + i * 16 + (lane & 15), s * 4 + (lane >> 4)));
+            }
+    }
+}
+
+// Two fragments from own index `first` on, at both K steps.
+template <typename E, bool kAcross>
+__device__ __forceinline__ void read_pair(const unsigned char* tile, int first, typename E::Frag (&f)[2][2]) {
+    if constexpr (kAcross && E::kBytes == 2) {
+        bf16x8 v[4];
+        across_read2x2<128>(across_addr<128>(tile, first), across_addr<128>(tile, first + 16), v);
+        f[0][0] = v[0], f[0][1] = v[1], f[1][0] = v[2], f[1][1] = v[3];
+    } else {
+        read_frags<E, kAcross, 2>(tile, first, f);
+    }
+}
+
 // Raw buffer descriptor over `bytes` bytes.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc_bytes(const void* base, uint32_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, (int)bytes, 0x00020000);
@@ -315,8 +371,12 @@ constexpr int STAGE = 16384;  // bytes of 128 rows' K tile
 
 // Requests of N instructions of 1 KB for 128 own indices of an operand:
 // instruction i fills the tile's LDS bytes (wave0 + i) * 1024 + lane * 16.
-template <typename E, bool kAcross, int N>
+// kOnce: nothing else reads these bytes (non-temporal).
+template <typename E, bool kAcross, int N, bool kOnce = false>
 struct Loader {
+    static __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rsrc, uint32_t voff, uint32_t soff, unsigned char* lds) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr_t*)lds, 16, voff, soff, 0, kOnce ? 2 : 0);
+    }
     const char* base;       // first element of the operand's part
     size_t step;            // bytes a K tile advances (across: 0 in the lane offsets)
     uint32_t off[N];        // lane offset, kOOB if its row or column does not exist
@@ -359,13 +419,13 @@ struct Loader {
         const int lim = depth - kt * E::kDepth;
         if constexpr (!kAcross) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) load_lds16(r, col[i] < lim ? off[i] : kOOB, (uint32_t)kt * ROWB, lds + i * 1024);
+            for (int i = 0; i < N; ++i) load(r, col[i] < lim ? off[i] : kOOB, (uint32_t)kt * ROWB, lds + i * 1024);
         } else {
             // the descriptor covers the depths that exist
             const int n = max(min(lim, E::kDepth), 0);
             r = make_rsrc_bytes(base + (size_t)kt * step, max((n - 1) * (int)ldb + (int)tail, 0) & -(int)(n > 0));
 #pragma unroll
-            for (int i = 0; i < N; ++i) load_lds16(r, off[i], 0, lds + i * 1024);
+            for (int i = 0; i < N; ++i) load(r, off[i], 0, lds + i * 1024);
         }
     }
 };
@@ -443,29 +503,33 @@ struct Operands {
 };
 
 // C's part of a tile that a wave holds: kRows fragments of 16 rows from C row
-// `first` on and 16 runs of 4 columns, run q at column(q), to C or to this
-// part's place among the partial sums.  value(i, j) is the accumulator of row
-// fragment i and runs 4j .. 4j + 3 (lane -> row lane % 16, run 4j + lane / 16).
+// `first` on and 4 * kCols runs (kCols 2 or 4) of 4 columns, run q at column(q),
+// to C or to this part's place among the partial sums.  value(i, j) is the
+// accumulator of row fragment i and runs 4j .. 4j + 3 (lane -> row lane % 16, run
+// 4j + lane / 16).
 // Each row fragment goes through 4 KB of LDS that are the wave's own, so that a
-// store covers 4 rows of 16 consecutive runs, whole cache lines, where straight
+// store covers 4 rows of 16 (8 of 8) consecutive runs, whole cache lines, where straight
 // from the accumulators it covers 16 rows of 4 runs (stores alone of 692 MB of
 // fp32 with four 128 x 128 tiles per compute unit: 190 -> 123 us).
-template <typename E, int kForm, bool kBf16Out, int kRows, typename Column, typename Value>
+template <typename E, int kForm, bool kBf16Out, int kRows, int kCols, typename Column, typename Value>
 __device__ __forceinline__ void store_tile(const GroupedParams& p, const GroupedTile& t, int first, unsigned char* scratch,
                                            Column&& column, Value&& value) {
     const int lane = threadIdx.x & 63, lr = lane & 15, lc = lane >> 4;
     const int cols = kForm == kForward ? p.N : p.K;
     const bool add = kForm == kWeightGrad && p.accumulate && p.splits == 1 && !p.slim;
-    const int c = column(lr);
+    constexpr int kRuns = 4 * kCols, kSteps = kCols;  // runs of a row; stores per fragment
+    const int run = lane % kRuns, sub = lane / kRuns;  // a store's run and row (of 64 / kRuns) for this lane
+    auto row_of = [&](int s) { return s * (64 / kRuns) + sub; };
+    const int c = column(run);
     auto crow_of = [&](int r) { return kForm == kWeightGrad ? (size_t)t.e * p.N + r : (size_t)t.row0 + r; };
     auto address = [&](int r) { return reinterpret_cast<char*>(p.c) + crow_of(r) * p.ldc * (kBf16Out ? 2 : 4); };
     // old values are read a fragment ahead: the compiler keeps a read behind
     // the stores before it
-    floatx4 old[kForm == kWeightGrad ? 2 : 1][4];
+    floatx4 old[kForm == kWeightGrad ? 2 : 1][kSteps];
     auto load_old = [&](int i) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int r = first + i * 16 + 4 * s + lc;
+        for (int s = 0; s < kSteps; ++s) {
+            const int r = first + i * 16 + row_of(s);
             if (r < t.r1 && c < cols) old[i & 1][s] = load_run<kBf16Out>(address(r), c, cols);
         }
     };
@@ -473,7 +537,7 @@ __device__ __forceinline__ void store_tile(const GroupedParams& p, const Grouped
         if (add) load_old(0);
     // int8: this lane's columns' and rows' scales, read before any store for
     // the same reason
-    float sb[4], sa[kRows][4];
+    float sb[4], sa[kRows][kSteps];
     if constexpr (E::kBytes == 1)
         if (p.splits == 1) {
 #pragma unroll
@@ -481,19 +545,19 @@ __device__ __forceinline__ void store_tile(const GroupedParams& p, const Grouped
 #pragma unroll
             for (int i = 0; i < kRows; ++i)
 #pragma unroll
-                for (int s = 0; s < 4; ++s) sa[i][s] = p.sa[crow_of(min(first + i * 16 + 4 * s + lc, t.r1 - 1))];
+                for (int s = 0; s < kSteps; ++s) sa[i][s] = p.sa[crow_of(min(first + i * 16 + row_of(s), t.r1 - 1))];
         }
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
         if constexpr (kForm == kWeightGrad)
             if (add && i + 1 < kRows) load_old(i + 1);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            *reinterpret_cast<typename E::Acc*>(scratch + lr * 256 + ((4 * j + lc) ^ lr) * 16) = value(i, j);
+        for (int j = 0; j < kCols; ++j)
+            *reinterpret_cast<typename E::Acc*>(scratch + lr * (kRuns * 16) + ((4 * j + lc) ^ (lr % kRuns)) * 16) = value(i, j);
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int row = 4 * s + lc, r = first + i * 16 + row;
-            typename E::Acc v = *reinterpret_cast<const typename E::Acc*>(scratch + row * 256 + (lr ^ row) * 16);
+        for (int s = 0; s < kSteps; ++s) {
+            const int row = row_of(s), r = first + i * 16 + row;
+            typename E::Acc v = *reinterpret_cast<const typename E::Acc*>(scratch + row * (kRuns * 16) + (run ^ (row % kRuns)) * 16);
             const int clim = r < t.rlim ? t.clim : 0;
             // what lies past a width is left as it is when C is added to
             const int end = kForm == kWeightGrad && p.accumulate && p.splits == 1 ? min(clim, cols) : cols;
@@ -526,6 +590,8 @@ __device__ __forceinline__ void store_tile(const GroupedParams& p, const Grouped
 
 // 128 x 128 tiles: every form and type
 hipError_t launch_grouped_mid(const GroupedParams& p, GroupedForm form, GroupedElem elem, long long grid, hipStream_t s);
+// 32 x 128 tiles: x W^T and dy W with few rows, every type
+hipError_t launch_grouped_few(const GroupedParams& p, GroupedForm form, GroupedElem elem, long long grid, hipStream_t s);
 // 256 x 256 tiles: bf16 (every form) and int8
 hipError_t launch_grouped_big(const GroupedParams& p, GroupedForm form, GroupedElem elem, long long grid, hipStream_t s);
 hipError_t launch_grouped_join(const GroupedParams& p, GroupedForm form, GroupedElem elem, hipStream_t s);
@@ -535,5 +601,6 @@ hipError_t launch_quantize_rows(const void* x, const void* x2, size_t ldx, int8_
 
 constexpr int kGroupTile = 128;     // rows and columns of a launch_grouped_mid tile
 constexpr int kGroupBigTile = 256;  // of a launch_grouped_big tile
+constexpr int kGroupFewRows = 32;   // rows of a launch_grouped_few tile (128 columns)
 
 }  // namespace flexmoe

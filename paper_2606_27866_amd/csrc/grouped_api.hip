@@ -59,7 +59,7 @@ int check_rows(const flexmoe_grouped_desc* D, int R, const char* who) {
 long long row_tiles_bound(int R, int E, int bm) { return std::min<long long>((long long)(R + bm - 1) / bm + E - 1, R); }
 
 // How a product is cut into workgroups.
-enum Tiles { kMid = 0, kSlim = 1, kBig = 2 };
+enum Tiles { kMid = 0, kSlim = 1, kBig = 2, kFew = 3 };
 struct Plan {
     GroupedForm form;
     GroupedElem elem;
@@ -72,41 +72,44 @@ constexpr int kUnits = 256;  // compute units
 
 // About the microseconds of a product on one kind of tiles with the reduction in
 // `splits` parts, from what the host knows (not how rows and widths spread).
-// Fitted to 2000 timings of 200 drawn products (1 to 128 groups, 1 to 32768
-// rows, sides of 24 to 20480, every form and type, 1 to 19 parts): the choice it
-// makes is 3 % slower on average than the fastest of those tried, and 8 % at
-// worst in 9 of 10 products.
+// Fitted to 3500 timings of 260 drawn products (1 to 128 groups, 1 to 32768
+// rows, sides of 24 to 20480, every form and type, 1 to 13 parts): the choice it
+// makes takes 4 % more time on average than the fastest of those tried, at most
+// 12 % more in 9 of 10 products.
 //   tiles     a K tile of 128 bytes costs a 256 x 256 tile 0.5 + 0.16 us per 64
-//             rows, a 128 x 128 tile alone on its compute unit 0.17 + 0.14 us
+//             rows; a 128 x 128 tile alone on its compute unit 0.17 + 0.14 us
 //             per 32 rows (fp32: 0.1 + 0.45), two that share it 1.7 times that
-//             (fp32: 2.1); a tile 3.3 or 1 us beside that; a last round of
-//             tiles that is not full costs 0.7 of the missing part
-//   memory    every operand and C once at 6.5 TB/s, 6 us at least
+//             (fp32: 2.1); n of up to four 32 x 128 tiles that share it n times
+//             0.1 + 0.08 us per 16 rows (fp32: 0.1 + 0.15), at least 0.45; a tile
+//             3.3, 1 or 1.5 us beside that; a last round of tiles that is not
+//             full costs 0.7 of the missing part
+//   memory    every operand and C once at 6.5 TB/s (32 x 128 tiles, but fp32: 5.7), 6 us at
+//             least
 //   together  the longer of the two and a quarter of the other
 //   joining   a launch, and the parts written and read
 // A width keeps 0.6 of what it limits.
 double product_us(const flexmoe_grouped_desc& D, GroupedForm form, GroupedElem elem, Tiles kind, int splits, int R) {
-    const int side = kind == kBig ? kGroupBigTile : kGroupTile;
+    const int side = kind == kBig ? kGroupBigTile : kGroupTile, rows_of = kind == kFew ? kGroupFewRows : side;
     const int kd = elem == kElemI8 ? 128 : elem == kElemBf16 ? 64 : 32;
+    const bool f32 = elem == kElemF32;
     const double es = 128.0 / kd, kept = D.keep_axis == FLEXMOE_KEEP_NONE ? 1.0 : 0.6;
     const int hit = std::max(1, std::min(D.groups, R));  // groups with rows, at most
     const int cols = form == kForward ? D.N : D.K;
-    double row_tiles, tile_rows, depth, weights, out;
+    double row_tiles, tile_rows, depth, in, out;
     if (form == kWeightGrad) {
-        row_tiles = (double)D.groups * ceil_div(D.N, side);
-        tile_rows = std::min(D.N, side);
-        depth = (double)R / D.groups;
-        weights = (double)R * D.N * es;
+        row_tiles = (double)D.groups * ceil_div(D.N, rows_of);
+        tile_rows = std::min(D.N, rows_of);
+        depth = (D.groups > 1 ? 1.5 : 1.0) * R / D.groups;  // groups differ, and the longest is waited for
+        in = (double)R * (D.N + (double)D.K) * es;
         out = (double)D.groups * D.N * cols;
     } else {
         const double rows = (double)R / hit;
-        row_tiles = rows <= side ? hit : R / (double)side + 0.5 * hit;
-        tile_rows = std::min<double>(rows, side);
+        row_tiles = rows <= rows_of ? hit : R / (double)rows_of + 0.5 * hit;
+        tile_rows = std::min<double>(rows, rows_of);
         depth = form == kForward ? D.K : D.N;
-        weights = (double)hit * D.N * D.K * es * kept;
+        in = (double)hit * D.N * D.K * es * kept + R * depth * es;
         out = (double)R * cols;
     }
-    const double in = form == kWeightGrad ? (double)R * D.K * es : R * depth * es;
     const double out_bytes = out * ((form == kWeightGrad ? D.dw_dtype : D.dtype) == FLEXMOE_BF16 ? 2 : 4);
     const double per_unit = row_tiles * ceil_div(cols, side) * splits / kUnits;
     const double k = std::ceil(std::ceil(depth / kd) / splits);
@@ -117,12 +120,15 @@ double product_us(const flexmoe_grouped_desc& D, GroupedForm form, GroupedElem e
     double tiles_us;
     if (kind == kBig) {
         tiles_us = 3.5 + rounds(per_unit) * (3.3 + k * kept * (0.5 + 0.16 * std::ceil(tile_rows / 64)));
+    } else if (kind == kFew) {
+        const double step = 0.1 + (f32 ? 0.15 : 0.08) * std::ceil(tile_rows / 16);
+        const double shared = std::min(std::max(per_unit, 1.0), 4.0) * step;
+        tiles_us = 3.5 + rounds(per_unit / 4) * (1.5 + k * (per_unit > 1 ? kept : 1.0) * std::max(0.45, shared));
     } else {
-        const bool f32 = elem == kElemF32;
         const double step = f32 ? 0.1 + 0.45 * std::ceil(tile_rows / 32) : 0.17 + 0.14 * std::ceil(tile_rows / 32);
         tiles_us = per_unit <= 1 ? 4.5 + k * step : 3.5 + rounds(per_unit / 2) * (1.0 + k * kept * step * (f32 ? 2.1 : 1.7));
     }
-    const double memory_us = 6.0 + (weights + in + out_bytes) / 6.5e6;
+    const double memory_us = 6.0 + (in + out_bytes) / (kind == kFew && !f32 ? 5.7e6 : 6.5e6);
     double us = std::max(tiles_us, memory_us) + 0.25 * std::min(tiles_us, memory_us);
     if (splits > 1) us += 3.0 + 2 * splits * out * 4 / 5.6e6;
     return us;
@@ -133,13 +139,13 @@ Plan plan(const flexmoe_grouped_desc& D, GroupedForm form, bool int8, int R) {
     const long long cols = form == kForward ? D.N : D.K;
     const long long out = (form == kWeightGrad ? (long long)D.groups * D.N : (long long)R) * ((cols + 3) / 4 * 4) * 4;
     double best = 1e30;
-    for (Tiles kind : {kMid, kBig}) {
-        if (kind == kBig && pl.elem == kElemF32) continue;
+    for (Tiles kind : {kMid, kFew, kBig}) {
+        if ((kind == kBig && pl.elem == kElemF32) || (kind == kFew && form == kWeightGrad)) continue;
         for (int splits = 1; splits <= 64; splits = splits < 4 ? splits + 1 : splits * 3 / 2) {
-            // parts of at least two K tiles, partial sums of at most 256 MB
+            // parts of at least one K tile, partial sums of at most 256 MB
             const int kd = pl.elem == kElemI8 ? 128 : pl.elem == kElemBf16 ? 64 : 32;
             const double depth = form == kWeightGrad ? (double)R / D.groups : form == kForward ? D.K : D.N;
-            if (splits > 1 && (depth < 2.0 * kd * splits || out * splits > (256LL << 20))) break;
+            if (splits > 1 && (depth < (double)kd * splits || out * splits > (256LL << 20))) break;
             const double us = product_us(D, form, pl.elem, kind, splits, R);
             if (us < best) {
                 best = us;
@@ -182,6 +188,11 @@ int launch(const flexmoe_grouped_desc* D, const Strides& st, GroupedForm form, b
     p.a = a, p.b = b, p.c = c, p.sa = sa, p.sb = sb, p.offsets = offsets, p.keep = keep, p.partial = ws;
     p.E = D->groups, p.R = R, p.N = D->N, p.K = D->K, p.keep_axis = D->keep_axis;
     p.slim = pl.tiles == kSlim;
+    // Weights of 96 MB and more are not found in the 256 MB last-level cache by
+    // the next call of a model's next layer (weights of several layers in turn:
+    // 134 MB 32.5 -> 28.1 us, 346 MB 65.0 -> 57.8, 1.2 GB 120 -> 108 with the hint;
+    // 67 MB 14.7 -> 18.7, 73 MB 17.8 -> 20.9).
+    p.once = form != kWeightGrad && (double)D->groups * D->N * D->K * (int8 ? 1 : elem_bytes(D->dtype)) >= 96e6;
     p.splits = pl.splits, p.accumulate = accumulate;
     p.out_bf16 = (form == kWeightGrad ? D->dw_dtype : D->dtype) == FLEXMOE_BF16;
     if (form == kForward) p.lda = st.x, p.ldb = st.w, p.ldc = st.y;
@@ -191,10 +202,14 @@ int launch(const flexmoe_grouped_desc* D, const Strides& st, GroupedForm form, b
     const int side = pl.tiles == kBig ? kGroupBigTile : kGroupTile;
     p.tiles_c = ceil_div(cols, side);
     p.tiles_r = ceil_div(D->N, side);
-    const long long row_tiles = form == kWeightGrad ? (long long)D->groups * p.tiles_r : row_tiles_bound(R, D->groups, side);
+    const long long row_tiles = form == kWeightGrad ? (long long)D->groups * p.tiles_r
+                                                    : row_tiles_bound(R, D->groups, pl.tiles == kFew ? kGroupFewRows : side);
     const long long tiles = row_tiles * p.tiles_c * p.splits;
-    if (tiles > (1LL << 30)) return fail(FLEXMOE_ESHAPE, "%s: %lld tiles are too many for one launch", who, tiles);
-    hipError_t err = pl.tiles == kBig ? launch_grouped_big(p, form, pl.elem, tiles, s) : launch_grouped_mid(p, form, pl.elem, tiles, s);
+    if (tiles > (1LL << 23) - 64) return  // a launch's threads are fewer than 2^32
+        fail(FLEXMOE_ESHAPE, "%s: %lld tiles are too many for one launch", who, tiles);
+    hipError_t err = pl.tiles == kBig   ? launch_grouped_big(p, form, pl.elem, tiles, s)
+                     : pl.tiles == kFew ? launch_grouped_few(p, form, pl.elem, tiles, s)
+                                        : launch_grouped_mid(p, form, pl.elem, tiles, s);
     if (err == hipSuccess && p.splits > 1) err = launch_grouped_join(p, form, pl.elem, s);
     if (err != hipSuccess) return hip_fail(err, who);
     return FLEXMOE_OK;

@@ -35,15 +35,6 @@ constexpr int BT = 512;                  // threads
 constexpr int NR = STAGE / 1024 / 8;     // requests per wave and half: 2
 constexpr int BIG_SMEM = 8 * STAGE;
 
-// N fragments of an along half from LDS row `first` on, at both K steps.
-template <typename E, int N>
-__device__ __forceinline__ void read_along(const unsigned char* half, int first, typename E::Frag (&f)[2][N]) {
-    const int lr = threadIdx.x & 15, lc = (threadIdx.x & 63) >> 4;
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int s = 0; s < 2; ++s) f[s][i] = __builtin_bit_cast(typename E::Frag, lds_frag(half, first + i * 16 + lr, s * 4 + lc));
-}
 // The depths from `valid` on set to zero.
 template <typename E, int N>
 __device__ __forceinline__ void clear_tail(typename E::Frag (&f)[2][N], int valid) {
@@ -53,13 +44,6 @@ __device__ __forceinline__ void clear_tail(typename E::Frag (&f)[2][N], int vali
 #pragma unroll
         for (int i = 0; i < N; ++i) f[s][i] = head<E>(f[s][i], valid - (s * 4 + lc) * E::kPer);
 }
-// Two bf16 fragments of an across half, at both K steps, in one block.
-__device__ __forceinline__ void across_read2(const unsigned char* half, int first, bf16x8 (&f)[2][2]) {
-    bf16x8 v[4];
-    across_read2x2<128>(across_addr<128>(half, first), across_addr<128>(half, first + 16), v);
-    f[0][0] = v[0], f[0][1] = v[1], f[1][0] = v[2], f[1][1] = v[3];
-}
-
 template <typename E, int kForm, bool kBf16Out>
 __global__ __launch_bounds__(BT, 2) void grouped_big_kernel(GroupedParams p) {
     constexpr bool kAcrossA = kForm == kWeightGrad, kAcrossB = kForm != kForward;
@@ -101,22 +85,14 @@ __global__ __launch_bounds__(BT, 2) void grouped_big_kernel(GroupedParams p) {
         };
         typename E::Frag fa[2][MF], fx[2][2], fy[2][2];  // [K step][fragment]
         auto read_a = [&](int half, int kt) {
-            if constexpr (kAcrossA) {
-                uint32_t addr[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) addr[i] = across_addr<128>(half_of(half, kt), wm * 64 + i * 16);
-                across_read4<128, 0>(addr, fa[0]);
-                across_read4<128, 1>(addr, fa[1]);
-            } else {
-                read_along<E, MF>(half_of(half, kt), wm * 16 * MF, fa);
+            read_frags<E, kAcrossA, MF>(half_of(half, kt), wm * 16 * MF, fa);
+            if constexpr (!kAcrossA) {
                 if (kTail && kt == nk - 1) clear_tail<E, MF>(fa, depth - kt * E::kDepth);
             }
         };
         auto read_b = [&](int half, int kt, typename E::Frag (&f)[2][2]) {
-            if constexpr (kAcrossB) {
-                across_read2(half_of(2 + half, kt), wn * 32, f);
-            } else {
-                read_along<E, 2>(half_of(2 + half, kt), wn * 32, f);
+            read_pair<E, kAcrossB>(half_of(2 + half, kt), wn * 32, f);
+            if constexpr (!kAcrossB) {
                 if (kTail && kt == nk - 1) clear_tail<E, 2>(f, depth - kt * E::kDepth);
             }
         };
@@ -183,7 +159,7 @@ __global__ __launch_bounds__(BT, 2) void grouped_big_kernel(GroupedParams p) {
 
 #pragma unroll
         for (int ah = 0; ah < 2; ++ah)
-            store_tile<E, kForm, kBf16Out, MF>(
+            store_tile<E, kForm, kBf16Out, MF, 4>(
                 p, t, t.r0 + ah * 32 * MF + wm * 16 * MF, smem + wave * 4096,
                 [&](int q) { return t.c0 + (q >> 3) * 128 + wn * 32 + (q & 7) * 4; },
                 [&](int i, int j) { return acc[ah][j >> 1][(j & 1) * MF + i]; });
@@ -208,6 +184,7 @@ void launch_big(const GroupedParams& p, unsigned grid, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_grouped_big(const GroupedParams& p, GroupedForm form, GroupedElem elem, long long tiles, hipStream_t s) {
+    if (elem == kElemF32) return hipErrorInvalidValue;
     if (tiles <= 0) return hipSuccess;
     const unsigned grid = (unsigned)((tiles + 63) / 64 * 64);
     if (elem == kElemI8) launch_big<I8, kForward>(p, grid, s);

@@ -26,46 +26,6 @@ constexpr int GT = 256;                   // threads
 constexpr int SMEM = 5 * STAGE;           // A0 A1 B0 B1 B2
 constexpr int NI = STAGE / 1024 / 4;      // requests per wave and operand: 4
 
-// F fragments from own index `first` on, at K step s.
-template <typename E, bool kAcross, int F>
-__device__ __forceinline__ void read_step(const unsigned char* tile, int first, int s, typename E::Frag (&f)[F]) {
-    const int lane = threadIdx.x & 63;
-    if constexpr (kAcross && E::kBytes == 2) {
-        uint32_t addr[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) addr[i] = across_addr<128>(tile, first + i * 16) + s * (32 * 256);
-        across_read4<128, 0>(addr, f);
-    } else {
-#pragma unroll
-        for (int i = 0; i < F; ++i) {
-            if constexpr (kAcross) f[i] = across_frag_f32<128>(tile, first + i * 16, s);
-            else f[i] = __builtin_bit_cast(typename E::Frag, lds_frag(tile, first + i * 16 + (lane & 15), s * 4 + (lane >> 4)));
-        }
-    }
-}
-
-// F fragments from own index `first` on, at both K steps.
-template <typename E, bool kAcross, int F>
-__device__ __forceinline__ void read_frags(const unsigned char* tile, int first, typename E::Frag (&f)[2][F]) {
-    const int lane = threadIdx.x & 63;
-    if constexpr (kAcross && E::kBytes == 2) {
-        static_assert(F == 4, "read four at a time");
-        uint32_t addr[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) addr[i] = across_addr<128>(tile, first + i * 16);
-        across_read4<128, 0>(addr, f[0]);
-        across_read4<128, 1>(addr, f[1]);
-    } else {
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int i = 0; i < F; ++i) {
-                if constexpr (kAcross) f[s][i] = across_frag_f32<128>(tile, first + i * 16, s);
-                else f[s][i] = __builtin_bit_cast(typename E::Frag, lds_frag(tile, first + i * 16 + (lane & 15), s * 4 + (lane >> 4)));
-            }
-    }
-}
-
 template <typename E, int kForm, bool kBf16Out, bool kSlim>
 __global__ __launch_bounds__(GT, kSlim ? 4 : 2) void grouped_mid_kernel(GroupedParams p) {
     constexpr bool kAcrossA = kForm == kWeightGrad, kAcrossB = kForm != kForward;
@@ -78,11 +38,12 @@ __global__ __launch_bounds__(GT, kSlim ? 4 : 2) void grouped_mid_kernel(GroupedP
     const Operands<E, kForm> op(p, t);
     const int nk = ceil_div(depth, E::kDepth);
 
-    auto run = [&](auto mf_c) {
+    auto run = [&](auto mf_c, auto once_c) {
         constexpr int MF = decltype(mf_c)::value;
+        constexpr bool kOnce = decltype(once_c)::value;
         constexpr int NA = kAcrossA ? NI : MF;  // along: 32 * MF rows of A
         Loader<E, kAcrossA, NA> la;
-        Loader<E, kAcrossB, NI> lb;
+        Loader<E, kAcrossB, NI, kOnce> lb;
         la.init(op.a, p.lda, op.own_a, depth, wave * NA);
         lb.init(op.b, p.ldb, op.own_b, depth, wave * NI);
         unsigned char* const sa = smem;
@@ -217,15 +178,20 @@ __global__ __launch_bounds__(GT, kSlim ? 4 : 2) void grouped_mid_kernel(GroupedP
 #pragma unroll
                 for (int i = 0; i < MF; ++i) acc[j][i] += total[j][i];
         barrier_no_fence();  // every wave has read its fragments: LDS becomes the stores' scratch
-        store_tile<E, kForm, kBf16Out, MF>(
+        store_tile<E, kForm, kBf16Out, MF, 4>(
             p, t, t.r0 + wm * 16 * MF, smem + wave * 4096, [&](int q) { return t.c0 + wn * 64 + q * 4; },
             [&](int i, int j) { return acc[j][i]; });
     };
-    if constexpr (kAcrossA) run(std::integral_constant<int, 4>{});
-    else if (nr > 96) run(std::integral_constant<int, 4>{});
-    else if (nr > 64) run(std::integral_constant<int, 3>{});
-    else if (nr > 32) run(std::integral_constant<int, 2>{});
-    else run(std::integral_constant<int, 1>{});
+    auto by_rows = [&](auto once_c) {
+        if (nr > 96) run(std::integral_constant<int, 4>{}, once_c);
+        else if (nr > 64) run(std::integral_constant<int, 3>{}, once_c);
+        else if (nr > 32) run(std::integral_constant<int, 2>{}, once_c);
+        else run(std::integral_constant<int, 1>{}, once_c);
+    };
+    // a group with one row tile reads its weights once
+    if constexpr (kAcrossA) run(std::integral_constant<int, 4>{}, std::false_type{});
+    else if (p.once && t.row_tiles == 1) by_rows(std::true_type{});
+    else by_rows(std::false_type{});
 }
 
 // The parts of a split reduction added in their order: one thread per run of 4

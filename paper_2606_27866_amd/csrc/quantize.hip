@@ -145,6 +145,16 @@ void launch(const void* x, const void* x2, size_t ldx, int8_t* q, size_t ldq, fl
 hipError_t launch_quantize_rows(const void* x, const void* x2, size_t ldx, int8_t* q, size_t ldq, float* scale, int rows, int cols,
                                 bool bf16, hipStream_t s) {
     if (rows <= 0) return hipSuccess;
+    constexpr int kSlice = 1 << 22;  // a launch's threads are fewer than 2^32
+    for (; rows > kSlice; rows -= kSlice) {
+        const hipError_t err = launch_quantize_rows(x, x2, ldx, q, ldq, scale, kSlice, cols, bf16, s);
+        if (err != hipSuccess) return err;
+        const size_t step = kSlice * ldx * (bf16 ? 2 : 4);
+        x = reinterpret_cast<const char*>(x) + step;
+        if (x2) x2 = reinterpret_cast<const char*>(x2) + step;
+        q += kSlice * ldq;
+        scale += kSlice;
+    }
     if (bf16 && x2) launch<true, true>(x, x2, ldx, q, ldq, scale, rows, cols, s);
     else if (bf16) launch<true, false>(x, x2, ldx, q, ldq, scale, rows, cols, s);
     else if (x2) launch<false, true>(x, x2, ldx, q, ldq, scale, rows, cols, s);

@@ -235,3 +235,43 @@ def test_refused_tensors():
         op.forward(torch.zeros(9, 24, device="cuda"), w, offsets)  # more rows than max_rows
     with pytest.raises(ValueError):
         op.weight_grad(torch.zeros(8, 16, device="cuda"), x, offsets, accumulate=True)
+
+
+# Sizes that reach every kind of tiles, with ends inside tiles, 16-byte units and K tiles, and reductions in parts.
+LARGE = [
+    ([1100, 0, 700, 300], 1000, 900),   # 256 x 256 tiles: 4, 3, 2 and 1 steps of 64 rows
+    ([2300], 2049, 1033),               # one group, rows of 16-byte units that end past the matrix
+    ([4100, 900], 520, 300),            # few tiles of a long reduction over rows: parts
+    ([70, 3, 33, 16], 700, 5000),       # few rows, long rows: parts of the forward
+    ([9, 1, 0, 31, 32, 40], 5000, 700),  # few rows, many columns: parts of the input gradient
+]
+
+
+@pytest.mark.parametrize("axis", ["none", "N", "K"])
+@pytest.mark.parametrize("rows,N,K", LARGE)
+def test_large_products(rows, N, K, axis):
+    Case(rows, N, K, BF, axis, pad=1 if axis == "K" else 0).run()
+
+
+@pytest.mark.parametrize("rows,N,K", [([600, 5], 300, 260), ([20, 2], 300, 2100), ([3000], 140, 200)])
+def test_large_products_fp32(rows, N, K):
+    Case(rows, N, K, F32, "N").run()
+
+
+def test_weights_larger_than_the_last_level_cache():
+    """Weights above 96 MB are read with another cache hint."""
+    Case([3, 40, 0, 140] * 4, 1500, 2100, BF, "N").run()
+
+
+def test_a_reduction_that_passes_2_31_bytes():
+    """One group whose rows lie further apart than 32 bits of bytes: 40000 rows, 32768 values apart."""
+    R, N, K, ld = 40000, 8, 16, 32768
+    g = torch.Generator(device="cuda")
+    x = torch.empty(R, ld, dtype=BF, device="cuda")[:, :K]
+    x.copy_(torch.randint(-2, 3, (R, K), generator=g, device="cuda"))
+    dy = torch.randint(-2, 3, (R, N), generator=g, device="cuda").to(BF)
+    w = torch.randint(-2, 3, (1, N, K), generator=g, device="cuda").to(BF)
+    op = fm.GroupedProduct(1, N, K, R)
+    offsets = torch.tensor([0, R], dtype=torch.int32, device="cuda")
+    assert torch.equal(op.weight_grad(dy, x, offsets)[0].double(), dy.double().T.contiguous() @ x.double())
+    assert torch.equal(op.forward(x, w, offsets).double(), x.double() @ w[0].double().T)

@@ -142,3 +142,11 @@ def test_whole_call(T):
     # independent: 2 / 127 of the norm is far outside them
     full = xp.double() @ wp[0].double().T
     assert float((y.double() - full).norm() / full.norm()) <= 2 / 127
+
+
+@pytest.mark.parametrize("axis", ["none", "N", "K"])
+@pytest.mark.parametrize("rows,N,K", [([1100, 0, 700, 300], 1000, 1800), ([2300], 2049, 1033), ([70, 3, 33, 16], 700, 9000),
+                                      ([3, 40, 0, 140] * 4, 1500, 4200)])
+def test_large_products(rows, N, K, axis):
+    """Sizes that reach every kind of tiles, reductions in parts, and weights above 96 MB."""
+    product_case(rows, N, K, torch.bfloat16, axis)
