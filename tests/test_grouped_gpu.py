@@ -239,7 +239,9 @@ def test_refused_tensors():
 
 # Sizes that reach every kind of tiles, with ends inside tiles, 16-byte units and K tiles, and reductions in parts.
 LARGE = [
-    ([1100, 0, 700, 300], 1000, 900),   # 256 x 256 tiles: 4, 3, 2 and 1 steps of 64 rows
+    ([9000, 300, 0, 2700], 4099, 2003),  # 256 x 256 tiles, 4 to 1 steps of 64 rows, odd sides
+    ([12000], 4096, 2048),              # the same with whole tiles
+    ([1100, 0, 700, 300], 1000, 900),
     ([2300], 2049, 1033),               # one group, rows of 16-byte units that end past the matrix
     ([4100, 900], 520, 300),            # few tiles of a long reduction over rows: parts
     ([70, 3, 33, 16], 700, 5000),       # few rows, long rows: parts of the forward

@@ -145,7 +145,7 @@ def test_whole_call(T):
 
 
 @pytest.mark.parametrize("axis", ["none", "N", "K"])
-@pytest.mark.parametrize("rows,N,K", [([1100, 0, 700, 300], 1000, 1800), ([2300], 2049, 1033), ([70, 3, 33, 16], 700, 9000),
+@pytest.mark.parametrize("rows,N,K", [([9000, 300, 0, 2700], 4099, 4003), ([12000], 4096, 2048), ([1100, 0, 700, 300], 1000, 1800), ([2300], 2049, 1033), ([70, 3, 33, 16], 700, 9000),
                                       ([3, 40, 0, 140] * 4, 1500, 4200)])
 def test_large_products(rows, N, K, axis):
     """Sizes that reach every kind of tiles, reductions in parts, and weights above 96 MB."""
