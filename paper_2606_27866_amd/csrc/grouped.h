@@ -502,6 +502,68 @@ struct Operands {
     }
 };
 
+// C's part of a tile that a wave holds, where C is bf16 and the accumulators hold
+// all of it: rounded before it goes through LDS (2 KB of the wave's own), so that a store
+// takes 8 columns of a lane and 16-byte accesses cover 8 rows of 64 columns.
+// Arguments as below; runs 2q and 2q + 1 are neighbours.
+template <typename E, int kForm, int kRows, int kCols, typename Column, typename Value>
+__device__ __forceinline__ void store_tile_bf16(const GroupedParams& p, const GroupedTile& t, int first, unsigned char* scratch,
+                                                Column&& column, Value&& value) {
+    constexpr int kChunks = 2 * kCols, kSteps = kCols / 2;  // 16-byte chunks of a row; stores per fragment
+    const int lane = threadIdx.x & 63, lr = lane & 15, lc = lane >> 4;
+    const int cols = kForm == kForward ? p.N : p.K;
+    auto crow_of = [&](int r) { return kForm == kWeightGrad ? (size_t)t.e * p.N + r : (size_t)t.row0 + r; };
+    // int8: the scales of this lane's columns and rows, before any store: the
+    // compiler keeps a read behind the stores before it
+    float sb[kCols][4], sa[kRows];
+    if constexpr (E::kBytes == 1) {
+#pragma unroll
+        for (int j = 0; j < kCols; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int c = column(4 * j + lc) + k;
+                sb[j][k] = c < cols ? p.sb[(size_t)t.e * p.N + c] : 0.f;
+            }
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) sa[i] = p.sa[crow_of(min(first + i * 16 + lr, t.r1 - 1))];
+    }
+    const int chunk = lane % kChunks, c8 = column(2 * chunk);
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int clim = first + i * 16 + lr < t.rlim ? t.clim : 0;
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) {
+            const int c = column(4 * j + lc);
+            const typename E::Acc v = value(i, j);
+            float f[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if constexpr (E::kBytes == 1) f[k] = (float)v[k] * (sa[i] * sb[j][k]);
+                else f[k] = v[k];
+                f[k] = c + k < clim ? f[k] : 0.f;
+            }
+            const int at = ((2 * j + (lc >> 1)) ^ (lr % kChunks)) * 16 + (lc & 1) * 8;
+            *reinterpret_cast<uint2*>(scratch + lr * (kChunks * 16) + at) = make_uint2(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]));
+        }
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const int row = s * (64 / kChunks) + lane / kChunks, r = first + i * 16 + row;
+            const u32x4 v = *reinterpret_cast<const u32x4*>(scratch + row * (kChunks * 16) + (chunk ^ (row % kChunks)) * 16);
+            // what lies past a width is left as it is when C is added to
+            const int end = kForm == kWeightGrad && p.accumulate ? (r < t.rlim ? min(t.clim, cols) : 0) : cols;
+            if (r >= t.r1 || c8 >= end) continue;
+            bf16_t* o = reinterpret_cast<bf16_t*>(p.c) + crow_of(r) * p.ldc + c8;
+            if (c8 + 7 < end) {
+                *reinterpret_cast<u32x4*>(o) = v;
+            } else {
+#pragma unroll
+                for (int k = 0; k < 7; ++k)
+                    if (c8 + k < end) o[k] = (bf16_t)(v[k >> 1] >> (16 * (k & 1)));
+            }
+        }
+    }
+}
+
 // C's part of a tile that a wave holds: kRows fragments of 16 rows from C row
 // `first` on and 4 * kCols runs (kCols 2 or 4) of 4 columns, run q at column(q),
 // to C or to this part's place among the partial sums.  value(i, j) is the
@@ -511,12 +573,23 @@ struct Operands {
 // store covers 4 rows of 16 (8 of 8) consecutive runs, whole cache lines, where straight
 // from the accumulators it covers 16 rows of 4 runs (stores alone of 692 MB of
 // fp32 with four 128 x 128 tiles per compute unit: 190 -> 123 us).
-template <typename E, int kForm, bool kBf16Out, int kRows, int kCols, typename Column, typename Value>
+// kWhole: the accumulators hold all of C (no parts, and what it is added to is in
+// them already).
+template <typename E, int kForm, bool kBf16Out, int kRows, int kCols, bool kWhole, typename Column, typename Value>
 __device__ __forceinline__ void store_tile(const GroupedParams& p, const GroupedTile& t, int first, unsigned char* scratch,
                                            Column&& column, Value&& value) {
+    if constexpr (kBf16Out && kWhole) {
+        store_tile_bf16<E, kForm, kRows, kCols>(p, t, first, scratch, column, value);
+        return;
+    } else {
+    if constexpr (kBf16Out)
+        if (p.splits == 1 && (kForm != kWeightGrad || !p.accumulate)) {
+            store_tile_bf16<E, kForm, kRows, kCols>(p, t, first, scratch, column, value);
+            return;
+        }
     const int lane = threadIdx.x & 63, lr = lane & 15, lc = lane >> 4;
     const int cols = kForm == kForward ? p.N : p.K;
-    const bool add = kForm == kWeightGrad && p.accumulate && p.splits == 1 && !p.slim;
+    const bool add = kForm == kWeightGrad && !kWhole && p.accumulate && p.splits == 1;
     constexpr int kRuns = 4 * kCols, kSteps = kCols;  // runs of a row; stores per fragment
     const int run = lane % kRuns, sub = lane / kRuns;  // a store's run and row (of 64 / kRuns) for this lane
     auto row_of = [&](int s) { return s * (64 / kRuns) + sub; };
@@ -565,7 +638,7 @@ __device__ __forceinline__ void store_tile(const GroupedParams& p, const Grouped
             const size_t crow = crow_of(r);
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[k] = c + k < clim ? v[k] : 0;
-            if (p.splits > 1) {
+            if (!kWhole && p.splits > 1) {
                 const size_t rows = kForm == kWeightGrad ? (size_t)p.E * p.N : (size_t)p.R;
                 const size_t ldp = (cols + 3) & ~3;
                 *reinterpret_cast<typename E::Acc*>(reinterpret_cast<char*>(p.partial) + ((t.split * rows + crow) * ldp + c) * 4) = v;
@@ -583,6 +656,7 @@ __device__ __forceinline__ void store_tile(const GroupedParams& p, const Grouped
                 if (add) f += old[i & 1][s];
             store_run<kBf16Out>(address(r), c, end, f);
         }
+    }
     }
 }
 

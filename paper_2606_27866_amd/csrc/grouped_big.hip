@@ -159,7 +159,7 @@ __global__ __launch_bounds__(BT, 2) void grouped_big_kernel(GroupedParams p) {
 
 #pragma unroll
         for (int ah = 0; ah < 2; ++ah)
-            store_tile<E, kForm, kBf16Out, MF, 4>(
+            store_tile<E, kForm, kBf16Out, MF, 4, false>(
                 p, t, t.r0 + ah * 32 * MF + wm * 16 * MF, smem + wave * 4096,
                 [&](int q) { return t.c0 + (q >> 3) * 128 + wn * 32 + (q & 7) * 4; },
                 [&](int i, int j) { return acc[ah][j >> 1][(j & 1) * MF + i]; });

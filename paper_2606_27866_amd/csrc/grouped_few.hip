@@ -94,7 +94,7 @@ __global__ __launch_bounds__(FT, 4) void grouped_few_kernel(GroupedParams p) {
                 for (int i = 0; i < MR; ++i) acc[j][i] += total[j][i];
         __builtin_amdgcn_s_waitcnt(waitcnt_vm(0) & kWaitLgkm0);  // no request may outlive the loop
         barrier_no_fence();  // LDS becomes the stores' scratch
-        store_tile<E, kForm, kBf16Out, MR, 2>(
+        store_tile<E, kForm, kBf16Out, MR, 2, false>(
             p, t, t.r0, smem + wave * 4096, [&](int q) { return t.c0 + wave * 32 + q * 4; }, [&](int i, int j) { return acc[j][i]; });
     };
     auto by_rows = [&](auto once_c) {

@@ -25,11 +25,67 @@ using namespace mfma;
 constexpr int GT = 256;                   // threads
 constexpr int SMEM = 5 * STAGE;           // A0 A1 B0 B1 B2
 constexpr int NI = STAGE / 1024 / 4;      // requests per wave and operand: 4
+constexpr int SCRATCH = 2048;             // a wave's, beside the stages of the small weight gradient
+
+// The accumulators of a wave's 64 x 64 of C from what is there, for columns and
+// rows within the widths.  bf16: read as store_tile_bf16 writes (16 bytes of 8
+// rows), through LDS.  `meanwhile` runs after the reads are under way.
+template <typename E, bool kBf16Out, typename F>
+__device__ __forceinline__ void old_tile(const GroupedParams& p, const GroupedTile& t, int wm, int wn, unsigned char* scratch,
+                                         typename E::Acc (&acc)[4][4], F&& meanwhile) {
+    const int lane = threadIdx.x & 63, lr = lane & 15, lc = lane >> 4;
+    const int rend = min(t.r1, t.rlim), cend = min(t.clim, p.K);
+    if constexpr (kBf16Out) {
+        const int chunk = lane & 7, c = t.c0 + wn * 64 + chunk * 8;
+        u32x4 raw[4][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int r = t.r0 + wm * 64 + i * 16 + s * 8 + (lane >> 3);
+                const bf16_t* o = reinterpret_cast<const bf16_t*>(p.c) + ((size_t)t.e * p.N + r) * p.ldc + c;
+                raw[i][s] = u32x4{0, 0, 0, 0};
+                if (r >= rend || c >= cend) continue;
+                if (c + 7 < cend) {
+                    raw[i][s] = *reinterpret_cast<const u32x4*>(o);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 7; ++k)
+                        if (c + k < cend) raw[i][s][k >> 1] |= (uint32_t)o[k] << (16 * (k & 1));
+                }
+            }
+        meanwhile();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int row = s * 8 + (lane >> 3);
+                *reinterpret_cast<u32x4*>(scratch + row * 128 + (chunk ^ (row & 7)) * 16) = raw[i][s];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint2 w = *reinterpret_cast<const uint2*>(scratch + lr * 128 + ((2 * j + (lc >> 1)) ^ (lr & 7)) * 16 + (lc & 1) * 8);
+                acc[j][i] = typename E::Acc{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                                            __uint_as_float(w.y & 0xffff0000u)};
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = t.r0 + wm * 64 + i * 16 + lr, c = t.c0 + wn * 64 + j * 16 + lc * 4;
+                if (r < rend && c < cend)
+                    acc[j][i] = load_run<false>(reinterpret_cast<const float*>(p.c) + ((size_t)t.e * p.N + r) * p.ldc, c, cend);
+            }
+        meanwhile();
+    }
+}
 
 template <typename E, int kForm, bool kBf16Out, bool kSlim>
 __global__ __launch_bounds__(GT, kSlim ? 4 : 2) void grouped_mid_kernel(GroupedParams p) {
     constexpr bool kAcrossA = kForm == kWeightGrad, kAcrossB = kForm != kForward;
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[kSlim ? 2 * STAGE : SMEM];
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[kSlim ? 2 * STAGE + 4 * SCRATCH : SMEM];
     GroupedTile t;
     if (!grouped_tile<kForm>(p, xcd_tile(8), kGroupTile, kGroupTile, 16, E::kDepth, t)) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -65,24 +121,20 @@ __global__ __launch_bounds__(GT, kSlim ? 4 : 2) void grouped_mid_kernel(GroupedP
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int i = 0; i < MF; ++i) acc[j][i] = typename E::Acc{0, 0, 0, 0};
-        if constexpr (kForm == kWeightGrad && kSlim)
-            if (p.accumulate && p.splits == 1) {
-#pragma unroll
-                for (int i = 0; i < MF; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int r = t.r0 + wm * 16 * MF + i * 16 + (lane & 15), c = t.c0 + wn * 64 + j * 16 + lc * 4;
-                        if (r < t.r1 && c < p.K)
-                            acc[j][i] = load_run<kBf16Out>(reinterpret_cast<const char*>(p.c) + ((size_t)t.e * p.N + r) * p.ldc * (kBf16Out ? 2 : 4), c, p.K);
-                    }
-            }
         if constexpr (kSlim) {
             // one stage: four workgroups share a compute unit and cover each
             // other's waits
             unsigned char* const sb1 = smem + STAGE;
-            for (int kt = 0; kt < nk; ++kt) {
+            auto request = [&](int kt) {
                 la.request(kt, smem + wave * (NA * 1024));
                 lb.request(kt, sb1 + wave * (NI * 1024));
+            };
+            // what C is added to starts the accumulators, read beside the first
+            // K tile
+            if (p.accumulate) old_tile<E, kBf16Out>(p, t, wm, wn, smem + 2 * STAGE + wave * SCRATCH, acc, [&] { request(0); });
+            else request(0);
+            for (int kt = 0; kt < nk; ++kt) {
+                if (kt > 0) request(kt);
                 __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
                 barrier_no_fence();
 #pragma unroll
@@ -178,7 +230,7 @@ __global__ __launch_bounds__(GT, kSlim ? 4 : 2) void grouped_mid_kernel(GroupedP
 #pragma unroll
                 for (int i = 0; i < MF; ++i) acc[j][i] += total[j][i];
         barrier_no_fence();  // every wave has read its fragments: LDS becomes the stores' scratch
-        store_tile<E, kForm, kBf16Out, MF, 4>(
+        store_tile<E, kForm, kBf16Out, MF, 4, kSlim>(
             p, t, t.r0 + wm * 16 * MF, smem + wave * 4096, [&](int q) { return t.c0 + wn * 64 + q * 4; },
             [&](int i, int j) { return acc[j][i]; });
     };
