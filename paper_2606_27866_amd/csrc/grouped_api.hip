@@ -157,12 +157,12 @@ Plan plan(const flexmoe_grouped_desc& D, GroupedForm form, bool int8, int R) {
     // A weight gradient that is not split is bound by its stores while groups
     // are short: four small workgroups per compute unit, whose stores and
     // requests cover each other.  Against 256 x 256 tiles, 60 groups of 1408 x
-    // 2048 at 34 / 136 / 273 / 546 rows each: 130 to 159, 189 to 209, 247 to
-    // 253, 340 to 336 us; 8 of 14336 x 4096 at 32 / 256 / 512: 349 to 385, 589
-    // to 543, 795 to 724.
+    // 2048 at 68 / 136 / 273 / 546 rows each: 140 to 181, 176 to 212, 226 to 258,
+    // 317 to 344 us; 8 of 14336 x 4096 at 512 / 1024 / 2048: 769 to 739, 1156 to
+    // 1096, 2177 to 1823.
     // (fp32 only up to 1024 rows: those workgroups have no registers for a second
     // level of sums.)
-    if (form == kWeightGrad && pl.splits == 1 && R < 256LL * D.groups && (pl.elem == kElemBf16 || R <= 1024)) pl.tiles = kSlim;
+    if (form == kWeightGrad && pl.splits == 1 && R < 512LL * D.groups && (pl.elem == kElemBf16 || R <= 1024)) pl.tiles = kSlim;
     if (pl.splits > 1) pl.workspace = (size_t)(out * pl.splits);
     return pl;
 }

@@ -14,6 +14,7 @@ namespace flexmoe {
 namespace {
 
 constexpr int QT = 256;
+constexpr int kManyRows = 1024;  // rows from which a wave takes a row of up to 4096 values
 
 template <bool kBf16>
 __device__ __forceinline__ void load8(const void* p, size_t i, bool upper, float (&v)[8]) {
@@ -128,8 +129,13 @@ __global__ __launch_bounds__(QT) void quantize_kernel(const void* x, const void*
 
 template <bool kBf16, bool kGated>
 void launch(const void* x, const void* x2, size_t ldx, int8_t* q, size_t ldq, float* scale, int rows, int cols, hipStream_t s) {
+    const int by4 = (rows + 3) / 4;
     if (cols <= 512)
-        quantize_kernel<kBf16, kGated, 1, 1><<<(rows + 3) / 4, QT, 0, s>>>(x, x2, ldx, q, ldq, scale, rows, cols);
+        quantize_kernel<kBf16, kGated, 1, 1><<<by4, QT, 0, s>>>(x, x2, ldx, q, ldq, scale, rows, cols);
+    else if (rows >= kManyRows && cols <= 2048)
+        quantize_kernel<kBf16, kGated, 1, 4><<<by4, QT, 0, s>>>(x, x2, ldx, q, ldq, scale, rows, cols);
+    else if (rows >= kManyRows && cols <= 4096)
+        quantize_kernel<kBf16, kGated, 1, 8><<<by4, QT, 0, s>>>(x, x2, ldx, q, ldq, scale, rows, cols);
     else if (cols <= 2048)
         quantize_kernel<kBf16, kGated, 4, 1><<<rows, QT, 0, s>>>(x, x2, ldx, q, ldq, scale, rows, cols);
     else if (cols <= 4096)
