@@ -11,12 +11,14 @@
  * offline-clipped mode (Table 2), the bucketed kernel design of App. C.3 as an
  * ablation, the channel saliency of Eq. 2 on the device, and one
  * action-learning step (Eqs. 5-8): sampled widths, the masked layer's
- * training forward and backward, and the action-logit gradient.
+ * training forward and backward, and the action-logit gradient.  For training
+ * pruned experts back and serving them in fewer bytes: the experts' products
+ * with both gradients, products in 8-bit integers, and AdamW.
  *
  * General rules for every entry point
  *   - All pointers except the descriptor, the host keep table of
- *     flexmoe_set_budget and the debug-output struct are DEVICE pointers of the
- *     current HIP device.  The caller owns and allocates every buffer,
+ *     flexmoe_set_budget, the debug-output struct and flexmoe_adamw_step's list
+ *     of tensors are DEVICE pointers of the current HIP device.  The caller owns and allocates every buffer,
  *     including the forward workspace; the library allocates no device memory
  *     and keeps no device data between calls, except the static scratch array
  *     of flexmoe_layer_forward_noalloc (below).
@@ -412,9 +414,12 @@ int flexmoe_layer_forward_bucketed(const flexmoe_layer_desc *desc, int32_t T, co
  * length, at most 2^21 and whole 16-byte units; 0 <= R <= max_rows <= 2^30.
  * Matrices start on 16-byte boundaries, and a row may be read up to the 16-byte
  * unit that its last element lies in; no element past the row is written.
- * Workspace: flexmoe_grouped_workspace_bytes(desc, R), 256-byte aligned; one
- * sized for max_rows serves every smaller R and all three products.  R = 0 is a
- * no-op for forward and input grad; weight grad writes its zeros. */
+ * Workspace (256-byte aligned, FLEXMOE_EWORKSPACE otherwise): partial sums of
+ * reductions that are split over workgroups where there are few tiles.
+ * flexmoe_grouped_workspace_bytes(desc, R) bytes serve all three products and
+ * every smaller R; with less (or NULL and 0) a reduction is split less, which
+ * may change the order of its sums.  R = 0 is a no-op for forward and input
+ * grad; weight grad writes its zeros. */
 enum { FLEXMOE_KEEP_NONE = 0, FLEXMOE_KEEP_N = 1, FLEXMOE_KEEP_K = 2 };
 typedef struct flexmoe_grouped_desc {
     int32_t groups;

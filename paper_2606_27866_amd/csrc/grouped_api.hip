@@ -12,6 +12,7 @@ using namespace flexmoe;
 namespace {
 
 constexpr long long kMaxStride = 1 << 21;  // elements: a tile's rows stay below 2^31 bytes apart
+constexpr size_t kMostPartial = 256u << 20;  // bytes of partial sums that are worth joining
 constexpr int kMaxInt8Depth = 131071;      // 128 * 128 * K stays below 2^31
 
 bool misaligned(const void* p, uintptr_t mask) { return ((uintptr_t)p & mask) != 0; }
@@ -134,7 +135,8 @@ double product_us(const flexmoe_grouped_desc& D, GroupedForm form, GroupedElem e
     return us;
 }
 
-Plan plan(const flexmoe_grouped_desc& D, GroupedForm form, bool int8, int R) {
+// The plan of a call whose workspace holds `room` bytes of partial sums.
+Plan plan(const flexmoe_grouped_desc& D, GroupedForm form, bool int8, int R, size_t room) {
     Plan pl{form, int8 ? kElemI8 : D.dtype == FLEXMOE_BF16 ? kElemBf16 : kElemF32, kMid, 1, 0};
     const long long cols = form == kForward ? D.N : D.K;
     const long long out = (form == kWeightGrad ? (long long)D.groups * D.N : (long long)R) * ((cols + 3) / 4 * 4) * 4;
@@ -142,10 +144,10 @@ Plan plan(const flexmoe_grouped_desc& D, GroupedForm form, bool int8, int R) {
     for (Tiles kind : {kMid, kFew, kBig}) {
         if ((kind == kBig && pl.elem == kElemF32) || (kind == kFew && form == kWeightGrad)) continue;
         for (int splits = 1; splits <= 64; splits = splits < 4 ? splits + 1 : splits * 3 / 2) {
-            // parts of at least one K tile, partial sums of at most 256 MB
+            // parts of at least one K tile
             const int kd = pl.elem == kElemI8 ? 128 : pl.elem == kElemBf16 ? 64 : 32;
             const double depth = form == kWeightGrad ? (double)R / D.groups : form == kForward ? D.K : D.N;
-            if (splits > 1 && (depth < (double)kd * splits || out * splits > (256LL << 20))) break;
+            if (splits > 1 && (depth < (double)kd * splits || (size_t)(out * splits) > room)) break;
             const double us = product_us(D, form, pl.elem, kind, splits, R);
             if (us < best) {
                 best = us;
@@ -179,11 +181,9 @@ int launch(const flexmoe_grouped_desc* D, const Strides& st, GroupedForm form, b
     if (misaligned(a, 15) || misaligned(b, 15) || misaligned(c, 15)) return fail(FLEXMOE_EINVAL, "%s: matrices must be 16-byte aligned", who);
     if (misaligned(offsets, 3) || misaligned(keep, 3) || misaligned(sa, 3) || misaligned(sb, 3))
         return fail(FLEXMOE_EINVAL, "%s: offsets, keep and scales must be 4-byte aligned", who);
-    const Plan pl = plan(*D, form, int8, R);
-    if (pl.workspace) {
-        if (!ws || ws_bytes < pl.workspace) return fail(FLEXMOE_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, ws ? ws_bytes : 0, pl.workspace);
-        if (misaligned(ws, 255)) return fail(FLEXMOE_EWORKSPACE, "%s: workspace must be 256-byte aligned", who);
-    }
+    if (!ws) ws_bytes = 0;
+    if (misaligned(ws, 255)) return fail(FLEXMOE_EWORKSPACE, "%s: workspace must be 256-byte aligned", who);
+    const Plan pl = plan(*D, form, int8, R, std::min(ws_bytes, kMostPartial));
     GroupedParams p{};
     p.a = a, p.b = b, p.c = c, p.sa = sa, p.sb = sb, p.offsets = offsets, p.keep = keep, p.partial = ws;
     p.E = D->groups, p.R = R, p.N = D->N, p.K = D->K, p.keep_axis = D->keep_axis;
@@ -219,10 +219,12 @@ size_t workspace_bytes(const flexmoe_grouped_desc* D, int R, bool int8, const ch
     Strides st;
     if (check(D, int8, who, &st) || check_rows(D, R, who)) return 0;
     size_t most = 256;  // 0 stands for an error
-    // what fewer rows need may be more: their reductions are split further
+    // Fewer rows may use more: their reductions are split further.  Not every
+    // smaller R is looked at; one between takes what there is.
     for (int form = kForward; form <= (int8 ? kForward : kWeightGrad); ++form)
-        for (int r = R; r > 0; r = r > 64 ? r * 15 / 16 : r - 1) most = std::max(most, plan(*D, (GroupedForm)form, int8, r).workspace);
-    return most;
+        for (int r = R; r > 0; r = r > 64 ? r * 15 / 16 : r - 1)
+            most = std::max(most, plan(*D, (GroupedForm)form, int8, r, kMostPartial).workspace);
+    return (most + 255) & ~size_t(255);
 }
 
 }  // namespace

@@ -681,36 +681,45 @@ class AdamW:
         if state_bits not in (8, 32):
             raise ValueError("state_bits must be 8 or 32, got %s" % (state_bits,))
         dt = self.params[0].dtype
-        for p in self.params:
-            self._like(p, p.numel(), dt, "params")
         sizes = [p.numel() for p in self.params]
+        st = torch.uint8 if state_bits == 8 else torch.float32
         if states is None:
             def zeros(n, dtype):
                 return torch.zeros(n, dtype=dtype, device=self.params[0].device)
 
-            st = torch.uint8 if state_bits == 8 else torch.float32
             states = ([zeros(n, st) for n in sizes], [zeros(n, st) for n in sizes])
             if state_bits == 8:
                 blocks = [-(-n // STATE_BLOCK) for n in sizes]
                 states += ([zeros(n, torch.float32) for n in blocks], [zeros(n, torch.float32) for n in blocks])
         self.m, self.v = states[:2]
         self.m_scale, self.v_scale = states[2:] if state_bits == 8 else (None, None)
-        st = torch.uint8 if state_bits == 8 else torch.float32
         self._table = (flexmoe_adamw_tensor * len(sizes))()
-        for i, n in enumerate(sizes):
-            e = self._table[i]
-            e.param, e.n = self.params[i].data_ptr(), n
-            e.m, e.v = (self._like(s[i], n, st, "states") for s in (self.m, self.v))
-            if state_bits == 8:
-                e.m_scale, e.v_scale = (self._like(s[i], -(-n // STATE_BLOCK), torch.float32, "scales")
-                                        for s in (self.m_scale, self.v_scale))
-            if masters is not None:
-                e.master = self._like(masters[i], n, torch.float32, "masters")
-        # the table's gradient column is filled by every step
         self._n = np.array(sizes, dtype=np.int64)
+        np.frombuffer(self._table, dtype=np.int64)[flexmoe_adamw_tensor.n.offset // 8::ctypes.sizeof(flexmoe_adamw_tensor) // 8] = self._n
+        blocks = [-(-n // STATE_BLOCK) for n in sizes]
+        self._fill("param", self.params, sizes, dt, "params")
+        self._fill("m", self.m, sizes, st, "states")
+        self._fill("v", self.v, sizes, st, "states")
+        if state_bits == 8:
+            self._fill("m_scale", self.m_scale, blocks, torch.float32, "scales")
+            self._fill("v_scale", self.v_scale, blocks, torch.float32, "scales")
+        if masters is not None:
+            self._fill("master", masters, sizes, torch.float32, "masters")
+        # the table's gradient column is filled by every step
         self._column = (self._n.ctypes.data, ctypes.addressof(self._table) + flexmoe_adamw_tensor.grad.offset,
                         ctypes.sizeof(flexmoe_adamw_tensor))
         self.sizes, self._param_code = sizes, _dtype_code(dt)
+
+    def _fill(self, field, tensors_, sizes, dtype, name):
+        """One column of the table; every tensor holds at least sizes[i] values."""
+        if len(tensors_) != len(sizes):
+            raise ValueError("%s: %d tensors for %d parameters" % (name, len(tensors_), len(sizes)))
+        at, stride = ctypes.addressof(self._table) + getattr(flexmoe_adamw_tensor, field).offset, ctypes.sizeof(flexmoe_adamw_tensor)
+        n = np.array(sizes, dtype=np.int64)
+        code = {"torch.float32": 0, "torch.bfloat16": 1, "torch.uint8": 2}.get(str(dtype))
+        if code is None or tensors().column(list(tensors_), n.ctypes.data, code, at, stride) >= 0:
+            for i, t in enumerate(tensors_):
+                setattr(self._table[i], field, self._like(t, sizes[i], dtype, name))
 
     @staticmethod
     def _like(t, n, dtype, name):

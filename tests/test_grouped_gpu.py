@@ -277,3 +277,12 @@ def test_a_reduction_that_passes_2_31_bytes():
     offsets = torch.tensor([0, R], dtype=torch.int32, device="cuda")
     assert torch.equal(op.weight_grad(dy, x, offsets)[0].double(), dy.double().T.contiguous() @ x.double())
     assert torch.equal(op.forward(x, w, offsets).double(), x.double() @ w[0].double().T)
+
+
+def test_without_a_workspace():
+    """No partial sums: one part, the same values within the sums' bound."""
+    c = Case([70, 3, 33, 16], 700, 5000, BF)
+    y = torch.empty(c.R, 704, dtype=BF, device="cuda")[:, :700]
+    c.op.forward(c.x, c.w, c.offsets)  # sets the descriptor's strides
+    fm.flexmoe_grouped_forward(c.op.desc, c.R, c.x, c.w, c.offsets, None, y, None, 0)
+    c.check(y, "forward")

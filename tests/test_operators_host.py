@@ -129,3 +129,22 @@ def test_adamw_read_state_refusals():
     assert code_of(f, 1, FAKE, FAKE, None, FAKE, 0, FAKE, FAKE, 0) == -1
     assert code_of(f, 1, FAKE, FAKE, FAKE, FAKE, 0, FAKE + 2, FAKE, 0) == -1
     f(0, None, None, None, None, 0, None, None, 0)
+
+
+def test_tensor_column_refuses_what_is_no_gpu_tensor():
+    import numpy as np
+    import torch
+    table, sizes = np.zeros(4, np.uint64), np.array([3, 4], np.int64)
+    column = fm.tensors().column
+    assert column([], 0, 0, 0, 8) == -1
+    assert column([torch.zeros(3), torch.zeros(4)], sizes.ctypes.data, 0, table.ctypes.data, 8) == 0  # not on the GPU
+    assert column([None, torch.zeros(4)], sizes.ctypes.data, 0, table.ctypes.data, 8) == 0
+    assert not table.any()
+    with pytest.raises(TypeError):
+        column((), 0, 0, 0, 8)
+
+
+def test_products_run_with_any_workspace():
+    """Too little workspace is no error (reductions are split less); a misaligned one is."""
+    D = grouped()
+    assert code_of(fm.flexmoe_grouped_forward, D, 1, FAKE, FAKE, FAKE, None, FAKE, FAKE + 8, 1 << 20, 0) == -4
