@@ -60,7 +60,8 @@ __device__ __forceinline__ int group_width(const GroupedParams& p, int e, int fu
 // counts groups 4l .. 4l + 3.  Groups are taken in their order, or, where their
 // widths set the length of the reduction, in four classes of width, the widest
 // first, so that a launch ends on short tiles (60 groups of 1408 x 2048, 16384
-// rows, input gradient 105 -> 96 us; 8 of 4096 x 14336, forward 992 -> 1010).  All 64 lanes must be active and q uniform.
+// rows with widths, input gradient 94 -> 85 us; 8 of 4096 x 14336, forward: no
+// difference).  All 64 lanes must be active and q uniform.
 __device__ __forceinline__ bool find_group(const GroupedParams& p, int bm, int q, bool by_width, int full, int& e, int& row0,
                                            int& rows, int& first, int& tiles) {
     static_assert(kMaxExperts <= 4 * kWave, "four groups per lane");
@@ -582,81 +583,81 @@ __device__ __forceinline__ void store_tile(const GroupedParams& p, const Grouped
         store_tile_bf16<E, kForm, kRows, kCols>(p, t, first, scratch, column, value);
         return;
     } else {
-    if constexpr (kBf16Out)
-        if (p.splits == 1 && (kForm != kWeightGrad || !p.accumulate)) {
-            store_tile_bf16<E, kForm, kRows, kCols>(p, t, first, scratch, column, value);
-            return;
-        }
-    const int lane = threadIdx.x & 63, lr = lane & 15, lc = lane >> 4;
-    const int cols = kForm == kForward ? p.N : p.K;
-    const bool add = kForm == kWeightGrad && !kWhole && p.accumulate && p.splits == 1;
-    constexpr int kRuns = 4 * kCols, kSteps = kCols;  // runs of a row; stores per fragment
-    const int run = lane % kRuns, sub = lane / kRuns;  // a store's run and row (of 64 / kRuns) for this lane
-    auto row_of = [&](int s) { return s * (64 / kRuns) + sub; };
-    const int c = column(run);
-    auto crow_of = [&](int r) { return kForm == kWeightGrad ? (size_t)t.e * p.N + r : (size_t)t.row0 + r; };
-    auto address = [&](int r) { return reinterpret_cast<char*>(p.c) + crow_of(r) * p.ldc * (kBf16Out ? 2 : 4); };
-    // old values are read a fragment ahead: the compiler keeps a read behind
-    // the stores before it
-    floatx4 old[kForm == kWeightGrad ? 2 : 1][kSteps];
-    auto load_old = [&](int i) {
+        if constexpr (kBf16Out)
+            if (p.splits == 1 && (kForm != kWeightGrad || !p.accumulate)) {
+                store_tile_bf16<E, kForm, kRows, kCols>(p, t, first, scratch, column, value);
+                return;
+            }
+        const int lane = threadIdx.x & 63, lr = lane & 15, lc = lane >> 4;
+        const int cols = kForm == kForward ? p.N : p.K;
+        const bool add = kForm == kWeightGrad && !kWhole && p.accumulate && p.splits == 1;
+        constexpr int kRuns = 4 * kCols, kSteps = kCols;  // runs of a row; stores per fragment
+        const int run = lane % kRuns, sub = lane / kRuns;  // a store's run and row (of 64 / kRuns) for this lane
+        auto row_of = [&](int s) { return s * (64 / kRuns) + sub; };
+        const int c = column(run);
+        auto crow_of = [&](int r) { return kForm == kWeightGrad ? (size_t)t.e * p.N + r : (size_t)t.row0 + r; };
+        auto address = [&](int r) { return reinterpret_cast<char*>(p.c) + crow_of(r) * p.ldc * (kBf16Out ? 2 : 4); };
+        // old values are read a fragment ahead: the compiler keeps a read behind
+        // the stores before it
+        floatx4 old[kForm == kWeightGrad ? 2 : 1][kSteps];
+        auto load_old = [&](int i) {
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const int r = first + i * 16 + row_of(s);
-            if (r < t.r1 && c < cols) old[i & 1][s] = load_run<kBf16Out>(address(r), c, cols);
-        }
-    };
-    if constexpr (kForm == kWeightGrad)
-        if (add) load_old(0);
-    // int8: this lane's columns' and rows' scales, read before any store for
-    // the same reason
-    float sb[4], sa[kRows][kSteps];
-    if constexpr (E::kBytes == 1)
-        if (p.splits == 1) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) sb[k] = c + k < cols ? p.sb[(size_t)t.e * p.N + c + k] : 0.f;
-#pragma unroll
-            for (int i = 0; i < kRows; ++i)
-#pragma unroll
-                for (int s = 0; s < kSteps; ++s) sa[i][s] = p.sa[crow_of(min(first + i * 16 + row_of(s), t.r1 - 1))];
-        }
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
+            for (int s = 0; s < kSteps; ++s) {
+                const int r = first + i * 16 + row_of(s);
+                if (r < t.r1 && c < cols) old[i & 1][s] = load_run<kBf16Out>(address(r), c, cols);
+            }
+        };
         if constexpr (kForm == kWeightGrad)
-            if (add && i + 1 < kRows) load_old(i + 1);
+            if (add) load_old(0);
+        // int8: this lane's columns' and rows' scales, read before any store for
+        // the same reason
+        float sb[4], sa[kRows][kSteps];
+        if constexpr (E::kBytes == 1)
+            if (p.splits == 1) {
 #pragma unroll
-        for (int j = 0; j < kCols; ++j)
-            *reinterpret_cast<typename E::Acc*>(scratch + lr * (kRuns * 16) + ((4 * j + lc) ^ (lr % kRuns)) * 16) = value(i, j);
+                for (int k = 0; k < 4; ++k) sb[k] = c + k < cols ? p.sb[(size_t)t.e * p.N + c + k] : 0.f;
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const int row = row_of(s), r = first + i * 16 + row;
-            typename E::Acc v = *reinterpret_cast<const typename E::Acc*>(scratch + row * (kRuns * 16) + (run ^ (row % kRuns)) * 16);
-            const int clim = r < t.rlim ? t.clim : 0;
-            // what lies past a width is left as it is when C is added to
-            const int end = kForm == kWeightGrad && p.accumulate && p.splits == 1 ? min(clim, cols) : cols;
-            if (r >= t.r1 || c >= end) continue;
-            const size_t crow = crow_of(r);
+                for (int i = 0; i < kRows; ++i)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = c + k < clim ? v[k] : 0;
-            if (!kWhole && p.splits > 1) {
-                const size_t rows = kForm == kWeightGrad ? (size_t)p.E * p.N : (size_t)p.R;
-                const size_t ldp = (cols + 3) & ~3;
-                *reinterpret_cast<typename E::Acc*>(reinterpret_cast<char*>(p.partial) + ((t.split * rows + crow) * ldp + c) * 4) = v;
-                continue;
+                    for (int s = 0; s < kSteps; ++s) sa[i][s] = p.sa[crow_of(min(first + i * 16 + row_of(s), t.r1 - 1))];
             }
-            floatx4 f;
-            if constexpr (E::kBytes == 1) {
-                // past the width the factor may be anything: not multiplied
 #pragma unroll
-                for (int k = 0; k < 4; ++k) f[k] = c + k < clim ? (float)v[k] * (sa[i][s] * sb[k]) : 0.f;
-            } else {
-                f = v;
-            }
+        for (int i = 0; i < kRows; ++i) {
             if constexpr (kForm == kWeightGrad)
-                if (add) f += old[i & 1][s];
-            store_run<kBf16Out>(address(r), c, end, f);
+                if (add && i + 1 < kRows) load_old(i + 1);
+#pragma unroll
+            for (int j = 0; j < kCols; ++j)
+                *reinterpret_cast<typename E::Acc*>(scratch + lr * (kRuns * 16) + ((4 * j + lc) ^ (lr % kRuns)) * 16) = value(i, j);
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                const int row = row_of(s), r = first + i * 16 + row;
+                typename E::Acc v = *reinterpret_cast<const typename E::Acc*>(scratch + row * (kRuns * 16) + (run ^ (row % kRuns)) * 16);
+                const int clim = r < t.rlim ? t.clim : 0;
+                // what lies past a width is left as it is when C is added to
+                const int end = kForm == kWeightGrad && p.accumulate && p.splits == 1 ? min(clim, cols) : cols;
+                if (r >= t.r1 || c >= end) continue;
+                const size_t crow = crow_of(r);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = c + k < clim ? v[k] : 0;
+                if (!kWhole && p.splits > 1) {
+                    const size_t rows = kForm == kWeightGrad ? (size_t)p.E * p.N : (size_t)p.R;
+                    const size_t ldp = (cols + 3) & ~3;
+                    *reinterpret_cast<typename E::Acc*>(reinterpret_cast<char*>(p.partial) + ((t.split * rows + crow) * ldp + c) * 4) = v;
+                    continue;
+                }
+                floatx4 f;
+                if constexpr (E::kBytes == 1) {
+                    // past the width the factor may be anything: not multiplied
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) f[k] = c + k < clim ? (float)v[k] * (sa[i][s] * sb[k]) : 0.f;
+                } else {
+                    f = v;
+                }
+                if constexpr (kForm == kWeightGrad)
+                    if (add) f += old[i & 1][s];
+                store_run<kBf16Out>(address(r), c, end, f);
+            }
         }
-    }
     }
 }
 

@@ -74,9 +74,12 @@ constexpr int kUnits = 256;  // compute units
 // About the microseconds of a product on one kind of tiles with the reduction in
 // `splits` parts, from what the host knows (not how rows and widths spread).
 // Fitted to 3500 timings of 260 drawn products (1 to 128 groups, 1 to 32768
-// rows, sides of 24 to 20480, every form and type, 1 to 13 parts): the choice it
-// makes takes 4 % more time on average than the fastest of those tried, at most
-// 12 % more in 9 of 10 products.
+// rows, sides of 24 to 20480, every form and type, 1 to 13 parts).  On 515 other
+// draws its choice takes 5 % more time on average than the fastest of those
+// tried, at most 16 % more in 9 of 10, 1.85 times at worst.  It misses most where
+// memory bounds a last round that is not full: 60 groups of 1408 x 2048 without
+// widths, bf16, 1024 rows 89 us on 128-row tiles (32-row ones: 62), 4096 rows 100 on
+// 256-row tiles (128-row ones: 84).
 //   tiles     a K tile of 128 bytes costs a 256 x 256 tile 0.5 + 0.16 us per 64
 //             rows; a 128 x 128 tile alone on its compute unit 0.17 + 0.14 us
 //             per 32 rows (fp32: 0.1 + 0.45), two that share it 1.7 times that

@@ -20,10 +20,11 @@
 // Across halves are read through the transposing LDS reads, whose wait is part
 // of the read: there the requests go out first.
 //
-// Bound by the matrix cores at the card's power limit: 8192^3 in bf16 1377 (x
-// W^T), 1300 (dy W at 2048 columns), 1250 TFLOP/s (dy^T x), where the vendor's
-// library reaches 1410; 8192^3 in int8 2350 TOP/s (library 2067).  Runs of 32
-// tiles per XCD instead of 8: 1150, 1220, 1200 and 2230.
+// Bound by the matrix cores at the card's power limit: 8192^3 in bf16 1500 (x
+// W^T), 1398 (dy W at 2048 columns), 1296 TFLOP/s (dy^T x), where the vendor's
+// library reaches 1615 (x W^T) in the same run; 8192^3 in int8, with the
+// rounding of the rows, 2610 TOP/s (library, without, 2490).  Another card, 1377
+// (x W^T), with runs of 32 tiles per XCD instead of 8: 1150.
 #include "grouped.h"
 
 namespace flexmoe {

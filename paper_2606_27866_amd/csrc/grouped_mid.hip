@@ -9,6 +9,10 @@
 // bytes, one that is not as K-tile rows of 128 values, which the fragment
 // reads transpose (across_frag).
 //
+// Between the other two kinds of tiles: 60 groups of 1408 x 2048, bf16 x W^T, at
+// 4096 rows 84 us (256 x 256 tiles: 100), at 16384 148 (147).  A small form with
+// one stage (40 KB, four workgroups) takes short weight gradients.
+//
 // What lies outside a group, a width or a matrix reads as zeros: whole rows
 // and 16-byte chunks by offsets past the descriptor, the elements of a chunk
 // that straddles the end of the reduction by clearing both fragments, C's
@@ -151,76 +155,76 @@ __global__ __launch_bounds__(GT, kSlim ? 4 : 2) void grouped_mid_kernel(GroupedP
                 if (kt + 1 < nk) barrier_no_fence();
             }
         } else {
-        request_a(0, 0);
-        request_b(0, 0);
-        request_b(1, 1);
-        int st_b = 0;
-        for (int kt = 0; kt < nk; ++kt) {
-            // tile kt is in when only B of tile kt + 1 is outstanding; this
-            // wave's LDS reads of tile kt - 1 are done, so that its stages may
-            // be refilled after the barrier
-            __builtin_amdgcn_s_waitcnt(waitcnt_vm(NI) & kWaitLgkm0);
-            barrier_no_fence();
-            request_a(kt + 1, (kt + 1) & 1);
-            request_b(kt + 2, st_b == 0 ? 2 : st_b - 1);
-            const unsigned char* at = sa + (kt & 1) * STAGE;
-            const unsigned char* bt = sb + st_b * STAGE;
-            st_b = st_b == 2 ? 0 : st_b + 1;
-            if constexpr (kTwoLevels) {
-                // one K step at a time: the fragments of both would not fit
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    typename E::Frag fa[MF], fb[4];
-                    read_step<E, kAcrossB, 4>(bt, wn * 64, s, fb);
-                    read_step<E, kAcrossA, MF>(at, wm * 16 * MF, s, fa);
-                    if constexpr (!kAcrossA)
-                        if (kt == nk - 1 && depth % E::kPer) {
-                            const int valid = depth - kt * E::kDepth - (s * 4 + lc) * E::kPer;
-#pragma unroll
-                            for (int i = 0; i < MF; ++i) fa[i] = head<E>(fa[i], valid);
-                            if constexpr (!kAcrossB)
-#pragma unroll
-                                for (int j = 0; j < 4; ++j) fb[j] = head<E>(fb[j], valid);
-                        }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int i = 0; i < MF; ++i) acc[j][i] = E::mma(fb[j], fa[i], acc[j][i]);
-                }
-                if (kt % kFlush == kFlush - 1)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int i = 0; i < MF; ++i) {
-                            total[j][i] += acc[j][i];
-                            acc[j][i] = typename E::Acc{0, 0, 0, 0};
-                        }
-                continue;
-            } else {
-            typename E::Frag fa[2][MF], fb[2][4];
-            read_frags<E, kAcrossB, 4>(bt, wn * 64, fb);
-            read_frags<E, kAcrossA, MF>(at, wm * 16 * MF, fa);
-            if constexpr (!kAcrossA)
-                if (kt == nk - 1 && depth % E::kPer) {
+            request_a(0, 0);
+            request_b(0, 0);
+            request_b(1, 1);
+            int st_b = 0;
+            for (int kt = 0; kt < nk; ++kt) {
+                // tile kt is in when only B of tile kt + 1 is outstanding; this
+                // wave's LDS reads of tile kt - 1 are done, so that its stages may
+                // be refilled after the barrier
+                __builtin_amdgcn_s_waitcnt(waitcnt_vm(NI) & kWaitLgkm0);
+                barrier_no_fence();
+                request_a(kt + 1, (kt + 1) & 1);
+                request_b(kt + 2, st_b == 0 ? 2 : st_b - 1);
+                const unsigned char* at = sa + (kt & 1) * STAGE;
+                const unsigned char* bt = sb + st_b * STAGE;
+                st_b = st_b == 2 ? 0 : st_b + 1;
+                if constexpr (kTwoLevels) {
+                    // one K step at a time: the fragments of both would not fit
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
-                        const int valid = depth - kt * E::kDepth - (s * 4 + lc) * E::kPer;
+                        typename E::Frag fa[MF], fb[4];
+                        read_step<E, kAcrossB, 4>(bt, wn * 64, s, fb);
+                        read_step<E, kAcrossA, MF>(at, wm * 16 * MF, s, fa);
+                        if constexpr (!kAcrossA)
+                            if (kt == nk - 1 && depth % E::kPer) {
+                                const int valid = depth - kt * E::kDepth - (s * 4 + lc) * E::kPer;
 #pragma unroll
-                        for (int i = 0; i < MF; ++i) fa[s][i] = head<E>(fa[s][i], valid);
-                        if constexpr (!kAcrossB)
+                                for (int i = 0; i < MF; ++i) fa[i] = head<E>(fa[i], valid);
+                                if constexpr (!kAcrossB)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) fb[s][j] = head<E>(fb[s][j], valid);
+                                    for (int j = 0; j < 4; ++j) fb[j] = head<E>(fb[j], valid);
+                            }
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                            for (int i = 0; i < MF; ++i) acc[j][i] = E::mma(fb[j], fa[i], acc[j][i]);
                     }
+                    if (kt % kFlush == kFlush - 1)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                            for (int i = 0; i < MF; ++i) {
+                                total[j][i] += acc[j][i];
+                                acc[j][i] = typename E::Acc{0, 0, 0, 0};
+                            }
+                    continue;
+                } else {
+                    typename E::Frag fa[2][MF], fb[2][4];
+                    read_frags<E, kAcrossB, 4>(bt, wn * 64, fb);
+                    read_frags<E, kAcrossA, MF>(at, wm * 16 * MF, fa);
+                    if constexpr (!kAcrossA)
+                        if (kt == nk - 1 && depth % E::kPer) {
+#pragma unroll
+                            for (int s = 0; s < 2; ++s) {
+                                const int valid = depth - kt * E::kDepth - (s * 4 + lc) * E::kPer;
+#pragma unroll
+                                for (int i = 0; i < MF; ++i) fa[s][i] = head<E>(fa[s][i], valid);
+                                if constexpr (!kAcrossB)
+#pragma unroll
+                                    for (int j = 0; j < 4; ++j) fb[s][j] = head<E>(fb[s][j], valid);
+                            }
+                        }
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                            for (int i = 0; i < MF; ++i) acc[j][i] = E::mma(fb[s][j], fa[s][i], acc[j][i]);
                 }
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int i = 0; i < MF; ++i) acc[j][i] = E::mma(fb[s][j], fa[s][i], acc[j][i]);
             }
-        }
         }
         __builtin_amdgcn_s_waitcnt(waitcnt_vm(0) & kWaitLgkm0);  // no request may outlive the loop
 
