@@ -185,6 +185,10 @@ __device__ __forceinline__ void read_values(const flexmoe_adamw_tensor& t, size_
 template <typename P, typename G, int kBits, bool kFull, bool kMaster>
 __device__ __forceinline__ void step_values(const AdamwArgs& a, const flexmoe_adamw_tensor& t, size_t i, int n, uint32_t key,
                                             Values<P>& x) {
+    // every product and sum rounded by itself: whether a code is rounded up hangs
+    // on the last bit, and the formula's own roundings decide, not which of them
+    // the compiler fuses
+#pragma clang fp contract(off)
     uint32_t top_m = 0, top_v = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -218,7 +222,7 @@ __device__ __forceinline__ void step_values(const AdamwArgs& a, const flexmoe_ad
         // scale of m: the power of two that top is at most 1.875 times of
         const uint32_t sb = max((top_m + 0xfffffu) & 0x7f800000u, 0x00800000u);
         const int down = 127 - (int)(sb >> 23);
-        const float per_v = 65025.f / tv;
+        const float per_v = 65025.f * (1.f / tv);
         constexpr float kLeast = 1.125f / 32768.f;  // code 1
         uint32_t mc = 0, vc = 0;
 #pragma unroll

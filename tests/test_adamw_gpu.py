@@ -165,6 +165,51 @@ def test_8_bit_states_follow_a_long_run():
     assert abs(float(v[rest].mean()) / 0.02 ** 2 - 1) < 0.05
 
 
+def test_8_bit_codes_come_from_sums_rounded_step_by_step():
+    """Every product and sum of the running means rounded by itself, 65025 times the reciprocal of v's largest: the codes of
+    that arithmetic and no others.  A value that one rounding less leaves a bit away can pass its random threshold, and
+    where v's code is small the next update doubles or halves.  No code may differ: both sides compute the same numbers.
+    (Only sqrt's last bit is not fixed, and it decides nothing: a root that falls just short of k has a remainder that
+    takes it up to k but for one draw in 65536 of the values, few, that lie within a bit of a square.)"""
+    n, t, seed = 1 << 22, 7, 5
+    g = torch.Generator(device="cuda").manual_seed(3)
+    grad = torch.empty(n, device="cuda").normal_(0, 1e-3, generator=g)
+    opt = fm.AdamW([torch.zeros(n, device="cuda")], state_bits=8, betas=(B1, 0.95), eps=EPS, step=t - 1, seed=seed)
+    opt.m[0].random_(0, 256, generator=g)
+    opt.v[0].random_(0, 256, generator=g)
+    for s in (opt.m_scale[0], opt.v_scale[0]):
+        s.uniform_(1e-5, 3e-5, generator=g)
+    opt.m_scale[0].copy_(torch.exp2(torch.floor(torch.log2(opt.m_scale[0]))))
+    f, u = np.float32, np.uint32
+    mc, vc = (x[0].cpu().numpy().reshape(-1, 256) for x in (opt.m, opt.v))
+    ms, vs = (x[0].cpu().numpy().reshape(-1, 1) for x in (opt.m_scale, opt.v_scale))
+    grad_h = grad.cpu().numpy().reshape(-1, 256)
+    opt.step([grad], LR)
+    k = (mc & 127).astype(u)
+    m = np.where(k > 0, ((k + u(896)) << u(20)).view(f), f(0)) * ms
+    m = np.where(mc > 127, -m, m) * f(B1) + grad_h * f(1 - B1)
+    root = vc.astype(f) * vs
+    v = (root * root) * f(0.95) + (grad_h * grad_h) * f(1 - 0.95)
+    h = np.arange(n, dtype=np.uint64) + np.uint64(seed * 0x3504F335 + t * 0x5851F42D)
+    h = h.astype(u)
+    h = (h ^ (h >> u(16))) * u(0x45D9F3B5)
+    h = (h ^ (h >> u(15))) * u(0x2C1B3C6D)
+    r = (h ^ (h >> u(16))).reshape(-1, 256)
+    top = np.abs(m).max(1, keepdims=True)
+    scale = ((top.view(u) + u(0xFFFFF)) & u(0x7F800000)).view(f)
+    y = np.abs(m) / scale
+    c = np.clip(((y.view(u).astype(np.int64) + ((r >> u(16)).astype(np.int64) << 4)) >> 20) - 896, 0, 127)
+    least = f(1.125 / 32768)
+    c = np.where(y < least, (r >> u(16)).astype(f) * (least / f(65536)) < y, c) + np.where(m < 0, 128, 0)
+    z = v * (f(65025) * (f(1) / v.max(1, keepdims=True)))
+    low = np.floor(np.sqrt(z))
+    up = (r & u(0xFFFF)).astype(f) * f(1 / 65536) * (2 * low + f(1)) < z - low * low
+    d = np.clip(low + up, (v > 0).astype(f), f(255))
+    assert z.dtype == f and y.dtype == f and m.dtype == f and v.dtype == f
+    assert int((opt.m[0].cpu().numpy().reshape(-1, 256) != c).sum()) == 0
+    assert int((opt.v[0].cpu().numpy().reshape(-1, 256) != d).sum()) == 0
+
+
 def test_same_bits_again_and_other_bits_from_another_seed():
     def run(seed):
         g = torch.Generator(device="cuda")
