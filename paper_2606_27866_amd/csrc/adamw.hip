@@ -27,7 +27,8 @@
 // consecutive values at a time (4 per lane: 16-byte accesses of fp32), with 8-bit
 // states one of those, with 32-bit ones four, or two in lists of less than 2^24
 // values (100 M values, bf16 with master: 8 bits 267 us for one, 276 for two, 279
-// for four: 6.0 TB/s; 32 bits 483, 481, 468: 6.0 TB/s; 1.5 M values in 192
+// for four with sums fused as the compiler likes, 278 for one with every rounding
+// kept, on another card: 5.8 TB/s; 32 bits 483, 481, 468: 6.0 TB/s; 1.5 M values in 192
 // tensors, 32 bits: 19, 17, 22 us).  Every value is read once and written once,
 // with the non-temporal hint (8 bits 307 -> 279 us, 32 bits 525 -> 468).  The
 // list travels in the kernel's arguments, 56 tensors a launch.
