@@ -472,7 +472,7 @@ def _matrix(t, shape, dtype, name):
     """Row stride of a [rows, cols] or [groups, rows, cols] tensor whose rows are contiguous."""
     if t.dtype is dtype and t.shape == shape and t.is_cuda and shape[-2] > 1:
         st = t.stride()
-        if st[-1] == 1 and (len(st) == 2 or st[0] == shape[1] * st[1]):
+        if st[-1] == 1 and st[-2] >= shape[-1] and (len(st) == 2 or st[0] == shape[1] * st[1]):
             return st[-2]
     return _matrix_checked(t, shape, dtype, name)
 
@@ -490,6 +490,9 @@ def _matrix_checked(t, shape, dtype, name):
             ld = t.stride(0)
         elif t.stride(0) != t.shape[1] * ld:
             raise ValueError("%s must hold its groups one after another (strides %s)" % (name, t.stride()))
+    # an expanded tensor repeats one row with stride 0, which in a descriptor would stand for packed rows
+    if t.numel() > t.shape[-1] and ld < t.shape[-1]:
+        raise ValueError("%s: rows overlap (strides %s); contiguous() makes a copy that can be used" % (name, t.stride()))
     return ld
 
 

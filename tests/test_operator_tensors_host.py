@@ -1,0 +1,90 @@
+"""What the holders of the experts' products, the 8-bit products and AdamW take from a tensor, without a GPU: CPU tensors
+that say they are on one (no call here reaches a kernel launch)."""
+import pytest
+
+torch = pytest.importorskip("torch")
+from paper_2606_27866_amd import flexmoe as fm  # noqa: E402
+
+BF, F32, I8 = torch.bfloat16, torch.float32, torch.int8
+
+
+class OnGpu(torch.Tensor):
+    is_cuda = property(lambda self: True)
+
+
+def on_gpu(t):
+    return t.as_subclass(OnGpu)
+
+
+@pytest.fixture
+def no_launch(monkeypatch):
+    """Any call of the library fails: what is refused must be refused before it."""
+    class Library:
+        def __getattr__(self, name):
+            def called(*_):
+                raise AssertionError("reached " + name)
+            return called
+
+    monkeypatch.setattr(fm, "lib", Library)
+
+
+def expanded(*shape, dtype=BF, over=0):
+    """A tensor that repeats one slice along dimension `over` with stride 0, as the gradient of a sum is."""
+    one = [1 if i == over else n for i, n in enumerate(shape)]
+    return on_gpu(torch.zeros(one, dtype=dtype).expand(shape))
+
+
+def holder(groups, N, K, rows=10, dtype=BF):
+    """A GroupedProduct without its workspace."""
+    op = object.__new__(fm.GroupedProduct)
+    op.groups, op.N, op.K, op.max_rows, op.keep_axis, op.dtype = groups, N, K, rows, "none", dtype
+    op._i32, op._f32, op._w_shape = torch.int32, F32, (groups, N, K)
+    op.desc, op._ws = fm.make_grouped_desc(groups, N, K, max_rows=rows), (0, 0)
+    return op
+
+
+def test_the_gradient_of_a_sum_is_an_expanded_tensor():
+    y = torch.zeros(10, 64, requires_grad=True)
+    z, seen = y * 1, []
+    z.register_hook(seen.append)
+    z.sum(0).backward(torch.ones(64))
+    assert seen[0].stride() == (0, 1)
+
+
+@pytest.mark.parametrize("t", [expanded(10, 64), expanded(10, 64, dtype=F32), expanded(10, 64, dtype=I8), expanded(10, 1),
+                               expanded(3, 4, 64, over=1), expanded(3, 1, 64), on_gpu(torch.zeros(3, 1, 64).expand(3, 4, 64)),
+                               on_gpu(torch.zeros(1, 1, 64).expand(3, 4, 64)),
+                               on_gpu(torch.zeros(100).as_strided((10, 64), (4, 1)))])
+def test_rows_that_overlap_are_refused(t):
+    with pytest.raises(ValueError):
+        fm._matrix(t, tuple(t.shape), t.dtype, "x")
+
+
+def test_rows_that_do_not_overlap_are_taken():
+    for t, ld in [(torch.zeros(10, 64), 64), (torch.zeros(10, 72)[:, :64], 72), (torch.zeros(1, 64).expand(1, 64), 64), (torch.zeros(0, 64), 64),
+                  (torch.zeros(3, 4, 64), 64), (torch.zeros(3, 1, 64), 64), (torch.zeros(3, 1, 72)[..., :64], 72), (torch.zeros(10, 8)[:, :1], 8)]:
+        assert fm._matrix(on_gpu(t), tuple(t.shape), F32, "x") == ld
+
+
+def test_products_refuse_expanded_tensors(no_launch):
+    E, N, K, R = 2, 16, 64, 10
+    op = holder(E, N, K)
+    offsets = on_gpu(torch.zeros(E + 1, dtype=torch.int32))
+    x, dy, w = (on_gpu(torch.zeros(s, dtype=BF)) for s in ((R, K), (R, N), (E, N, K)))
+    for f, args in [(op.forward, (expanded(R, K), w, offsets)), (op.forward, (x, expanded(E, N, K, over=0), offsets)),
+                    (op.forward, (x, expanded(E, N, K, over=1), offsets)), (op.input_grad, (expanded(R, N), w, offsets)),
+                    (op.weight_grad, (expanded(R, N), x, offsets)), (op.weight_grad, (dy, expanded(R, K), offsets))]:
+        with pytest.raises(ValueError, match="overlap|one after another"):
+            f(*args)
+    with pytest.raises(ValueError):
+        op.forward(x, w, offsets, y=expanded(R, N))
+    with pytest.raises(ValueError):
+        op.weight_grad(dy, x, offsets, dw=expanded(E, N, K, dtype=F32, over=1), accumulate=True)
+
+
+def test_rounded_rows_refuse_expanded_tensors(no_launch):
+    x = on_gpu(torch.zeros(10, 64))
+    for kw in (dict(x=expanded(10, 64, dtype=F32)), dict(x=x, gate=expanded(10, 64, dtype=F32)), dict(x=x, q=expanded(10, 64, dtype=I8)),
+               dict(x=expanded(10, 64, dtype=F32), gate=expanded(10, 64, dtype=F32))):
+        with pytest.raises(ValueError, match="overlap"):
+            fm.quantize_rows(**kw)
