@@ -156,6 +156,10 @@ __global__ __launch_bounds__(BT, 2) void grouped_big_kernel(GroupedParams p) {
         if (kt < nk) tile(kt, fx, fy);
         __builtin_amdgcn_s_waitcnt(waitcnt_vm(0) & kWaitLgkm0);
         if (wm == 0) barrier_no_fence();
+        // the lagging waves meet that barrier with up to five phases' zero fills
+        // in flight: one more, behind every wave's wait, before LDS becomes the
+        // stores' scratch
+        barrier_no_fence();
         __builtin_amdgcn_sched_barrier(0);
 
 #pragma unroll
