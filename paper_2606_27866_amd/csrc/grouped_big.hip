@@ -148,6 +148,9 @@ __global__ __launch_bounds__(BT, 2) void grouped_big_kernel(GroupedParams p) {
         if (wm == 1) barrier_no_fence();  // the lagging waves; the leading ones wait at the end
         __builtin_amdgcn_sched_barrier(0);
         read_b(0, 0, fx);
+        // its half is refilled in phase 1 of the leading waves, a slot sooner after
+        // this read than the loop's are after theirs
+        __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
         int kt = 0;
         for (; kt + 1 < nk; kt += 2) {
             tile(kt, fx, fy);

@@ -1,6 +1,5 @@
 """The 256 x 256 tiles' K loop and stores, compiled for the host from grouped_big.hip with requests, waits, barriers and LDS
-reads that write down when they happen: the stores' scratch is ordered behind whatever else uses its bytes, by a wait and a
-barrier.
+reads that write down when they happen: whatever two waves do to the same LDS bytes is ordered by a wait and a barrier.
 
 A wave's accesses carry the number of barriers it had passed when they began and when they were known to be done (a
 request: the wait that drains it; a read: the wait for LDS, or at once where the wait is part of the read).  An access that
@@ -13,12 +12,13 @@ import pytest
 
 from paper_2606_27866_amd import flexmoe as fm
 
-HALF, WAVES, REQUEST, SCRATCH = 16384, 8, 2048, 4096
+HALF, WAVES, REQUEST, SCRATCH = 16384, 8, 1024, 4096
 
-STUBS = """
+COMMON = """
 #include <cstdio>
 #include <type_traits>
-typedef unsigned int uint32_t_;
+#include <cstddef>
+#include <cstdint>
 constexpr int STAGE = 16384, NR = 2;
 static unsigned char memory[8 * STAGE];
 static unsigned char* const smem = memory;
@@ -29,7 +29,10 @@ inline void __builtin_amdgcn_s_waitcnt(int w) { std::printf("wait %d %d\\n", w &
 inline void barrier_no_fence() { std::printf("barrier\\n"); }
 inline void __builtin_amdgcn_sched_barrier(int) {}
 inline void __builtin_amdgcn_s_setprio(int) {}
-struct Loader { void request(int kt, unsigned char* dst) { std::printf("request %d %d\\n", kt, (int)(dst - smem)); } };
+inline void requested(int kt, const unsigned char* dst) { std::printf("request %d %d\\n", kt, (int)(dst - smem)); }
+"""
+
+STUBS = COMMON + """
 struct Tile { int r0, c0; };
 struct E { struct Frag {}; struct Acc {}; static constexpr int kDepth = 64; static Acc mma(Frag, Frag, Acc c) { return c; } };
 template <typename T, bool kAcross, int F> void read_frags(const unsigned char* at, int, typename T::Frag (&)[2][F]) {
@@ -42,6 +45,7 @@ template <typename T, int N> void clear_tail(typename T::Frag (&)[2][N], int) {}
 template <typename T, int kForm, bool kBf16Out, int kRows, int kCols, bool kWhole, typename P, typename C, typename V>
 void store_tile(P, const Tile&, int, unsigned char* scratch, C, V) { std::printf("store %d\\n", (int)(scratch - smem)); }
 
+struct Loader { void request(int kt, unsigned char* dst) { for (int i = 0; i < NR; ++i) requested(kt, dst + i * 1024); } };
 template <typename E, int MF, bool kAcrossA, bool kAcrossB>
 void run(int wave, int depth) {
     constexpr bool kTail = false, kBf16Out = false;
@@ -53,29 +57,46 @@ void run(int wave, int depth) {
 """
 
 MAIN = """
-}
-extern "C" void trace(int wave, int depth, int across) {
-    if (across == 2) run<E, 4, true, true>(wave, depth);
-    else if (across == 1) run<E, 1, false, true>(wave, depth);
-    else run<E, 3, false, false>(wave, depth);
-    std::fflush(stdout);
-}
 int main(int argc, char** argv) {
-    int across, nk;
-    std::sscanf(argv[1], "%d", &across), std::sscanf(argv[2], "%d", &nk);
-    for (int w = 0; w < 8; ++w) std::printf("wave\\n"), trace(w, nk * E::kDepth, across);
+    int form, nk;
+    std::sscanf(argv[1], "%d", &form), std::sscanf(argv[2], "%d", &nk);
+    for (int w = 0; w < 8; ++w) std::printf("wave\\n"), trace(w, nk, form);
+}
+"""
+
+GROUPED_TRACE = """
+}
+void trace(int wave, int nk, int form) {
+    if (form == 2) run<E, 4, true, true>(wave, nk * E::kDepth);
+    else if (form == 1) run<E, 1, false, true>(wave, nk * E::kDepth);
+    else run<E, 3, false, false>(wave, nk * E::kDepth);
 }
 """
 
 
+FORMS = [("grouped", 0), ("grouped", 1), ("grouped", 2)]
+
+
 @pytest.fixture(scope="module")
-def program(tmp_path_factory):
-    src = open(os.path.join(os.path.dirname(fm.__file__), "csrc", "grouped_big.hip")).read()
-    body = re.search(r"^        // halves: 0 A0.*?\* MF \+ i\]; \}\);$", src, re.S | re.M).group(0)
+def lines(tmp_path_factory):
+    """lines(form, nk): what the eight waves of a tile of nk K tiles write down."""
+    csrc = os.path.join(os.path.dirname(fm.__file__), "csrc")
     d = tmp_path_factory.mktemp("order")
-    (d / "t.cpp").write_text(STUBS + body + MAIN)
-    subprocess.run(["g++", "-std=c++17", "-w", "-o", str(d / "t"), str(d / "t.cpp")], check=True)
-    return str(d / "t")
+
+    def part(name, pattern):
+        return re.search(pattern, open(os.path.join(csrc, name)).read(), re.S | re.M).group(0)
+
+    texts = dict(grouped=STUBS + part("grouped_big.hip", r"^        // halves: 0 A0.*?\* MF \+ i\]; \}\);$") + GROUPED_TRACE + MAIN)
+    for name, text in texts.items():
+        (d / (name + ".cpp")).write_text(text)
+        subprocess.run(["g++", "-std=c++17", "-w", "-o", str(d / name), str(d / (name + ".cpp"))], check=True)
+
+    def run(form, nk):
+        out = subprocess.run([str(d / form[0]), str(form[1]), str(nk)], check=True, capture_output=True, text=True).stdout.splitlines()
+        # a read of several fragments is one access
+        return [x for i, x in enumerate(out) if not (x.startswith("read") and i and out[i - 1] == x)]
+
+    return run
 
 
 class Access:
@@ -106,7 +127,7 @@ def accesses(lines):
         elif op == "request":
             a = Access(wave, "write", args[1], REQUEST, slot, index, args[0])
             out.append(a)
-            flying += [a] * (REQUEST // 1024)  # instructions that the wait counts
+            flying.append(a)
         elif op == "wait":
             while len(flying) > args[0]:
                 flying.pop(0).finish(slot, index)
@@ -126,32 +147,28 @@ def accesses(lines):
     return out, barriers
 
 
-@pytest.mark.parametrize("across", [0, 1, 2])
+@pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("nk", range(8))
-def test_the_scratch_of_the_stores_is_free(program, across, nk):
-    lines = subprocess.run([program, str(across), str(nk)], check=True, capture_output=True, text=True).stdout.splitlines()
-    acc, barriers = accesses(lines)
+def test_accesses_to_the_same_bytes_are_ordered(lines, form, nk):
+    acc, barriers = accesses(lines(form, nk))
     assert len(barriers) == WAVES and len(set(barriers)) == 1  # every wave meets the same barriers
     assert sum(a.kind == "store" for a in acc) == 2 * WAVES
     unordered = set()
     for i, a in enumerate(acc):
         for b in acc[i + 1:]:
-            if "store" not in (a.kind, b.kind):
-                continue
-            if a.at < b.end and b.at < a.end and not a.before(b) and not b.before(a):
+            if a.at < b.end and b.at < a.end and (a.kind != "read" or b.kind != "read") and not a.before(b) and not b.before(a):
                 if a.wave == b.wave and a.kind == b.kind == "store":
                     continue  # one wave's scratch, in its own order
                 unordered.add((a.kind, a.wave, b.kind, b.wave))
     assert not unordered, sorted(unordered)
 
 
-@pytest.mark.parametrize("across", [0, 1, 2])
-def test_a_read_sees_its_own_tile(program, across):
+@pytest.mark.parametrize("form", FORMS)
+def test_a_read_sees_its_own_tile(lines, form):
     """Of the requests for a half before a read of it, the last is the K tile that the phase multiplies: A0 B1 A1 of tile kt,
     then B0 of the next."""
     nk = 5
-    lines = subprocess.run([program, str(across), str(nk)], check=True, capture_output=True, text=True).stdout.splitlines()
-    acc, _ = accesses(lines)
+    acc, _ = accesses(lines(form, nk))
     for w in range(WAVES):
         reads = [a for a in acc if a.wave == w and a.kind == "read"]
         want = [(2, 0)] + [h for kt in range(nk) for h in ((0, kt), (3, kt), (1, kt), (2, kt + 1))]
@@ -160,4 +177,4 @@ def test_a_read_sees_its_own_tile(program, across):
             assert a.at == ((kt & 1) * 4 + half) * HALF
             for other in range(WAVES):
                 past = [b.tag for b in acc if b.wave == other and b.kind == "write" and a.at <= b.at < a.end and b.before(a)]
-                assert past and max(past) == kt
+                assert len(past) >= 2 and max(past) == kt
