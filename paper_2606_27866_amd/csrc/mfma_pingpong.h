@@ -232,6 +232,9 @@ __device__ __forceinline__ void pp_loop(unsigned char* smem, const PPOperands& o
     if (wm == 1) barrier_no_fence();  // the lagging waves; the leading ones wait at the end
     __builtin_amdgcn_sched_barrier(0);
     read_b(0, 0, fx);
+    // its half is refilled in phase 1 of the leading waves, a slot sooner after
+    // this read than the loop's are after theirs
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
     int kt = 0;
     if constexpr (kTail)  // the pairs of tiles whose requests stay before the end
         for (; kt + 3 < nk; kt += 2) {

@@ -1,5 +1,6 @@
-"""The 256 x 256 tiles' K loop and stores, compiled for the host from grouped_big.hip with requests, waits, barriers and LDS
-reads that write down when they happen: whatever two waves do to the same LDS bytes is ordered by a wait and a barrier.
+"""The K loops of the 256 x 256 tiles (grouped_big.hip with its stores, mfma_pingpong.h), compiled for the host with
+requests, waits, barriers and LDS reads that write down when they happen: whatever two waves do to the same LDS bytes is
+ordered by a wait and a barrier.
 
 A wave's accesses carry the number of barriers it had passed when they began and when they were known to be done (a
 request: the wait that drains it; a read: the wait for LDS, or at once where the wait is part of the read).  An access that
@@ -56,6 +57,27 @@ void run(int wave, int depth) {
     typename E::Acc acc[2][2][2 * MF];
 """
 
+PINGPONG = COMMON + """
+#define __device__
+#define __forceinline__ inline
+constexpr int BK = 64, PP_HALF = STAGE, PP_ND = 2, PP_RPI = 8, ROWB = 128;
+constexpr uint32_t kOOB = 0x80000000u;
+typedef int __amdgpu_buffer_rsrc_t;
+struct floatx4 { float v[4]; };
+struct bf16x8 {};
+struct bf16_t {};
+struct PPOperands { int ra, rb[2]; uint32_t aoff[2][PP_ND], boff[2][PP_ND]; int col[PP_ND]; int K; };
+struct PPSecond { const bf16_t *a, *a2, *b, *b2; size_t aext, bext; };
+struct PPNoSecond {};
+struct PPZeroTail { void operator()(int, int, unsigned char*) const {} };
+template <int MF> using PPAcc = floatx4[2][2][2 * MF];
+inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
+inline int make_rsrc(const bf16_t*, size_t) { return 0; }
+inline void load_lds16(int, uint32_t, uint32_t soff, unsigned char* dst) { requested(soff / (BK * 2), dst); }
+inline bf16x8 lds_frag(const unsigned char* at, int, int) { std::printf("read %d 0\\n", (int)(at - smem)); return {}; }
+inline floatx4 __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16x8, bf16x8, floatx4 c, int, int, int) { return c; }
+"""
+
 MAIN = """
 int main(int argc, char** argv) {
     int form, nk;
@@ -73,8 +95,25 @@ void trace(int wave, int nk, int form) {
 }
 """
 
+# the loop's callers meet at a barrier before they use LDS for themselves
+PINGPONG_TRACE = """
+template <int MF>
+void run(int wave, int nk) {
+    PPAcc<MF> acc;
+    PPOperands op{};
+    op.K = nk * BK;
+    pp_loop<MF, false>(smem, op, wave, 0, acc, PPZeroTail{});
+    barrier_no_fence();
+    for (int h = 0; h < 2; ++h) std::printf("store %d\\n", h * 8 * 4096 + wave * 4096);
+}
+void trace(int wave, int nk, int form) {
+    if (form) run<4>(wave, nk);
+    else run<1>(wave, nk);
+}
+"""
 
-FORMS = [("grouped", 0), ("grouped", 1), ("grouped", 2)]
+
+FORMS = [("grouped", 0), ("grouped", 1), ("grouped", 2), ("pingpong", 0), ("pingpong", 1)]
 
 
 @pytest.fixture(scope="module")
@@ -86,7 +125,8 @@ def lines(tmp_path_factory):
     def part(name, pattern):
         return re.search(pattern, open(os.path.join(csrc, name)).read(), re.S | re.M).group(0)
 
-    texts = dict(grouped=STUBS + part("grouped_big.hip", r"^        // halves: 0 A0.*?\* MF \+ i\]; \}\);$") + GROUPED_TRACE + MAIN)
+    texts = dict(grouped=STUBS + part("grouped_big.hip", r"^        // halves: 0 A0.*?\* MF \+ i\]; \}\);$") + GROUPED_TRACE + MAIN,
+                 pingpong=PINGPONG + part("mfma_pingpong.h", r"^template <int MF, bool kSwap, typename Tail.*?^}$") + PINGPONG_TRACE + MAIN)
     for name, text in texts.items():
         (d / (name + ".cpp")).write_text(text)
         subprocess.run(["g++", "-std=c++17", "-w", "-o", str(d / name), str(d / (name + ".cpp"))], check=True)
