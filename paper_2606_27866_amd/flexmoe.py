@@ -9,6 +9,7 @@ raised.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import Optional, Sequence
 
@@ -469,10 +470,10 @@ def _dtype_code(dtype) -> int:
 
 
 def _matrix(t, shape, dtype, name):
-    """Row stride of a [rows, cols] or [groups, rows, cols] tensor whose rows are contiguous."""
+    """Row stride of a [..., rows, cols] tensor whose rows are contiguous and follow each other at one distance."""
     if t.dtype is dtype and t.shape == shape and t.is_cuda and shape[-2] > 1:
         st = t.stride()
-        if st[-1] == 1 and st[-2] >= shape[-1] and (len(st) == 2 or st[0] == shape[1] * st[1]):
+        if st[-1] == 1 and st[-2] >= shape[-1] and (len(st) == 2 or len(st) == 3 and st[0] == shape[1] * st[1]):
             return st[-2]
     return _matrix_checked(t, shape, dtype, name)
 
@@ -482,16 +483,22 @@ def _matrix_checked(t, shape, dtype, name):
         raise ValueError("%s must be %s %s, got %s %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
     if not t.is_cuda:
         raise ValueError("%s must be on the GPU" % name)
-    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+    cols = t.shape[-1]
+    if t.numel() and cols > 1 and t.stride(-1) != 1:
         raise ValueError("%s must be contiguous in its last dimension" % name)
-    ld = t.stride(-2) if t.shape[-2] > 1 else _pitch(t.shape[-1], t.element_size())
-    if len(shape) == 3 and t.shape[0] > 1:
-        if t.shape[1] == 1:
-            ld = t.stride(0)
-        elif t.stride(0) != t.shape[1] * ld:
+    ld, rows = None, 1  # of the dimensions so far, from the last but one on
+    for n, step in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n == 1:
+            continue
+        if ld is None:
+            ld = step
+        elif step != rows * ld and t.numel():
             raise ValueError("%s must hold its groups one after another (strides %s)" % (name, t.stride()))
+        rows *= n
+    if ld is None or not t.numel():
+        return _pitch(cols, t.element_size())
     # an expanded tensor repeats one row with stride 0, which in a descriptor would stand for packed rows
-    if t.numel() > t.shape[-1] and ld < t.shape[-1]:
+    if ld < cols:
         raise ValueError("%s: rows overlap (strides %s); contiguous() makes a copy that can be used" % (name, t.stride()))
     return ld
 
@@ -583,11 +590,13 @@ class GroupedProduct:
 
 
 def quantize_rows(x, gate=None, q=None, scale=None, stream=None):
-    """Rows of x (or silu(gate) * x) as whole numbers up to 127 and a scale each: (q int8 like x, scale)."""
+    """Rows of x [..., rows, cols] (or silu(gate) * x) as whole numbers up to 127 and a scale each: (q int8 like x, scale)."""
     import torch
     shape = x.shape
+    if len(shape) < 2:
+        raise ValueError("x must have rows and columns, got %s" % (tuple(shape),))
     cols = shape[-1]
-    rows = shape[0] if len(shape) == 2 else x.numel() // cols
+    rows = shape[0] if len(shape) == 2 else math.prod(shape[:-1])
     ldx = _matrix(x, shape, x.dtype, "x")
     if gate is not None and _matrix(gate, shape, x.dtype, "gate") != ldx:
         raise ValueError("x and gate must have the same strides")

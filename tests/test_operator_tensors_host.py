@@ -88,3 +88,21 @@ def test_rounded_rows_refuse_expanded_tensors(no_launch):
                dict(x=expanded(10, 64, dtype=F32), gate=expanded(10, 64, dtype=F32))):
         with pytest.raises(ValueError, match="overlap"):
             fm.quantize_rows(**kw)
+
+
+def test_every_leading_stride_of_a_stack_is_checked():
+    """Stacks of any number of dimensions whose rows follow each other at one distance, and no others."""
+    z = torch.zeros
+    for t, ld in [(z(2, 3, 8, 16), 16), (z(2, 3, 8, 24)[..., :16], 24), (z(2, 3, 1, 16), 16), (z(2, 1, 8, 16)[:, :, :, :], 16),
+                  (z(1, 3, 8, 16), 16), (z(4, 2, 3, 8, 16), 16), (z(5, 1, 1, 24)[..., :16], 24), (z(1, 1, 16), 16), (z(2, 1, 1, 1, 16), 16),
+                  (z(2, 8, 16)[:, :8], 16), (z(3, 8, 16)[1:], 16)]:
+        assert fm._matrix(on_gpu(t), tuple(t.shape), F32, "x") == ld, t.shape
+    for t in [z(2, 3, 8, 16)[:, :, :4], z(2, 3, 8, 16)[:, :2], z(3, 2, 8, 16).transpose(0, 1), z(2, 8, 3, 16).transpose(1, 2), z(4, 8, 16)[::2],
+              z(2, 3, 1, 16)[:, :2], z(2, 1, 16).expand(2, 3, 16), z(2, 1, 8, 16).expand(2, 3, 8, 16), z(2, 2, 3, 8, 16)[:, :, :2]]:
+        with pytest.raises(ValueError):
+            fm._matrix(on_gpu(t), tuple(t.shape), F32, "x")
+
+
+def test_a_row_alone_is_no_matrix(no_launch):
+    with pytest.raises(ValueError):
+        fm.quantize_rows(on_gpu(torch.zeros(16)))
