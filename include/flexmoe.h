@@ -399,8 +399,9 @@ int flexmoe_layer_forward_bucketed(const flexmoe_layer_desc *desc, int32_t T, co
  * empty: its dW_e is 0 (or unchanged when added to).
  *   x, dx [R][ldx], y, dy [R][ldy] (dtype), w [groups][N][ldw] (dtype),
  *   dw [groups][N][lddw] (dw_dtype), offsets [groups + 1] int32 on the device,
- *   ascending, within [0, R]; rows outside [offsets[0], offsets[groups]) are
- *   neither read nor written.
+ *   ascending, cut to [0, R] (for one group {0, INT32_MAX} stands for all rows of
+ *   any call); rows outside [offsets[0], offsets[groups]) are neither read nor
+ *   written.
  * keep [groups] int32 (device; with keep_axis other than FLEXMOE_KEEP_NONE,
  * NULL otherwise) limits W_e to its first k_e rows (FLEXMOE_KEEP_N, as gate and
  * up) or columns (FLEXMOE_KEEP_K, as down): what lies past it is read into no

@@ -632,6 +632,8 @@ class Int8Product:
         self._ws = (self.workspace.data_ptr(), self.workspace.numel())
         self.q = _padded((max_rows, self.K), torch.int8, w.device)
         self.q_scale = torch.empty(max_rows, dtype=torch.float32, device=w.device)
+        # all rows of any call, for one group: the kernels cut offsets to [0, R]
+        self._all_rows = torch.tensor([0, 2 ** 31 - 1], dtype=torch.int32, device=w.device) if self.groups == 1 else None
 
     @classmethod
     def from_weights(cls, w, max_rows, keep_axis="none", out_dtype=None):
@@ -661,15 +663,15 @@ class Int8Product:
 
     def _product(self, R, q, q_scale, offsets, keep, y, device, stream):
         if offsets is None:
-            import torch
             if self.groups != 1:
                 raise ValueError("offsets are needed for %d groups" % self.groups)
-            offsets = torch.tensor([0, R], dtype=torch.int32, device=device)
+            offsets = self._all_rows.data_ptr()
+        else:
+            offsets = _vector(offsets, self.groups + 1, self._i32, "offsets")
         if y is None:
             y = _padded((R, self.N), self.out_dtype, device)
         self.desc.ldy = _matrix(y, (R, self.N), self.out_dtype, "y")
-        _check(lib().flexmoe_quantized_forward(self._desc, R, q, q_scale, self.w.data_ptr(), self.w_scale.data_ptr(),
-                                               _vector(offsets, self.groups + 1, self._i32, "offsets"),
+        _check(lib().flexmoe_quantized_forward(self._desc, R, q, q_scale, self.w.data_ptr(), self.w_scale.data_ptr(), offsets,
                                                None if keep is None else _vector(keep, self.groups, self._i32, "keep"),
                                                y.data_ptr(), *self._ws, stream))
         return y

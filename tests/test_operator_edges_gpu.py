@@ -20,3 +20,55 @@ def test_rounded_rows_of_a_stack(shape):
     qf, sf = fm.quantize_rows(flat)
     assert q.shape == shape and s.shape == shape[:-1]
     assert torch.equal(q.reshape(qf.shape), qf) and torch.equal(s.reshape(-1), sf)
+
+
+def dense(N=200, K=336, max_rows=300):
+    g = torch.Generator(device="cuda")
+    op = fm.Int8Product.from_weights(torch.randn(1, N, K, generator=g, device="cuda"), max_rows, out_dtype=F32)
+    return op, torch.randn(max_rows, K, generator=g, device="cuda").to(BF)
+
+
+@pytest.mark.parametrize("T", [1, 33, 130, 300])
+def test_dense_call_without_offsets(T):
+    """The bits of the call with offsets; rows past T are left alone."""
+    op, x = dense()
+    want = op(x[:T], torch.tensor([0, T], dtype=torch.int32, device="cuda"))
+    y = torch.full((300, 200), 7.0, device="cuda")
+    op(x[:T], y=y[:T])
+    assert torch.equal(y[:T], want) and bool((y[T:] == 7).all())
+    assert torch.equal(op.product(op.q[:T], op.q_scale[:T]), want)
+
+
+def test_dense_call_on_another_stream():
+    """Work that follows on the current stream takes memory freed by the call: what the call reads is not among it."""
+    op, x = dense()
+    want = op(x)
+    y = torch.zeros_like(want)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    busy = torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        for _ in range(4):
+            busy = (busy @ busy).clamp_(-1, 1)  # the call's kernels wait behind these
+    op(x, y=y, stream=s)
+    for _ in range(64):
+        torch.zeros(2, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    assert torch.equal(y, want)
+
+
+def test_dense_call_in_a_graph():
+    op, x = dense()
+    want = op(x)
+    y = torch.zeros_like(want)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        op(x, y=y)
+    for _ in range(3):
+        y.fill_(-1.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
+        op(x.neg())  # eager work in between

@@ -106,3 +106,52 @@ def test_every_leading_stride_of_a_stack_is_checked():
 def test_a_row_alone_is_no_matrix(no_launch):
     with pytest.raises(ValueError):
         fm.quantize_rows(on_gpu(torch.zeros(16)))
+
+
+class Recorder:
+    """Stands for the library: writes down the arguments of every call."""
+
+    def __init__(self, real):
+        self.real, self.calls = real, []
+
+    def __getattr__(self, name):
+        if name.endswith("_bytes"):
+            return getattr(self.real, name)
+
+        def call(*args):
+            self.calls.append((name, args))
+            return 0
+        return call
+
+
+@pytest.fixture
+def recorder(monkeypatch):
+    r = Recorder(fm.lib())
+    monkeypatch.setattr(fm, "lib", lambda: r)
+    return r
+
+
+def test_a_dense_call_keeps_no_temporary_offsets(recorder, monkeypatch):
+    """One group without offsets: every call passes the holder's own, which stay while the holder does; nothing is made on
+    the current stream for work on another, nothing copied from the host."""
+    op = fm.Int8Product(on_gpu(torch.zeros(1, 32, 64, dtype=I8)), on_gpu(torch.zeros(1, 32)), max_rows=8)
+
+    def made(*_, **__):
+        raise AssertionError("a tensor made during the call")
+
+    monkeypatch.setattr(torch, "tensor", made)
+    for R in (1, 5, 8):
+        y = on_gpu(torch.zeros(R, 32, dtype=BF))
+        op(on_gpu(torch.zeros(R, 64, dtype=BF)), y=y, stream=0)
+        op.product(on_gpu(torch.zeros(R, 64, dtype=I8)), on_gpu(torch.zeros(R)), y=y, stream=0)
+    used = {args[6] for name, args in recorder.calls if name == "flexmoe_quantized_forward"}
+    assert len(recorder.calls) == 9 and len(used) == 1
+    whole = [t for t in vars(op).values() if isinstance(t, torch.Tensor) and t.data_ptr() in used]
+    assert len(whole) == 1 and whole[0].dtype == torch.int32
+    assert whole[0].tolist()[0] == 0 and whole[0].tolist()[1] >= 8  # the kernels cut it to a call's rows
+
+
+def test_several_groups_need_offsets(recorder):
+    op = fm.Int8Product(on_gpu(torch.zeros(2, 32, 64, dtype=I8)), on_gpu(torch.zeros(2, 32)), max_rows=8)
+    with pytest.raises(ValueError, match="offsets"):
+        op(on_gpu(torch.zeros(3, 64, dtype=BF)), y=on_gpu(torch.zeros(3, 32, dtype=BF)), stream=0)
