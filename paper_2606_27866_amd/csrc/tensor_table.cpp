@@ -6,19 +6,21 @@
 
 namespace {
 
-// column(tensors: list, sizes: address of int64[len], code: 0 fp32 / 1 bf16 / 2 uint8, dst: address, stride: bytes)
+// column(tensors: list, sizes: address of int64[len], code: 0 fp32 / 1 bf16 / 2 uint8, dst: address, stride: bytes,
+//        longer: 0 / 1, optional)
 // writes tensor i's address to dst + i * stride.  Returns -1, or the index of the
 // first tensor that is not contiguous on the GPU, of that type and of sizes[i]
-// values (nothing after it is written).
+// values, or, with longer, at least as many (nothing after it is written).
 PyObject* column(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    if (n != 5 || !PyList_Check(args[0])) {
-        PyErr_SetString(PyExc_TypeError, "column(list, sizes, code, dst, stride)");
+    if ((n != 5 && n != 6) || !PyList_Check(args[0])) {
+        PyErr_SetString(PyExc_TypeError, "column(list, sizes, code, dst, stride, longer=0)");
         return nullptr;
     }
     const int64_t* sizes = static_cast<const int64_t*>(PyLong_AsVoidPtr(args[1]));
     const long code = PyLong_AsLong(args[2]);
     char* dst = static_cast<char*>(PyLong_AsVoidPtr(args[3]));
     const long stride = PyLong_AsLong(args[4]);
+    const bool longer = n == 6 && PyLong_AsLong(args[5]) != 0;
     if (PyErr_Occurred()) return nullptr;
     const at::ScalarType want = code == 0 ? at::kFloat : code == 1 ? at::kBFloat16 : at::kByte;
     const Py_ssize_t count = PyList_GET_SIZE(args[0]);
@@ -26,8 +28,8 @@ PyObject* column(PyObject*, PyObject* const* args, Py_ssize_t n) {
         PyObject* o = PyList_GET_ITEM(args[0], i);
         if (!THPVariable_Check(o)) return PyLong_FromSsize_t(i);
         const at::Tensor& t = THPVariable_Unpack(o);
-        if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || t.scalar_type() != want || t.numel() != sizes[i] ||
-            !t.is_contiguous())
+        if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || t.scalar_type() != want ||
+            (longer ? t.numel() < sizes[i] : t.numel() != sizes[i]) || !t.is_contiguous())
             return PyLong_FromSsize_t(i);
         *reinterpret_cast<void**>(dst + i * stride) = t.data_ptr();
     }

@@ -682,13 +682,13 @@ class AdamW:
 
     params: bf16 or fp32, all alike.  masters: fp32 copies that the step works on (bf16 parameters).  states: (m, v) or,
     with 8 bits, (m, v, m_scale, v_scale) lists to continue from; zeros otherwise.  step(grads) takes one gradient per
-    parameter.
+    parameter.  Every step reads the tensors' addresses again: their storages may be replaced between steps.
     """
 
     def __init__(self, params, masters=None, states=None, state_bits=32, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0,
                  step=0, seed=0):
         import torch
-        self.params, self.masters, self.state_bits = list(params), masters, state_bits
+        self.params, self.state_bits = list(params), state_bits
         self.betas, self.eps, self.weight_decay, self.t, self.seed = betas, eps, weight_decay, step, seed
         if not self.params:
             raise ValueError("no parameters")
@@ -696,6 +696,7 @@ class AdamW:
             raise ValueError("state_bits must be 8 or 32, got %s" % (state_bits,))
         dt = self.params[0].dtype
         sizes = [p.numel() for p in self.params]
+        blocks = [-(-n // STATE_BLOCK) for n in sizes]
         st = torch.uint8 if state_bits == 8 else torch.float32
         if states is None:
             def zeros(n, dtype):
@@ -703,43 +704,46 @@ class AdamW:
 
             states = ([zeros(n, st) for n in sizes], [zeros(n, st) for n in sizes])
             if state_bits == 8:
-                blocks = [-(-n // STATE_BLOCK) for n in sizes]
                 states += ([zeros(n, torch.float32) for n in blocks], [zeros(n, torch.float32) for n in blocks])
-        self.m, self.v = states[:2]
-        self.m_scale, self.v_scale = states[2:] if state_bits == 8 else (None, None)
-        self._table = (flexmoe_adamw_tensor * len(sizes))()
-        self._n = np.array(sizes, dtype=np.int64)
-        np.frombuffer(self._table, dtype=np.int64)[flexmoe_adamw_tensor.n.offset // 8::ctypes.sizeof(flexmoe_adamw_tensor) // 8] = self._n
-        blocks = [-(-n // STATE_BLOCK) for n in sizes]
-        self._fill("param", self.params, sizes, dt, "params")
-        self._fill("m", self.m, sizes, st, "states")
-        self._fill("v", self.v, sizes, st, "states")
-        if state_bits == 8:
-            self._fill("m_scale", self.m_scale, blocks, torch.float32, "scales")
-            self._fill("v_scale", self.v_scale, blocks, torch.float32, "scales")
-        if masters is not None:
-            self._fill("master", masters, sizes, torch.float32, "masters")
-        # the table's gradient column is filled by every step
-        self._column = (self._n.ctypes.data, ctypes.addressof(self._table) + flexmoe_adamw_tensor.grad.offset,
-                        ctypes.sizeof(flexmoe_adamw_tensor))
+        self.m, self.v = (self._list(t) for t in states[:2])
+        self.m_scale, self.v_scale = (self._list(t) for t in states[2:]) if state_bits == 8 else (None, None)
+        self.masters = None if masters is None else self._list(masters)
         self.sizes, self._param_code = sizes, _dtype_code(dt)
-
-    def _fill(self, field, tensors_, sizes, dtype, name):
-        """One column of the table; every tensor holds at least sizes[i] values."""
-        if len(tensors_) != len(sizes):
-            raise ValueError("%s: %d tensors for %d parameters" % (name, len(tensors_), len(sizes)))
-        at, stride = ctypes.addressof(self._table) + getattr(flexmoe_adamw_tensor, field).offset, ctypes.sizeof(flexmoe_adamw_tensor)
-        n = np.array(sizes, dtype=np.int64)
-        code = {"torch.float32": 0, "torch.bfloat16": 1, "torch.uint8": 2}.get(str(dtype))
-        if code is None or tensors().column(list(tensors_), n.ctypes.data, code, at, stride) >= 0:
-            for i, t in enumerate(tensors_):
-                setattr(self._table[i], field, self._like(t, sizes[i], dtype, name))
+        self._table = (flexmoe_adamw_tensor * len(sizes))()
+        self._n, self._blocks = np.array(sizes, dtype=np.int64), np.array(blocks, dtype=np.int64)
+        np.frombuffer(self._table, dtype=np.int64)[flexmoe_adamw_tensor.n.offset // 8::ctypes.sizeof(flexmoe_adamw_tensor) // 8] = self._n
+        # (field, its tensors, numbers of values, type, whether a tensor may be longer): the table's columns, filled by every
+        # step, since a tensor's storage may have been replaced since the last one (p.data = ..., module.to())
+        self._columns = [self._column("param", self.params, self._n, dt, 0), self._column("m", self.m, self._n, st, 1),
+                         self._column("v", self.v, self._n, st, 1)]
+        if state_bits == 8:
+            self._columns += [self._column(f, t, self._blocks, torch.float32, 1) for f, t in (("m_scale", self.m_scale), ("v_scale", self.v_scale))]
+        if masters is not None:
+            self._columns.append(self._column("master", self.masters, self._n, torch.float32, 1))
+        self._grads = (self._n.ctypes.data, ctypes.addressof(self._table) + flexmoe_adamw_tensor.grad.offset,
+                       ctypes.sizeof(flexmoe_adamw_tensor))
+        self._fill()
 
     @staticmethod
-    def _like(t, n, dtype, name):
-        if t.dtype != dtype or t.numel() < n or not t.is_contiguous() or not t.is_cuda:
-            raise ValueError("%s: need %d contiguous %s values on the GPU, got %s %s" % (name, n, dtype, t.dtype, tuple(t.shape)))
-        return t.data_ptr()
+    def _list(tensors_):
+        return tensors_ if type(tensors_) is list else list(tensors_)
+
+    def _column(self, field, tensors_, n, dtype, longer):
+        code = 2 if dtype.itemsize == 1 else _dtype_code(dtype)
+        return (field, tensors_, n, dtype, n.ctypes.data, code,
+                ctypes.addressof(self._table) + getattr(flexmoe_adamw_tensor, field).offset, longer)
+
+    def _fill(self):
+        """The addresses of parameters, states and masters into the table, each tensor checked."""
+        column, count, stride = tensors().column, len(self.sizes), ctypes.sizeof(flexmoe_adamw_tensor)
+        for field, tensors_, n, dtype, sizes, code, dst, longer in self._columns:
+            if len(tensors_) != count:
+                raise ValueError("%s: %d tensors for %d parameters" % (field, len(tensors_), count))
+            bad = column(tensors_, sizes, code, dst, stride, longer)
+            if bad >= 0:
+                t = tensors_[bad]
+                raise ValueError("%s %d: need %d contiguous %s values on the GPU, got %s %s"
+                                 % (field, bad, n[bad], dtype, t.dtype, tuple(t.shape)))
 
     def step(self, grads, lr, grad_scale=1.0, stream=None):
         """One step with the gradients `grads` (bf16 or fp32, all alike, contiguous)."""
@@ -747,7 +751,8 @@ class AdamW:
         if len(grads) != len(self.sizes):
             raise ValueError("%d gradients for %d parameters" % (len(grads), len(self.sizes)))
         code = _dtype_code(grads[0].dtype)
-        sizes, dst, stride = self._column
+        self._fill()
+        sizes, dst, stride = self._grads
         bad = tensors().column(grads, sizes, code, dst, stride)
         if bad >= 0:
             g = grads[bad]

@@ -72,3 +72,20 @@ def test_dense_call_in_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(y, want)
         op(x.neg())  # eager work in between
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_adamw_steps_the_storage_that_a_parameter_has_now(bits):
+    g = torch.Generator(device="cuda")
+    p = torch.randn(1000, generator=g, device="cuda")
+    q, grad = p.clone(), torch.randn(1000, generator=g, device="cuda")
+    a, b = fm.AdamW([p], state_bits=bits, seed=3), fm.AdamW([q], state_bits=bits, seed=3)
+    a.step([grad], 1e-2)
+    b.step([grad], 1e-2)
+    old, m = p.data, a.m[0].data
+    before = old.clone(), m.clone()
+    p.data, a.m[0].data = p.data.clone(), a.m[0].data.clone()
+    a.step([grad], 1e-2)
+    b.step([grad], 1e-2)
+    assert torch.equal(p, q) and torch.equal(a.m[0], b.m[0])
+    assert torch.equal(old, before[0]) and torch.equal(m, before[1])  # nothing was written to the storages it had

@@ -155,3 +155,79 @@ def test_several_groups_need_offsets(recorder):
     op = fm.Int8Product(on_gpu(torch.zeros(2, 32, 64, dtype=I8)), on_gpu(torch.zeros(2, 32)), max_rows=8)
     with pytest.raises(ValueError, match="offsets"):
         op(on_gpu(torch.zeros(3, 64, dtype=BF)), y=on_gpu(torch.zeros(3, 32, dtype=BF)), stream=0)
+
+
+class Columns:
+    """Stands for the native module: the same column, of tensors that say they are on a GPU."""
+
+    @staticmethod
+    def column(tensors, sizes, code, dst, stride, longer=0):
+        import ctypes
+        want = {0: F32, 1: BF, 2: torch.uint8}[code]
+        n = (ctypes.c_int64 * len(tensors)).from_address(sizes) if tensors else []
+        for i, t in enumerate(tensors):
+            if not t.is_cuda or t.dtype != want or not t.is_contiguous() or (t.numel() < n[i] if longer else t.numel() != n[i]):
+                return i
+            ctypes.c_void_p.from_address(dst + i * stride).value = t.data_ptr()
+        return -1
+
+
+@pytest.fixture
+def steps(recorder, monkeypatch):
+    """The tables that flexmoe_adamw_step was given."""
+    monkeypatch.setattr(fm, "tensors", lambda: Columns)
+    seen = []
+
+    def step(desc, table, count, stream):
+        seen.append([{f: getattr(t, f) for f, _ in fm.flexmoe_adamw_tensor._fields_}
+                     for t in (fm.flexmoe_adamw_tensor * count).from_address(table)])
+        return 0
+
+    recorder.flexmoe_adamw_step = step
+    return seen
+
+
+def adamw(bits=32, master=False):
+    sizes = [300, 5]
+    st = torch.uint8 if bits == 8 else F32
+
+    def zeros(ns, dtype):
+        return [on_gpu(torch.zeros(n, dtype=dtype)) for n in ns]
+
+    p = zeros(sizes, BF if master else F32)
+    states = (zeros(sizes, st), zeros(sizes, st)) + ((zeros([2, 1], F32), zeros([2, 1], F32)) if bits == 8 else ())
+    opt = fm.AdamW(p, masters=zeros(sizes, F32) if master else None, states=states, state_bits=bits)
+    return opt, zeros(sizes, F32)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_adamw_follows_tensors_whose_storage_is_replaced(steps, bits):
+    opt, grads = adamw(bits, master=True)
+    lists = dict(param=opt.params, m=opt.m, v=opt.v, master=opt.masters)
+    if bits == 8:
+        lists.update(m_scale=opt.m_scale, v_scale=opt.v_scale)
+    opt.step(grads, 1e-3, stream=0)
+    kept = []
+    for ts in lists.values():
+        for t in ts:
+            kept.append(t.data)  # the old storage stays, so that the new one is another
+            t.data = on_gpu(torch.ones(t.shape, dtype=t.dtype))
+    opt.step(grads, 1e-3, stream=0)
+    for i in range(2):
+        for field, ts in lists.items():
+            assert steps[1][i][field] == ts[i].data_ptr() != steps[0][i][field]
+        assert steps[1][i]["grad"] == grads[i].data_ptr() and steps[1][i]["n"] == grads[i].numel()
+
+
+def test_adamw_refuses_tensors_that_no_longer_fit(steps):
+    for field, bad in [("params", torch.zeros(299)), ("params", torch.zeros(301)), ("params", torch.zeros(300, dtype=BF)), ("m", torch.zeros(299)),
+                       ("v", torch.zeros(600)[::2])]:
+        opt, grads = adamw()
+        getattr(opt, field)[0] = on_gpu(bad)
+        with pytest.raises(ValueError):
+            opt.step(grads, 1e-3, stream=0)
+    opt, grads = adamw()
+    opt.params.append(opt.params[0])  # the table has no place for it
+    with pytest.raises(ValueError):
+        opt.step(grads, 1e-3, stream=0)
+    assert not steps and opt.t == 0
