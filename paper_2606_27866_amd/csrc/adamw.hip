@@ -301,12 +301,16 @@ __global__ __launch_bounds__(AT) void adamw_read_kernel(const uint8_t* m, const 
     else store4<false>(om + i, c, x), store4<false>(ov + i, c, y);
 }
 
+// hipLaunchKernel itself: the arguments, 4 KB, are not copied on the way, and the
+// error is the launch's own.
 template <int kBits, int kUnroll>
-void launch(const AdamwArgs& a, bool param_bf16, bool grad_bf16, unsigned grid, hipStream_t s) {
-    if (param_bf16 && grad_bf16) adamw_kernel<bf16_t, bf16_t, kBits, kUnroll><<<grid, AT, 0, s>>>(a);
-    else if (param_bf16) adamw_kernel<bf16_t, float, kBits, kUnroll><<<grid, AT, 0, s>>>(a);
-    else if (grad_bf16) adamw_kernel<float, bf16_t, kBits, kUnroll><<<grid, AT, 0, s>>>(a);
-    else adamw_kernel<float, float, kBits, kUnroll><<<grid, AT, 0, s>>>(a);
+hipError_t launch(AdamwArgs& a, bool param_bf16, bool grad_bf16, unsigned grid, hipStream_t s) {
+    auto* const f = param_bf16 && grad_bf16 ? adamw_kernel<bf16_t, bf16_t, kBits, kUnroll>
+                    : param_bf16            ? adamw_kernel<bf16_t, float, kBits, kUnroll>
+                    : grad_bf16             ? adamw_kernel<float, bf16_t, kBits, kUnroll>
+                                            : adamw_kernel<float, float, kBits, kUnroll>;
+    void* args[] = {&a};
+    return hipLaunchKernel(reinterpret_cast<const void*>(f), dim3(grid), dim3(AT), args, 0, s);
 }
 
 bool misaligned(const void* p, uintptr_t mask) { return ((uintptr_t)p & mask) != 0; }
@@ -380,10 +384,9 @@ int flexmoe_adamw_step(const flexmoe_adamw_desc* D, const flexmoe_adamw_tensor* 
         if (!groups) continue;
         const unsigned grid = (unsigned)groups;
         const bool pb = D->param_dtype == FLEXMOE_BF16, gb = D->grad_dtype == FLEXMOE_BF16;
-        if (unroll == 1) launch<8, 1>(a, pb, gb, grid, s);
-        else if (unroll == 2) launch<32, 2>(a, pb, gb, grid, s);
-        else launch<32, 4>(a, pb, gb, grid, s);
-        const hipError_t err = hipGetLastError();
+        const hipError_t err = unroll == 1   ? launch<8, 1>(a, pb, gb, grid, s)
+                               : unroll == 2 ? launch<32, 2>(a, pb, gb, grid, s)
+                                             : launch<32, 4>(a, pb, gb, grid, s);
         if (err != hipSuccess) return hip_fail(err, "adamw_step launch");
     }
     return FLEXMOE_OK;

@@ -75,6 +75,9 @@ class flexmoe_adamw_tensor(ctypes.Structure):
                [("n", ctypes.c_int64)]
 
 
+_TENSOR_BYTES = ctypes.sizeof(flexmoe_adamw_tensor)
+
+
 class flexmoe_adamw_desc(ctypes.Structure):
     _fields_ = [("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("state_bits", ctypes.c_int32),
                 ("seed", ctypes.c_uint32), ("step", ctypes.c_int64)] + \
@@ -462,11 +465,17 @@ def flexmoe_adamw_read_state(n, m, v, m_scale, v_scale, dtype, m_out, v_out, str
                                           _stream(stream)))
 
 
+_DTYPE_CODES = {}  # filled by the first call: the module does not import torch
+
+
 def _dtype_code(dtype) -> int:
-    import torch
-    if dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError("dtype must be torch.bfloat16 or torch.float32, got %s" % dtype)
-    return FLEXMOE_BF16 if dtype == torch.bfloat16 else FLEXMOE_F32
+    code = _DTYPE_CODES.get(dtype)
+    if code is None:
+        import torch
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("dtype must be torch.bfloat16 or torch.float32, got %s" % dtype)
+        code = _DTYPE_CODES[dtype] = FLEXMOE_BF16 if dtype == torch.bfloat16 else FLEXMOE_F32
+    return code
 
 
 def _matrix(t, shape, dtype, name):
@@ -710,40 +719,39 @@ class AdamW:
         self.masters = None if masters is None else self._list(masters)
         self.sizes, self._param_code = sizes, _dtype_code(dt)
         self._table = (flexmoe_adamw_tensor * len(sizes))()
+        self._table_at = ctypes.addressof(self._table)
         self._n, self._blocks = np.array(sizes, dtype=np.int64), np.array(blocks, dtype=np.int64)
-        np.frombuffer(self._table, dtype=np.int64)[flexmoe_adamw_tensor.n.offset // 8::ctypes.sizeof(flexmoe_adamw_tensor) // 8] = self._n
-        # (field, its tensors, numbers of values, type, whether a tensor may be longer): the table's columns, filled by every
-        # step, since a tensor's storage may have been replaced since the last one (p.data = ..., module.to())
-        self._columns = [self._column("param", self.params, self._n, dt, 0), self._column("m", self.m, self._n, st, 1),
-                         self._column("v", self.v, self._n, st, 1)]
+        np.frombuffer(self._table, dtype=np.int64)[flexmoe_adamw_tensor.n.offset // 8::_TENSOR_BYTES // 8] = self._n
+        # the table's columns, filled by every step, since a tensor's storage may have been replaced since the last one
+        # (p.data = ..., module.to()): states and masters may hold more values than the parameter
+        kept = [("param", self.params, self._n, dt, 0), ("m", self.m, self._n, st, 1), ("v", self.v, self._n, st, 1)]
         if state_bits == 8:
-            self._columns += [self._column(f, t, self._blocks, torch.float32, 1) for f, t in (("m_scale", self.m_scale), ("v_scale", self.v_scale))]
+            kept += [("m_scale", self.m_scale, self._blocks, torch.float32, 1), ("v_scale", self.v_scale, self._blocks, torch.float32, 1)]
         if masters is not None:
-            self._columns.append(self._column("master", self.masters, self._n, torch.float32, 1))
-        self._grads = (self._n.ctypes.data, ctypes.addressof(self._table) + flexmoe_adamw_tensor.grad.offset,
-                       ctypes.sizeof(flexmoe_adamw_tensor))
-        self._fill()
+            kept.append(("master", self.masters, self._n, torch.float32, 1))
+        self._fields = [(name, n) for name, _, n, _, _ in kept] + [("gradient", self._n)]
+        self._columns = tuple((ts, n.ctypes.data, 2 if t == torch.uint8 else _dtype_code(t), self._at(name), longer)
+                              for name, ts, n, t, longer in kept)
+        self._sizes_at, self._grad_at = self._n.ctypes.data, self._at("grad")
+        bad = tensors().columns(self._columns, len(sizes), _TENSOR_BYTES)
+        if bad >= 0:
+            self._refuse(self._columns, bad)
 
     @staticmethod
     def _list(tensors_):
         return tensors_ if type(tensors_) is list else list(tensors_)
 
-    def _column(self, field, tensors_, n, dtype, longer):
-        code = 2 if dtype.itemsize == 1 else _dtype_code(dtype)
-        return (field, tensors_, n, dtype, n.ctypes.data, code,
-                ctypes.addressof(self._table) + getattr(flexmoe_adamw_tensor, field).offset, longer)
+    def _at(self, field):
+        return self._table_at + getattr(flexmoe_adamw_tensor, field).offset
 
-    def _fill(self):
-        """The addresses of parameters, states and masters into the table, each tensor checked."""
-        column, count, stride = tensors().column, len(self.sizes), ctypes.sizeof(flexmoe_adamw_tensor)
-        for field, tensors_, n, dtype, sizes, code, dst, longer in self._columns:
-            if len(tensors_) != count:
-                raise ValueError("%s: %d tensors for %d parameters" % (field, len(tensors_), count))
-            bad = column(tensors_, sizes, code, dst, stride, longer)
-            if bad >= 0:
-                t = tensors_[bad]
-                raise ValueError("%s %d: need %d contiguous %s values on the GPU, got %s %s"
-                                 % (field, bad, n[bad], dtype, t.dtype, tuple(t.shape)))
+    def _refuse(self, columns, bad):
+        c, i = divmod(bad, len(self.sizes) + 1)
+        (name, n), (ts, _, code, _, _) = self._fields[c], columns[c]
+        if i == len(self.sizes):
+            raise ValueError("%s: %d tensors for %d parameters" % (name, len(ts), i))
+        raise ValueError("%s %d: need %d contiguous %s values on the GPU, got %s %s"
+                         % (name, i, n[i], ("float32", "bfloat16", "uint8")[code], getattr(ts[i], "dtype", type(ts[i])),
+                            tuple(getattr(ts[i], "shape", ()))))
 
     def step(self, grads, lr, grad_scale=1.0, stream=None):
         """One step with the gradients `grads` (bf16 or fp32, all alike, contiguous)."""
@@ -751,16 +759,13 @@ class AdamW:
         if len(grads) != len(self.sizes):
             raise ValueError("%d gradients for %d parameters" % (len(grads), len(self.sizes)))
         code = _dtype_code(grads[0].dtype)
-        self._fill()
-        sizes, dst, stride = self._grads
-        bad = tensors().column(grads, sizes, code, dst, stride)
+        columns = (*self._columns, (grads, self._sizes_at, code, self._grad_at, 0))
+        bad = tensors().columns(columns, len(grads), _TENSOR_BYTES)
         if bad >= 0:
-            g = grads[bad]
-            raise ValueError("gradient %d: need %d contiguous %s values on the GPU, got %s %s"
-                             % (bad, self.sizes[bad], grads[0].dtype, g.dtype, tuple(g.shape)))
+            self._refuse(columns, bad)
         d = flexmoe_adamw_desc(self._param_code, code, self.state_bits, self.seed & 0xffffffff, self.t + 1, lr,
                                self.betas[0], self.betas[1], self.eps, self.weight_decay, grad_scale)
-        flexmoe_adamw_step(d, self._table, stream=stream)
+        _check(lib().flexmoe_adamw_step(ctypes.byref(d), self._table_at, len(self.sizes), _stream(stream)))
         self.t += 1
 
 

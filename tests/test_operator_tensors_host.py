@@ -158,17 +158,20 @@ def test_several_groups_need_offsets(recorder):
 
 
 class Columns:
-    """Stands for the native module: the same column, of tensors that say they are on a GPU."""
+    """Stands for the native module: the same columns, of tensors that say they are on a GPU."""
 
     @staticmethod
-    def column(tensors, sizes, code, dst, stride, longer=0):
+    def columns(cols, count, stride):
         import ctypes
-        want = {0: F32, 1: BF, 2: torch.uint8}[code]
-        n = (ctypes.c_int64 * len(tensors)).from_address(sizes) if tensors else []
-        for i, t in enumerate(tensors):
-            if not t.is_cuda or t.dtype != want or not t.is_contiguous() or (t.numel() < n[i] if longer else t.numel() != n[i]):
-                return i
-            ctypes.c_void_p.from_address(dst + i * stride).value = t.data_ptr()
+        for c, (tensors, sizes, code, dst, longer) in enumerate(cols):
+            if len(tensors) != count:
+                return c * (count + 1) + count
+            n = (ctypes.c_int64 * count).from_address(sizes)
+            for i, t in enumerate(tensors):
+                if (not t.is_cuda or t.dtype != (F32, BF, torch.uint8)[code] or not t.is_contiguous()
+                        or (t.numel() < n[i] if longer else t.numel() != n[i])):
+                    return c * (count + 1) + i
+                ctypes.c_void_p.from_address(dst + i * stride).value = t.data_ptr()
         return -1
 
 
@@ -179,6 +182,7 @@ def steps(recorder, monkeypatch):
     seen = []
 
     def step(desc, table, count, stream):
+        assert not stream
         seen.append([{f: getattr(t, f) for f, _ in fm.flexmoe_adamw_tensor._fields_}
                      for t in (fm.flexmoe_adamw_tensor * count).from_address(table)])
         return 0
@@ -231,3 +235,18 @@ def test_adamw_refuses_tensors_that_no_longer_fit(steps):
     with pytest.raises(ValueError):
         opt.step(grads, 1e-3, stream=0)
     assert not steps and opt.t == 0
+
+
+def test_native_columns_refuse_what_does_not_fit():
+    import numpy as np
+    table, sizes = np.zeros(4, np.uint64), np.array([3, 4], np.int64)
+    f, p, at = fm.tensors().columns, sizes.ctypes.data, table.ctypes.data
+    cpu = [torch.zeros(3), torch.zeros(4)]
+    assert f(((cpu, p, 0, at, 0),), 2, 8) == 0               # not on the GPU
+    assert f(((cpu[:1], p, 0, at, 0),), 2, 8) == 2           # another number of tensors
+    assert f((([], p, 0, at, 0), (cpu, p, 0, at, 0)), 0, 8) == 1
+    assert f((([None, None], p, 0, at, 1),), 2, 8) == 0
+    assert not table.any()
+    for bad in [((), 2), ([], 2, 8), ((), 2, 8), (((cpu, p, 0, at),), 2, 8), ((((), p, 0, at, 0),), 0, 8), (((cpu, p, "0", at, 0),), 2, 8)]:
+        with pytest.raises(TypeError):
+            f(*bad)
