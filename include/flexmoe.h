@@ -486,7 +486,20 @@ int flexmoe_quantized_forward(const flexmoe_grouped_desc *desc, int32_t R, const
  * for NaN from then on.  flexmoe_adamw_read_state writes what 8-bit states of
  * one tensor stand for as dtype (checkpoints, inspection).
  * n from 0 to 2^33 and any alignment to the elements (16-byte alignment is fastest;
- * scales, fp32 arrays: 4 bytes).  step >= 1, betas in [0, 1), eps >= 1e-30. */
+ * scales, fp32 arrays: 4 bytes).  step >= 1, betas in [0, 1), eps >= 1e-30.
+ * step, lr and the other numbers are arguments of the launches.  A call that is
+ * captured in a graph keeps them: every replay is the same step, with the same
+ * bias corrections and the same random bits (with 8-bit states, rounded by the
+ * same bits each time, the running means drift).  To replay a captured step as
+ * the next step, give a clock (device memory, 8-byte aligned): each call and each
+ * replay adds 1 to clock->step, by a launch of its own before the others, and
+ * that is its number; the rest of the clock is the library's, and desc->step is
+ * not read. */
+typedef struct flexmoe_adamw_clock {
+    int64_t step;       /* steps done                                            */
+    float step_size, inv_bias2;
+    uint32_t key, pad;
+} flexmoe_adamw_clock;
 typedef struct flexmoe_adamw_tensor {
     void *param;        /* param_dtype                                           */
     const void *grad;   /* grad_dtype                                            */
@@ -501,6 +514,7 @@ typedef struct flexmoe_adamw_desc {
     uint32_t seed;
     int64_t step;                     /* 1 for the first step                    */
     double lr, beta1, beta2, eps, weight_decay, grad_scale;
+    flexmoe_adamw_clock *clock;       /* device memory, or NULL                  */
 } flexmoe_adamw_desc;
 int flexmoe_adamw_step(const flexmoe_adamw_desc *desc, const flexmoe_adamw_tensor *tensors,
                        int32_t count, void *stream);

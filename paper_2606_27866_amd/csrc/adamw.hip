@@ -57,6 +57,7 @@ struct AdamwArgs {
     float beta1, beta2, one_minus_beta1, one_minus_beta2, grad_scale, keep, step_size, inv_bias2, eps;
     uint32_t key;                  // seed and step
     int tensor0;                   // number of t[0] in the list
+    const flexmoe_adamw_clock* clock;  // holds step_size, inv_bias2 and key, or NULL
 };
 static_assert(sizeof(AdamwArgs) <= 4096, "kernel arguments");
 
@@ -159,6 +160,26 @@ __device__ __forceinline__ void store4(uint8_t* p, int n, uint32_t v) {
     }
 }
 
+// What a step's number decides.
+struct StepNumbers {
+    float step_size, inv_bias2;
+    uint32_t key;
+};
+__host__ __device__ inline StepNumbers numbers_of(uint32_t seed, int64_t step, double lr, double beta1, double beta2) {
+    return StepNumbers{(float)(lr / (1.0 - pow(beta1, (double)step))), (float)(1.0 / (1.0 - pow(beta2, (double)step))),
+                       seed * kSeedStep + (uint32_t)step * kTimeStep};
+}
+
+// A step counted on the device: its number and what follows from it.
+__global__ void adamw_clock_kernel(flexmoe_adamw_clock* clock, uint32_t seed, double lr, double beta1, double beta2) {
+    const int64_t step = clock->step + 1;
+    const StepNumbers n = numbers_of(seed, step, lr, beta1, beta2);
+    clock->step = step;
+    clock->step_size = n.step_size;
+    clock->inv_bias2 = n.inv_bias2;
+    clock->key = n.key;
+}
+
 // The parameter that is read and stepped: the master copy where there is one.
 template <typename P>
 struct Values {
@@ -184,8 +205,8 @@ __device__ __forceinline__ void read_values(const flexmoe_adamw_tensor& t, size_
 }
 
 template <typename P, typename G, int kBits, bool kFull, bool kMaster>
-__device__ __forceinline__ void step_values(const AdamwArgs& a, const flexmoe_adamw_tensor& t, size_t i, int n, uint32_t key,
-                                            Values<P>& x) {
+__device__ __forceinline__ void step_values(const AdamwArgs& a, const flexmoe_adamw_tensor& t, size_t i, int n,
+                                            const StepNumbers& step, Values<P>& x) {
     // every product and sum rounded by itself: whether a code is rounded up hangs
     // on the last bit, and the formula's own roundings decide, not which of them
     // the compiler fuses
@@ -202,8 +223,8 @@ __device__ __forceinline__ void step_values(const AdamwArgs& a, const flexmoe_ad
         x.v[k] = x.v[k] * a.beta2 + g * g * a.one_minus_beta2;
         // the hardware root and reciprocal (1 ulp each): a few ulps of the
         // update, which is itself a small part of p
-        const float den = __builtin_amdgcn_sqrtf(x.v[k] * a.inv_bias2) + a.eps;
-        x.p[k] = x.p[k] * a.keep - a.step_size * (x.m[k] * __builtin_amdgcn_rcpf(den));
+        const float den = __builtin_amdgcn_sqrtf(x.v[k] * step.inv_bias2) + a.eps;
+        x.p[k] = x.p[k] * a.keep - step.step_size * (x.m[k] * __builtin_amdgcn_rcpf(den));
         if constexpr (kBits == 8)
             if (kFull || k < n) {
                 top_m = max(top_m, __float_as_uint(x.m[k]) & 0x7fffffffu);
@@ -228,7 +249,7 @@ __device__ __forceinline__ void step_values(const AdamwArgs& a, const flexmoe_ad
         uint32_t mc = 0, vc = 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint32_t r = random_bits(key + (uint32_t)i + k);
+            const uint32_t r = random_bits(step.key + (uint32_t)i + k);
             const float y = __builtin_amdgcn_ldexpf(fabsf(x.m[k]), down);
             int c = (int)((__float_as_uint(y) + ((r >> 16) << 4)) >> 20) - 896;
             c = y < kLeast ? (int)((float)(r >> 16) * (kLeast / 65536.f) < y) : min(max(c, 0), 127);
@@ -248,7 +269,7 @@ __device__ __forceinline__ void step_values(const AdamwArgs& a, const flexmoe_ad
 }
 
 template <typename P, typename G, int kBits, int kUnroll, bool kMaster>
-__device__ __forceinline__ void step_chunk(const AdamwArgs& a, const flexmoe_adamw_tensor& t, size_t at, uint32_t key) {
+__device__ __forceinline__ void step_chunk(const AdamwArgs& a, const flexmoe_adamw_tensor& t, size_t at, const StepNumbers& step) {
     const int lane = threadIdx.x & 63;
     const size_t left = (size_t)t.n - at;  // from this wave's first value on
     const uintptr_t bits = (uintptr_t)t.param | (uintptr_t)t.grad | (uintptr_t)t.m | (uintptr_t)t.v | (uintptr_t)t.master;
@@ -257,14 +278,14 @@ __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const flexmoe_ada
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) read_values<P, G, kBits, true, kMaster>(t, at + u * kBlock + lane * 4, 4, x[u]);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) step_values<P, G, kBits, true, kMaster>(a, t, at + u * kBlock + lane * 4, 4, key, x[u]);
+        for (int u = 0; u < kUnroll; ++u) step_values<P, G, kBits, true, kMaster>(a, t, at + u * kBlock + lane * 4, 4, step, x[u]);
     } else {
         for (int u = 0; u < kUnroll && (size_t)u * kBlock < left; ++u) {
             // every lane stays: the block's largest value is the wave's
             const int n = (int)min((long long)4, max((long long)0, (long long)left - u * kBlock - lane * 4));
             Values<P> x;
             read_values<P, G, kBits, false, kMaster>(t, at + u * kBlock + lane * 4, n, x);
-            step_values<P, G, kBits, false, kMaster>(a, t, at + u * kBlock + lane * 4, n, key, x);
+            step_values<P, G, kBits, false, kMaster>(a, t, at + u * kBlock + lane * 4, n, step, x);
         }
     }
 }
@@ -278,9 +299,11 @@ __global__ __launch_bounds__(AT) void adamw_kernel(AdamwArgs a) {
     const flexmoe_adamw_tensor& t = a.t[j];
     const size_t at = (size_t)(blockIdx.x - a.first[j]) * chunk(kUnroll) + wave * (kUnroll * kBlock);
     if (at >= (size_t)t.n) return;
-    const uint32_t key = a.key + (uint32_t)(a.tensor0 + j) * kTensorStep;
-    if (sizeof(P) == 2 && t.master) step_chunk<P, G, kBits, kUnroll, true>(a, t, at, key);
-    else step_chunk<P, G, kBits, kUnroll, false>(a, t, at, key);
+    StepNumbers step{a.step_size, a.inv_bias2, a.key};
+    if (a.clock) step = StepNumbers{a.clock->step_size, a.clock->inv_bias2, a.clock->key};
+    step.key += (uint32_t)(a.tensor0 + j) * kTensorStep;
+    if (sizeof(P) == 2 && t.master) step_chunk<P, G, kBits, kUnroll, true>(a, t, at, step);
+    else step_chunk<P, G, kBits, kUnroll, false>(a, t, at, step);
 }
 
 template <typename O>
@@ -330,7 +353,8 @@ int flexmoe_adamw_step(const flexmoe_adamw_desc* D, const flexmoe_adamw_tensor* 
             return fail(FLEXMOE_EDTYPE, "adamw_step: dtype %d is neither FLEXMOE_F32 nor FLEXMOE_BF16", dt);
     if (D->state_bits != 8 && D->state_bits != 32) return fail(FLEXMOE_EINVAL, "adamw_step: state_bits = %d is neither 8 nor 32", D->state_bits);
     if (count < 0 || (count > 0 && !tensors)) return fail(FLEXMOE_EINVAL, "adamw_step: count = %d, or tensors is NULL", count);
-    if (D->step < 1) return fail(FLEXMOE_EINVAL, "adamw_step: step = %lld must be at least 1", (long long)D->step);
+    if (D->clock && misaligned(D->clock, 7)) return fail(FLEXMOE_EINVAL, "adamw_step: clock must be 8-byte aligned");
+    if (!D->clock && D->step < 1) return fail(FLEXMOE_EINVAL, "adamw_step: step = %lld must be at least 1", (long long)D->step);
     if (!(D->beta1 >= 0 && D->beta1 < 1 && D->beta2 >= 0 && D->beta2 < 1))
         return fail(FLEXMOE_EINVAL, "adamw_step: beta1 = %g, beta2 = %g outside [0, 1)", D->beta1, D->beta2);
     if (!(D->eps >= 1e-30 && std::isfinite(D->eps))) return fail(FLEXMOE_EINVAL, "adamw_step: eps = %g must be at least 1e-30", D->eps);
@@ -358,11 +382,18 @@ int flexmoe_adamw_step(const flexmoe_adamw_desc* D, const flexmoe_adamw_tensor* 
     a.one_minus_beta2 = (float)(1.0 - D->beta2);
     a.grad_scale = (float)D->grad_scale;
     a.keep = (float)(1.0 - D->lr * D->weight_decay);
-    a.step_size = (float)(D->lr / (1.0 - std::pow(D->beta1, (double)D->step)));
-    a.inv_bias2 = (float)(1.0 / (1.0 - std::pow(D->beta2, (double)D->step)));
+    const StepNumbers numbers = D->clock ? StepNumbers{} : numbers_of(D->seed, D->step, D->lr, D->beta1, D->beta2);
+    a.step_size = numbers.step_size;
+    a.inv_bias2 = numbers.inv_bias2;
     a.eps = (float)D->eps;
-    a.key = D->seed * kSeedStep + (uint32_t)D->step * kTimeStep;
+    a.key = numbers.key;
+    a.clock = D->clock;
     const hipStream_t s = (hipStream_t)stream;
+    if (D->clock) {
+        adamw_clock_kernel<<<1, 1, 0, s>>>(D->clock, D->seed, D->lr, D->beta1, D->beta2);
+        const hipError_t err = hipGetLastError();
+        if (err != hipSuccess) return hip_fail(err, "adamw_step launch");
+    }
     uint64_t total = 0;
     for (int i = 0; i < count; ++i) total += (uint64_t)tensors[i].n;
     const int unroll = D->state_bits == 8 ? 1 : total < (1u << 24) ? 2 : 4;

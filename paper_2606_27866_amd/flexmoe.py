@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import warnings
 from typing import Optional, Sequence
 
 import numpy as np
@@ -81,7 +82,8 @@ _TENSOR_BYTES = ctypes.sizeof(flexmoe_adamw_tensor)
 class flexmoe_adamw_desc(ctypes.Structure):
     _fields_ = [("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("state_bits", ctypes.c_int32),
                 ("seed", ctypes.c_uint32), ("step", ctypes.c_int64)] + \
-               [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay", "grad_scale")]
+               [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay", "grad_scale")] + \
+               [("clock", ctypes.c_void_p)]
 
 
 class flexmoe_action_set(ctypes.Structure):
@@ -223,6 +225,14 @@ def _stream(stream) -> Optional[int]:
     import torch
     # the raw handle of torch's current stream (torch.cuda.current_stream builds objects around it: 2.8 us against 0.1)
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
+def _capturing() -> bool:
+    """Whether torch's current stream is being captured (tensors on the GPU exist, so CUDA is initialised)."""
+    global _capturing
+    import torch
+    _capturing = torch._C._cuda_isCurrentStreamCapturing
+    return _capturing()
 
 
 def make_desc(d, E, I, top_k, I_shared=0, dtype=FLEXMOE_BF16, norm_topk=1, max_tokens=0):
@@ -692,10 +702,14 @@ class AdamW:
     params: bf16 or fp32, all alike.  masters: fp32 copies that the step works on (bf16 parameters).  states: (m, v) or,
     with 8 bits, (m, v, m_scale, v_scale) lists to continue from; zeros otherwise.  step(grads) takes one gradient per
     parameter.  Every step reads the tensors' addresses again: their storages may be replaced between steps.
+
+    In a graph: addresses, lr and the step's number are fixed by the capture, so that every replay is the same step again,
+    its bias corrections and (8 bits) its random bits.  With device_step the number is counted on the device instead
+    (clock[0], the steps done; t stays what it was): every call and every replay is the next step.
     """
 
     def __init__(self, params, masters=None, states=None, state_bits=32, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0,
-                 step=0, seed=0):
+                 step=0, seed=0, device_step=False):
         import torch
         self.params, self.state_bits = list(params), state_bits
         self.betas, self.eps, self.weight_decay, self.t, self.seed = betas, eps, weight_decay, step, seed
@@ -703,6 +717,8 @@ class AdamW:
             raise ValueError("no parameters")
         if state_bits not in (8, 32):
             raise ValueError("state_bits must be 8 or 32, got %s" % (state_bits,))
+        # a flexmoe_adamw_clock
+        self.clock = torch.tensor([step, 0, 0], dtype=torch.int64, device=self.params[0].device) if device_step else None
         dt = self.params[0].dtype
         sizes = [p.numel() for p in self.params]
         blocks = [-(-n // STATE_BLOCK) for n in sizes]
@@ -765,8 +781,14 @@ class AdamW:
             self._refuse(columns, bad)
         d = flexmoe_adamw_desc(self._param_code, code, self.state_bits, self.seed & 0xffffffff, self.t + 1, lr,
                                self.betas[0], self.betas[1], self.eps, self.weight_decay, grad_scale)
+        if self.clock is not None:
+            d.clock = self.clock.data_ptr()
+        elif _capturing():
+            warnings.warn("the captured AdamW step repeats itself on every replay; AdamW(..., device_step=True) counts steps on the device",
+                          stacklevel=2)
         _check(lib().flexmoe_adamw_step(ctypes.byref(d), self._table_at, len(self.sizes), _stream(stream)))
-        self.t += 1
+        if self.clock is None:
+            self.t += 1
 
 
 def adamw_state_values(m, v, m_scale, v_scale, dtype=None, stream=None):

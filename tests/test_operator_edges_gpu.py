@@ -89,3 +89,58 @@ def test_adamw_steps_the_storage_that_a_parameter_has_now(bits):
     b.step([grad], 1e-2)
     assert torch.equal(p, q) and torch.equal(a.m[0], b.m[0])
     assert torch.equal(old, before[0]) and torch.equal(m, before[1])  # nothing was written to the storages it had
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_captured_adamw_step_that_counts_on_the_device(bits):
+    """Replays and eager calls in turn are the steps of an optimizer that counts on the host, bit for bit: each has its own
+    bias corrections and its own random bits."""
+    g = torch.Generator(device="cuda")
+    sizes = [3000, 257] * 40  # two launches
+    p = [torch.randn(n, generator=g, device="cuda") for n in sizes]
+    q, grads = [t.clone() for t in p], [torch.randn(n, generator=g, device="cuda") for n in sizes]
+    a = fm.AdamW(p, state_bits=bits, seed=3, weight_decay=0.1, device_step=True)
+    b = fm.AdamW(q, state_bits=bits, seed=3, weight_decay=0.1)
+    a.step(grads, 1e-2)
+    b.step(grads, 1e-2)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.step(grads, 1e-2)
+    for k in range(4):
+        for t in grads:
+            t.mul_(0.9)
+        graph.replay()
+        b.step(grads, 1e-2)
+        if k == 1:
+            a.step(grads, 1e-2)
+            b.step(grads, 1e-2)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(p + a.m + a.v, q + b.m + b.v))
+    assert int(a.clock[0]) == b.t == 6
+
+
+def test_replays_that_count_on_the_device_keep_the_mean():
+    """A constant gradient through replays of one captured step: the 8-bit states reach it, as those of separate calls do."""
+    n = 4096
+    g = torch.full((n,), 0.02, device="cuda")
+    g[::256] = 0.05
+    opt = fm.AdamW([torch.zeros(n, device="cuda")], state_bits=8, betas=(0.9, 0.99), seed=9, device_step=True)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step([g], 0.0)
+    for _ in range(600):
+        graph.replay()
+    m, v = fm.adamw_state_values(opt.m[0], opt.v[0], opt.m_scale[0], opt.v_scale[0])
+    rest = torch.ones(n, dtype=torch.bool, device="cuda")
+    rest[::256] = False
+    assert abs(float(m[rest].mean()) / 0.02 - 1) < 0.02
+    assert abs(float(v[rest].mean()) / 0.02 ** 2 - 1) < 0.05
+
+
+def test_a_captured_step_without_a_clock_says_that_it_repeats():
+    p = torch.ones(300, device="cuda")
+    opt = fm.AdamW([p], state_bits=8)
+    graph = torch.cuda.CUDAGraph()
+    with pytest.warns(UserWarning, match="device_step"):
+        with torch.cuda.graph(graph):
+            opt.step([p], 1e-3)

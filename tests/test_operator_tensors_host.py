@@ -179,6 +179,7 @@ class Columns:
 def steps(recorder, monkeypatch):
     """The tables that flexmoe_adamw_step was given."""
     monkeypatch.setattr(fm, "tensors", lambda: Columns)
+    monkeypatch.setattr(fm, "_capturing", lambda: False)
     seen = []
 
     def step(desc, table, count, stream):
@@ -250,3 +251,21 @@ def test_native_columns_refuse_what_does_not_fit():
     for bad in [((), 2), ([], 2, 8), ((), 2, 8), (((cpu, p, 0, at),), 2, 8), ((((), p, 0, at, 0),), 0, 8), (((cpu, p, "0", at, 0),), 2, 8)]:
         with pytest.raises(TypeError):
             f(*bad)
+
+
+def test_adamw_clock_arguments(steps, recorder):
+    p = on_gpu(torch.zeros(8))
+    states = ([on_gpu(torch.zeros(8))], [on_gpu(torch.zeros(8))])
+    opt = fm.AdamW([p], states=states, step=7, device_step=True)
+    seen = []
+    step = recorder.flexmoe_adamw_step
+    recorder.flexmoe_adamw_step = lambda d, *rest: (seen.append(d._obj.clock), step(d, *rest))[1]
+    opt.step([p], 1e-3, stream=0)
+    assert seen == [opt.clock.data_ptr()] and opt.clock.numel() * 8 == 24
+    assert opt.clock[0] == 7 and opt.t == 7  # the kernels count, not the holder
+
+
+def test_adamw_refuses_a_misaligned_clock():
+    D = fm.flexmoe_adamw_desc(0, 0, 32, 0, 0, 1e-3, 0.9, 0.99, 1e-8, 0.0, 1.0, 0x100004)
+    assert fm.lib().flexmoe_adamw_step(fm.ctypes.byref(D), None, 0, None) == -1
+    assert "clock" in fm.flexmoe_last_error()
