@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import threading
 import warnings
 from typing import Optional, Sequence
 
@@ -549,7 +550,7 @@ class GroupedProduct:
     A holder around the C calls (no arithmetic): it keeps the workspace for up to max_rows rows and allocates outputs.
     offsets [groups + 1] int32 on the device are the groups' row ranges (the forward's routing copies hold them); keep
     [groups] int32 limits W_e's rows (keep_axis "N") or columns ("K").  Calls on different streams need holders of their
-    own: they share the workspace.
+    own: they share the workspace.  Threads may share a holder: its calls take their turn.
     """
 
     def __init__(self, groups, N, K, max_rows, dtype=None, keep_axis="none", device="cuda"):
@@ -564,6 +565,7 @@ class GroupedProduct:
         self._desc = ctypes.byref(self.desc)
         self.workspace = torch.empty(flexmoe_grouped_workspace_bytes(self.desc, max_rows), dtype=torch.uint8, device=device)
         self._ws = (self.workspace.data_ptr(), self.workspace.numel())
+        self._lock = threading.Lock()  # holds the descriptor's strides: the library's calls run without the interpreter's lock
 
     def _groups(self, offsets, keep):
         return (_vector(offsets, self.groups + 1, self._i32, "offsets"),
@@ -574,10 +576,11 @@ class GroupedProduct:
         R, d, dt = x.shape[0], self.desc, self.dtype
         if y is None:
             y = _padded((R, self.N), dt, x.device)
-        d.ldx, d.ldw = _matrix(x, (R, self.K), dt, "x"), _matrix(w, self._w_shape, dt, "w")
-        d.ldy = _matrix(y, (R, self.N), dt, "y")
-        _check(lib().flexmoe_grouped_forward(self._desc, R, x.data_ptr(), w.data_ptr(), *self._groups(offsets, keep),
-                                             y.data_ptr(), *self._ws, _stream(stream)))
+        with self._lock:
+            d.ldx, d.ldw = _matrix(x, (R, self.K), dt, "x"), _matrix(w, self._w_shape, dt, "w")
+            d.ldy = _matrix(y, (R, self.N), dt, "y")
+            _check(lib().flexmoe_grouped_forward(self._desc, R, x.data_ptr(), w.data_ptr(), *self._groups(offsets, keep),
+                                                 y.data_ptr(), *self._ws, _stream(stream)))
         return y
 
     def input_grad(self, dy, w, offsets, keep=None, dx=None, stream=None):
@@ -585,10 +588,11 @@ class GroupedProduct:
         R, d, dt = dy.shape[0], self.desc, self.dtype
         if dx is None:
             dx = _padded((R, self.K), dt, dy.device)
-        d.ldy, d.ldw = _matrix(dy, (R, self.N), dt, "dy"), _matrix(w, self._w_shape, dt, "w")
-        d.ldx = _matrix(dx, (R, self.K), dt, "dx")
-        _check(lib().flexmoe_grouped_input_grad(self._desc, R, dy.data_ptr(), w.data_ptr(), *self._groups(offsets, keep),
-                                                dx.data_ptr(), *self._ws, _stream(stream)))
+        with self._lock:
+            d.ldy, d.ldw = _matrix(dy, (R, self.N), dt, "dy"), _matrix(w, self._w_shape, dt, "w")
+            d.ldx = _matrix(dx, (R, self.K), dt, "dx")
+            _check(lib().flexmoe_grouped_input_grad(self._desc, R, dy.data_ptr(), w.data_ptr(), *self._groups(offsets, keep),
+                                                    dx.data_ptr(), *self._ws, _stream(stream)))
         return dx
 
     def weight_grad(self, dy, x, offsets, keep=None, dw=None, accumulate=False, dw_dtype=None, stream=None):
@@ -600,11 +604,12 @@ class GroupedProduct:
             dw = _padded(self._w_shape, self._f32 if dw_dtype is None else dw_dtype, dy.device)
         elif dw_dtype is not None and dw.dtype != dw_dtype:
             raise ValueError("dw is %s, not %s" % (dw.dtype, dw_dtype))
-        d.dw_dtype = _dtype_code(dw.dtype)
-        d.ldy, d.ldx = _matrix(dy, (R, self.N), dt, "dy"), _matrix(x, (R, self.K), dt, "x")
-        d.lddw = _matrix(dw, self._w_shape, dw.dtype, "dw")
-        _check(lib().flexmoe_grouped_weight_grad(self._desc, R, dy.data_ptr(), x.data_ptr(), *self._groups(offsets, keep),
-                                                 dw.data_ptr(), int(accumulate), *self._ws, _stream(stream)))
+        with self._lock:
+            d.dw_dtype = _dtype_code(dw.dtype)
+            d.ldy, d.ldx = _matrix(dy, (R, self.N), dt, "dy"), _matrix(x, (R, self.K), dt, "x")
+            d.lddw = _matrix(dw, self._w_shape, dw.dtype, "dw")
+            _check(lib().flexmoe_grouped_weight_grad(self._desc, R, dy.data_ptr(), x.data_ptr(), *self._groups(offsets, keep),
+                                                     dw.data_ptr(), int(accumulate), *self._ws, _stream(stream)))
         return dw
 
 
@@ -634,7 +639,7 @@ class Int8Product:
 
     w [groups, N, K] int8 and w_scale [groups, N] (quantize_rows of the weights).  Calling it rounds the rows of x and
     multiplies; `product` takes rows that are rounded already.  It keeps the workspace and the rounded rows' buffers for
-    up to max_rows rows: calls on different streams need holders of their own.
+    up to max_rows rows: calls on different streams need holders of their own; threads may share one.
     """
 
     def __init__(self, w, w_scale, max_rows, keep_axis="none", out_dtype=None):
@@ -651,6 +656,7 @@ class Int8Product:
         self._ws = (self.workspace.data_ptr(), self.workspace.numel())
         self.q = _padded((max_rows, self.K), torch.int8, w.device)
         self.q_scale = torch.empty(max_rows, dtype=torch.float32, device=w.device)
+        self._lock = threading.Lock()  # holds the descriptor's strides, and q from its rounding to the product's launch
         # all rows of any call, for one group: the kernels cut offsets to [0, R]
         self._all_rows = torch.tensor([0, 2 ** 31 - 1], dtype=torch.int32, device=w.device) if self.groups == 1 else None
 
@@ -670,15 +676,17 @@ class Int8Product:
             raise ValueError("x and gate must have the same strides")
         q, scale, d = self.q.data_ptr(), self.q_scale.data_ptr(), self.desc
         ldq = self.q.stride(0) if self.max_rows > 1 else _pitch(self.K, 1)
-        _check(lib().flexmoe_quantize_rows(R, self.K, _dtype_code(x.dtype), x.data_ptr(), None if gate is None else gate.data_ptr(), ldx,
-                                           q, ldq, scale, stream))
-        d.ldx = ldq
-        return self._product(R, q, scale, offsets, keep, y, x.device, stream)
+        with self._lock:
+            _check(lib().flexmoe_quantize_rows(R, self.K, _dtype_code(x.dtype), x.data_ptr(), None if gate is None else gate.data_ptr(), ldx,
+                                               q, ldq, scale, stream))
+            d.ldx = ldq
+            return self._product(R, q, scale, offsets, keep, y, x.device, stream)
 
     def product(self, q, q_scale, offsets=None, keep=None, y=None, stream=None):
         R = q.shape[0]
-        self.desc.ldx = _matrix(q, (R, self.K), self._i8, "q")
-        return self._product(R, q.data_ptr(), _vector(q_scale, R, self._f32, "q_scale"), offsets, keep, y, q.device, _stream(stream))
+        with self._lock:
+            self.desc.ldx = _matrix(q, (R, self.K), self._i8, "q")
+            return self._product(R, q.data_ptr(), _vector(q_scale, R, self._f32, "q_scale"), offsets, keep, y, q.device, _stream(stream))
 
     def _product(self, R, q, q_scale, offsets, keep, y, device, stream):
         if offsets is None:
@@ -736,6 +744,7 @@ class AdamW:
         self.sizes, self._param_code = sizes, _dtype_code(dt)
         self._table = (flexmoe_adamw_tensor * len(sizes))()
         self._table_at = ctypes.addressof(self._table)
+        self._lock = threading.Lock()  # holds the table and t
         self._n, self._blocks = np.array(sizes, dtype=np.int64), np.array(blocks, dtype=np.int64)
         np.frombuffer(self._table, dtype=np.int64)[flexmoe_adamw_tensor.n.offset // 8::_TENSOR_BYTES // 8] = self._n
         # the table's columns, filled by every step, since a tensor's storage may have been replaced since the last one
@@ -775,20 +784,21 @@ class AdamW:
         if len(grads) != len(self.sizes):
             raise ValueError("%d gradients for %d parameters" % (len(grads), len(self.sizes)))
         code = _dtype_code(grads[0].dtype)
-        columns = (*self._columns, (grads, self._sizes_at, code, self._grad_at, 0))
-        bad = tensors().columns(columns, len(grads), _TENSOR_BYTES)
-        if bad >= 0:
-            self._refuse(columns, bad)
-        d = flexmoe_adamw_desc(self._param_code, code, self.state_bits, self.seed & 0xffffffff, self.t + 1, lr,
-                               self.betas[0], self.betas[1], self.eps, self.weight_decay, grad_scale)
-        if self.clock is not None:
-            d.clock = self.clock.data_ptr()
-        elif _capturing():
-            warnings.warn("the captured AdamW step repeats itself on every replay; AdamW(..., device_step=True) counts steps on the device",
-                          stacklevel=2)
-        _check(lib().flexmoe_adamw_step(ctypes.byref(d), self._table_at, len(self.sizes), _stream(stream)))
-        if self.clock is None:
-            self.t += 1
+        with self._lock:
+            columns = (*self._columns, (grads, self._sizes_at, code, self._grad_at, 0))
+            bad = tensors().columns(columns, len(grads), _TENSOR_BYTES)
+            if bad >= 0:
+                self._refuse(columns, bad)
+            d = flexmoe_adamw_desc(self._param_code, code, self.state_bits, self.seed & 0xffffffff, self.t + 1, lr,
+                                   self.betas[0], self.betas[1], self.eps, self.weight_decay, grad_scale)
+            if self.clock is not None:
+                d.clock = self.clock.data_ptr()
+            elif _capturing():
+                warnings.warn("the captured AdamW step repeats itself on every replay; AdamW(..., device_step=True) counts steps on the device",
+                              stacklevel=2)
+            _check(lib().flexmoe_adamw_step(ctypes.byref(d), self._table_at, len(self.sizes), _stream(stream)))
+            if self.clock is None:
+                self.t += 1
 
 
 def adamw_state_values(m, v, m_scale, v_scale, dtype=None, stream=None):

@@ -34,15 +34,6 @@ def expanded(*shape, dtype=BF, over=0):
     return on_gpu(torch.zeros(one, dtype=dtype).expand(shape))
 
 
-def holder(groups, N, K, rows=10, dtype=BF):
-    """A GroupedProduct without its workspace."""
-    op = object.__new__(fm.GroupedProduct)
-    op.groups, op.N, op.K, op.max_rows, op.keep_axis, op.dtype = groups, N, K, rows, "none", dtype
-    op._i32, op._f32, op._w_shape = torch.int32, F32, (groups, N, K)
-    op.desc, op._ws = fm.make_grouped_desc(groups, N, K, max_rows=rows), (0, 0)
-    return op
-
-
 def test_the_gradient_of_a_sum_is_an_expanded_tensor():
     y = torch.zeros(10, 64, requires_grad=True)
     z, seen = y * 1, []
@@ -66,9 +57,10 @@ def test_rows_that_do_not_overlap_are_taken():
         assert fm._matrix(on_gpu(t), tuple(t.shape), F32, "x") == ld
 
 
-def test_products_refuse_expanded_tensors(no_launch):
+def test_products_refuse_expanded_tensors(request):
     E, N, K, R = 2, 16, 64, 10
-    op = holder(E, N, K)
+    op = fm.GroupedProduct(E, N, K, R, device="cpu")
+    request.getfixturevalue("no_launch")
     offsets = on_gpu(torch.zeros(E + 1, dtype=torch.int32))
     x, dy, w = (on_gpu(torch.zeros(s, dtype=BF)) for s in ((R, K), (R, N), (E, N, K)))
     for f, args in [(op.forward, (expanded(R, K), w, offsets)), (op.forward, (x, expanded(E, N, K, over=0), offsets)),
@@ -269,3 +261,88 @@ def test_adamw_refuses_a_misaligned_clock():
     D = fm.flexmoe_adamw_desc(0, 0, 32, 0, 0, 1e-3, 0.9, 0.99, 1e-8, 0.0, 1.0, 0x100004)
     assert fm.lib().flexmoe_adamw_step(fm.ctypes.byref(D), None, 0, None) == -1
     assert "clock" in fm.flexmoe_last_error()
+
+
+def both(*calls):
+    """The calls in turn in a thread each, many times at once; their exceptions."""
+    import threading
+    errors = []
+
+    def loop(f):
+        try:
+            for _ in range(30):
+                f()
+        except Exception as e:  # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=loop, args=(f,)) for f in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    return errors
+
+
+def test_threads_that_share_a_holder_keep_their_strides(recorder):
+    """A call of the library runs without the interpreter's lock: another thread's strides must not reach its descriptor."""
+    import time
+    E, N, K, R = 2, 16, 64, 10
+    op = fm.GroupedProduct(E, N, K, R, device="cpu")
+    w, offsets = on_gpu(torch.zeros(E, N, K, dtype=BF)), on_gpu(torch.zeros(E + 1, dtype=torch.int32))
+    xs = [on_gpu(torch.zeros(R, ld, dtype=BF)[:, :K]) for ld in (64, 72)]
+    ys = [on_gpu(torch.zeros(R, ld, dtype=BF)[:, :N]) for ld in (16, 40)]
+    want = {x.data_ptr(): (x.stride(0), y.stride(0)) for x, y in zip(xs, ys)}
+
+    def forward(desc, rows, x, *_):
+        d = desc._obj
+        before = d.ldx, d.ldy
+        time.sleep(0.0005)
+        assert before == (d.ldx, d.ldy) == want[x]
+        return 0
+
+    recorder.flexmoe_grouped_forward = forward
+    assert not both(*[lambda x=x, y=y: op.forward(x, w, offsets, y=y, stream=0) for x, y in zip(xs, ys)])
+
+
+def test_threads_that_share_an_int8_holder_keep_their_rows(recorder):
+    """The rounded rows lie in the holder's buffer until the product is launched."""
+    import time
+    op = fm.Int8Product(on_gpu(torch.zeros(1, 32, 64, dtype=I8)), on_gpu(torch.zeros(1, 32)), max_rows=8)
+    xs = [on_gpu(torch.zeros(R, 64, dtype=BF)) for R in (3, 5)]
+    ys = [on_gpu(torch.zeros(x.shape[0], 32, dtype=BF)) for x in xs]
+    held = []
+
+    def quantize(rows, *_):
+        held.append(rows)
+        time.sleep(0.0005)
+        return 0
+
+    def product(desc, rows, *_):
+        assert held.pop() == rows and not held
+        time.sleep(0.0005)
+        return 0
+
+    recorder.flexmoe_quantize_rows, recorder.flexmoe_quantized_forward = quantize, product
+    assert not both(*[lambda x=x, y=y: op(x, y=y, stream=0) for x, y in zip(xs, ys)])
+
+
+def test_threads_that_share_an_optimizer_keep_their_gradients(steps, recorder):
+    import threading
+    import time
+    opt, one = adamw()
+    two = [on_gpu(torch.ones_like(g)) for g in one]
+    step, own = recorder.flexmoe_adamw_step, {}
+
+    def slow(*args):
+        time.sleep(0.0005)
+        step(*args)
+        assert [t["grad"] for t in steps[-1]] == own[threading.get_ident()]
+        return 0
+
+    def call(grads):
+        own[threading.get_ident()] = [g.data_ptr() for g in grads]
+        opt.step(grads, 1e-3, stream=0)
+
+    recorder.flexmoe_adamw_step = slow
+    assert not both(lambda: call(one), lambda: call(two))
+    assert len(steps) == opt.t == 60
