@@ -160,6 +160,18 @@ __device__ __forceinline__ void store4(uint8_t* p, int n, uint32_t v) {
     }
 }
 
+// The hardware root takes a denormal, whose root is below 1.1e-19, for 0.  That
+// shows beside an eps below kSmallest only, 2^24 times as much: there small values
+// are lifted by a power of four (in every step it would take 1 to 2 % longer).
+constexpr double kSmallest = 2e-12;
+template <bool kSmallEps>
+__device__ __forceinline__ float root(float x) {
+    if constexpr (!kSmallEps) return __builtin_amdgcn_sqrtf(x);
+    const bool small = x < 0x1p-96f;
+    const float r = __builtin_amdgcn_sqrtf(small ? x * 0x1p+64f : x);
+    return small ? r * 0x1p-32f : r;
+}
+
 // What a step's number decides.
 struct StepNumbers {
     float step_size, inv_bias2;
@@ -204,7 +216,7 @@ __device__ __forceinline__ void read_values(const flexmoe_adamw_tensor& t, size_
     }
 }
 
-template <typename P, typename G, int kBits, bool kFull, bool kMaster>
+template <typename P, typename G, int kBits, bool kFull, bool kMaster, bool kSmallEps>
 __device__ __forceinline__ void step_values(const AdamwArgs& a, const flexmoe_adamw_tensor& t, size_t i, int n,
                                             const StepNumbers& step, Values<P>& x) {
     // every product and sum rounded by itself: whether a code is rounded up hangs
@@ -223,7 +235,7 @@ __device__ __forceinline__ void step_values(const AdamwArgs& a, const flexmoe_ad
         x.v[k] = x.v[k] * a.beta2 + g * g * a.one_minus_beta2;
         // the hardware root and reciprocal (1 ulp each): a few ulps of the
         // update, which is itself a small part of p
-        const float den = __builtin_amdgcn_sqrtf(x.v[k] * step.inv_bias2) + a.eps;
+        const float den = root<kSmallEps>(x.v[k] * step.inv_bias2) + a.eps;
         x.p[k] = x.p[k] * a.keep - step.step_size * (x.m[k] * __builtin_amdgcn_rcpf(den));
         if constexpr (kBits == 8)
             if (kFull || k < n) {
@@ -268,7 +280,7 @@ __device__ __forceinline__ void step_values(const AdamwArgs& a, const flexmoe_ad
     }
 }
 
-template <typename P, typename G, int kBits, int kUnroll, bool kMaster>
+template <typename P, typename G, int kBits, int kUnroll, bool kMaster, bool kSmallEps>
 __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const flexmoe_adamw_tensor& t, size_t at, const StepNumbers& step) {
     const int lane = threadIdx.x & 63;
     const size_t left = (size_t)t.n - at;  // from this wave's first value on
@@ -278,19 +290,19 @@ __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const flexmoe_ada
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) read_values<P, G, kBits, true, kMaster>(t, at + u * kBlock + lane * 4, 4, x[u]);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) step_values<P, G, kBits, true, kMaster>(a, t, at + u * kBlock + lane * 4, 4, step, x[u]);
+        for (int u = 0; u < kUnroll; ++u) step_values<P, G, kBits, true, kMaster, kSmallEps>(a, t, at + u * kBlock + lane * 4, 4, step, x[u]);
     } else {
         for (int u = 0; u < kUnroll && (size_t)u * kBlock < left; ++u) {
             // every lane stays: the block's largest value is the wave's
             const int n = (int)min((long long)4, max((long long)0, (long long)left - u * kBlock - lane * 4));
             Values<P> x;
             read_values<P, G, kBits, false, kMaster>(t, at + u * kBlock + lane * 4, n, x);
-            step_values<P, G, kBits, false, kMaster>(a, t, at + u * kBlock + lane * 4, n, step, x);
+            step_values<P, G, kBits, false, kMaster, kSmallEps>(a, t, at + u * kBlock + lane * 4, n, step, x);
         }
     }
 }
 
-template <typename P, typename G, int kBits, int kUnroll>
+template <typename P, typename G, int kBits, int kUnroll, bool kSmallEps>
 __global__ __launch_bounds__(AT) void adamw_kernel(AdamwArgs a) {
     static_assert(kTensors < 64, "one lane per tensor");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -302,8 +314,8 @@ __global__ __launch_bounds__(AT) void adamw_kernel(AdamwArgs a) {
     StepNumbers step{a.step_size, a.inv_bias2, a.key};
     if (a.clock) step = StepNumbers{a.clock->step_size, a.clock->inv_bias2, a.clock->key};
     step.key += (uint32_t)(a.tensor0 + j) * kTensorStep;
-    if (sizeof(P) == 2 && t.master) step_chunk<P, G, kBits, kUnroll, true>(a, t, at, step);
-    else step_chunk<P, G, kBits, kUnroll, false>(a, t, at, step);
+    if (sizeof(P) == 2 && t.master) step_chunk<P, G, kBits, kUnroll, true, kSmallEps>(a, t, at, step);
+    else step_chunk<P, G, kBits, kUnroll, false, kSmallEps>(a, t, at, step);
 }
 
 template <typename O>
@@ -326,14 +338,19 @@ __global__ __launch_bounds__(AT) void adamw_read_kernel(const uint8_t* m, const 
 
 // hipLaunchKernel itself: the arguments, 4 KB, are not copied on the way, and the
 // error is the launch's own.
-template <int kBits, int kUnroll>
+template <int kBits, int kUnroll, bool kSmallEps>
 hipError_t launch(AdamwArgs& a, bool param_bf16, bool grad_bf16, unsigned grid, hipStream_t s) {
-    auto* const f = param_bf16 && grad_bf16 ? adamw_kernel<bf16_t, bf16_t, kBits, kUnroll>
-                    : param_bf16            ? adamw_kernel<bf16_t, float, kBits, kUnroll>
-                    : grad_bf16             ? adamw_kernel<float, bf16_t, kBits, kUnroll>
-                                            : adamw_kernel<float, float, kBits, kUnroll>;
+    auto* const f = param_bf16 && grad_bf16 ? adamw_kernel<bf16_t, bf16_t, kBits, kUnroll, kSmallEps>
+                    : param_bf16            ? adamw_kernel<bf16_t, float, kBits, kUnroll, kSmallEps>
+                    : grad_bf16             ? adamw_kernel<float, bf16_t, kBits, kUnroll, kSmallEps>
+                                            : adamw_kernel<float, float, kBits, kUnroll, kSmallEps>;
     void* args[] = {&a};
     return hipLaunchKernel(reinterpret_cast<const void*>(f), dim3(grid), dim3(AT), args, 0, s);
+}
+template <int kBits, int kUnroll>
+hipError_t launch(AdamwArgs& a, bool param_bf16, bool grad_bf16, unsigned grid, hipStream_t s) {
+    return a.eps < (float)kSmallest ? launch<kBits, kUnroll, true>(a, param_bf16, grad_bf16, grid, s)
+                                    : launch<kBits, kUnroll, false>(a, param_bf16, grad_bf16, grid, s);
 }
 
 bool misaligned(const void* p, uintptr_t mask) { return ((uintptr_t)p & mask) != 0; }

@@ -1,5 +1,7 @@
 """Calls at the edges of the experts' products, the 8-bit products and AdamW: stacks, whole tensors without offsets, streams,
 graphs, threads, moved storages, very small values, and every kind of tiles in one part and in several."""
+import math
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -144,3 +146,16 @@ def test_a_captured_step_without_a_clock_says_that_it_repeats():
     with pytest.warns(UserWarning, match="device_step"):
         with torch.cuda.graph(graph):
             opt.step([p], 1e-3)
+
+
+def test_adamw_with_second_moments_below_the_normal_range():
+    """v from 1e-44 to 1e-30 with eps = 1e-30: the root of a denormal is far above eps and must not be taken for 0.  Many steps
+    done, so that the corrections are 1; the step's own v is the reference's (it rounds as fp32 denormals do), which leaves
+    the root, the sum, the reciprocal and the products: 16 units of 2^-23 as for other values."""
+    v = torch.logspace(-44, -30, 4096, dtype=torch.float64, device="cuda").float()
+    m = v.double().sqrt().float()
+    p, grad = torch.zeros_like(v), torch.zeros_like(v)
+    opt = fm.AdamW([p], states=([m], [v]), betas=(0.9, 0.99), eps=1e-30, step=10000)
+    opt.step([grad], 1e-2)
+    want = -1e-2 * m.double() / (v.double().sqrt() + 1e-30)
+    assert bool((v > 0).all()) and bool(((p.double() - want).abs() <= want.abs() * 16 * 2.0 ** -23).all())
