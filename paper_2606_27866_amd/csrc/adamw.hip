@@ -251,11 +251,18 @@ __device__ __forceinline__ void step_values(const AdamwArgs& a, const flexmoe_ad
     } else {
         top_m = wave_max_bits(top_m);
         top_v = wave_max_bits(top_v);
-        const float tv = __uint_as_float(top_v);
+        float tv = __uint_as_float(top_v);
         const float nan = __uint_as_float(0x7fc00000u);
         // scale of m: the power of two that top is at most 1.875 times of
         const uint32_t sb = max((top_m + 0xfffffu) & 0x7f800000u, 0x00800000u);
         const int down = 127 - (int)(sb >> 23);
+        // 65025 / tv leaves fp32's range below 1.9e-34: such a block (all zeros is
+        // one too) is lifted by a power of two first
+        if (tv < 0x1p-100f) {
+            tv *= 0x1p+64f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x.v[k] *= 0x1p+64f;
+        }
         const float per_v = 65025.f * (1.f / tv);
         constexpr float kLeast = 1.125f / 32768.f;  // code 1
         uint32_t mc = 0, vc = 0;
@@ -275,7 +282,7 @@ __device__ __forceinline__ void step_values(const AdamwArgs& a, const flexmoe_ad
         store4<kFull>(reinterpret_cast<uint8_t*>(t.v) + i, n, vc);
         if ((threadIdx.x & 63) == 0) {
             t.m_scale[i / kBlock] = top_m >= 0x7f800000u ? nan : top_m ? __uint_as_float(sb) : 0.f;
-            t.v_scale[i / kBlock] = top_v >= 0x7f800000u ? nan : sqrtf(tv) / 255.f;
+            t.v_scale[i / kBlock] = top_v >= 0x7f800000u ? nan : sqrtf(__uint_as_float(top_v)) / 255.f;
         }
     }
 }

@@ -159,3 +159,30 @@ def test_adamw_with_second_moments_below_the_normal_range():
     opt.step([grad], 1e-2)
     want = -1e-2 * m.double() / (v.double().sqrt() + 1e-30)
     assert bool((v > 0).all()) and bool(((p.double() - want).abs() <= want.abs() * 16 * 2.0 ** -23).all())
+
+
+@pytest.mark.parametrize("size", [1e-16, 1e-17, 1e-18, 1e-20, 1e-21, 3e-22])
+def test_8_bit_second_moments_of_tiny_gradients(size):
+    """Gradients whose squares lie below 1e-31, where 65025 / v leaves fp32's range at 1.9e-34: a stored v is one of the two
+    codes next to the exact one (which is at least fp32's smallest denormal off), its mean over a block's draws the exact
+    one (6 standard errors)."""
+    n = 1 << 16
+    g = torch.full((n,), 0.3 * size, device="cuda")
+    g[::256] = size
+    opt = fm.AdamW([torch.zeros(n, device="cuda")], state_bits=8, betas=(0.9, 0.99), seed=5)
+    opt.step([g], 0.0)
+    k = opt.v[0].double()
+    one = torch.tensor(1.0 - 0.99, dtype=torch.float64).float().double()
+    exact = (one * g.double() ** 2)
+    top = float(exact[0])
+    grain = 2.0 ** -149                     # of the exact values as fp32 holds them
+    root = (exact / top).sqrt() * 255       # the code that stands for them
+    slack = 255 * (2 * grain / top + 2.0 ** -20)
+    assert bool((opt.v[0][::256] == 255).all())
+    assert bool(((k >= root.floor() - slack) & (k <= root.ceil() + slack)).all())
+    assert bool(((k > 0) == (g * g * float(one) > 0)).all())  # a v above 0 keeps a code above 0
+    rest = torch.ones(n, dtype=torch.bool, device="cuda")
+    rest[::256] = False
+    count, mid = int(rest.sum()), float(root[1])
+    spread = (2 * math.floor(mid) + 1) / 2  # of k^2 about its mean, at most
+    assert abs(float((k[rest] ** 2).mean()) - mid ** 2) <= 6 * spread / math.sqrt(count) + mid ** 2 * (4 * grain / (0.09 * top) + 1e-5)
