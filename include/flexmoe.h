@@ -447,7 +447,9 @@ int flexmoe_grouped_weight_grad(const flexmoe_grouped_desc *desc, int32_t R, con
  * flexmoe_quantize_rows: row r of v [rows][cols] as whole numbers
  *   q_r = round(v_r * ((1 / m) * 127)) in fp32, ties to even, and scale[r] =
  *   m / 127 for m = max |v_r|; v = x, or silu(x_gate) * x with x_gate (NULL otherwise; same
- *   shape, stride and type).  A row of zeros has scale 0; a row with a NaN or an
+ *   shape, stride and type).  Rows with m below 2^-100 are multiplied by 2^64
+ *   first (127 / m would leave fp32's range; scale[r] is still m / 127, itself a
+ *   denormal below 1.5e-36).  A row of zeros has scale 0; a row with a NaN or an
  *   infinity has the scale NaN and zeros.  x [rows][ldx] (dtype; rows of
  *   whole 16-byte units), q [rows][ldq] int8 (ldq a multiple of 16; up to 7 values past the
  *   row are written as 0, inside its stride), strides of 0 = packed.  The rows

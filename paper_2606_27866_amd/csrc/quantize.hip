@@ -107,25 +107,28 @@ __global__ __launch_bounds__(QT) void quantize_kernel(const void* x, const void*
     }
     const float top = __uint_as_float(m);
     const bool finite = m < 0x7f800000u;
-    const float inv = finite && m ? fminf(1.f / top * 127.f, 3.4028234e38f) : 0.f;
+    // 127 / top leaves fp32's range below 3.7e-37: the values of such a row (of
+    // zeros too) are lifted by a power of two first
+    const bool low = top < 0x1p-100f;
+    const float inv = finite && m ? 1.f / (low ? top * 0x1p+64f : top) * 127.f : 0.f;
     if (t == 0) scale[row] = finite ? top / 127.f : __uint_as_float(0x7fc00000u);
     if constexpr (kChunks > 0) {
 #pragma unroll
         for (int i = 0; i < kChunks; ++i) {
             const int c = t + i * kLanes;
             if (c < chunks) {
-                if (!finite)
+                if (!finite || low)
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) v[i][k] = 0.f;
+                    for (int k = 0; k < 8; ++k) v[i][k] = finite ? v[i][k] * 0x1p+64f : 0.f;
                 store_q(qr + 8 * c, v[i], inv);
             }
         }
     } else {
         for (int c = t; c < chunks; c += kLanes) {
             row_chunk<kBf16, kGated>(x, x2, at, c, cols, v[0]);
-            if (!finite)
+            if (!finite || low)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[0][k] = 0.f;
+                for (int k = 0; k < 8; ++k) v[0][k] = finite ? v[0][k] * 0x1p+64f : 0.f;
             store_q(qr + 8 * c, v[0], inv);
         }
     }

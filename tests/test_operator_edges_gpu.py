@@ -186,3 +186,26 @@ def test_8_bit_second_moments_of_tiny_gradients(size):
     count, mid = int(rest.sum()), float(root[1])
     spread = (2 * math.floor(mid) + 1) / 2  # of k^2 about its mean, at most
     assert abs(float((k[rest] ** 2).mean()) - mid ** 2) <= 6 * spread / math.sqrt(count) + mid ** 2 * (4 * grain / (0.09 * top) + 1e-5)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("cols", [40, 600, 20000])
+def test_rounded_rows_of_very_small_values(dtype, cols):
+    """Rows whose largest value lies on both sides of 3.7e-37, where 127 / m leaves fp32's range, down to its smallest
+    numbers: whole numbers up to 127 as for any other row, from the same fp32 operations on the row times 2^64."""
+    import numpy as np
+    g = torch.Generator(device="cuda")
+    tops = [1e-30, 8e-31, 1e-36, 3e-37, 1e-37, 2e-38, 1e-38, 1e-39] + [1e-42, 1e-44] * (dtype == F32)  # bf16 ends at 9.2e-41
+    x = fm._padded((len(tops), cols), dtype, "cuda")
+    x.copy_(torch.rand(len(tops), cols, generator=g, device="cuda") * 2 - 1)
+    x[:, 7] = 1.0
+    x.copy_(x.double() * torch.tensor(tops, dtype=torch.float64, device="cuda").unsqueeze(1))
+    q, s = fm.quantize_rows(x)
+    v = x.float().cpu().numpy()
+    top = np.abs(v).max(1, keepdims=True)
+    lift = np.where(top < np.float32(2.0) ** -100, np.float32(2.0) ** 64, np.float32(1)).astype(np.float32)
+    want = np.rint((v * lift) * (np.float32(1) / (top * lift) * np.float32(127)))
+    assert (top > 0).all() and want.dtype == np.float32
+    np.testing.assert_array_equal(q.cpu().numpy(), want.astype(np.int8))
+    np.testing.assert_array_equal(s.cpu().numpy(), (top / np.float32(127))[:, 0])
+    assert bool((q[:, 7] == 127).all())
