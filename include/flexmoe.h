@@ -451,9 +451,9 @@ int flexmoe_grouped_weight_grad(const flexmoe_grouped_desc *desc, int32_t R, con
  *   first (127 / m would leave fp32's range; scale[r] is still m / 127, itself a
  *   denormal below 1.5e-36).  A row of zeros has scale 0; a row with a NaN or an
  *   infinity has the scale NaN and zeros.  x [rows][ldx] (dtype; rows of
- *   whole 16-byte units), q [rows][ldq] int8 (ldq a multiple of 16; up to 7 values past the
- *   row are written as 0, inside its stride), strides of 0 = packed.  The rows
- *   of a weight matrix give its channels' scales.
+ *   whole 16-byte units), q [rows][ldq] int8 (ldq a multiple of 16; nothing past a row is
+ *   written), strides of 0 = packed.  The rows of a weight matrix give its
+ *   channels' scales.
  * flexmoe_quantized_forward: y_r[n] = q_scale[r] w_scale[e][n] sum_k q_r[k] W_e[n][k],
  *   the sum exact in 32-bit integers (K <= 131071).  q [R][ldx] and
  *   w [groups][N][ldw] int8, w_scale [groups][N]; y [R][ldy] of desc->dtype.

@@ -58,19 +58,28 @@ __device__ __forceinline__ uint32_t max_bits(const float (&v)[8], uint32_t m) {
     return m;
 }
 
-__device__ __forceinline__ void store_q(int8_t* q, const float (&v)[8], float inv) {
+// Whole numbers of 8 values, the first cols - at of which exist (kWhole: all).
+template <bool kWhole>
+__device__ __forceinline__ void store_q(int8_t* q, const float (&v)[8], float inv, int at, int cols) {
     uint32_t w[2] = {0, 0};
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const int n = (int)fminf(fmaxf(rintf(v[k] * inv), -127.f), 127.f);
         w[k >> 2] |= (uint32_t)(n & 255) << (8 * (k & 3));
     }
-    *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
+    if (kWhole || at + 8 <= cols) {
+        *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 7; ++k)
+            if (at + k < cols) q[k] = (int8_t)(w[k >> 2] >> (8 * (k & 3)));
+    }
 }
 
 // kWaves waves per row, kChunks 8-value chunks per lane in registers (0: read
-// again).
-template <bool kBf16, bool kGated, int kWaves, int kChunks>
+// again).  kWhole: rows of whole chunks (the test for the last one in every store
+// takes 2 % longer).
+template <bool kBf16, bool kGated, int kWaves, int kChunks, bool kWhole>
 __global__ __launch_bounds__(QT) void quantize_kernel(const void* x, const void* x2, size_t ldx, int8_t* q, size_t ldq, float* scale,
                                                       int rows, int cols) {
     constexpr int kLanes = 64 * kWaves, kRows = QT / kLanes;
@@ -120,7 +129,7 @@ __global__ __launch_bounds__(QT) void quantize_kernel(const void* x, const void*
                 if (!finite || low)
 #pragma unroll
                     for (int k = 0; k < 8; ++k) v[i][k] = finite ? v[i][k] * 0x1p+64f : 0.f;
-                store_q(qr + 8 * c, v[i], inv);
+                store_q<kWhole>(qr + 8 * c, v[i], inv, 8 * c, cols);
             }
         }
     } else {
@@ -129,26 +138,31 @@ __global__ __launch_bounds__(QT) void quantize_kernel(const void* x, const void*
             if (!finite || low)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[0][k] = finite ? v[0][k] * 0x1p+64f : 0.f;
-            store_q(qr + 8 * c, v[0], inv);
+            store_q<kWhole>(qr + 8 * c, v[0], inv, 8 * c, cols);
         }
     }
 }
 
-template <bool kBf16, bool kGated>
+template <bool kBf16, bool kGated, bool kWhole>
 void launch(const void* x, const void* x2, size_t ldx, int8_t* q, size_t ldq, float* scale, int rows, int cols, hipStream_t s) {
     const int by4 = (rows + 3) / 4;
     if (cols <= 512)
-        quantize_kernel<kBf16, kGated, 1, 1><<<by4, QT, 0, s>>>(x, x2, ldx, q, ldq, scale, rows, cols);
+        quantize_kernel<kBf16, kGated, 1, 1, kWhole><<<by4, QT, 0, s>>>(x, x2, ldx, q, ldq, scale, rows, cols);
     else if (rows >= kManyRows && cols <= 2048)
-        quantize_kernel<kBf16, kGated, 1, 4><<<by4, QT, 0, s>>>(x, x2, ldx, q, ldq, scale, rows, cols);
+        quantize_kernel<kBf16, kGated, 1, 4, kWhole><<<by4, QT, 0, s>>>(x, x2, ldx, q, ldq, scale, rows, cols);
     else if (cols <= 2048)
-        quantize_kernel<kBf16, kGated, 4, 1><<<rows, QT, 0, s>>>(x, x2, ldx, q, ldq, scale, rows, cols);
+        quantize_kernel<kBf16, kGated, 4, 1, kWhole><<<rows, QT, 0, s>>>(x, x2, ldx, q, ldq, scale, rows, cols);
     else if (cols <= 4096)
-        quantize_kernel<kBf16, kGated, 4, 2><<<rows, QT, 0, s>>>(x, x2, ldx, q, ldq, scale, rows, cols);
+        quantize_kernel<kBf16, kGated, 4, 2, kWhole><<<rows, QT, 0, s>>>(x, x2, ldx, q, ldq, scale, rows, cols);
     else if (cols <= 16384)
-        quantize_kernel<kBf16, kGated, 4, 8><<<rows, QT, 0, s>>>(x, x2, ldx, q, ldq, scale, rows, cols);
+        quantize_kernel<kBf16, kGated, 4, 8, kWhole><<<rows, QT, 0, s>>>(x, x2, ldx, q, ldq, scale, rows, cols);
     else
-        quantize_kernel<kBf16, kGated, 4, 0><<<rows, QT, 0, s>>>(x, x2, ldx, q, ldq, scale, rows, cols);
+        quantize_kernel<kBf16, kGated, 4, 0, kWhole><<<rows, QT, 0, s>>>(x, x2, ldx, q, ldq, scale, rows, cols);
+}
+template <bool kBf16, bool kGated>
+void launch(const void* x, const void* x2, size_t ldx, int8_t* q, size_t ldq, float* scale, int rows, int cols, hipStream_t s) {
+    if (cols % 8 == 0) launch<kBf16, kGated, true>(x, x2, ldx, q, ldq, scale, rows, cols, s);
+    else launch<kBf16, kGated, false>(x, x2, ldx, q, ldq, scale, rows, cols, s);
 }
 
 }  // namespace

@@ -209,3 +209,15 @@ def test_rounded_rows_of_very_small_values(dtype, cols):
     np.testing.assert_array_equal(q.cpu().numpy(), want.astype(np.int8))
     np.testing.assert_array_equal(s.cpu().numpy(), (top / np.float32(127))[:, 0])
     assert bool((q[:, 7] == 127).all())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 20), (5, 23), (4, 513), (1100, 601), (2, 4099), (2, 16391)])
+def test_rounded_rows_write_nothing_past_a_row(dtype, rows, cols):
+    """Into columns of a wider buffer: its other columns keep what they hold."""
+    g = torch.Generator(device="cuda")
+    x = fm._padded((rows, cols), dtype, "cuda")
+    x.copy_(torch.randn(rows, cols, generator=g, device="cuda"))
+    buf = torch.full((rows, (cols + 31) // 16 * 16), 55, dtype=I8, device="cuda")
+    q, _ = fm.quantize_rows(x, q=buf[:, :cols])
+    assert torch.equal(q, fm.quantize_rows(x)[0]) and bool((buf[:, cols:] == 55).all())
