@@ -491,10 +491,14 @@ def _dtype_code(dtype) -> int:
 
 def _matrix(t, shape, dtype, name):
     """Row stride of a [..., rows, cols] tensor whose rows are contiguous and follow each other at one distance."""
-    if t.dtype is dtype and t.shape == shape and t.is_cuda and shape[-2] > 1:
+    if t.dtype is dtype and t.shape == shape and t.is_cuda:
         st = t.stride()
-        if st[-1] == 1 and st[-2] >= shape[-1] and (len(st) == 2 or len(st) == 3 and st[0] == shape[1] * st[1]):
-            return st[-2]
+        if st[-1] == 1:
+            if shape[-2] > 1:
+                if st[-2] >= shape[-1] and (len(st) == 2 or len(st) == 3 and st[0] == shape[1] * st[1]):
+                    return st[-2]
+            elif len(st) == 2:  # one row, or none
+                return _pitch(shape[1], dtype.itemsize)
     return _matrix_checked(t, shape, dtype, name)
 
 
