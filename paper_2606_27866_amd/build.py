@@ -5,15 +5,19 @@
 The library is one shared object holding every kernel and the C ABI of
 include/flexmoe.h.  All device code is compiled with packed-fp32 arithmetic
 disabled (-packed-fp32-ops); hipcc's host pass warns that it does not know
-the feature, which is harmless.  _tensors.so (host code, g++) reads lists of
-tensors for the binding.
+the feature, which is harmless.  _tensors.so (host code, g++ and torch's C++
+headers) reads lists of tensors for the binding's optimizer; without them the
+library is built all the same.
 """
 from __future__ import annotations
 
 import glob
+import importlib.util
 import os
+import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -40,9 +44,17 @@ def compile_command(out: str, extra=()):
             "-I", os.path.join(ROOT, "include"), "-o", out, *extra, *sources()]
 
 
-def tensors_command(out: str):
-    import sysconfig
+def tensors_missing() -> str:
+    """What _tensors.so needs and this machine does not have; empty if nothing."""
+    torch = importlib.util.find_spec("torch")
+    needs = {"g++": shutil.which("g++"), "torch": torch,
+             "torch's C++ headers": torch and os.path.exists(os.path.join(os.path.dirname(torch.origin), "include", "torch", "csrc",
+                                                                          "autograd", "python_variable.h")),
+             "Python.h": os.path.exists(os.path.join(sysconfig.get_path("include"), "Python.h"))}
+    return ", ".join(name for name, found in needs.items() if not found)
 
+
+def tensors_command(out: str):
     import torch
     from torch.utils.cpp_extension import include_paths
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
@@ -59,7 +71,16 @@ def build_tensors() -> str:
 
 
 def build(verbose: bool = False) -> str:
-    build_tensors()
+    build_library(verbose)
+    missing = tensors_missing()
+    if missing:
+        sys.stderr.write("without _tensors.so, which the optimizer needs: no %s here\n" % missing)
+    else:
+        build_tensors()
+    return LIB
+
+
+def build_library(verbose: bool = False) -> str:
     tmp = LIB + ".tmp%d" % os.getpid()
     cmd = compile_command(tmp)
     if verbose:
@@ -77,11 +98,10 @@ def build(verbose: bool = False) -> str:
 
 
 def is_stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(TENSORS):
-        return True
-    t = os.path.getmtime(LIB)
-    return (any(os.path.getmtime(f) > t for f in sources() + headers())
-            or os.path.getmtime(TENSORS_SRC) > os.path.getmtime(TENSORS))
+    def older(out, files):
+        return not os.path.exists(out) or any(os.path.getmtime(f) > os.path.getmtime(out) for f in files)
+
+    return older(LIB, sources() + headers()) or not tensors_missing() and older(TENSORS, [TENSORS_SRC])
 
 
 if __name__ == "__main__":

@@ -199,7 +199,7 @@ def tensors():
     global _tensors
     if _tensors is None:
         if not os.path.exists(TENSORS):
-            raise RuntimeError("_tensors.so is not built (%s); run `python -m paper_2606_27866_amd.build`" % TENSORS)
+            raise RuntimeError("_tensors.so, which the optimizer needs, is not built (%s); run `python -m paper_2606_27866_amd.build`" % TENSORS)
         import torch  # noqa: F401  (its libraries are loaded first)
         from . import _tensors as module
         _tensors = module
