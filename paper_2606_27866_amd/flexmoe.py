@@ -533,13 +533,24 @@ def _pitch(cols, element_size) -> int:
     return -(-cols // unit) * unit
 
 
-def _padded(shape, dtype, device):
-    """A new tensor of `shape` whose rows start on 16-byte boundaries (a view of wider rows where they must)."""
+def _new(shape, dtype, device, stream=None):
+    """A new tensor, made on the stream that will write it: memory of torch's current stream may still be in use there, and
+    is used again there as soon as the tensor is dropped."""
     import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _padded(shape, dtype, device, stream=None):
+    """A new tensor of `shape` whose rows start on 16-byte boundaries (a view of wider rows where they must)."""
     cols = _pitch(shape[-1], dtype.itemsize)
     if cols == shape[-1]:
-        return torch.empty(shape, dtype=dtype, device=device)
-    return torch.empty((*shape[:-1], cols), dtype=dtype, device=device)[..., :shape[-1]]
+        return _new(shape, dtype, device, stream)
+    return _new((*shape[:-1], cols), dtype, device, stream)[..., :shape[-1]]
 
 
 def _vector(t, n, dtype, name):
@@ -579,7 +590,7 @@ class GroupedProduct:
         """y_r = x_r W_e^T for x [R, K], w [groups, N, K]."""
         R, d, dt = x.shape[0], self.desc, self.dtype
         if y is None:
-            y = _padded((R, self.N), dt, x.device)
+            y = _padded((R, self.N), dt, x.device, stream)
         with self._lock:
             d.ldx, d.ldw = _matrix(x, (R, self.K), dt, "x"), _matrix(w, self._w_shape, dt, "w")
             d.ldy = _matrix(y, (R, self.N), dt, "y")
@@ -591,7 +602,7 @@ class GroupedProduct:
         """dx_r = dy_r W_e for dy [R, N]."""
         R, d, dt = dy.shape[0], self.desc, self.dtype
         if dx is None:
-            dx = _padded((R, self.K), dt, dy.device)
+            dx = _padded((R, self.K), dt, dy.device, stream)
         with self._lock:
             d.ldy, d.ldw = _matrix(dy, (R, self.N), dt, "dy"), _matrix(w, self._w_shape, dt, "w")
             d.ldx = _matrix(dx, (R, self.K), dt, "dx")
@@ -605,7 +616,7 @@ class GroupedProduct:
         if dw is None:
             if accumulate:
                 raise ValueError("accumulate needs dw")
-            dw = _padded(self._w_shape, self._f32 if dw_dtype is None else dw_dtype, dy.device)
+            dw = _padded(self._w_shape, self._f32 if dw_dtype is None else dw_dtype, dy.device, stream)
         elif dw_dtype is not None and dw.dtype != dw_dtype:
             raise ValueError("dw is %s, not %s" % (dw.dtype, dw_dtype))
         with self._lock:
@@ -629,9 +640,9 @@ def quantize_rows(x, gate=None, q=None, scale=None, stream=None):
     if gate is not None and _matrix(gate, shape, x.dtype, "gate") != ldx:
         raise ValueError("x and gate must have the same strides")
     if q is None:
-        q = _padded(shape, torch.int8, x.device)
+        q = _padded(shape, torch.int8, x.device, stream)
     if scale is None:
-        scale = torch.empty(shape[:-1], dtype=torch.float32, device=x.device)
+        scale = _new(shape[:-1], torch.float32, x.device, stream)
     _check(lib().flexmoe_quantize_rows(rows, cols, _dtype_code(x.dtype), x.data_ptr(), None if gate is None else gate.data_ptr(), ldx,
                                        q.data_ptr(), _matrix(q, shape, torch.int8, "q"), _vector(scale, rows, torch.float32, "scale"),
                                        _stream(stream)))
@@ -674,7 +685,6 @@ class Int8Product:
         R = x.shape[0]
         if x.shape != (R, self.K) or R > self.max_rows:
             raise ValueError("x must be [R, %d] with at most %d rows, got %s" % (self.K, self.max_rows, tuple(x.shape)))
-        stream = _stream(stream)
         ldx = _matrix(x, x.shape, x.dtype, "x")
         if gate is not None and _matrix(gate, x.shape, x.dtype, "gate") != ldx:
             raise ValueError("x and gate must have the same strides")
@@ -682,7 +692,7 @@ class Int8Product:
         ldq = self.q.stride(0) if self.max_rows > 1 else _pitch(self.K, 1)
         with self._lock:
             _check(lib().flexmoe_quantize_rows(R, self.K, _dtype_code(x.dtype), x.data_ptr(), None if gate is None else gate.data_ptr(), ldx,
-                                               q, ldq, scale, stream))
+                                               q, ldq, scale, _stream(stream)))
             d.ldx = ldq
             return self._product(R, q, scale, offsets, keep, y, x.device, stream)
 
@@ -690,7 +700,7 @@ class Int8Product:
         R = q.shape[0]
         with self._lock:
             self.desc.ldx = _matrix(q, (R, self.K), self._i8, "q")
-            return self._product(R, q.data_ptr(), _vector(q_scale, R, self._f32, "q_scale"), offsets, keep, y, q.device, _stream(stream))
+            return self._product(R, q.data_ptr(), _vector(q_scale, R, self._f32, "q_scale"), offsets, keep, y, q.device, stream)
 
     def _product(self, R, q, q_scale, offsets, keep, y, device, stream):
         if offsets is None:
@@ -700,11 +710,11 @@ class Int8Product:
         else:
             offsets = _vector(offsets, self.groups + 1, self._i32, "offsets")
         if y is None:
-            y = _padded((R, self.N), self.out_dtype, device)
+            y = _padded((R, self.N), self.out_dtype, device, stream)
         self.desc.ldy = _matrix(y, (R, self.N), self.out_dtype, "y")
         _check(lib().flexmoe_quantized_forward(self._desc, R, q, q_scale, self.w.data_ptr(), self.w_scale.data_ptr(), offsets,
                                                None if keep is None else _vector(keep, self.groups, self._i32, "keep"),
-                                               y.data_ptr(), *self._ws, stream))
+                                               y.data_ptr(), *self._ws, _stream(stream)))
         return y
 
 
@@ -809,7 +819,7 @@ def adamw_state_values(m, v, m_scale, v_scale, dtype=None, stream=None):
     """What 8-bit states stand for: (m, v) as fp32 or bf16."""
     import torch
     dtype = torch.float32 if dtype is None else dtype
-    mo, vo = torch.empty(m.numel(), dtype=dtype, device=m.device), torch.empty(m.numel(), dtype=dtype, device=m.device)
+    mo, vo = (_new(m.numel(), dtype, m.device, stream) for _ in range(2))
     blocks = -(-m.numel() // STATE_BLOCK)
     flexmoe_adamw_read_state(m.numel(), _vector(m, m.numel(), torch.uint8, "m"), _vector(v, m.numel(), torch.uint8, "v"),
                              _vector(m_scale, blocks, torch.float32, "m_scale"), _vector(v_scale, blocks, torch.float32, "v_scale"),

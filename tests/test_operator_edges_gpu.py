@@ -221,3 +221,31 @@ def test_rounded_rows_write_nothing_past_a_row(dtype, rows, cols):
     buf = torch.full((rows, (cols + 31) // 16 * 16), 55, dtype=I8, device="cuda")
     q, _ = fm.quantize_rows(x, q=buf[:, :cols])
     assert torch.equal(q, fm.quantize_rows(x)[0]) and bool((buf[:, cols:] == 55).all())
+
+
+def stream_of(t):
+    """The stream in whose pool torch's allocator keeps t's memory."""
+    for seg in torch.cuda.memory_snapshot():
+        if seg["address"] <= t.data_ptr() < seg["address"] + seg["total_size"]:
+            return seg["stream"]
+    raise AssertionError("no segment holds the tensor")
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_outputs_are_made_on_the_stream_that_writes_them(raw):
+    """Memory of the current stream's pool can be in use there while another stream writes it."""
+    E, N, K, R = 2, 24, 40, 6
+    side = torch.cuda.Stream()
+    s = side.cuda_stream if raw else side
+    x, dy, w = (torch.ones(shape, device="cuda") for shape in ((R, K), (R, N), (E, N, K)))
+    offsets = torch.tensor([0, 2, 6], dtype=torch.int32, device="cuda")
+    op, q8 = fm.GroupedProduct(E, N, K, R, F32), fm.Int8Product.from_weights(w, R)
+    opt = fm.AdamW([torch.zeros(300, device="cuda")], state_bits=8)
+    side.wait_stream(torch.cuda.current_stream())
+    made = [op.forward(x, w, offsets, stream=s), op.input_grad(dy, w, offsets, stream=s), op.weight_grad(dy, x, offsets, stream=s),
+            q8(x, offsets, stream=s), *fm.quantize_rows(x, stream=s),
+            *fm.adamw_state_values(opt.m[0], opt.v[0], opt.m_scale[0], opt.v_scale[0], stream=s)]
+    made.append(q8.product(*made[4:6], offsets, stream=s))
+    side.synchronize()
+    assert [stream_of(t) for t in made] == [side.cuda_stream] * len(made)
+    assert bool((made[0] == K).all()) and stream_of(op.forward(x, w, offsets)) == torch.cuda.current_stream().cuda_stream
