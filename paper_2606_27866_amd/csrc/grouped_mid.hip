@@ -260,6 +260,14 @@ __global__ __launch_bounds__(256) void grouped_join_kernel(GroupedParams p, int 
         const size_t r = i / runs;
         const int c = (int)(i - r * runs) * 4;
         if (kRowGroups && ((int)r < first || (int)r >= end)) continue;
+        int stop = cols;
+        if (!kRowGroups && p.accumulate && p.keep) {
+            // what lies past a width is left as it is, to the sign of a zero
+            const int e = (int)(r / p.N), w = group_width(p, e, p.keep_axis == 1 ? p.N : p.K);
+            if (p.keep_axis == 1 && (int)(r - (size_t)e * p.N) >= w) continue;
+            if (p.keep_axis == 2) stop = min(cols, w);
+            if (c >= stop) continue;
+        }
         const char* src = reinterpret_cast<const char*>(p.partial) + (r * ldp + c) * 4;
         floatx4 v{0.f, 0.f, 0.f, 0.f};
         if constexpr (kI8) {
@@ -281,8 +289,8 @@ __global__ __launch_bounds__(256) void grouped_join_kernel(GroupedParams p, int 
             for (int k = 0; k < p.splits; ++k) v += *reinterpret_cast<const floatx4*>(src + (size_t)k * rows * ldp * 4);
         }
         char* const crow = reinterpret_cast<char*>(p.c) + r * p.ldc * (kBf16Out ? 2 : 4);
-        if (!kRowGroups && p.accumulate) v += load_run<kBf16Out>(crow, c, cols);
-        store_run<kBf16Out>(crow, c, cols, v);
+        if (!kRowGroups && p.accumulate) v += load_run<kBf16Out>(crow, c, stop);
+        store_run<kBf16Out>(crow, c, stop, v);
     }
 }
 

@@ -249,3 +249,31 @@ def test_outputs_are_made_on_the_stream_that_writes_them(raw):
     side.synchronize()
     assert [stream_of(t) for t in made] == [side.cuda_stream] * len(made)
     assert bool((made[0] == K).all()) and stream_of(op.forward(x, w, offsets)) == torch.cuda.current_stream().cuda_stream
+
+
+@pytest.mark.parametrize("axis", ["N", "K"])
+@pytest.mark.parametrize("result", [BF, F32])
+@pytest.mark.parametrize("R", [40, 4000])
+def test_an_added_gradient_leaves_what_lies_past_a_width(axis, result, R):
+    """Bit for bit, the sign of a zero too, with the reduction in one part and in several (R = 4000)."""
+    E, N, K = 2, 45, 50
+    g = torch.Generator(device="cuda")
+    x, dy = fm._padded((R, K), BF, "cuda"), fm._padded((R, N), BF, "cuda")
+    x.copy_(torch.randn(R, K, generator=g, device="cuda"))
+    dy.copy_(torch.randn(R, N, generator=g, device="cuda"))
+    offsets = torch.tensor([0, R // 3, R], dtype=torch.int32, device="cuda")
+    keep = torch.tensor([0, 17], dtype=torch.int32, device="cuda")
+    op = fm.GroupedProduct(E, N, K, R, BF, axis)
+    dw = fm._padded((E, N, K), result, "cuda")
+    dw.fill_(-0.0)
+    dw[:, ::3] = float("nan")
+    bits = {BF: torch.int16, F32: torch.int32}[result]
+    before = dw.clone()
+    op.weight_grad(dy, x, offsets, keep, dw=dw, accumulate=True)
+    past = torch.ones(E, N, K, dtype=torch.bool, device="cuda")
+    if axis == "N":
+        past[1, :17] = False
+    else:
+        past[1, :, :17] = False
+    assert torch.equal(dw.contiguous().view(bits)[past], before.contiguous().view(bits)[past])
+    assert not torch.equal(dw.contiguous().view(bits)[~past], before.contiguous().view(bits)[~past])
