@@ -453,7 +453,10 @@ int flexmoe_grouped_weight_grad(const flexmoe_grouped_desc *desc, int32_t R, con
  *   infinity has the scale NaN and zeros.  x [rows][ldx] (dtype; rows of
  *   whole 16-byte units), q [rows][ldq] int8 (ldq a multiple of 16; nothing past a row is
  *   written), strides of 0 = packed.  The rows of a weight matrix give its
- *   channels' scales.
+ *   channels' scales.  A row's scale is that of the whole row: it knows no keep
+ *   counts, so that for a product under FLEXMOE_KEEP_K what lies past a width
+ *   should be zeros, as the products write it (a large value there coarsens what
+ *   is kept, a NaN makes the row NaN).
  * flexmoe_quantized_forward: y_r[n] = q_scale[r] w_scale[e][n] sum_k q_r[k] W_e[n][k],
  *   the sum exact in 32-bit integers (K <= 131071).  q [R][ldx] and
  *   w [groups][N][ldw] int8, w_scale [groups][N]; y [R][ldy] of desc->dtype.

@@ -681,7 +681,11 @@ class Int8Product:
         return cls(*quantize_rows(w), max_rows, keep_axis, out_dtype)
 
     def __call__(self, x, offsets=None, keep=None, gate=None, y=None, stream=None):
-        """x [R, K] bf16 or fp32 (with gate: silu(gate) * x); offsets may be left out for one group."""
+        """x [R, K] bf16 or fp32 (with gate: silu(gate) * x); offsets may be left out for one group.
+
+        A row's scale is that of its whole length: with keep_axis "K" what lies past a width should be zeros, as the
+        products write it.
+        """
         R = x.shape[0]
         if x.shape != (R, self.K) or R > self.max_rows:
             raise ValueError("x must be [R, %d] with at most %d rows, got %s" % (self.K, self.max_rows, tuple(x.shape)))
