@@ -20,11 +20,14 @@
 // Across halves are read through the transposing LDS reads, whose wait is part
 // of the read: there the requests go out first.
 //
-// Bound by the matrix cores at the card's power limit: 8192^3 in bf16 1500 (x
-// W^T), 1398 (dy W at 2048 columns), 1296 TFLOP/s (dy^T x), where the vendor's
-// library reaches 1615 (x W^T) in the same run; 8192^3 in int8, with the
-// rounding of the rows, 2610 TOP/s (library, without, 2490).  Another card, 1377
-// (x W^T), with runs of 32 tiles per XCD instead of 8: 1150.
+// The order of all waves' accesses to LDS is that of mfma_pingpong.h's loop; both
+// are checked on the host from their own text.
+//
+// Bound by the matrix cores at the card's power limit: 8192^3 in bf16 1519 (x
+// W^T), 1454 (dy W at 2048 columns), 1345 TFLOP/s (dy^T x), where the vendor's
+// library reaches 1574 to 1600 (x W^T) in the same run; 8192^3 in int8, with the
+// rounding of the rows, 2555 TOP/s.  Another card, 1377 (x W^T), with runs of 32
+// tiles per XCD instead of 8: 1150.
 #include "grouped.h"
 
 namespace flexmoe {
