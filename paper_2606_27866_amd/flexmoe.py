@@ -842,6 +842,12 @@ class ClippedWeights:
         self.keep_dev = keep_dev
 
 
+def _packed(t, n, name):
+    """The layer's calls take addresses alone: t must hold n values one after another (an expanded gradient holds fewer)."""
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s must be %d contiguous values, got %s with strides %s" % (name, n, tuple(t.shape), t.stride()))
+
+
 class Layer:
     """Device-resident masked MoE layer: weights, keep table, workspace.
 
@@ -887,6 +893,10 @@ class Layer:
         T = x.shape[0]
         if y is None:
             y = torch.empty((T, self.desc.d), dtype=self.tdtype, device=self.device)
+        D = self.desc
+        _packed(x, T * D.d, "x")
+        _packed(logits, T * D.E, "logits")
+        _packed(y, T * D.d, "y")
         if bucketed is not None:
             flexmoe_layer_forward_bucketed(self.desc, T, x, logits, self.w_gate, self.w_up, self.w_down,
                                            bucketed[0], bucketed[1], self.ws_gate, self.ws_up,
@@ -927,8 +937,11 @@ class Saliency:
                                       None, None, self.w_down_t, None, None, None)
 
     def add_batch(self, x, logits, y_target, scale=1.0, stream=None):
-        L = self.layer
-        flexmoe_channel_saliency(self.desc, x.shape[0], x, logits, L.w_gate, L.w_up, L.w_down, self.w_down_t,
+        L, T = self.layer, x.shape[0]
+        _packed(x, T * self.desc.d, "x")
+        _packed(logits, T * self.desc.E, "logits")
+        _packed(y_target, T * self.desc.d, "y_target")
+        flexmoe_channel_saliency(self.desc, T, x, logits, L.w_gate, L.w_up, L.w_down, self.w_down_t,
                                  L.ws_gate, L.ws_up, L.ws_down, y_target, scale, self.scores, self.workspace,
                                  stream=stream)
 
@@ -980,6 +993,8 @@ class ActionLearner:
                                   *self.wt, *self.wst, stream=stream)
 
     def sample(self, alpha, gumbel, stream=None):
+        _packed(alpha, self.desc.E * self.actions.K, "alpha")
+        _packed(gumbel, self.desc.E * self.actions.K, "gumbel")
         flexmoe_sample_actions(self.desc, self.actions, alpha, gumbel, self.keep, self.action, stream=stream)
 
     def forward(self, x, logits, y=None, keep=None, stream=None):
@@ -988,6 +1003,9 @@ class ActionLearner:
         self.T = x.shape[0]
         if y is None:
             y = torch.empty((self.T, self.desc.d), dtype=L.tdtype, device=L.device)
+        _packed(x, self.T * self.desc.d, "x")
+        _packed(logits, self.T * self.desc.E, "logits")
+        _packed(y, self.T * self.desc.d, "y")
         flexmoe_train_forward(self.desc, self.T, x, logits, L.w_gate, L.w_up, L.w_down,
                               self.keep if keep is None else keep, L.ws_gate, L.ws_up, L.ws_down, y,
                               self.workspace, stream=stream)
@@ -996,6 +1014,8 @@ class ActionLearner:
     def backward(self, logits, dy, stream=None):
         import torch
         D, dev = self.desc, self.layer.device
+        _packed(logits, self.T * D.E, "logits")
+        _packed(dy, self.T * D.d, "dy")
         dx = torch.empty((self.T, D.d), dtype=torch.float32, device=dev)
         dl = torch.empty((self.T, D.E), dtype=torch.float32, device=dev)
         dm = torch.empty((D.E, D.I), dtype=torch.float32, device=dev)
@@ -1005,6 +1025,9 @@ class ActionLearner:
 
     def action_grad(self, alpha, gumbel, tau, lambda_cost, beta, dmask, stream=None):
         import torch
+        _packed(alpha, self.desc.E * self.actions.K, "alpha")
+        _packed(gumbel, self.desc.E * self.actions.K, "gumbel")
+        _packed(dmask, self.desc.E * self.desc.I, "dmask")
         dalpha = torch.empty_like(alpha)
         stats = torch.empty((2,), dtype=torch.float32, device=alpha.device)
         flexmoe_action_grad(self.desc, self.T, self.actions, alpha, gumbel, tau, lambda_cost, beta, dmask, dalpha,

@@ -346,3 +346,32 @@ def test_threads_that_share_an_optimizer_keep_their_gradients(steps, recorder):
     recorder.flexmoe_adamw_step = slow
     assert not both(lambda: call(one), lambda: call(two))
     assert len(steps) == opt.t == 60
+
+
+def test_layer_holders_refuse_what_is_not_packed(request):
+    """The layer's calls take addresses alone: an expanded gradient, a transposed batch or one row too few would be read past
+    its end or in the wrong places."""
+    d, E, I, T, K = 16, 4, 24, 6, 3
+    layer = fm.Layer(d, E, I, 2, max_tokens=T, device="cpu")
+    layer.set_weights(torch.zeros(E, I, d, dtype=BF), torch.zeros(E, I, d, dtype=BF), torch.zeros(E, d, I, dtype=BF))
+    sal = fm.Saliency(layer, T, transpose_once=False)
+    act = fm.ActionLearner(layer, T, [0.5, 0.75, 1.0])
+    recorder = request.getfixturevalue("recorder")
+    x, logits, y = torch.zeros(T, d, dtype=BF), torch.zeros(T, E), torch.zeros(T, d, dtype=BF)
+    dy, alpha, mask = torch.zeros(T, d), torch.zeros(E, K), torch.zeros(E, I)
+    act.T = T
+    good = {"forward": (layer.forward, [x, logits, y]), "saliency": (sal.add_batch, [x, logits, y]), "train": (act.forward, [x, logits, y]),
+            "backward": (act.backward, [logits, dy]), "sample": (act.sample, [alpha, alpha]),
+            "action_grad": (act.action_grad, [alpha, alpha, 1.0, 0.1, 0.0, mask])}
+    for f, args in good.values():
+        f(*args, stream=0)
+    calls = len(recorder.calls)
+    assert calls == len(good)
+    for f, args in good.values():
+        for i, t in enumerate(args):
+            if not isinstance(t, torch.Tensor):
+                continue
+            for bad in (t[:1].expand(t.shape), t.T.contiguous().T, torch.cat([t, t], 1)[:, :t.shape[1]], t[:, 1:].contiguous()):
+                with pytest.raises(ValueError):
+                    f(*args[:i], bad, *args[i + 1:], stream=0)
+    assert len(recorder.calls) == calls
