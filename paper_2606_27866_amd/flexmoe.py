@@ -537,7 +537,7 @@ def _new(shape, dtype, device, stream=None):
     """A new tensor, made on the stream that will write it: memory of torch's current stream may still be in use there, and
     is used again there as soon as the tensor is dropped."""
     import torch
-    if stream is None:
+    if stream is None or torch.device(device).type == "cpu":
         return torch.empty(shape, dtype=dtype, device=device)
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
@@ -878,8 +878,7 @@ class Layer:
         """Pack the current ranked weights for the budget keep_host."""
         import torch
         P = flexmoe_clipped_channels(self.desc, keep_host)
-        bufs = [torch.empty((max(P, 1) * self.desc.d,), dtype=self.tdtype, device=self.device)
-                for _ in range(3)]
+        bufs = [_new((max(P, 1) * self.desc.d,), self.tdtype, self.device, stream) for _ in range(3)]
         flexmoe_export_clipped(self.desc, keep_host, self.w_gate, self.w_up, self.w_down, *bufs,
                                stream=stream)
         keep_dev = torch.from_numpy(np.asarray(keep_host, dtype=np.int32).copy()).to(self.device)
@@ -889,10 +888,9 @@ class Layer:
                 bucketed=None):
         """clipped: a ClippedWeights of this layer -> the offline-clipped path;
         bucketed: (keep_host, k_align) -> the bucketed ablation."""
-        import torch
         T = x.shape[0]
         if y is None:
-            y = torch.empty((T, self.desc.d), dtype=self.tdtype, device=self.device)
+            y = _new((T, self.desc.d), self.tdtype, self.device, stream)
         D = self.desc
         _packed(x, T * D.d, "x")
         _packed(logits, T * D.E, "logits")
@@ -949,8 +947,8 @@ class Saliency:
         """Ranked copies of the layer's weights and the permutation (Eq. 3)."""
         import torch
         L = self.layer
-        out = [torch.empty_like(w) for w in (L.w_gate, L.w_up, L.w_down)]
-        perm = torch.empty((L.desc.E, L.desc.I), dtype=torch.int32, device=L.device)
+        out = [_new(w.shape, w.dtype, w.device, stream) for w in (L.w_gate, L.w_up, L.w_down)]
+        perm = _new((L.desc.E, L.desc.I), torch.int32, L.device, stream)
         flexmoe_rank_reorder(L.desc, self.scores, L.w_gate, L.w_up, L.w_down, *out, perm, stream=stream)
         return (*out, perm)
 
@@ -998,11 +996,10 @@ class ActionLearner:
         flexmoe_sample_actions(self.desc, self.actions, alpha, gumbel, self.keep, self.action, stream=stream)
 
     def forward(self, x, logits, y=None, keep=None, stream=None):
-        import torch
         L = self.layer
         self.T = x.shape[0]
         if y is None:
-            y = torch.empty((self.T, self.desc.d), dtype=L.tdtype, device=L.device)
+            y = _new((self.T, self.desc.d), L.tdtype, L.device, stream)
         _packed(x, self.T * self.desc.d, "x")
         _packed(logits, self.T * self.desc.E, "logits")
         _packed(y, self.T * self.desc.d, "y")
@@ -1016,9 +1013,7 @@ class ActionLearner:
         D, dev = self.desc, self.layer.device
         _packed(logits, self.T * D.E, "logits")
         _packed(dy, self.T * D.d, "dy")
-        dx = torch.empty((self.T, D.d), dtype=torch.float32, device=dev)
-        dl = torch.empty((self.T, D.E), dtype=torch.float32, device=dev)
-        dm = torch.empty((D.E, D.I), dtype=torch.float32, device=dev)
+        dx, dl, dm = (_new(shape, torch.float32, dev, stream) for shape in ((self.T, D.d), (self.T, D.E), (D.E, D.I)))
         flexmoe_train_backward(D, self.T, logits, dy, *self.wt, *self.wst, dx, dl, dm, self.workspace,
                                stream=stream)
         return dx, dl, dm
@@ -1028,8 +1023,8 @@ class ActionLearner:
         _packed(alpha, self.desc.E * self.actions.K, "alpha")
         _packed(gumbel, self.desc.E * self.actions.K, "gumbel")
         _packed(dmask, self.desc.E * self.desc.I, "dmask")
-        dalpha = torch.empty_like(alpha)
-        stats = torch.empty((2,), dtype=torch.float32, device=alpha.device)
+        dalpha = _new(alpha.shape, alpha.dtype, alpha.device, stream)
+        stats = _new((2,), torch.float32, alpha.device, stream)
         flexmoe_action_grad(self.desc, self.T, self.actions, alpha, gumbel, tau, lambda_cost, beta, dmask, dalpha,
                             stats, self.workspace, stream=stream)
         return dalpha, stats

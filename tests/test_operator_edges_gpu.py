@@ -277,3 +277,33 @@ def test_an_added_gradient_leaves_what_lies_past_a_width(axis, result, R):
         past[1, :, :17] = False
     assert torch.equal(dw.contiguous().view(bits)[past], before.contiguous().view(bits)[past])
     assert not torch.equal(dw.contiguous().view(bits)[~past], before.contiguous().view(bits)[~past])
+
+
+def test_outputs_of_the_layer_are_made_on_the_stream_that_writes_them():
+    d, E, I, T = 64, 4, 48, 10
+    g = torch.Generator(device="cuda")
+
+    def normal(*shape, dtype=BF):
+        return (torch.randn(shape, generator=g, device="cuda") * 0.1).to(dtype)
+
+    side = torch.cuda.Stream()
+    layer = fm.Layer(d, E, I, 2, max_tokens=T)
+    layer.set_weights(normal(E, I, d), normal(E, I, d), normal(E, d, I))
+    layer.set_budget([I, 7, 20, 40])
+    x, logits, dy = normal(T, d), normal(T, E, dtype=F32), normal(T, d, dtype=F32)
+    want = layer.forward(x, logits)
+    act, sal = fm.ActionLearner(layer, T, [0.5, 1.0]), fm.Saliency(layer, T)
+    act.transpose_weights()
+    alpha, gumbel = normal(E, 2, dtype=F32), normal(E, 2, dtype=F32)
+    side.wait_stream(torch.cuda.current_stream())
+    sal.add_batch(x, logits, dy, stream=side)
+    act.sample(alpha, gumbel, stream=side)
+    made = [layer.forward(x, logits, stream=side), act.forward(x, logits, stream=side)]
+    made += act.backward(logits, dy, stream=side)
+    made += act.action_grad(alpha, gumbel, 1.0, 0.1, 0.0, made[-1], stream=side)
+    made += sal.rank_reorder(stream=side)
+    c = layer.export_clipped([I, 7, 20, 40], stream=side)
+    made += [c.w_gate_c, c.w_up_c, c.w_down_c]
+    side.synchronize()
+    assert [stream_of(t) for t in made] == [side.cuda_stream] * len(made)
+    assert torch.equal(made[0], want)
