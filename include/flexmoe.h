@@ -527,6 +527,98 @@ int flexmoe_adamw_read_state(int64_t n, const void *m, const void *v, const floa
                              const float *v_scale, int32_t dtype, void *m_out, void *v_out,
                              void *stream);
 
+/* ---- Routing with scores, a bias and groups --------------------------------
+ * flexmoe_route, for T tokens' logits l [T][ldl] over E experts:
+ *   s = softmax(l) or sigmoid(l), c = s + bias (bias [E] fp32, or NULL)
+ *   groups > 1: experts lie in `groups` groups of E / groups one after another;
+ *   a group's score is the sum of its group_best (1 or 2) largest c, and the
+ *   top_groups best groups stay
+ *   topk_idx: the top_k largest c of the experts that stay, largest first
+ *   topk_w = scale s, divided by the sum of the chosen s with normalize
+ * Ties go to the lower id (of groups too), NaN comes last.  The order is that of
+ * the exact values: of the logits where no bias and no sum decides, else of c in
+ * 64 bits.  An expert with a logit or a bias of -inf is masked: it is never
+ * chosen and has no part in its group's score.  Where no expert is left a slot
+ * gets the id -1, the weight 0, the position -1 and no row; a token of nothing
+ * but -inf (padding) goes nowhere.  A softmax row with a NaN has NaN weights.
+ * With a bias the choice follows c alone: a balance step that raises the bias of
+ * experts with few `counts` and lowers it for others acts on no weight.
+ * out (device pointers): topk_idx and topk_w; counts, offsets, perm and pos, all
+ * or none, as a forward's routing copies hold them for a layer whose experts all
+ * keep channels, but that perm is -1 from offsets[E] on.
+ * flexmoe_route_backward: dlogits [T][lddl] from dw [T][top_k], the gradient of
+ * topk_w, with logits and topk_idx as they were; written in full.  The choice
+ * has no gradient, nor has the bias.  With g = scale dw: softmax s (g - sum g s),
+ * sigmoid g s (1 - s); normalised w (g - sum g w) over the chosen alone, times
+ * (1 - s) for sigmoid, w before its scale.
+ * logits and dlogits are of dtype, aligned to their elements.  Shapes
+ * (FLEXMOE_ESHAPE otherwise): 1 <= E <= 256, 1 <= top_k <= min(E, 16), groups at
+ * most 64 and dividing E, top_k <= top_groups E / groups; strides (elements, 0 =
+ * packed) from E to 2^21; 0 <= T <= max_tokens, max_tokens (top_k + 1) <= 2^30.
+ * The workspace (256-byte aligned; flexmoe_route_workspace_bytes, the same for
+ * every T) is needed for the tables of more than a few tokens. */
+enum { FLEXMOE_SOFTMAX = 0, FLEXMOE_SIGMOID = 1 };
+typedef struct flexmoe_router_desc {
+    int32_t E, top_k;
+    int32_t score;      /* FLEXMOE_SOFTMAX or FLEXMOE_SIGMOID                    */
+    int32_t normalize;
+    int32_t groups, top_groups, group_best;  /* 1, 1, 1: no groups              */
+    int32_t dtype;      /* flexmoe_dtype of logits and dlogits                   */
+    int32_t max_tokens;
+    int32_t ldl;
+    float scale;
+} flexmoe_router_desc;
+size_t flexmoe_route_workspace_bytes(const flexmoe_router_desc *desc, int32_t T);
+int flexmoe_route(const flexmoe_router_desc *desc, int32_t T, const void *logits,
+                  const float *bias, const flexmoe_route_out *out, void *workspace,
+                  size_t workspace_bytes, void *stream);
+int flexmoe_route_backward(const flexmoe_router_desc *desc, int32_t T, const void *logits,
+                           const int32_t *topk_idx, const float *dw, void *dlogits, int64_t lddl,
+                           void *stream);
+
+/* ---- Root-mean-square norm ------------------------------------------------
+ * flexmoe_rms_norm, for rows of `cols` values:
+ *   r = x + residual, rounded to dtype (without a residual: r = x, r is NULL)
+ *   y = r / sqrt(mean(r^2) + eps) * w, in fp32, rounded once
+ *   q, scale: that y before its rounding, as flexmoe_quantize_rows rounds rows
+ *   to 8 bits (what flexmoe_quantized_forward takes)
+ * y or q and scale may be NULL (not all of them), rstd too: rstd [rows] is
+ * 1 / sqrt(mean(r^2) + eps), which the backward takes.  Sums are in fp32; rows
+ * whose squares leave its range are summed from values 2^80 smaller.
+ *   x [rows][ldx], residual [rows][ldres], r [rows][ldr], y [rows][ldy] (dtype),
+ *   q [rows][ldq] int8, w [cols] (w_dtype), scale, rstd [rows] fp32
+ * r may be residual or x itself (the residual stream kept in place); y is a
+ * buffer of its own (FLEXMOE_EINVAL).
+ * flexmoe_rms_norm_backward, for the gradients dy of y and dr of r (NULL: none):
+ *   g = dy w, n = r rstd
+ *   dx = rstd (g - n mean(g n)) + dr     (the gradient of x and of residual)
+ *   dw = sum over rows of dy n, in fp32, written or with accumulate added
+ *   dy [rows][ldy], r [rows][ldr], dr [rows][ldres], dx [rows][ldx] (dtype); dw [cols]
+ *   fp32, or NULL where it isn't wanted (then no workspace is needed).
+ * dx may be dy or dr itself.  Deterministic.  The workspace (256-byte aligned,
+ * flexmoe_rms_norm_workspace_bytes(desc, rows), FLEXMOE_EWORKSPACE if smaller)
+ * holds parts of dw; one for max_rows serves every call.
+ * Shapes (FLEXMOE_ESHAPE otherwise): cols from 1 to 2^21; strides (elements, 0 =
+ * packed) at least cols, at most 2^21 and whole 16-byte units, as for the
+ * grouped products; 0 <= rows <= max_rows <= 2^30.  eps from 1e-30 to 1.
+ * rows = 0 is a no-op; the backward then writes a dw of zeros. */
+typedef struct flexmoe_norm_desc {
+    int32_t cols;
+    int32_t dtype;      /* flexmoe_dtype of x, residual, r, y and their gradients */
+    int32_t w_dtype;    /* flexmoe_dtype of w                                    */
+    int32_t max_rows;
+    float eps;
+    int32_t ldx, ldres, ldr, ldy, ldq;
+} flexmoe_norm_desc;
+int flexmoe_rms_norm(const flexmoe_norm_desc *desc, int32_t rows, const void *x,
+                     const void *residual, const void *w, void *r, void *y, void *q, float *scale,
+                     float *rstd, void *stream);
+size_t flexmoe_rms_norm_workspace_bytes(const flexmoe_norm_desc *desc, int32_t rows);
+int flexmoe_rms_norm_backward(const flexmoe_norm_desc *desc, int32_t rows, const void *dy,
+                              const void *r, const void *w, const float *rstd, const void *dr,
+                              void *dx, float *dw, int32_t accumulate, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
 /* k = ceil(r * I) for a retention ratio r in [0, 1] (Sec. 3.1).  A slack of
  * 1e-9 absorbs the binary representation error of decimal ratios (0.7 * 1000
  * gives 700).  Returns -1 for r outside [0, 1], NaN, or I < 1. */

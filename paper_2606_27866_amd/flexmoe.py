@@ -13,7 +13,7 @@ import math
 import os
 import threading
 import warnings
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence
 
 import numpy as np
 
@@ -41,13 +41,16 @@ EXPORTED = ("flexmoe_workspace_bytes", "flexmoe_rank_reorder", "flexmoe_set_budg
             "flexmoe_action_grad", "flexmoe_layer_forward_noalloc",
             "flexmoe_grouped_workspace_bytes", "flexmoe_grouped_forward", "flexmoe_grouped_input_grad",
             "flexmoe_grouped_weight_grad", "flexmoe_quantize_rows", "flexmoe_quantized_workspace_bytes",
-            "flexmoe_quantized_forward", "flexmoe_adamw_step", "flexmoe_adamw_read_state")
+            "flexmoe_quantized_forward", "flexmoe_adamw_step", "flexmoe_adamw_read_state",
+            "flexmoe_route_workspace_bytes", "flexmoe_route", "flexmoe_route_backward",
+            "flexmoe_rms_norm", "flexmoe_rms_norm_workspace_bytes", "flexmoe_rms_norm_backward")
 
 # kernel indices of flexmoe_kernel_times
 KERNELS = ("route", "dispatch_scan", "dispatch_scatter", "gate_up", "down", "combine",
            "gate_up_shared", "down_shared", "sal_transpose", "sal_prep", "sal_dgrad", "sal_wgrad",
            "sal_reduce", "act_dgrad", "act_dx", "act_other")
 MAX_ACTIONS = 16
+SCORES = {"softmax": 0, "sigmoid": 1}    # FLEXMOE_SOFTMAX, FLEXMOE_SIGMOID
 KEEP_AXES = {"none": 0, "N": 1, "K": 2}  # FLEXMOE_KEEP_*
 STATE_BLOCK = 256                        # values that share a scale in 8-bit optimizer states
 
@@ -85,6 +88,16 @@ class flexmoe_adamw_desc(ctypes.Structure):
                 ("seed", ctypes.c_uint32), ("step", ctypes.c_int64)] + \
                [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay", "grad_scale")] + \
                [("clock", ctypes.c_void_p)]
+
+
+class flexmoe_router_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("E", "top_k", "score", "normalize", "groups", "top_groups", "group_best", "dtype",
+                                              "max_tokens", "ldl")] + [("scale", ctypes.c_float)]
+
+
+class flexmoe_norm_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("cols", "dtype", "w_dtype", "max_rows")] + [("eps", ctypes.c_float)] + \
+               [(n, ctypes.c_int32) for n in ("ldx", "ldres", "ldr", "ldy", "ldq")]
 
 
 class flexmoe_action_set(ctypes.Structure):
@@ -179,6 +192,20 @@ def lib():
         L.flexmoe_adamw_step.restype = ctypes.c_int
         L.flexmoe_adamw_read_state.argtypes = [i64] + [vp] * 4 + [i32] + [vp] * 3
         L.flexmoe_adamw_read_state.restype = ctypes.c_int
+        RD = ctypes.POINTER(flexmoe_router_desc)
+        L.flexmoe_route_workspace_bytes.argtypes = [RD, i32]
+        L.flexmoe_route_workspace_bytes.restype = sz
+        L.flexmoe_route.argtypes = [RD, i32, vp, vp, ctypes.POINTER(flexmoe_route_out), vp, sz, vp]
+        L.flexmoe_route.restype = ctypes.c_int
+        L.flexmoe_route_backward.argtypes = [RD, i32, vp, vp, vp, vp, i64, vp]
+        L.flexmoe_route_backward.restype = ctypes.c_int
+        N = ctypes.POINTER(flexmoe_norm_desc)
+        L.flexmoe_rms_norm.argtypes = [N, i32] + [vp] * 9
+        L.flexmoe_rms_norm.restype = ctypes.c_int
+        L.flexmoe_rms_norm_workspace_bytes.argtypes = [N, i32]
+        L.flexmoe_rms_norm_workspace_bytes.restype = sz
+        L.flexmoe_rms_norm_backward.argtypes = [N, i32] + [vp] * 7 + [i32, vp, sz, vp]
+        L.flexmoe_rms_norm_backward.restype = ctypes.c_int
         L.flexmoe_keep_from_ratio.argtypes = [ctypes.c_double, i32]
         L.flexmoe_keep_from_ratio.restype = ctypes.c_int
         L.flexmoe_timing_enable.argtypes = [ctypes.c_int]
@@ -474,6 +501,52 @@ def flexmoe_adamw_step(desc, tensors, count=None, stream=None):
 def flexmoe_adamw_read_state(n, m, v, m_scale, v_scale, dtype, m_out, v_out, stream=None):
     _check(lib().flexmoe_adamw_read_state(int(n), _p(m), _p(v), _p(m_scale), _p(v_scale), int(dtype), _p(m_out), _p(v_out),
                                           _stream(stream)))
+
+
+# ---- norms, routing, log probabilities, distillation -------------------------
+def make_router_desc(E, top_k, score="softmax", normalize=1, groups=1, top_groups=1, group_best=1, dtype=FLEXMOE_F32, max_tokens=0,
+                     ldl=0, scale=1.0):
+    return flexmoe_router_desc(E, top_k, SCORES[score], normalize, groups, top_groups, group_best, dtype, max_tokens, ldl, scale)
+
+
+def flexmoe_route_workspace_bytes(desc, T: int) -> int:
+    n = lib().flexmoe_route_workspace_bytes(ctypes.byref(desc), int(T))
+    if n == 0:
+        raise FlexMoEError(-2, flexmoe_last_error())
+    return int(n)
+
+
+def flexmoe_route(desc, T, logits, bias, out, workspace, workspace_bytes=None, stream=None):
+    """out: dict of topk_idx, topk_w and, together, counts, offsets, perm and pos tensors."""
+    ro = flexmoe_route_out(*[_p(out.get(n)) for n, _ in flexmoe_route_out._fields_])
+    _check(lib().flexmoe_route(ctypes.byref(desc), int(T), _p(logits), _p(bias), ctypes.byref(ro), _p(workspace),
+                               _nbytes(workspace, workspace_bytes), _stream(stream)))
+
+
+def flexmoe_route_backward(desc, T, logits, topk_idx, dw, dlogits, lddl=0, stream=None):
+    _check(lib().flexmoe_route_backward(ctypes.byref(desc), int(T), _p(logits), _p(topk_idx), _p(dw), _p(dlogits), int(lddl),
+                                        _stream(stream)))
+
+
+def make_norm_desc(cols, dtype=FLEXMOE_BF16, w_dtype=FLEXMOE_BF16, max_rows=0, eps=1e-6, ldx=0, ldres=0, ldr=0, ldy=0, ldq=0):
+    return flexmoe_norm_desc(cols, dtype, w_dtype, max_rows, eps, ldx, ldres, ldr, ldy, ldq)
+
+
+def flexmoe_rms_norm(desc, rows, x, residual, w, r, y, q, scale, rstd, stream=None):
+    _check(lib().flexmoe_rms_norm(ctypes.byref(desc), int(rows), _p(x), _p(residual), _p(w), _p(r), _p(y), _p(q), _p(scale), _p(rstd),
+                                  _stream(stream)))
+
+
+def flexmoe_rms_norm_workspace_bytes(desc, rows: int) -> int:
+    n = lib().flexmoe_rms_norm_workspace_bytes(ctypes.byref(desc), int(rows))
+    if n == 0:
+        raise FlexMoEError(-2, flexmoe_last_error())
+    return int(n)
+
+
+def flexmoe_rms_norm_backward(desc, rows, dy, r, w, rstd, dr, dx, dw, accumulate, workspace, workspace_bytes=None, stream=None):
+    _check(lib().flexmoe_rms_norm_backward(ctypes.byref(desc), int(rows), _p(dy), _p(r), _p(w), _p(rstd), _p(dr), _p(dx), _p(dw),
+                                           int(accumulate), _p(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)))
 
 
 _DTYPE_CODES = {}  # filled by the first call: the module does not import torch
@@ -829,6 +902,168 @@ def adamw_state_values(m, v, m_scale, v_scale, dtype=None, stream=None):
                              _vector(m_scale, blocks, torch.float32, "m_scale"), _vector(v_scale, blocks, torch.float32, "v_scale"),
                              _dtype_code(dtype), mo, vo, stream)
     return mo, vo
+
+
+class Routing(NamedTuple):
+    """Where tokens go: ids [T, top_k] (-1: nowhere) and weights, and the rows grouped by expert (None without tables)."""
+    topk_idx: object
+    topk_w: object
+    counts: object = None
+    offsets: object = None
+    perm: object = None
+    pos: object = None
+
+
+class Router:
+    """Routing of tokens to experts: scores, balance bias, groups, top-k, weights, tables, and the logits' gradient.
+
+    The tables are those of the products: row i of a grouped x is token perm[i] // top_k for i < offsets[E], and a token's
+    rows are pos (-1: none).  A holder around the C calls (no arithmetic): it keeps the workspace; calls on different
+    streams need holders of their own.  Threads may share a holder.
+    """
+
+    def __init__(self, E, top_k, max_tokens, score="softmax", normalize=True, scale=1.0, groups=1, top_groups=1, group_best=1,
+                 device="cuda"):
+        import torch
+        if score not in SCORES:
+            raise ValueError("score must be one of %s, got %r" % (", ".join(SCORES), score))
+        self.E, self.top_k, self.max_tokens = E, top_k, max_tokens
+        self._i32, self._f32 = torch.int32, torch.float32
+        self.desc = make_router_desc(E, top_k, score, int(normalize), groups, top_groups, group_best, FLEXMOE_F32, max_tokens, E, scale)
+        self._desc = ctypes.byref(self.desc)
+        self.workspace = torch.empty(flexmoe_route_workspace_bytes(self.desc, max_tokens), dtype=torch.uint8, device=device)
+        self._ws = (self.workspace.data_ptr(), self.workspace.numel())
+        self._lock = threading.Lock()  # holds the descriptor's type and stride
+
+    def _logits(self, logits):
+        if logits.dim() != 2:
+            raise ValueError("logits must be [T, %d], got %s" % (self.E, tuple(logits.shape)))
+        T, dt = logits.shape[0], logits.dtype
+        self.desc.dtype, self.desc.ldl = _dtype_code(dt), _matrix(logits, (T, self.E), dt, "logits")
+        return T
+
+    def route(self, logits, bias=None, tables=True, stream=None) -> Routing:
+        """logits [T, E] bf16 or fp32, bias [E] fp32."""
+        T, k, dev = logits.shape[0], self.top_k, logits.device
+        idx, w = _new((T, k), self._i32, dev, stream), _new((T, k), self._f32, dev, stream)
+        more = ()
+        if tables:
+            t = _new((2 * self.E + 1 + 2 * T * k,), self._i32, dev, stream)
+            more = t.split((self.E, self.E + 1, T * k, T * k))
+        ro = flexmoe_route_out(idx.data_ptr(), w.data_ptr(), *[m.data_ptr() for m in more])
+        with self._lock:
+            self._logits(logits)
+            _check(lib().flexmoe_route(self._desc, T, logits.data_ptr(), None if bias is None else _vector(bias, self.E, self._f32, "bias"),
+                                       ctypes.byref(ro), *self._ws, _stream(stream)))
+        return Routing(idx, w, *more)
+
+    def backward(self, logits, topk_idx, dw, dlogits=None, stream=None):
+        """The logits' gradient [T, E] from dw [T, top_k], that of the weights."""
+        T = logits.shape[0]
+        if dlogits is None:
+            dlogits = _new((T, self.E), logits.dtype, logits.device, stream)
+        with self._lock:
+            self._logits(logits)
+            _check(lib().flexmoe_route_backward(self._desc, T, logits.data_ptr(), _vector(topk_idx, T * self.top_k, self._i32, "topk_idx"),
+                                                _vector(dw, T * self.top_k, self._f32, "dw"), dlogits.data_ptr(),
+                                                _matrix(dlogits, (T, self.E), logits.dtype, "dlogits"), _stream(stream)))
+        return dlogits
+
+
+class RMSNorm:
+    """Root-mean-square norm of rows with the residual's addition, as rows of their type or in 8 bits, and its gradients.
+
+    weight [cols], bf16 or fp32; the rows may be of either type.  forward and quantized keep nothing; backward uses the
+    holder's workspace for up to max_rows rows: backward calls on different streams need holders of their own.  Threads
+    may share a holder.
+    """
+
+    def __init__(self, weight, max_rows, eps=1e-6):
+        import torch
+        if weight.dim() != 1:
+            raise ValueError("weight must have one dimension, got %s" % (tuple(weight.shape),))
+        self.weight, self.cols, self.max_rows, self.eps = weight, weight.shape[0], max_rows, eps
+        self._f32, self._i8 = torch.float32, torch.int8
+        self._w_code = _dtype_code(weight.dtype)
+        self.desc = make_norm_desc(self.cols, FLEXMOE_BF16, self._w_code, max_rows, eps, *[_pitch(self.cols, 2)] * 4, _pitch(self.cols, 1))
+        self._desc = ctypes.byref(self.desc)
+        self.workspace = torch.empty(flexmoe_rms_norm_workspace_bytes(self.desc, max_rows), dtype=torch.uint8, device=weight.device)
+        self._ws = (self.workspace.data_ptr(), self.workspace.numel())
+        self._lock = threading.Lock()  # holds the descriptor's type and strides
+
+    def _rows(self, x, name):
+        if x.dim() != 2:
+            raise ValueError("%s must be [rows, %d], got %s" % (name, self.cols, tuple(x.shape)))
+        return x.shape[0], x.dtype, (x.shape[0], self.cols)
+
+    def forward(self, x, residual=None, r=None, y=None, stream=None):
+        """(y, r, rstd) for x [R, cols]: r = x + residual (r may be residual itself; without one r is x), y = r rstd weight."""
+        y, _, _, r, rstd = self._forward(x, residual, r, y, None, None, True, False, stream)
+        return y, r, rstd
+
+    def quantized(self, x, residual=None, r=None, q=None, scale=None, stream=None):
+        """(q, scale, r): y in 8 bits with a scale for each row, as Int8Product.product takes it."""
+        _, q, scale, r, _ = self._forward(x, residual, r, None, q, scale, False, True, stream)
+        return q, scale, r
+
+    def both(self, x, residual=None, r=None, stream=None):
+        """(y, q, scale, r): y as it is, for a router, and in 8 bits, for the experts, in one pass."""
+        return self._forward(x, residual, r, None, None, None, True, True, stream)[:4]
+
+    def _forward(self, x, residual, r, y, q, scale, want_y, want_q, stream):
+        R, dt, shape = self._rows(x, "x")
+        d, dev, w = self.desc, x.device, self.weight
+        if residual is not None and r is None:
+            r = _padded(shape, dt, dev, stream)
+        elif residual is None and r is not None:
+            raise ValueError("r goes with a residual")
+        rstd = None
+        if want_y:
+            y = _padded(shape, dt, dev, stream) if y is None else y
+            if not want_q:
+                rstd = _new((R,), self._f32, dev, stream)
+        if want_q:
+            q = _padded(shape, self._i8, dev, stream) if q is None else q
+            scale = _new((R,), self._f32, dev, stream) if scale is None else scale
+        with self._lock:
+            d.dtype, d.ldx = _dtype_code(dt), _matrix(x, shape, dt, "x")
+            if residual is not None:
+                d.ldres, d.ldr = _matrix(residual, shape, dt, "residual"), _matrix(r, shape, dt, "r")
+            else:
+                d.ldres = d.ldr = d.ldx
+            d.ldy = _matrix(y, shape, dt, "y") if want_y else d.ldx
+            if want_q:
+                d.ldq = _matrix(q, shape, self._i8, "q")
+            _check(lib().flexmoe_rms_norm(self._desc, R, x.data_ptr(), _p(residual), _vector(w, self.cols, w.dtype, "weight"), _p(r),
+                                          _p(y), _p(q), _vector(scale, R, self._f32, "scale") if want_q else None, _p(rstd),
+                                          _stream(stream)))
+        return y, q, scale, x if residual is None else r, rstd
+
+    def backward(self, dy, r, rstd, dr=None, dx=None, dw=None, accumulate=False, weight_grad=True, stream=None):
+        """(dx, dw) from the gradients of y and (dr) of r; dx, which may be dr or dy itself, is that of x and of the residual.
+
+        dw [cols] fp32 is written or, with accumulate, added to; None without weight_grad.
+        """
+        R, dt, shape = self._rows(dy, "dy")
+        d, dev, w = self.desc, dy.device, self.weight
+        if dx is None:
+            dx = _padded(shape, dt, dev, stream)
+        if not weight_grad:
+            if dw is not None or accumulate:
+                raise ValueError("dw and accumulate go with weight_grad")
+        elif dw is None:
+            if accumulate:
+                raise ValueError("accumulate needs dw")
+            dw = _new((self.cols,), self._f32, dev, stream)
+        with self._lock:
+            d.dtype, d.ldy, d.ldr = _dtype_code(dt), _matrix(dy, shape, dt, "dy"), _matrix(r, shape, dt, "r")
+            d.ldx = _matrix(dx, shape, dt, "dx")
+            d.ldres = d.ldx if dr is None else _matrix(dr, shape, dt, "dr")
+            _check(lib().flexmoe_rms_norm_backward(self._desc, R, dy.data_ptr(), r.data_ptr(), _vector(w, self.cols, w.dtype, "weight"),
+                                                   _vector(rstd, R, self._f32, "rstd"), _p(dr), dx.data_ptr(),
+                                                   None if dw is None else _vector(dw, self.cols, self._f32, "dw"), int(accumulate),
+                                                   *self._ws, _stream(stream)))
+        return dx, dw
 
 
 class ClippedWeights:

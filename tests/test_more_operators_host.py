@@ -1,0 +1,141 @@
+"""Refusals of routing, norms, log probabilities and distillation: every bad argument is reported on the host, before any
+device work (no call here reaches a kernel launch)."""
+import pytest
+
+torch = pytest.importorskip("torch")
+from paper_2606_27866_amd import flexmoe as fm  # noqa: E402
+
+FAKE = 0x100000  # never dereferenced
+
+
+def code_of(f, *args, **kw):
+    with pytest.raises(fm.FlexMoEError) as ei:
+        f(*args, **kw)
+    assert fm.flexmoe_last_error()
+    return ei.value.code
+
+
+# ---- routing ----------------------------------------------------------------
+def router(**kw):
+    a = dict(E=16, top_k=2, max_tokens=100)
+    a.update(kw)
+    return fm.make_router_desc(**a)
+
+
+OUT = dict(topk_idx=FAKE, topk_w=FAKE, counts=FAKE, offsets=FAKE, perm=FAKE, pos=FAKE)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(dtype=4), -5), (dict(E=0), -2), (dict(E=257), -2), (dict(top_k=0), -2), (dict(top_k=17), -2), (dict(E=1), -2),
+    (dict(normalize=2), -1), (dict(groups=0), -2), (dict(groups=3), -2), (dict(E=130, groups=65), -2), (dict(groups=4, top_groups=0), -2),
+    (dict(groups=4, top_groups=5), -2), (dict(top_k=5, groups=4, top_groups=1), -2), (dict(group_best=0), -2), (dict(group_best=3), -2),
+    (dict(groups=16, top_groups=2, group_best=2), -2), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(max_tokens=-1), -2),
+    (dict(max_tokens=1 << 29), -2), (dict(ldl=15), -2), (dict(ldl=(1 << 21) + 1), -2)])
+def test_router_descriptor(kw, code):
+    D = router(**kw)
+    assert code_of(fm.flexmoe_route_workspace_bytes, D, 1) == -2
+    assert code_of(fm.flexmoe_route, D, 1, FAKE, None, OUT, FAKE, 1 << 30, 0) == code
+    assert code_of(fm.flexmoe_route_backward, D, 1, FAKE, FAKE, FAKE, FAKE, 0, 0) == code
+
+
+def test_router_score_out_of_range():
+    D = router()
+    D.score = 2
+    assert code_of(fm.flexmoe_route, D, 1, FAKE, None, OUT, FAKE, 1 << 30, 0) == -1
+    with pytest.raises(ValueError, match="score"):
+        fm.Router(16, 2, 10, score="relu", device="cpu")
+
+
+def test_router_arguments():
+    def call(T=50, logits=FAKE, bias=None, ws=FAKE, nbytes=1 << 30, **out):
+        fm.flexmoe_route(router(), T, logits, bias, dict(OUT, **out), ws, nbytes, 0)
+
+    for kw, code in [(dict(T=-1), -1), (dict(T=101), -2), (dict(logits=None), -1), (dict(topk_idx=None), -1), (dict(topk_w=None), -1),
+                     (dict(counts=None), -1), (dict(offsets=None), -1), (dict(perm=None), -1), (dict(pos=None), -1), (dict(logits=FAKE + 2), -1),
+                     (dict(bias=FAKE + 2), -1), (dict(topk_idx=FAKE + 1), -1), (dict(pos=FAKE + 2), -1), (dict(ws=None), -4), (dict(nbytes=100), -4),
+                     (dict(ws=FAKE + 16), -4)]:
+        assert code_of(call, **kw) == code, kw
+    fm.flexmoe_route(router(), 0, None, None, {}, None, 0, 0)  # nothing to do
+
+    def back(T=50, logits=FAKE, idx=FAKE, dw=FAKE, dl=FAKE, lddl=0):
+        fm.flexmoe_route_backward(router(), T, logits, idx, dw, dl, lddl, 0)
+
+    for kw, code in [(dict(T=-1), -1), (dict(T=101), -2), (dict(logits=None), -1), (dict(idx=None), -1), (dict(dw=None), -1), (dict(dl=None), -1),
+                     (dict(lddl=15), -2), (dict(dl=FAKE + 2), -1), (dict(idx=FAKE + 2), -1)]:
+        assert code_of(back, **kw) == code, kw
+    back(T=0)
+
+
+def test_router_tensors():
+    r = fm.Router(16, 2, 10, device="cpu")
+    ok = torch.zeros(4, 16)
+    for bad in (ok[0], ok[:, :8], ok.half(), ok):  # the last is not on the GPU
+        with pytest.raises(ValueError):
+            r.route(bad)
+    with pytest.raises(ValueError):
+        r.backward(ok, torch.zeros(4, 2, dtype=torch.int32), torch.zeros(4, 2))
+
+
+# ---- norm -------------------------------------------------------------------
+def norm(**kw):
+    a = dict(cols=64, max_rows=100)
+    a.update(kw)
+    return fm.make_norm_desc(**a)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(dtype=3), -5), (dict(w_dtype=-1), -5), (dict(cols=0), -2), (dict(cols=(1 << 21) + 8), -2), (dict(max_rows=-1), -2),
+    (dict(max_rows=(1 << 30) + 1), -2), (dict(eps=0.0), -1), (dict(eps=1e-31), -1), (dict(eps=2.0), -1), (dict(eps=float("nan")), -1),
+    (dict(cols=60), -2), (dict(ldx=56), -2), (dict(ldx=68), -2), (dict(ldres=70), -2), (dict(ldr=60), -2), (dict(ldy=(1 << 21) + 8), -2)])
+def test_norm_descriptor(kw, code):
+    D = norm(**kw)
+    assert code_of(fm.flexmoe_rms_norm_workspace_bytes, D, 1) == -2
+    assert code_of(fm.flexmoe_rms_norm, D, 1, FAKE, None, FAKE, None, FAKE, None, None, None, 0) == code
+    assert code_of(fm.flexmoe_rms_norm_backward, D, 1, FAKE, FAKE, FAKE, FAKE, None, FAKE, FAKE, 0, FAKE, 1 << 30, 0) == code
+
+
+def test_norm_arguments():
+    at = dict(zip("x residual w r y q scale rstd".split(), [FAKE + 4096 * i for i in range(8)]))
+
+    def call(rows=10, D=norm(), **kw):
+        a = dict(at, **kw)
+        fm.flexmoe_rms_norm(D, rows, a["x"], a["residual"], a["w"], a["r"], a["y"], a["q"], a["scale"], a["rstd"], 0)
+
+    for kw, code in [(dict(rows=-1), -1), (dict(rows=101), -2), (dict(x=None), -1), (dict(w=None), -1), (dict(y=None, q=None, scale=None), -1),
+                     (dict(scale=None), -1), (dict(q=None), -1), (dict(r=None), -1), (dict(residual=None), -1), (dict(x=FAKE + 8), -1),
+                     (dict(r=FAKE + 2), -1), (dict(w=FAKE + 4), -1), (dict(scale=FAKE + 2), -1), (dict(rstd=FAKE + 1), -1),
+                     (dict(D=norm(ldq=72)), -2), (dict(D=norm(ldq=48)), -2), (dict(y=at["x"]), -1), (dict(y=at["residual"]), -1),
+                     (dict(y=at["r"]), -1)]:
+        assert code_of(call, **kw) == code, kw
+    call(rows=0, x=None)
+
+    def back(rows=10, dy=FAKE, r=FAKE, w=FAKE, rstd=FAKE, dr=None, dx=FAKE, dw=FAKE, accumulate=0, ws=FAKE, nbytes=1 << 30):
+        fm.flexmoe_rms_norm_backward(norm(), rows, dy, r, w, rstd, dr, dx, dw, accumulate, ws, nbytes, 0)
+
+    for kw, code in [(dict(rows=-1), -1), (dict(rows=101), -2), (dict(dy=None), -1), (dict(r=None), -1), (dict(w=None), -1), (dict(rstd=None), -1),
+                     (dict(dx=None), -1), (dict(accumulate=2), -1), (dict(dr=FAKE + 8), -1), (dict(dw=FAKE + 2), -1), (dict(ws=None), -4),
+                     (dict(nbytes=255), -4), (dict(ws=FAKE + 128), -4)]:
+        assert code_of(back, **kw) == code, kw
+    back(rows=0, dw=None, ws=None, nbytes=0)
+
+
+def test_norm_workspace_serves_fewer_rows():
+    for cols in (8, 512, 2048, 2056, 40000):
+        sizes = [fm.flexmoe_rms_norm_workspace_bytes(norm(cols=cols, max_rows=1 << 20), n) for n in (0, 1, 255, 1023, 1024, 1030, 5000, 1 << 20)]
+        assert sizes == sorted(sizes) and sizes[0] >= 256
+
+
+def test_norm_tensors():
+    n = fm.RMSNorm(torch.ones(64), 10)
+    x = torch.zeros(4, 64)
+    for bad in (x[0], x[:, :32], x.half(), x):  # the last is not on the GPU
+        with pytest.raises(ValueError):
+            n.forward(bad)
+    with pytest.raises(ValueError, match="residual"):
+        n.forward(x, r=x)
+    with pytest.raises(ValueError, match="accumulate"):
+        n.backward(x, x, torch.zeros(4), accumulate=True)
+    with pytest.raises(ValueError, match="weight_grad"):
+        n.backward(x, x, torch.zeros(4), dw=torch.zeros(64), weight_grad=False)
+    with pytest.raises(ValueError, match="dimension"):
+        fm.RMSNorm(torch.ones(1, 64), 10)

@@ -1,0 +1,237 @@
+"""Norm of rows after the residual's addition, its 8-bit form and its gradients, against their formulas in 64 bits.
+
+Bounds, u = 2^-24.  r is one rounding: compared for equality.  A sum of cols squares is taken in runs of at most
+max(8, cols / 64) values and joined in 10 steps, all positive: its relative error is below (max(8, cols / 64) + 10) u; the root halves
+it, and mean, eps, root, quotient and the two products add 6 u.  A result is rounded once more (eps / 2 of its type).  Sums with signs (mean of
+g n, dw) are held to the same number of units of the sum of their terms' sizes."""
+import pytest
+
+torch = pytest.importorskip("torch")
+from paper_2606_27866_amd import flexmoe as fm  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+BF16, F32 = torch.bfloat16, torch.float32
+SHAPES = [(1, 1), (3, 7), (5, 8), (2, 9), (4, 512), (3, 513), (7, 2048), (1030, 520), (1025, 2047), (2, 2050), (3, 4096), (2, 4097), (1, 16384), (2, 16399)]
+
+
+def units(cols):
+    return (max(8, cols / 64) + 10) / 2 + 6
+
+
+def half_step(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def matrix(g, rows, cols, dtype, std=1.0, extra=8, device="cuda"):
+    """A view of wider rows that hold NaN past `cols`."""
+    t = torch.full((rows, -(-cols // 8) * 8 + extra), float("nan"), dtype=dtype, device=device)
+    t[:, :cols] = torch.empty(rows, cols, device=device).normal_(0, std, generator=g).to(dtype)
+    return t[:, :cols]
+
+
+def copy_of(t):
+    """A copy whose rows start on 16-byte boundaries (clone packs a view's rows)."""
+    out = fm._padded(t.shape, t.dtype, t.device)
+    return out.copy_(t)
+
+
+def make(rows, cols, dtype, w_dtype=None, seed=0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed + cols)
+    x, res = matrix(g, rows, cols, dtype), matrix(g, rows, cols, dtype, 2.0, 16)
+    w = torch.empty(cols, device="cuda").normal_(1, 0.3, generator=g).to(w_dtype or dtype)
+    return g, x, res, w
+
+
+def reference(r, w, eps):
+    r64 = r.double()
+    rstd = (r64.square().mean(1) + eps).rsqrt()
+    return rstd, r64 * rstd.unsqueeze(1) * w.double()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_forward(dtype, rows, cols):
+    _, x, res, w = make(rows, cols, dtype)
+    norm = fm.RMSNorm(w, rows, eps=1e-5)
+    for residual in (None, res):
+        y, r, rstd = norm.forward(x, residual)
+        want = x if residual is None else (x.float() + res.float()).to(dtype)
+        assert torch.equal(r, want)
+        rs, ref = reference(want, w, 1e-5)
+        assert bool(((rstd.double() - rs).abs() <= units(cols) * U * rs).all())
+        assert bool(((y.double() - ref).abs() <= (units(cols) * U + half_step(dtype)) * ref.abs()).all())
+
+
+@pytest.mark.parametrize("dtype,w_dtype", [(BF16, F32), (F32, BF16)])
+def test_weights_of_another_type(dtype, w_dtype):
+    _, x, _, w = make(5, 1000, dtype, w_dtype)
+    y, _, _ = fm.RMSNorm(w, 5).forward(x)
+    _, ref = reference(x, w, 1e-6)
+    assert bool(((y.double() - ref).abs() <= (units(1000) * U + half_step(dtype)) * ref.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_quantized(dtype, rows, cols):
+    """Values: half a step of the row's scale, and 127 steps' share of the relative error of y."""
+    _, x, res, w = make(rows, cols, dtype)
+    norm = fm.RMSNorm(w, rows)
+    q, scale, r = norm.quantized(x, res)
+    assert torch.equal(r, (x.float() + res.float()).to(dtype))
+    _, ref = reference(r, w, 1e-6)
+    top = ref.abs().amax(1)
+    rel = (units(cols) + 3) * U
+    assert bool(((scale.double() - top / 127).abs() <= rel * top / 127).all())
+    assert q.dtype == torch.int8 and int(q.abs().max()) <= 127
+    err = (q.double() * scale.double().unsqueeze(1) - ref).abs()
+    assert bool((err <= (0.5 + 127 * 3 * rel) * (top / 127).unsqueeze(1)).all())
+    y, q2, scale2, r2 = norm.both(x, res)  # both at once: the same bits
+    assert torch.equal(q, q2) and torch.equal(scale, scale2) and torch.equal(r, r2)
+    assert torch.equal(y, norm.forward(x, res)[0])
+
+
+def test_quantized_feeds_the_8_bit_product():
+    _, x, _, w = make(33, 512, BF16)
+    g = torch.Generator(device="cuda")
+    weights = torch.empty(1, 96, 512, device="cuda").normal_(0, 0.05, generator=g)
+    product = fm.Int8Product.from_weights(weights, 33, out_dtype=F32)
+    norm = fm.RMSNorm(w, 33)
+    q, scale, _ = norm.quantized(x)
+    y = product.product(q, scale)
+    ref = (q.double() * scale.double().unsqueeze(1)) @ (product.w[0].double() * product.w_scale[0].double().unsqueeze(1)).T
+    assert bool(((y.double() - ref).abs() <= 4 * U * ref.abs() + 1e-30).all())
+
+
+def test_nothing_past_a_row_is_written():
+    _, x, res, w = make(6, 100, BF16)
+    norm = fm.RMSNorm(w, 6)
+    wide = [torch.full((6, 136), 7, dtype=t, device="cuda") for t in (BF16, BF16, torch.int8)]
+    y, r, q = (t[:, :100] for t in wide)
+    norm.forward(x, res, r=r, y=y)
+    norm.quantized(x, res, r=r, q=torch.full((6, 144), 7, dtype=torch.int8, device="cuda")[:, :100])
+    dx, _ = norm.backward(x, r, torch.ones(6, device="cuda"), dx=wide[0][:, :100])
+    assert all(bool((t[:, 100:] == 7).all()) for t in wide)
+
+
+def test_residual_kept_in_place():
+    _, x, res, w = make(40, 600, BF16)
+    norm = fm.RMSNorm(w, 40)
+    want = norm.forward(x, res)
+    kept = res.clone()
+    y, r, rstd = norm.forward(x, kept, r=kept)
+    assert r is kept and all(torch.equal(a, b) for a, b in zip((y, kept, rstd), want))
+    _, x, res, w = make(3, 20000, F32)  # a row that is read again
+    norm = fm.RMSNorm(w, 3)
+    want = norm.quantized(x, res)
+    x = x.clone()
+    got = norm.quantized(x, res, r=x)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("cols", [64, 3000, 20000])
+def test_extremes(cols):
+    """Zeros, squares past fp32's range, squares below it, and NaN or infinity in one row of several."""
+    x = torch.ones(7, cols, device="cuda")
+    x[0] = 0
+    x[1] = 3e38
+    x[2, 0], x[2, 1:] = 1e30, 1e-30
+    x[3] = 1e-25
+    x[4, cols // 2] = float("nan")
+    x[5, cols // 3] = float("inf")
+    w = torch.ones(cols, device="cuda")
+    norm = fm.RMSNorm(w, 7, eps=1e-12)
+    y, _, rstd = norm.forward(x)
+    rs, ref = reference(x, w, 1e-12)
+    ok = [0, 1, 2, 3, 6]
+    # 1 / 3e38 is a denormal: 2^-149 beside the relative error
+    assert bool(((rstd.double() - rs).abs()[ok] <= (units(cols) * U * rs + 2.0 ** -149)[ok]).all())
+    assert bool(((y.double() - ref).abs()[ok] <= (2 * units(cols) * U * ref.abs() + x.double().abs() * 2.0 ** -149 + 2.0 ** -149)[ok]).all())
+    assert bool(torch.isnan(y[4]).all()) and bool(torch.isnan(rstd[4])) and bool(torch.isfinite(y[6]).all())
+    q, scale, _ = norm.quantized(x)
+    assert float(scale[0]) == 0 and bool((q[0] == 0).all()) and bool(torch.isnan(scale[4])) and bool((q[4] == 0).all())
+    assert bool((q[1] == 127).all()) and int(q[2, 0]) == 127
+
+
+def grad_reference(dy, r, w, rstd, dr):
+    dy, r, w, rstd = dy.double(), r.double(), w.double(), rstd.double().unsqueeze(1)
+    g, n = dy * w, r * rstd
+    dx = rstd * (g - n * (g * n).mean(1, keepdim=True))
+    size = rstd * (g.abs() + n.abs() * (g * n).abs().mean(1, keepdim=True))
+    if dr is not None:
+        dx, size = dx + dr.double(), size + dr.double().abs()
+    return dx, size, (dy * n).sum(0), (dy * n).abs().sum(0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,cols", SHAPES + [(300, 2048), (1100, 64), (2500, 4000)])
+def test_backward(dtype, rows, cols):
+    g, x, _, w = make(rows, cols, dtype)
+    dy, dr = matrix(g, rows, cols, dtype, 0.1), matrix(g, rows, cols, dtype, 0.1, 24)
+    norm = fm.RMSNorm(w, rows)
+    _, r, rstd = norm.forward(x)
+    for d in (None, dr):
+        dx, dw = norm.backward(dy, r, rstd, dr=d)
+        ref, size, dw_ref, dw_size = grad_reference(dy, r, w, rstd, d)
+        many = max(8, cols / 64) + 18  # terms of a run, joins, and eight roundings
+        assert bool(((dx.double() - ref).abs() <= many * U * size + half_step(dtype) * ref.abs()).all())
+        assert bool(((dw.double() - dw_ref).abs() <= (min(rows, 64) + 24) * U * dw_size).all())
+    base = torch.full((cols,), 3.0, device="cuda")
+    _, added = norm.backward(dy, r, rstd, dw=base.clone(), accumulate=True)
+    assert bool(((added.double() - 3 - dw_ref).abs() <= (min(rows, 64) + 25) * U * (dw_size + 3)).all())
+    only, none = norm.backward(dy, r, rstd, dr=dr, weight_grad=False)
+    assert none is None and torch.equal(only, dx)
+    into = copy_of(dr)
+    norm.backward(dy, r, rstd, dr=into, dx=into, weight_grad=False)  # in the place of dr
+    assert torch.equal(into, dx)
+    into = copy_of(dy)
+    norm.backward(into, r, rstd, dr=dr, dx=into, weight_grad=False)
+    assert torch.equal(into, dx)
+
+
+def test_gradient_against_differences():
+    """Central differences of a sum over the outputs, in fp32 rows; step 1e-2, whose third-order term is below 1e-4 here."""
+    g, x, res, w = make(4, 24, F32)
+    c = torch.empty(4, 24, device="cuda").normal_(generator=g)
+    norm = fm.RMSNorm(w, 4)
+
+    def loss(xx, ww):
+        y, r, _ = fm.RMSNorm(ww, 4).forward(xx, res)
+        return float((y.double() * c + 0.5 * r.double()).sum())
+
+    _, r, rstd = norm.forward(x, res)
+    dx, dw = norm.backward(c, r, rstd, dr=torch.full_like(r, 0.5))
+    h = 1e-2
+    for i, j in ((0, 0), (1, 7), (3, 23)):
+        up, down = x.clone(), x.clone()
+        up[i, j] += h
+        down[i, j] -= h
+        assert abs((loss(up, w) - loss(down, w)) / (2 * h) - float(dx[i, j])) < 1e-3
+        up, down = w.clone(), w.clone()
+        up[j] += h
+        down[j] -= h
+        assert abs((loss(x, up) - loss(x, down)) / (2 * h) - float(dw[j])) < 1e-3
+
+
+def test_no_rows():
+    w = torch.ones(40, device="cuda")
+    norm = fm.RMSNorm(w, 8)
+    x = torch.empty(0, 40, device="cuda")
+    y, _, rstd = norm.forward(x)
+    assert y.shape == (0, 40) and rstd.shape == (0,)
+    dw = torch.full((40,), 5.0, device="cuda")
+    assert bool((norm.backward(x, x, rstd, dw=dw)[1] == 0).all())
+    dw.fill_(5.0)
+    assert bool((norm.backward(x, x, rstd, dw=dw, accumulate=True)[1] == 5).all())
+
+
+def test_deterministic_and_smaller_calls():
+    """The same bits again, and from a holder for more rows."""
+    g, x, _, w = make(1500, 1200, BF16)
+    dy = matrix(g, 1500, 1200, BF16)
+    a, b = fm.RMSNorm(w, 1500), fm.RMSNorm(w, 100000)
+    _, r, rstd = a.forward(x)
+    first = a.backward(dy, r, rstd)
+    for n in (a, b, a):
+        assert all(torch.equal(p, q) for p, q in zip(n.backward(dy, r, rstd), first))
