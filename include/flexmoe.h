@@ -619,6 +619,38 @@ int flexmoe_rms_norm_backward(const flexmoe_norm_desc *desc, int32_t rows, const
                               void *dx, float *dw, int32_t accumulate, void *workspace,
                               size_t workspace_bytes, void *stream);
 
+/* ---- Log probabilities of tokens -------------------------------------------
+ * For rows of logits l [rows][ld] (dtype) over V tokens, with x = l / temperature:
+ *   lse [rows]      log of the sum of exp(x)
+ *   logprob [rows]  x of the row's token minus lse (tokens [rows] int32; 0 for a
+ *                   token outside [0, V)); both NULL or none
+ *   entropy [rows]  lse - sum p x, p = exp(x - lse)
+ *   top_ids, top_logprobs [rows][top]: the top largest l, largest first, ties to
+ *                   the lower id, NaN last; both NULL where top = 0
+ * in fp32.  Logits of -inf are masked tokens: they have no part in the sums and
+ * are listed last (before NaN), with -inf.  A row of nothing but -inf has lse
+ * and log probabilities of -inf and the entropy 0; with a NaN or +inf all of
+ * them are NaN.  Deterministic.
+ * Shapes (FLEXMOE_ESHAPE otherwise): 1 <= V <= 2^21, 0 <= top <= min(V, 128); ld
+ * (elements, 0 = packed) at least V, at most 2^22 and a whole number of 16-byte
+ * units, rows start on 16-byte boundaries and may be read up to the unit that
+ * their last element lies in; 0 <= rows <= max_rows <= 2^24; temperature from
+ * 1e-6 to 1e6.  The workspace (256-byte aligned) of
+ * flexmoe_token_logprobs_workspace_bytes(desc, rows) serves every smaller call of
+ * the same V and top; it is needed while rows are few or V is above 131072. */
+typedef struct flexmoe_logprob_desc {
+    int32_t V, top;
+    int32_t dtype;      /* flexmoe_dtype of the logits                           */
+    int32_t max_rows;
+    int32_t ld;
+    float temperature;
+} flexmoe_logprob_desc;
+size_t flexmoe_token_logprobs_workspace_bytes(const flexmoe_logprob_desc *desc, int32_t rows);
+int flexmoe_token_logprobs(const flexmoe_logprob_desc *desc, int32_t rows, const void *logits,
+                           const int32_t *tokens, float *logprob, float *entropy, float *lse,
+                           int32_t *top_ids, float *top_logprobs, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
 /* k = ceil(r * I) for a retention ratio r in [0, 1] (Sec. 3.1).  A slack of
  * 1e-9 absorbs the binary representation error of decimal ratios (0.7 * 1000
  * gives 700).  Returns -1 for r outside [0, 1], NaN, or I < 1. */

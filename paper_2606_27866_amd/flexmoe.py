@@ -43,7 +43,8 @@ EXPORTED = ("flexmoe_workspace_bytes", "flexmoe_rank_reorder", "flexmoe_set_budg
             "flexmoe_grouped_weight_grad", "flexmoe_quantize_rows", "flexmoe_quantized_workspace_bytes",
             "flexmoe_quantized_forward", "flexmoe_adamw_step", "flexmoe_adamw_read_state",
             "flexmoe_route_workspace_bytes", "flexmoe_route", "flexmoe_route_backward",
-            "flexmoe_rms_norm", "flexmoe_rms_norm_workspace_bytes", "flexmoe_rms_norm_backward")
+            "flexmoe_rms_norm", "flexmoe_rms_norm_workspace_bytes", "flexmoe_rms_norm_backward",
+            "flexmoe_token_logprobs_workspace_bytes", "flexmoe_token_logprobs")
 
 # kernel indices of flexmoe_kernel_times
 KERNELS = ("route", "dispatch_scan", "dispatch_scatter", "gate_up", "down", "combine",
@@ -98,6 +99,10 @@ class flexmoe_router_desc(ctypes.Structure):
 class flexmoe_norm_desc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("cols", "dtype", "w_dtype", "max_rows")] + [("eps", ctypes.c_float)] + \
                [(n, ctypes.c_int32) for n in ("ldx", "ldres", "ldr", "ldy", "ldq")]
+
+
+class flexmoe_logprob_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("V", "top", "dtype", "max_rows", "ld")] + [("temperature", ctypes.c_float)]
 
 
 class flexmoe_action_set(ctypes.Structure):
@@ -206,6 +211,11 @@ def lib():
         L.flexmoe_rms_norm_workspace_bytes.restype = sz
         L.flexmoe_rms_norm_backward.argtypes = [N, i32] + [vp] * 7 + [i32, vp, sz, vp]
         L.flexmoe_rms_norm_backward.restype = ctypes.c_int
+        LD = ctypes.POINTER(flexmoe_logprob_desc)
+        L.flexmoe_token_logprobs_workspace_bytes.argtypes = [LD, i32]
+        L.flexmoe_token_logprobs_workspace_bytes.restype = sz
+        L.flexmoe_token_logprobs.argtypes = [LD, i32] + [vp] * 8 + [sz, vp]
+        L.flexmoe_token_logprobs.restype = ctypes.c_int
         L.flexmoe_keep_from_ratio.argtypes = [ctypes.c_double, i32]
         L.flexmoe_keep_from_ratio.restype = ctypes.c_int
         L.flexmoe_timing_enable.argtypes = [ctypes.c_int]
@@ -547,6 +557,24 @@ def flexmoe_rms_norm_workspace_bytes(desc, rows: int) -> int:
 def flexmoe_rms_norm_backward(desc, rows, dy, r, w, rstd, dr, dx, dw, accumulate, workspace, workspace_bytes=None, stream=None):
     _check(lib().flexmoe_rms_norm_backward(ctypes.byref(desc), int(rows), _p(dy), _p(r), _p(w), _p(rstd), _p(dr), _p(dx), _p(dw),
                                            int(accumulate), _p(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)))
+
+
+def make_logprob_desc(V, top=0, dtype=FLEXMOE_BF16, max_rows=0, ld=0, temperature=1.0):
+    return flexmoe_logprob_desc(V, top, dtype, max_rows, ld, temperature)
+
+
+def flexmoe_token_logprobs_workspace_bytes(desc, rows: int) -> int:
+    n = lib().flexmoe_token_logprobs_workspace_bytes(ctypes.byref(desc), int(rows))
+    if n == 0:
+        raise FlexMoEError(-2, flexmoe_last_error())
+    return int(n)
+
+
+def flexmoe_token_logprobs(desc, rows, logits, tokens, logprob, entropy, lse, top_ids, top_logprobs, workspace, workspace_bytes=None,
+                           stream=None):
+    _check(lib().flexmoe_token_logprobs(ctypes.byref(desc), int(rows), _p(logits), _p(tokens), _p(logprob), _p(entropy), _p(lse),
+                                        _p(top_ids), _p(top_logprobs), _p(workspace), _nbytes(workspace, workspace_bytes),
+                                        _stream(stream)))
 
 
 _DTYPE_CODES = {}  # filled by the first call: the module does not import torch
@@ -1064,6 +1092,49 @@ class RMSNorm:
                                                    None if dw is None else _vector(dw, self.cols, self._f32, "dw"), int(accumulate),
                                                    *self._ws, _stream(stream)))
         return dx, dw
+
+
+class Logprobs(NamedTuple):
+    """Of each row: its token's log probability (None without tokens), entropy, log sum of exponentials, and the most likely tokens."""
+    logprob: object
+    entropy: object
+    lse: object
+    top_ids: object
+    top_logprobs: object
+
+
+class TokenLogprobs:
+    """Log probabilities of given tokens under rows of logits, with entropy and the `top` most likely tokens.
+
+    logits [R, V], bf16 or fp32, are divided by the temperature; tokens [R] int32.  It keeps the workspace for up to
+    max_rows rows: calls on different streams need holders of their own; threads may share one.
+    """
+
+    def __init__(self, V, max_rows, top=0, temperature=1.0, device="cuda"):
+        import torch
+        self.V, self.max_rows, self.top = V, max_rows, top
+        self._i32, self._f32 = torch.int32, torch.float32
+        self.desc = make_logprob_desc(V, top, FLEXMOE_BF16, max_rows, _pitch(V, 2), temperature)
+        self._desc = ctypes.byref(self.desc)
+        self.workspace = torch.empty(flexmoe_token_logprobs_workspace_bytes(self.desc, max_rows), dtype=torch.uint8, device=device)
+        self._ws = (self.workspace.data_ptr(), self.workspace.numel())
+        self._lock = threading.Lock()  # holds the descriptor's type and stride
+
+    def __call__(self, logits, tokens=None, stream=None) -> Logprobs:
+        if logits.dim() != 2:
+            raise ValueError("logits must be [R, %d], got %s" % (self.V, tuple(logits.shape)))
+        R, K, dt, d, dev = logits.shape[0], self.top, logits.dtype, self.desc, logits.device
+        values = _new((R * (3 + K),), self._f32, dev, stream)
+        logprob, entropy, lse, top = values.split((R, R, R, R * K))
+        ids, top = _new((R, K), self._i32, dev, stream), top.view(R, K)
+        with self._lock:
+            d.dtype, d.ld = _dtype_code(dt), _matrix(logits, (R, self.V), dt, "logits")
+            _check(lib().flexmoe_token_logprobs(self._desc, R, logits.data_ptr(),
+                                                None if tokens is None else _vector(tokens, R, self._i32, "tokens"),
+                                                None if tokens is None else logprob.data_ptr(), entropy.data_ptr(), lse.data_ptr(),
+                                                ids.data_ptr() if K else None, top.data_ptr() if K else None, *self._ws,
+                                                _stream(stream)))
+        return Logprobs(None if tokens is None else logprob, entropy, lse, ids, top)
 
 
 class ClippedWeights:

@@ -139,3 +139,46 @@ def test_norm_tensors():
         n.backward(x, x, torch.zeros(4), dw=torch.zeros(64), weight_grad=False)
     with pytest.raises(ValueError, match="dimension"):
         fm.RMSNorm(torch.ones(1, 64), 10)
+
+
+# ---- log probabilities --------------------------------------------------------
+def logprobs(**kw):
+    a = dict(V=1000, top=8, max_rows=100)
+    a.update(kw)
+    return fm.make_logprob_desc(**a)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(dtype=2), -5), (dict(V=0), -2), (dict(V=(1 << 21) + 8), -2), (dict(top=-1), -2), (dict(top=129), -2), (dict(V=8, top=9), -2),
+    (dict(max_rows=-1), -2), (dict(max_rows=(1 << 24) + 1), -2), (dict(V=1001), -2), (dict(ld=992), -2), (dict(ld=1004), -2), (dict(ld=(1 << 22) + 8), -2),
+    (dict(temperature=0.0), -1), (dict(temperature=-1.0), -1), (dict(temperature=1e7), -1), (dict(temperature=float("nan")), -1)])
+def test_logprobs_descriptor(kw, code):
+    D = logprobs(**kw)
+    assert code_of(fm.flexmoe_token_logprobs_workspace_bytes, D, 1) == -2
+    assert code_of(fm.flexmoe_token_logprobs, D, 1, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 1 << 30, 0) == code
+
+
+def test_logprobs_arguments():
+    def call(rows=10, D=logprobs(V=20000), logits=FAKE, tokens=FAKE, logprob=FAKE, entropy=FAKE, lse=FAKE, ids=FAKE, top=FAKE, ws=FAKE, nbytes=1 << 30):
+        fm.flexmoe_token_logprobs(D, rows, logits, tokens, logprob, entropy, lse, ids, top, ws, nbytes, 0)
+
+    for kw, code in [(dict(rows=-1), -1), (dict(rows=101), -2), (dict(logits=None), -1), (dict(tokens=None), -1), (dict(logprob=None), -1),
+                     (dict(entropy=None), -1), (dict(lse=None), -1), (dict(ids=None), -1), (dict(top=None), -1), (dict(D=logprobs(top=0)), -1),
+                     (dict(logits=FAKE + 8), -1), (dict(tokens=FAKE + 2), -1), (dict(top=FAKE + 1), -1), (dict(ws=None), -4), (dict(nbytes=300), -4),
+                     (dict(ws=FAKE + 64), -4)]:
+        assert code_of(call, **kw) == code, kw
+    call(rows=0, logits=None)
+
+
+def test_logprobs_workspace_serves_fewer_rows():
+    for V in (100, 5000, 131072, 300000):
+        sizes = [fm.flexmoe_token_logprobs_workspace_bytes(logprobs(V=V, ld=1 << 21, max_rows=1 << 20), n) for n in (0, 1, 2, 9, 64, 511, 512, 513, 5000, 1 << 20)]
+        assert sizes == sorted(sizes) and sizes[0] >= 256
+
+
+def test_logprobs_tensors():
+    h = fm.TokenLogprobs(64, 10, top=3, device="cpu")
+    x = torch.zeros(4, 64)
+    for bad in (x[0], x[:, :32], x.half(), x):  # the last is not on the GPU
+        with pytest.raises(ValueError):
+            h(bad)
