@@ -651,6 +651,51 @@ int flexmoe_token_logprobs(const flexmoe_logprob_desc *desc, int32_t rows, const
                            int32_t *top_ids, float *top_logprobs, void *workspace,
                            size_t workspace_bytes, void *stream);
 
+/* ---- Distillation from a teacher's top log probabilities --------------------
+ * The recovery objective on the logits (Eq. 12), for rows of the student's
+ * logits l [rows][ld] (dtype) over V tokens.  A row of the teacher is a list of
+ * `top` tokens, ids [rows][top] int32, with their log probabilities logprobs
+ * [rows][top] fp32 at the temperature t (what flexmoe_token_logprobs lists).  With
+ * q = softmax(l / t) and q1 = softmax(l):
+ *   tail = 0: p = the listed probabilities divided by their sum (logits over t
+ *             do as well), KL = sum p (log p - log q)
+ *   tail = 1: p = the listed probabilities, p_rest = max(0, 1 - sum p) and
+ *             q_rest = the q of all tokens that are not listed as one more class,
+ *             KL = sum p (log p - log q) + p_rest (log p_rest - log q_rest)
+ *   CE = -log q1[label]    (labels [rows] int32, or NULL; a label outside [0, V): 0)
+ *   kl, ce [rows] fp32: KL and CE of each row
+ *   dlogits [rows][ldd] (dtype; NULL: not wanted) the gradient of
+ *     sum over rows of row_scale (kl_weight t^2 KL + ce_weight CE)
+ *   row_scale [rows] fp32, or NULL for 1.  A row whose scale is 0 (padding) is not
+ *   read, has losses of 0 and a gradient of zeros.
+ * An id outside [0, V) is left out (a shorter list), and so is a token that the
+ * list names again; a log probability of -inf is a probability of 0.  A row
+ * without teacher (tail = 0, nothing listed) has KL 0 and no gradient from it.
+ * Logits of -inf are masked tokens: KL and CE are inf where the teacher or the
+ * label is on one, or where the teacher leaves more than 1e-5 and no token but
+ * the listed ones has a probability.  Rows with a NaN or +inf give NaN; a row of
+ * nothing but -inf gets gradients of 0.  Deterministic.
+ * The listed tokens' logarithms and p are in 64 bits, sums over V in fp32.
+ * dlogits may be logits itself (with ldd = ld).  Shapes (FLEXMOE_ESHAPE
+ * otherwise): 1 <= V <= 2^21, 1 <= top <= 128; ld and ldd as
+ * flexmoe_token_logprobs' ld; nothing past V is written; 0 <= rows <= max_rows <=
+ * 2^24; temperature from 1e-6 to 1e6.  The workspace (256-byte aligned) of
+ * flexmoe_distill_workspace_bytes(desc, rows) serves every smaller call of the same
+ * V and top. */
+typedef struct flexmoe_distill_desc {
+    int32_t V, top;
+    int32_t dtype;      /* flexmoe_dtype of logits and dlogits                   */
+    int32_t max_rows;
+    int32_t tail;
+    int32_t ld, ldd;
+    float temperature, kl_weight, ce_weight;
+} flexmoe_distill_desc;
+size_t flexmoe_distill_workspace_bytes(const flexmoe_distill_desc *desc, int32_t rows);
+int flexmoe_distill(const flexmoe_distill_desc *desc, int32_t rows, const void *logits,
+                    const int32_t *ids, const float *logprobs, const int32_t *labels,
+                    const float *row_scale, float *kl, float *ce, void *dlogits, void *workspace,
+                    size_t workspace_bytes, void *stream);
+
 /* k = ceil(r * I) for a retention ratio r in [0, 1] (Sec. 3.1).  A slack of
  * 1e-9 absorbs the binary representation error of decimal ratios (0.7 * 1000
  * gives 700).  Returns -1 for r outside [0, 1], NaN, or I < 1. */

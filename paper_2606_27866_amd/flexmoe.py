@@ -44,7 +44,8 @@ EXPORTED = ("flexmoe_workspace_bytes", "flexmoe_rank_reorder", "flexmoe_set_budg
             "flexmoe_quantized_forward", "flexmoe_adamw_step", "flexmoe_adamw_read_state",
             "flexmoe_route_workspace_bytes", "flexmoe_route", "flexmoe_route_backward",
             "flexmoe_rms_norm", "flexmoe_rms_norm_workspace_bytes", "flexmoe_rms_norm_backward",
-            "flexmoe_token_logprobs_workspace_bytes", "flexmoe_token_logprobs")
+            "flexmoe_token_logprobs_workspace_bytes", "flexmoe_token_logprobs",
+            "flexmoe_distill_workspace_bytes", "flexmoe_distill")
 
 # kernel indices of flexmoe_kernel_times
 KERNELS = ("route", "dispatch_scan", "dispatch_scatter", "gate_up", "down", "combine",
@@ -103,6 +104,11 @@ class flexmoe_norm_desc(ctypes.Structure):
 
 class flexmoe_logprob_desc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("V", "top", "dtype", "max_rows", "ld")] + [("temperature", ctypes.c_float)]
+
+
+class flexmoe_distill_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("V", "top", "dtype", "max_rows", "tail", "ld", "ldd")] + \
+               [(n, ctypes.c_float) for n in ("temperature", "kl_weight", "ce_weight")]
 
 
 class flexmoe_action_set(ctypes.Structure):
@@ -216,6 +222,11 @@ def lib():
         L.flexmoe_token_logprobs_workspace_bytes.restype = sz
         L.flexmoe_token_logprobs.argtypes = [LD, i32] + [vp] * 8 + [sz, vp]
         L.flexmoe_token_logprobs.restype = ctypes.c_int
+        DD = ctypes.POINTER(flexmoe_distill_desc)
+        L.flexmoe_distill_workspace_bytes.argtypes = [DD, i32]
+        L.flexmoe_distill_workspace_bytes.restype = sz
+        L.flexmoe_distill.argtypes = [DD, i32] + [vp] * 9 + [sz, vp]
+        L.flexmoe_distill.restype = ctypes.c_int
         L.flexmoe_keep_from_ratio.argtypes = [ctypes.c_double, i32]
         L.flexmoe_keep_from_ratio.restype = ctypes.c_int
         L.flexmoe_timing_enable.argtypes = [ctypes.c_int]
@@ -575,6 +586,22 @@ def flexmoe_token_logprobs(desc, rows, logits, tokens, logprob, entropy, lse, to
     _check(lib().flexmoe_token_logprobs(ctypes.byref(desc), int(rows), _p(logits), _p(tokens), _p(logprob), _p(entropy), _p(lse),
                                         _p(top_ids), _p(top_logprobs), _p(workspace), _nbytes(workspace, workspace_bytes),
                                         _stream(stream)))
+
+
+def make_distill_desc(V, top, dtype=FLEXMOE_BF16, max_rows=0, tail=0, ld=0, ldd=0, temperature=1.0, kl_weight=1.0, ce_weight=0.0):
+    return flexmoe_distill_desc(V, top, dtype, max_rows, tail, ld, ldd, temperature, kl_weight, ce_weight)
+
+
+def flexmoe_distill_workspace_bytes(desc, rows: int) -> int:
+    n = lib().flexmoe_distill_workspace_bytes(ctypes.byref(desc), int(rows))
+    if n == 0:
+        raise FlexMoEError(-2, flexmoe_last_error())
+    return int(n)
+
+
+def flexmoe_distill(desc, rows, logits, ids, logprobs, labels, row_scale, kl, ce, dlogits, workspace, workspace_bytes=None, stream=None):
+    _check(lib().flexmoe_distill(ctypes.byref(desc), int(rows), _p(logits), _p(ids), _p(logprobs), _p(labels), _p(row_scale), _p(kl), _p(ce),
+                                 _p(dlogits), _p(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)))
 
 
 _DTYPE_CODES = {}  # filled by the first call: the module does not import torch
@@ -1135,6 +1162,52 @@ class TokenLogprobs:
                                                 ids.data_ptr() if K else None, top.data_ptr() if K else None, *self._ws,
                                                 _stream(stream)))
         return Logprobs(None if tokens is None else logprob, entropy, lse, ids, top)
+
+
+class Distillation:
+    """KL to a teacher's top log probabilities and cross entropy of labels, of each row, and the logits' gradient.
+
+    ids and logprobs [R, top] are a teacher's list at the temperature (TokenLogprobs gives one; -1 fills a shorter list);
+    the loss is the sum over rows of row_scale (kl_weight temperature^2 kl + ce_weight ce).  tail: what the list leaves is
+    one more class, else its probabilities are renormalised.  It keeps the workspace for up to max_rows rows: calls on
+    different streams need holders of their own; threads may share one.
+    """
+
+    def __init__(self, V, top, max_rows, temperature=1.0, tail=False, kl_weight=1.0, ce_weight=0.0, device="cuda"):
+        import torch
+        self.V, self.top, self.max_rows = V, top, max_rows
+        self._i32, self._f32 = torch.int32, torch.float32
+        self.desc = make_distill_desc(V, top, FLEXMOE_BF16, max_rows, int(tail), _pitch(V, 2), _pitch(V, 2), temperature, kl_weight, ce_weight)
+        self._desc = ctypes.byref(self.desc)
+        self.workspace = torch.empty(flexmoe_distill_workspace_bytes(self.desc, max_rows), dtype=torch.uint8, device=device)
+        self._ws = (self.workspace.data_ptr(), self.workspace.numel())
+        self._lock = threading.Lock()  # holds the descriptor's type and strides
+
+    def forward(self, logits, ids, logprobs, labels=None, row_scale=None, stream=None):
+        """(kl, ce) of each row; rows whose row_scale is 0 are not read."""
+        return self._run(logits, ids, logprobs, labels, row_scale, False, None, stream)[:2]
+
+    def gradient(self, logits, ids, logprobs, labels=None, row_scale=None, dlogits=None, stream=None):
+        """(kl, ce, dlogits), dlogits the loss's gradient; it may be logits itself."""
+        return self._run(logits, ids, logprobs, labels, row_scale, True, dlogits, stream)
+
+    def _run(self, logits, ids, logprobs, labels, row_scale, grad, dlogits, stream):
+        if logits.dim() != 2:
+            raise ValueError("logits must be [R, %d], got %s" % (self.V, tuple(logits.shape)))
+        R, K, dt, d, dev = logits.shape[0], self.top, logits.dtype, self.desc, logits.device
+        shape = (R, self.V)
+        kl, ce = _new((2, R), self._f32, dev, stream)
+        if grad and dlogits is None:
+            dlogits = _padded(shape, dt, dev, stream)
+        with self._lock:
+            d.dtype, d.ld = _dtype_code(dt), _matrix(logits, shape, dt, "logits")
+            d.ldd = _matrix(dlogits, shape, dt, "dlogits") if grad else d.ld
+            _check(lib().flexmoe_distill(self._desc, R, logits.data_ptr(), _vector(ids, R * K, self._i32, "ids"),
+                                         _vector(logprobs, R * K, self._f32, "logprobs"),
+                                         None if labels is None else _vector(labels, R, self._i32, "labels"),
+                                         None if row_scale is None else _vector(row_scale, R, self._f32, "row_scale"), kl.data_ptr(),
+                                         ce.data_ptr(), dlogits.data_ptr() if grad else None, *self._ws, _stream(stream)))
+        return kl, ce, dlogits
 
 
 class ClippedWeights:

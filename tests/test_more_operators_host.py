@@ -182,3 +182,48 @@ def test_logprobs_tensors():
     for bad in (x[0], x[:, :32], x.half(), x):  # the last is not on the GPU
         with pytest.raises(ValueError):
             h(bad)
+
+
+# ---- distillation -------------------------------------------------------------
+def distill(**kw):
+    a = dict(V=1000, top=8, max_rows=100)
+    a.update(kw)
+    return fm.make_distill_desc(**a)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(dtype=2), -5), (dict(V=0), -2), (dict(V=(1 << 21) + 8), -2), (dict(top=0), -2), (dict(top=129), -2), (dict(max_rows=-1), -2),
+    (dict(max_rows=(1 << 24) + 1), -2), (dict(V=1001), -2), (dict(ld=992), -2), (dict(ldd=1004), -2), (dict(ldd=(1 << 22) + 8), -2),
+    (dict(temperature=0.0), -1), (dict(temperature=float("inf")), -1), (dict(tail=2), -1), (dict(kl_weight=float("nan")), -1),
+    (dict(ce_weight=float("inf")), -1)])
+def test_distill_descriptor(kw, code):
+    D = distill(**kw)
+    assert code_of(fm.flexmoe_distill_workspace_bytes, D, 1) == -2
+    assert code_of(fm.flexmoe_distill, D, 1, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 1 << 40, 0) == code
+
+
+def test_distill_arguments():
+    def call(rows=10, D=distill(), logits=FAKE, ids=FAKE, lp=FAKE, labels=None, scale=None, kl=FAKE, ce=FAKE, d=None, ws=FAKE, nbytes=1 << 30):
+        fm.flexmoe_distill(D, rows, logits, ids, lp, labels, scale, kl, ce, d, ws, nbytes, 0)
+
+    for kw, code in [(dict(rows=-1), -1), (dict(rows=101), -2), (dict(logits=None), -1), (dict(ids=None), -1), (dict(lp=None), -1),
+                     (dict(kl=None), -1), (dict(ce=None), -1), (dict(logits=FAKE + 8), -1), (dict(d=FAKE + 4), -1), (dict(ids=FAKE + 2), -1),
+                     (dict(labels=FAKE + 2), -1), (dict(scale=FAKE + 1), -1), (dict(d=FAKE, D=distill(ldd=1008)), -1), (dict(ws=None), -4),
+                     (dict(nbytes=300), -4), (dict(ws=FAKE + 64), -4)]:
+        assert code_of(call, **kw) == code, kw
+    call(rows=0, logits=None)
+
+
+def test_distill_workspace_serves_fewer_rows():
+    for V in (100, 5000, 131072, 300000):
+        sizes = [fm.flexmoe_distill_workspace_bytes(distill(V=V, ld=1 << 21, ldd=1 << 21, max_rows=1 << 20), n)
+                 for n in (0, 1, 2, 9, 64, 511, 512, 513, 5000, 1 << 20)]
+        assert sizes == sorted(sizes) and sizes[0] >= 256
+
+
+def test_distill_tensors():
+    h = fm.Distillation(64, 3, 10, device="cpu")
+    x, ids, lp = torch.zeros(4, 64), torch.zeros(4, 3, dtype=torch.int32), torch.zeros(4, 3)
+    for bad in (x[0], x[:, :32], x.half(), x):  # the last is not on the GPU
+        with pytest.raises(ValueError):
+            h.forward(bad, ids, lp)
