@@ -555,8 +555,8 @@ int flexmoe_adamw_read_state(int64_t n, const void *m, const void *v, const floa
  * (FLEXMOE_ESHAPE otherwise): 1 <= E <= 256, 1 <= top_k <= min(E, 16), groups at
  * most 64 and dividing E, top_k <= top_groups E / groups; strides (elements, 0 =
  * packed) from E to 2^21; 0 <= T <= max_tokens, max_tokens (top_k + 1) <= 2^30.
- * The workspace (256-byte aligned; flexmoe_route_workspace_bytes, the same for
- * every T) is needed for the tables of more than a few tokens. */
+ * The workspace (256-byte aligned; flexmoe_route_workspace_bytes(desc, T) bytes
+ * serve every smaller T) is needed for the tables of more than a few tokens. */
 enum { FLEXMOE_SOFTMAX = 0, FLEXMOE_SIGMOID = 1 };
 typedef struct flexmoe_router_desc {
     int32_t E, top_k;

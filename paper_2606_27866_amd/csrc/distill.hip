@@ -133,10 +133,7 @@ __global__ __launch_bounds__(kVT) void distill_sums_kernel(const DistillArgs a) 
     const int begin = p * a.length, end = min(a.V, begin + a.length);
     if constexpr (kTail) map_listed(bits, a.ids + row * a.K, a.K, begin, end);
     TwoSums<kTwo> sums;
-    for (int at = begin; at < end; at += W::step) {
-        float v[W::units][W::n];
-#pragma unroll
-        for (int u = 0; u < W::units; ++u) load_values<kBf16>(logits, at + u * W::run + t * W::n, end, v[u]);
+    each_step<kBf16>(logits, begin, end, [&](int, int at, float (&v)[W::units][W::n]) {
         float gm = -INFINITY;
 #pragma unroll
         for (int u = 0; u < W::units; ++u) gm = max_of(v[u], gm);
@@ -149,7 +146,7 @@ __global__ __launch_bounds__(kVT) void distill_sums_kernel(const DistillArgs a) 
 #pragma unroll
             for (int k = 0; k < W::n; ++k) sums.add(v[u][k], a.c);
         }
-    }
+    });
     sums.settle(a.c);
     TwoSums<kTwo> all = join_threads(sums, a.c, part);
     if (!(all.s < 3.0e38f && all.s1 < 3.0e38f) && all.m > -INFINITY && all.m < INFINITY) {
@@ -347,45 +344,40 @@ __global__ __launch_bounds__(kVT) void distill_grad_kernel(const DistillArgs a) 
     char* const out = reinterpret_cast<char*>(a.dlogits) + row * a.ldd * elem_size<kBf16>();
     const int begin = p * a.length, end = min(a.V, begin + a.length);
     const float m = a.factors[4 * row], f = a.factors[4 * row + 1], f1 = kTwo ? a.factors[4 * row + 2] : 0.f;
-    const bool zero = f == 0.f && f1 == 0.f;  // padding is not read
-    for (int at = begin; at < end; at += W::step) {
-        float v[W::units][W::n];
-        if (!zero) {
+    auto write = [&](int i, const u32x4& w) {
+        if (i + W::n <= end) {
+            *reinterpret_cast<u32x4*>(out + (size_t)i * elem_size<kBf16>()) = w;
+        } else {
 #pragma unroll
-            for (int u = 0; u < W::units; ++u) load_values<kBf16>(logits, at + u * W::run + t * W::n, end, v[u]);
+            for (int k = 0; k < W::n - 1; ++k)
+                if (i + k < end) {
+                    if constexpr (kBf16) reinterpret_cast<bf16_t*>(out)[i + k] = (bf16_t)(w[k >> 1] >> (16 * (k & 1)));
+                    else reinterpret_cast<uint32_t*>(out)[i + k] = w[k];
+                }
         }
+    };
+    const bool zero = f == 0.f && f1 == 0.f;  // padding, which is not read, or nothing off the list
+    if (zero)
+        for (int i = begin + t * W::n; i < end; i += W::run) write(i, u32x4{0, 0, 0, 0});
+    each_step<kBf16>(logits, begin, zero ? begin : end, [&](int, int at, float (&v)[W::units][W::n]) {
 #pragma unroll
         for (int u = 0; u < W::units; ++u) {
             const int i = at + u * W::run + t * W::n;
-            if (i >= end) continue;
-            u32x4 w = {0, 0, 0, 0};
-            if (!zero) {
 #pragma unroll
-                for (int k = 0; k < W::n; ++k) {
-                    float g = f * exp2_fast((v[u][k] - m) * a.c);
-                    if constexpr (kTwo) g = fmaf(f1, exp2_fast((v[u][k] - m) * kLog2E), g);
-                    v[u][k] = g;
-                }
-                if constexpr (kBf16) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) w[k] = pack_bf16x2(v[u][2 * k], v[u][2 * k + 1]);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) w[k] = __float_as_uint(v[u][k]);
-                }
+            for (int k = 0; k < W::n; ++k) {
+                float g = f * exp2_fast((v[u][k] - m) * a.c);
+                if constexpr (kTwo) g = fmaf(f1, exp2_fast((v[u][k] - m) * kLog2E), g);
+                v[u][k] = g;
             }
-            if (i + W::n <= end) {
-                *reinterpret_cast<u32x4*>(out + (size_t)i * elem_size<kBf16>()) = w;
-            } else {
+            u32x4 w;
 #pragma unroll
-                for (int k = 0; k < W::n - 1; ++k)
-                    if (i + k < end) {
-                        if constexpr (kBf16) reinterpret_cast<bf16_t*>(out)[i + k] = (bf16_t)(w[k >> 1] >> (16 * (k & 1)));
-                        else reinterpret_cast<uint32_t*>(out)[i + k] = w[k];
-                    }
+            for (int k = 0; k < 4; ++k) {
+                if constexpr (kBf16) w[k] = pack_bf16x2(v[u][2 * k], v[u][2 * k + 1]);
+                else w[k] = __float_as_uint(v[u][k]);
             }
+            if (i < end) write(i, w);
         }
-    }
+    });
     __syncthreads();  // the listed tokens' gradients go over what was written there
     for (int k = t; k <= a.K; k += kVT) {
         const int2 mark = a.marks[row * (a.K + 1) + k];

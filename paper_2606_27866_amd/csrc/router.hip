@@ -16,13 +16,16 @@
 // their order), else on scores in 64 bits.  Weights are in fp32, the normalised
 // ones from differences of log scores, which neither overflow nor vanish.
 //
-//   route_kernel         one wave per token; a histogram for each chunk of tokens
-//   route_tables_kernel  every chunk sums the histograms before its own (and all
-//                        of them, for the experts' starts), then places its
-//                        tokens: stable, and no atomic's order is in a result
+//   route_kernel         one wave per token; a histogram for each few tokens
+//   route_tables_kernel  every chunk of tokens sums the histograms before its own
+//                        (and all of them, for the experts' starts), then places
+//                        its tokens: stable, and no atomic's order is in a result
 //   both in one workgroup for few tokens
 //
-// Latency and instructions, not bytes, bound these launches.
+// Latency and instructions, not bytes, bound these launches.  So scores are first
+// taken in 32 bits: where the chosen ones and the best of the others (groups too)
+// are further apart than those can be wrong, the order is the exact one, and only
+// the other tokens (1 in 1000 of usual logits) are routed again in 64 bits.
 #include <algorithm>
 #include <cmath>
 
@@ -35,7 +38,9 @@ using namespace flexmoe;
 namespace {
 
 constexpr int kWaves = 16, kThreads = 64 * kWaves;
-constexpr int kChunks = 128;      // chunks of tokens, at most (a workgroup of route_tables_kernel reads all their histograms)
+constexpr int kChunks = 128;      // chunks of tokens, at most: workgroups of route_tables_kernel, which read all histograms
+constexpr int kHistograms = 256;  // wanted number of those
+constexpr int kMostCounted = 240; // tokens of one: its counts are bytes
 constexpr int kOneWorkgroup = 16; // tokens up to which one workgroup does it all
 constexpr int kMaxGroups = 64;
 constexpr int kQ = kMaxExperts / 64;
@@ -45,9 +50,11 @@ struct RouteArgs {
     const float* bias;
     int32_t *idx, *counts, *offsets, *perm, *pos;
     float* w;
-    int32_t* hist;  // [chunks][E]
+    uint32_t* hist;  // [histograms][words]: a byte for each expert
     size_t ldl;
-    int T, E, k, sigmoid, normalize, groups, top_groups, best, chunk;
+    int T, E, k, bf16, sigmoid, normalize, groups, top_groups, best;
+    int counted, chunk;  // tokens of a histogram, and of a workgroup of the tables (a multiple)
+    int words;
     float scale;
 };
 
@@ -65,15 +72,6 @@ __device__ __forceinline__ uint64_t score_key(double c) {
     return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
 }
 
-__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        const uint64_t u = (uint64_t)__shfl_xor((unsigned long long)v, o, 64);
-        v = u > v ? u : v;
-    }
-    return v;
-}
-
 __device__ __forceinline__ float wave_max_f(float v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
@@ -89,61 +87,86 @@ __device__ __forceinline__ double wave_sum_d(double v) {
 __device__ __forceinline__ float log_sigmoid(float x) { return fminf(x, 0.f) - log1pf(expf(-fabsf(x))); }
 
 struct RouteScratch {
-    double c[kMaxExperts];
+    double c[kMaxExperts];  // scores in 64 bits, or the first half in 32
+    float v[kMaxExperts];   // logits
 };
 
-// One wave routes one token, whose logits are in v (expert lane + 64 q; -inf past E):
-// lane j < k gets the j-th chosen expert (-1: none) and its weight.
-__device__ void route_token(const RouteArgs& a, const float (&v)[kQ], int lane, RouteScratch& rs, int& my_id, float& my_w) {
-    const bool exact = a.bias || (a.groups > 1 && a.best > 1);  // scores decide, else logits
-    float top = -INFINITY;
-    bool nan = false;
+// Largest of the wave's keys, in every lane.
+__device__ __forceinline__ uint32_t wave_max_u(uint32_t v) {
+#define FLEXMOE_USTEP(C, M) v = max(v, (uint32_t)dpp_shift<C, M>((int)v))
+    FLEXMOE_USTEP(0x111, 0xf);
+    FLEXMOE_USTEP(0x112, 0xf);
+    FLEXMOE_USTEP(0x114, 0xf);
+    FLEXMOE_USTEP(0x118, 0xf);
+    FLEXMOE_USTEP(0x142, 0xa);
+    FLEXMOE_USTEP(0x143, 0xc);
+#undef FLEXMOE_USTEP
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+
+// Order of values that are no NaN as whole numbers: -inf (masked) 0.
+__device__ __forceinline__ uint32_t key32(float c) {
+    const uint32_t u = __float_as_uint(c + 0.f);  // -0 + 0 = 0
+    return c == -INFINITY ? 0u : (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+__device__ __forceinline__ float key32_value(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
+
+// Largest of the wave's keys, in every lane: upper halves first.
+__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
+    const uint32_t hi = wave_max_u((uint32_t)(v >> 32));
+    const uint32_t lo = wave_max_u((uint32_t)(v >> 32) == hi ? (uint32_t)v : 0u);
+    return ((uint64_t)hi << 32) | lo;
+}
+
+// The score of a logit without its bias, in 64 bits; top and z: of the softmax.
+__device__ __forceinline__ double exact_score(const RouteArgs& a, float v, double top, double z) {
+    return a.sigmoid ? 1.0 / (1.0 + exp(-(double)v)) : exp((double)v - top) / z;
+}
+
+template <int NQ>
+__device__ __forceinline__ double exact_sum(const float (&v)[NQ], float top) {
+    double z = 0.0;
 #pragma unroll
-    for (int q = 0; q < kQ; ++q) {
-        top = fmaxf(top, v[q]);
-        nan |= __builtin_isnan(v[q]);
+    for (int q = 0; q < NQ; ++q) z += v[q] == -INFINITY ? 0.0 : exp((double)v[q] - (double)top);
+    return wave_sum_d(z);
+}
+
+// The choice of one token by one wave, in 64 bits, from its logits v (expert lane NQ + q;
+// -inf past E): lane j < k gets the j-th chosen expert (-1: none).
+template <int NQ>
+__device__ __forceinline__ int choose_exact(const RouteArgs& a, const float (&v)[NQ], int lane, RouteScratch& rs) {
+    const bool by_score = a.bias || (a.groups > 1 && a.best > 1);  // scores decide, else logits
+    double z = 1.0, c[NQ];
+    float top = 0.f;
+    if (by_score && !a.sigmoid) {
+        top = v[0];
+#pragma unroll
+        for (int q = 1; q < NQ; ++q) top = fmaxf(top, v[q]);
+        top = wave_max_f(top);
+        z = exact_sum<NQ>(v, top);
     }
-    top = wave_max_f(top);
-    const bool any_nan = __any(nan);
-    double c[kQ];
-    if (!exact) {
 #pragma unroll
-        for (int q = 0; q < kQ; ++q) c[q] = v[q];
-    } else {
-        double z = 0.0;
-#pragma unroll
-        for (int q = 0; q < kQ; ++q) {
-            if (a.sigmoid) c[q] = 1.0 / (1.0 + exp(-(double)v[q]));
-            else z += c[q] = v[q] == -INFINITY ? 0.0 : exp((double)v[q] - (double)top);
-        }
-        if (!a.sigmoid) {
-            z = wave_sum_d(z);
-#pragma unroll
-            for (int q = 0; q < kQ; ++q) c[q] /= z;
-        }
-#pragma unroll
-        for (int q = 0; q < kQ; ++q) {
-            const int e = lane + 64 * q;
-            if (a.bias && e < a.E) c[q] += (double)a.bias[e];
+    for (int q = 0; q < NQ; ++q) {
+        c[q] = v[q];
+        if (by_score) {
+            c[q] = exact_score(a, v[q], (double)top, z);
+            if (a.bias) c[q] += (double)a.bias[min(lane * NQ + q, a.E - 1)];
             if (v[q] == -INFINITY) c[q] = -INFINITY;
         }
     }
-    uint64_t key[kQ];
-#pragma unroll
-    for (int q = 0; q < kQ; ++q) key[q] = score_key(c[q]);
+    uint64_t kept = ~0ull;
+    const int members = a.E / a.groups;
     if (a.groups > 1) {
-        const int size = a.E / a.groups;
 #pragma unroll
-        for (int q = 0; q < kQ; ++q)
-            if (lane + 64 * q < a.E) rs.c[lane + 64 * q] = c[q];
+        for (int q = 0; q < NQ; ++q) rs.c[lane * NQ + q] = c[q];
         __builtin_amdgcn_wave_barrier();
         __atomic_signal_fence(__ATOMIC_SEQ_CST);
         uint64_t group = 0;
         if (lane < a.groups) {
             double c1 = -INFINITY, c2 = -INFINITY;
             uint64_t k1 = 0, k2 = 0;
-            for (int i = 0, j = lane % size; i < size; ++i, j = j + 1 == size ? 0 : j + 1) {
-                const double x = rs.c[lane * size + j];
+            for (int i = 0, j = lane % members; i < members; ++i, j = j + 1 == members ? 0 : j + 1) {
+                const double x = rs.c[lane * members + j];
                 const uint64_t kx = score_key(x);
                 if (kx > k1) k2 = k1, c2 = c1, k1 = kx, c1 = x;
                 else if (kx > k2) k2 = kx, c2 = x;
@@ -152,105 +175,305 @@ __device__ void route_token(const RouteArgs& a, const float (&v)[kQ], int lane, 
         }
         __builtin_amdgcn_wave_barrier();
         __atomic_signal_fence(__ATOMIC_SEQ_CST);
-        int better = 0;
-        for (int g = 0; g < a.groups; ++g) {
-            const uint64_t other = (uint64_t)__shfl((unsigned long long)group, g, 64);
-            better += other > group || (other == group && g < lane);
+        kept = 0;
+        for (int j = 0; j < a.top_groups; ++j) {
+            const uint64_t m = wave_max(group);
+            if (m == 0) break;
+            const uint64_t all = __ballot(group == m), first = all & -all;
+            kept |= first;
+            if ((first >> lane) & 1) group = 0;
         }
-        const uint64_t kept = __ballot(lane < a.groups && better < a.top_groups);
-#pragma unroll
-        for (int q = 0; q < kQ; ++q)
-            if (!((kept >> ((lane + 64 * q) / size & 63)) & 1)) key[q] = 0;
     }
-    my_id = -1;
-    float my_logit = -INFINITY;
+    uint64_t key[NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        const int e = lane * NQ + q;
+        key[q] = a.groups == 1 || (e < a.E && ((kept >> (e / members)) & 1)) ? score_key(c[q]) : 0;
+    }
+    int my_id = -1;
     for (int j = 0; j < a.k; ++j) {
-        uint64_t m = 0;
+        uint64_t best = key[0];
+        int at = lane * NQ;
 #pragma unroll
-        for (int q = 0; q < kQ; ++q) m = key[q] > m ? key[q] : m;
-        m = wave_max(m);
+        for (int q = 1; q < NQ; ++q)
+            if (key[q] > best) best = key[q], at = lane * NQ + q;  // the lower place of equal ones
+        const uint64_t m = wave_max(best);
         if (m == 0) break;
-        int id = -1;
-        float logit = 0.f;
+        const int from = __ffsll((unsigned long long)__ballot(best == m)) - 1;
+        const int id = __builtin_amdgcn_readlane(at, from);
+        if (lane == j) my_id = id;
 #pragma unroll
-        for (int q = kQ - 1; q >= 0; --q) {
-            const uint64_t has = __ballot(key[q] == m);
-            if (has) {  // the last q that has it is the lowest
-                id = 64 * q + __ffsll((unsigned long long)has) - 1;
-                logit = __shfl(v[q], id & 63, 64);
+        for (int q = 0; q < NQ; ++q)
+            if (lane * NQ + q == id) key[q] = 0;
+    }
+    return my_id;
+}
+
+// Whether two scores of 32 bits, a >= b, may stand in another order than the exact
+// ones.  A score is off by at most 16 units of 2^-24 of itself (difference, exp, a sum
+// of 256, quotient), with its bias by one of the sum more; `bias` is the sum of both
+// values' largest possible biases, so that the scores are at most |a| + |b| + bias.
+__device__ __forceinline__ bool too_near(float a, float b, float bias) { return a - b <= 20.f * 0x1p-24f * (fabsf(a) + fabsf(b) + bias); }
+
+__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
+// x's relative error in the exponent weighs s (1 - s) |x| < 0.3 in s: 4 units of 2^-24 with exp, sum and reciprocal
+__device__ __forceinline__ float sigmoid_fast(float x) { return __builtin_amdgcn_rcpf(1.f + exp_fast(-x)); }
+
+// What decides: the logits themselves, or scores, with a bias or in sums of a group's two best.
+enum { kByLogits = 0, kBySigmoid = 1, kBySoftmax = 2 };
+
+// The choice of one token, whose logits are in v (expert lane NQ + q; -inf past E), also
+// in rs.v, from values of 32 bits; `unsure`: they do not tell.
+template <int NQ, int kBy, bool kGroups>
+__device__ __forceinline__ int choose_fast(const RouteArgs& a, const float (&v)[NQ], int lane, RouteScratch& rs, float top, bool& unsure) {
+    float c[NQ], bias = 0.f;
+    bool again = false;
+    if constexpr (kBy == kByLogits) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) c[q] = v[q], again |= __builtin_isnan(v[q]);
+    } else {
+        float z = 0.f;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            if constexpr (kBy == kBySigmoid) c[q] = sigmoid_fast(v[q]);
+            else z += c[q] = v[q] == -INFINITY ? 0.f : expf(v[q] - top);
+        }
+        if constexpr (kBy == kBySoftmax) {
+            const float inv = 1.f / wave_total_f(z);
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) c[q] *= inv;
+        }
+        if (a.bias) {
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) {
+                const float b = a.bias[min(lane * NQ + q, a.E - 1)];
+                bias = fmaxf(bias, b > -INFINITY ? 2.f * fabsf(b) : 0.f);
+                c[q] += b;
             }
+            bias = __uint_as_float(wave_max_u(__float_as_uint(bias)));  // not negative: ordered as its bits
         }
 #pragma unroll
-        for (int q = 0; q < kQ; ++q)
-            if (lane + 64 * q == id) key[q] = 0;
-        if (lane == j) my_id = id, my_logit = logit;
+        for (int q = 0; q < NQ; ++q) {
+            c[q] = v[q] == -INFINITY ? -INFINITY : c[q];
+            again |= !(c[q] < INFINITY);  // NaN, or +inf from a bias
+        }
     }
+    unsure = __any(again);
+    if (unsure) return -1;
+    uint32_t key[NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) key[q] = key32(c[q]);
+    if constexpr (kGroups) {
+        float* const sc = reinterpret_cast<float*>(rs.c);
+        if constexpr (kBy != kByLogits) {
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) sc[lane * NQ + q] = c[q];
+            __builtin_amdgcn_wave_barrier();
+            __atomic_signal_fence(__ATOMIC_SEQ_CST);
+        }
+        const float* const of_group = kBy == kByLogits ? rs.v : sc;
+        // `share` lanes for each group
+        const int members = a.E / a.groups, share = 1 << (31 - __builtin_clz(64 / a.groups)), g = lane / share;
+        float c1 = -INFINITY, c2 = -INFINITY;
+        if (g < a.groups)
+#pragma unroll 4
+            for (int i = lane & (share - 1); i < members; i += share) {
+                const float x = of_group[g * members + i];
+                c2 = fmaxf(c2, fminf(c1, x));
+                c1 = fmaxf(c1, x);
+            }
+        __builtin_amdgcn_wave_barrier();
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);
+        for (int o = 1; o < share; o <<= 1) {
+            const float d1 = __shfl_xor(c1, o, 64), d2 = __shfl_xor(c2, o, 64);
+            c2 = fmaxf(fmaxf(c2, d2), fminf(c1, d1));
+            c1 = fmaxf(c1, d1);
+        }
+        const float score = kBy != kByLogits && a.best > 1 && c2 > -INFINITY ? c1 + c2 : c1;
+        uint32_t group = g < a.groups && (lane & (share - 1)) == 0 ? key32(score) : 0u;
+        // the best groups, one after another
+        uint64_t kept = 0;  // bit g share
+        uint32_t last = 0;
+        for (int j = 0; j < a.top_groups; ++j) {
+            const uint32_t m = wave_max_u(group);
+            if (m == 0) break;
+            const uint64_t all = __ballot(group == m), first = all & -all;
+            kept |= first;
+            if ((first >> lane) & 1) group = 0;
+            last = m;
+        }
+        if constexpr (kBy != kByLogits) {
+            const uint32_t next = wave_max_u(group);
+            if (next) unsure |= too_near(key32_value(last), key32_value(next), 2.f * bias);
+        }
+        // lane NQ + q is in group (lane NQ + q) / members: the product is exact below 2^16
+        const uint32_t inv = (65536 + members - 1) / members;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            const uint32_t of = ((uint32_t)(lane * NQ + q) * inv) >> 16;
+            if (!((kept >> ((of * share) & 63)) & 1)) key[q] = 0;  // past E all keys are 0
+        }
+    }
+    // each lane's keys in order, the lower place first among equal ones
+    uint32_t place[NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) place[q] = lane * NQ + q;
+    auto order = [&](int i, int j) {
+        const bool swap = key[i] < key[j];
+        const uint32_t x = key[i], y = place[i];
+        key[i] = swap ? key[j] : x, place[i] = swap ? place[j] : y;
+        key[j] = swap ? x : key[j], place[j] = swap ? y : place[j];
+    };
+    if constexpr (NQ == 2) order(0, 1);
+    if constexpr (NQ == 4) {  // neighbours only: stable
+        order(0, 1), order(1, 2), order(2, 3);
+        order(0, 1), order(1, 2);
+        order(0, 1);
+    }
+    // lane j gets the j-th; where scores decide, the list goes on until one is clearly behind
+    uint32_t mine = 0, last = 0;
+    int my_id = -1, listed = 0;
+    for (int j = 0; j < 64; ++j) {
+        const uint32_t m = wave_max_u(key[0]);
+        if (m == 0) break;
+        if (j >= a.k && (kBy == kByLogits || !too_near(key32_value(last), key32_value(m), bias))) break;
+        const int from = __ffsll((unsigned long long)__ballot(key[0] == m)) - 1;
+        const int id = __builtin_amdgcn_readlane((int)place[0], from);
+        if (lane == j) mine = m, my_id = id;
+        const bool pop = lane == from;
+#pragma unroll
+        for (int q = 0; q + 1 < NQ; ++q) {
+            key[q] = pop ? key[q + 1] : key[q];
+            place[q] = pop ? place[q + 1] : place[q];
+        }
+        key[NQ - 1] = pop ? 0u : key[NQ - 1];
+        last = m;
+        listed = j + 1;
+    }
+    if constexpr (kBy != kByLogits) {
+        const uint32_t after = (uint32_t)__shfl_down((int)mine, 1, 64);
+        const uint64_t close = __ballot(lane + 1 < listed && too_near(key32_value(mine), key32_value(after), bias));
+        unsure |= listed == 64;  // more of them than lanes
+        if (close && !unsure) {  // the listed ones' scores in 64 bits, ranked by counting
+            const double z = kBy == kBySoftmax ? exact_sum<NQ>(v, top) : 1.0;
+            double exact = -INFINITY;
+            if (lane < listed) exact = exact_score(a, rs.v[my_id], (double)top, z) + (a.bias ? (double)a.bias[my_id] : 0.0);
+            int rank = 0;
+            for (int j = 0; j < listed; ++j) {
+                const double other = __longlong_as_double(((long long)__builtin_amdgcn_readlane((int)(__double_as_longlong(exact) >> 32), j) << 32) |
+                                                          (uint32_t)__builtin_amdgcn_readlane((int)__double_as_longlong(exact), j));
+                const int id = __builtin_amdgcn_readlane(my_id, j);
+                rank += other > exact || (other == exact && id < my_id);
+            }
+            int* const slot = reinterpret_cast<int*>(rs.c);
+            __builtin_amdgcn_wave_barrier();
+            __atomic_signal_fence(__ATOMIC_SEQ_CST);
+            if (lane < listed) slot[rank] = my_id;
+            __builtin_amdgcn_wave_barrier();
+            __atomic_signal_fence(__ATOMIC_SEQ_CST);
+            my_id = lane < listed ? slot[lane] : -1;
+            __builtin_amdgcn_wave_barrier();
+            __atomic_signal_fence(__ATOMIC_SEQ_CST);
+        }
+    }
+    return lane < a.k ? my_id : -1;
+}
+
+// One wave routes token t: lane j < k gets the j-th chosen expert (-1: none) and its weight.
+template <int NQ, int kBy, bool kGroups>
+__device__ __forceinline__ void route_token(const RouteArgs& a, int t, int lane, RouteScratch& rs, int& my_id, float& my_w) {
+    float v[NQ], top = -INFINITY;
+    bool nan = false;
+    const size_t at = (size_t)t * a.ldl;
+    if (a.bf16) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) v[q] = load1<true>(a.logits, at + min(lane * NQ + q, a.E - 1));
+    } else {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) v[q] = load1<false>(a.logits, at + min(lane * NQ + q, a.E - 1));
+    }
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        v[q] = lane * NQ + q < a.E ? v[q] : -INFINITY;
+        rs.v[lane * NQ + q] = v[q];
+        top = fmaxf(top, v[q]);
+        nan |= __builtin_isnan(v[q]);
+    }
+    __builtin_amdgcn_wave_barrier();
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    const bool whole = !a.sigmoid && !a.normalize;  // weights out of a softmax over all experts
+    if (kBy == kBySoftmax || whole) top = wave_max_f(top);
+    bool unsure;
+    my_id = choose_fast<NQ, kBy, kGroups>(a, v, lane, rs, top, unsure);
+    if (unsure) my_id = choose_exact<NQ>(a, v, lane, rs);
+    const float my_logit = my_id < 0 ? -INFINITY : rs.v[my_id];
+    __builtin_amdgcn_wave_barrier();  // the scratch is reused by the wave's next token
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
     float w;
     if (a.normalize) {
-        const float ls = my_id < 0 ? -INFINITY : a.sigmoid ? log_sigmoid(my_logit) : my_logit;
-        const float m = wave_max_f(ls);
-        w = my_id < 0 ? 0.f : expf(ls - m);
+        const float m = wave_max_f(my_logit);
+        if (!a.sigmoid) {
+            w = my_id < 0 ? 0.f : exp_fast(my_logit - m);
+        } else if (m > -60.f) {
+            w = my_id < 0 ? 0.f : sigmoid_fast(my_logit);
+        } else {  // scores near the end of fp32's range, or past it: differences of their logarithms
+            const float ls = my_id < 0 ? -INFINITY : log_sigmoid(my_logit);
+            const float most = wave_max_f(ls);
+            w = my_id < 0 ? 0.f : expf(ls - most);
+        }
         w /= wave_total_f(w);
     } else if (a.sigmoid) {
         w = 1.f / (1.f + expf(-my_logit));
     } else {
         float z = 0.f;
 #pragma unroll
-        for (int q = 0; q < kQ; ++q) z += v[q] == -INFINITY ? 0.f : expf(v[q] - top);
-        w = expf(my_logit - top) / wave_total_f(z);
+        for (int q = 0; q < NQ; ++q) z += v[q] == -INFINITY ? 0.f : exp_fast(v[q] - top);
+        w = exp_fast(my_logit - top) / wave_total_f(z);
     }
-    if (any_nan && !a.sigmoid) w = NAN;
+    if (!a.sigmoid && __any(nan)) w = NAN;
     my_w = my_id < 0 ? 0.f : w * a.scale;
 }
 
-template <bool kBf16>
-__device__ __forceinline__ void load_logits(const RouteArgs& a, int t, int lane, float (&v)[kQ]) {
-#pragma unroll
-    for (int q = 0; q < kQ; ++q) {
-        const int e = lane + 64 * q;
-        const float x = load1<kBf16>(a.logits, (size_t)t * a.ldl + min(e, a.E - 1));
-        v[q] = e < a.E ? x : -INFINITY;
-    }
-}
-
-// Tokens [t0, t1), one after another; their experts are counted in hist.
-template <bool kBf16>
-__device__ void route_range(const RouteArgs& a, int t0, int t1, int step, int lane, RouteScratch& rs, int* hist) {
+// Tokens [t0, t1), every `step`-th; their experts are counted in hist.
+template <int NQ, int kBy, bool kGroups>
+__device__ __forceinline__ void route_range(const RouteArgs& a, int t0, int t1, int step, int lane, RouteScratch& rs, int* hist) {
     for (int t = t0; t < t1; t += step) {
-        float v[kQ], w;
+        float w;
         int id;
-        load_logits<kBf16>(a, t, lane, v);
-        route_token(a, v, lane, rs, id, w);
+        route_token<NQ, kBy, kGroups>(a, t, lane, rs, id, w);
         if (lane < a.k) {
             a.idx[(size_t)t * a.k + lane] = id;
             a.w[(size_t)t * a.k + lane] = w;
-            if (hist && id >= 0) atomicAdd(&hist[id], 1);  // a count: arrival order does not matter
+            if (id >= 0) atomicAdd(&hist[id], 1);  // a count: arrival order does not matter
         }
     }
 }
 
-template <bool kBf16>
+template <int NQ, int kBy, bool kGroups>
 __global__ __launch_bounds__(kThreads) void route_kernel(const RouteArgs a) {
     __shared__ int hist[kMaxExperts];
     __shared__ RouteScratch rs[kWaves];
-    for (int e = threadIdx.x; e < a.E; e += kThreads) hist[e] = 0;
+    if (threadIdx.x < kMaxExperts) hist[threadIdx.x] = 0;
     __syncthreads();
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int t0 = blockIdx.x * a.chunk, t1 = min(a.T, t0 + a.chunk);
-    route_range<kBf16>(a, t0 + wave, t1, kWaves, lane, rs[wave], hist);
+    const int t0 = blockIdx.x * a.counted, t1 = min(a.T, t0 + a.counted);
+    route_range<NQ, kBy, kGroups>(a, t0 + wave, t1, kWaves, lane, rs[wave], hist);
     if (!a.hist) return;
     __syncthreads();
-    for (int e = threadIdx.x; e < a.E; e += kThreads) a.hist[(size_t)blockIdx.x * a.E + e] = hist[e];
+    const int e = 4 * threadIdx.x;
+    if ((int)threadIdx.x < a.words)
+        a.hist[(size_t)blockIdx.x * a.words + threadIdx.x] =
+            (uint32_t)hist[e] | (uint32_t)hist[e + 1] << 8 | (uint32_t)hist[e + 2] << 16 | (uint32_t)hist[e + 3] << 24;
 }
 
-// Places the assignments of tokens [t0, t1), one wave: rank among equal ids from
-// ballots, `run` the next place of each expert.
-__device__ __forceinline__ void place(const RouteArgs& a, const int32_t* idx, long long a0, long long a1, int* run) {
+// Places the assignments [a0, a1), one wave: rank among equal ids from ballots, `run`
+// the next place of each expert.  first_ids: those of a0 + lane.
+__device__ __forceinline__ void place(const RouteArgs& a, long long a0, long long a1, int first_ids, int* run) {
     const int lane = threadIdx.x & 63;
     const uint64_t lower = lane ? (~0ull) >> (64 - lane) : 0ull;
     for (long long r0 = a0; r0 < a1; r0 += 64) {
         const long long i = r0 + lane;
-        const int e = i < a1 ? idx[i] : -1;
+        const int e = i >= a1 ? -1 : r0 == a0 ? first_ids : a.idx[i];
         const bool valid = e >= 0;
         uint64_t match = __ballot(valid);
 #pragma unroll
@@ -276,40 +499,63 @@ __device__ __forceinline__ void place(const RouteArgs& a, const int32_t* idx, lo
 }
 
 // kRoute: the one workgroup routes its tokens too.
-template <bool kBf16, bool kRoute>
+template <bool kRoute, int NQ, int kBy, bool kGroups>
 __global__ __launch_bounds__(kThreads) void route_tables_kernel(const RouteArgs a) {
     __shared__ int run[kWaves][kMaxExperts];  // counts of each wave's tokens, then where they go
-    __shared__ int sums[2][4][kMaxExperts];   // all chunks' counts, and those of the chunks before this one
+    __shared__ int sums[2][kMaxExperts];      // all histograms, and those of the chunks before this one
     __shared__ int start[kMaxExperts + 1];
     __shared__ RouteScratch rs[kRoute ? kWaves : 1];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, E = a.E;
     const int t0 = blockIdx.x * a.chunk, t1 = min(a.T, t0 + a.chunk);
     const int per = (t1 - t0 + kWaves - 1) / kWaves;
     const int w0 = min(t1, t0 + wave * per), w1 = min(t1, w0 + per);
+    const long long a0 = (long long)w0 * a.k, a1 = (long long)w1 * a.k;
+    int first_ids = -1;
+    if (!kRoute && a0 + lane < a1) first_ids = a.idx[a0 + lane];
     for (int e = lane; e < E; e += 64) run[wave][e] = 0;
-    __builtin_amdgcn_wave_barrier();
-    __atomic_signal_fence(__ATOMIC_SEQ_CST);
     if constexpr (kRoute) {
-        route_range<kBf16>(a, w0, w1, 1, lane, rs[wave], run[wave]);
+        __builtin_amdgcn_wave_barrier();
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);
+        route_range<NQ, kBy, kGroups>(a, w0, w1, 1, lane, rs[wave], run[wave]);
+        if (a0 + lane < a1) first_ids = a.idx[a0 + lane];
+        __syncthreads();
     } else {
-        for (long long i = (long long)w0 * a.k + lane; i < (long long)w1 * a.k; i += 64) {
-            const int e = a.idx[i];
+        if (threadIdx.x < kMaxExperts) sums[0][threadIdx.x] = sums[1][threadIdx.x] = 0;
+        __syncthreads();
+        for (long long i = a0 + lane; i < a1; i += 64) {
+            const int e = i == a0 + lane ? first_ids : a.idx[i];
             if (e >= 0) atomicAdd(&run[wave][e], 1);  // a count
         }
-        const int e = threadIdx.x & 255, part = threadIdx.x >> 8, chunks = gridDim.x;
-        const int per_part = (chunks + 3) / 4, c0 = part * per_part, c1 = min(chunks, c0 + per_part);
-        int all = 0, before = 0;
-        if (e < E)
-#pragma unroll 8
-            for (int c = c0; c < c1; ++c) {
-                const int n = a.hist[(size_t)c * E + e];
-                all += n;
-                before += c < (int)blockIdx.x ? n : 0;
+        // four experts a lane (expert 4 lane + j at [j 64 + lane], so that no two lanes meet in a bank),
+        // every 16th histogram a wave; sums of whole numbers
+        const int rows = (a.T + a.counted - 1) / a.counted, mine = t0 / a.counted;
+        if (lane < a.words) {
+            // 32 of them requested together; two experts' counts in the halves of a word (32 times 240 at most)
+            constexpr int kTogether = 32;
+            int all[4] = {}, before[4] = {};
+            for (int h0 = wave; h0 < rows; h0 += kTogether * kWaves) {
+                uint32_t n[kTogether], even[2] = {}, odd[2] = {};
+#pragma unroll
+                for (int i = 0; i < kTogether; ++i) n[i] = a.hist[(size_t)min(h0 + i * kWaves, rows - 1) * a.words + lane];
+                __builtin_amdgcn_sched_barrier(0);  // else the compiler waits for one after another (12 us where this takes 5)
+#pragma unroll
+                for (int i = 0; i < kTogether; ++i) {
+                    const int h = h0 + i * kWaves;
+                    const uint32_t x = h < rows ? n[i] : 0u, y = h < mine ? x : 0u;
+                    even[0] += x & 0x00ff00ffu, odd[0] += (x >> 8) & 0x00ff00ffu;
+                    even[1] += y & 0x00ff00ffu, odd[1] += (y >> 8) & 0x00ff00ffu;
+                }
+                all[0] += even[0] & 0xffff, all[1] += odd[0] & 0xffff, all[2] += even[0] >> 16, all[3] += odd[0] >> 16;
+                before[0] += even[1] & 0xffff, before[1] += odd[1] & 0xffff, before[2] += even[1] >> 16, before[3] += odd[1] >> 16;
             }
-        sums[0][part][e] = all;
-        sums[1][part][e] = before;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                atomicAdd(&sums[0][64 * j + lane], all[j]);
+                if (mine) atomicAdd(&sums[1][64 * j + lane], before[j]);
+            }
+        }
+        __syncthreads();
     }
-    __syncthreads();
     if (wave == 0) {  // the experts' starts: four experts a lane
         int n[kQ], local = 0;
 #pragma unroll
@@ -318,9 +564,10 @@ __global__ __launch_bounds__(kThreads) void route_tables_kernel(const RouteArgs 
             n[q] = 0;
             if (e < E) {
                 if constexpr (kRoute)
+#pragma unroll
                     for (int w = 0; w < kWaves; ++w) n[q] += run[w][e];
                 else
-                    for (int p = 0; p < 4; ++p) n[q] += sums[0][p][e];
+                    n[q] = sums[0][64 * q + lane];
             }
             local += n[q];
         }
@@ -346,19 +593,39 @@ __global__ __launch_bounds__(kThreads) void route_tables_kernel(const RouteArgs 
     __syncthreads();
     for (int e = threadIdx.x; e < E; e += kThreads) {
         int to = start[e];
-        if constexpr (!kRoute)
-            for (int p = 0; p < 4; ++p) to += sums[1][p][e];
+        if constexpr (!kRoute) to += sums[1][64 * (e & 3) + (e >> 2)];
+        int n[kWaves];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) n[w] = run[w][e];
+#pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            const int n = run[w][e];
             run[w][e] = to;
-            to += n;
+            to += n[w];
         }
     }
     __syncthreads();
-    place(a, a.idx, (long long)w0 * a.k, (long long)w1 * a.k, run[wave]);
+    place(a, a0, a1, first_ids, run[wave]);
     // behind the last row
     const long long rows = start[E], A = (long long)a.T * a.k;
     for (long long i = rows + blockIdx.x * (long long)kThreads + threadIdx.x; i < A; i += (long long)gridDim.x * kThreads) a.perm[i] = -1;
+}
+
+template <int NQ, int kBy, bool kGroups>
+hipError_t launch_route(const RouteArgs& a, bool tables, hipStream_t s) {
+    if (tables && a.T <= kOneWorkgroup) {
+        route_tables_kernel<true, NQ, kBy, kGroups><<<1, kThreads, 0, s>>>(a);
+        return hipGetLastError();
+    }
+    route_kernel<NQ, kBy, kGroups><<<(a.T + a.counted - 1) / a.counted, kThreads, 0, s>>>(a);
+    if (tables) route_tables_kernel<false, 1, 0, false><<<(a.T + a.chunk - 1) / a.chunk, kThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+template <int NQ>
+hipError_t launch_route(const RouteArgs& a, bool tables, hipStream_t s) {
+    if (!a.bias && (a.groups == 1 || a.best == 1))
+        return a.groups > 1 ? launch_route<NQ, kByLogits, true>(a, tables, s) : launch_route<NQ, kByLogits, false>(a, tables, s);
+    if (a.sigmoid) return a.groups > 1 ? launch_route<NQ, kBySigmoid, true>(a, tables, s) : launch_route<NQ, kBySigmoid, false>(a, tables, s);
+    return a.groups > 1 ? launch_route<NQ, kBySoftmax, true>(a, tables, s) : launch_route<NQ, kBySoftmax, false>(a, tables, s);
 }
 
 struct RouteGradArgs {
@@ -468,10 +735,23 @@ int check_router(const flexmoe_router_desc* D, int T, const char* who, long long
     return FLEXMOE_OK;
 }
 
-// Tokens of a chunk: a multiple of a workgroup's waves.
-int chunk_tokens(int T) { return std::max(kWaves, ((T + kChunks - 1) / kChunks + kWaves - 1) / kWaves * kWaves); }
+// Tokens of a histogram (a multiple of a workgroup's waves) and of a chunk.
+int counted_tokens(int T) {
+    const int per = (T + kHistograms - 1) / kHistograms;
+    return std::min(kMostCounted, std::max(1, (per + kWaves - 1) / kWaves) * kWaves);
+}
+int chunk_tokens(int T, int counted) {
+    const int per = (T + kChunks - 1) / kChunks;
+    return std::max(1, (per + counted - 1) / counted) * counted;
+}
 
-size_t route_bytes(const flexmoe_router_desc* D) { return ((size_t)kChunks * D->E * sizeof(int32_t) + 255) & ~size_t(255); }
+int hist_words(int E) { return (E + 3) / 4; }
+
+size_t route_bytes(const flexmoe_router_desc* D, int T) {
+    // up to kHistograms of them while each counts fewer than kMostCounted tokens, then as many as there are
+    const size_t rows = std::max<size_t>(kHistograms + 1, ((size_t)T + kMostCounted - 1) / kMostCounted);
+    return (rows * hist_words(D->E) * 4 + 255) & ~size_t(255);
+}
 
 }  // namespace
 
@@ -480,7 +760,7 @@ extern "C" {
 size_t flexmoe_route_workspace_bytes(const flexmoe_router_desc* desc, int32_t T) {
     long long ldl;
     if (check_router(desc, T, "route_workspace_bytes", &ldl)) return 0;
-    return route_bytes(desc);
+    return route_bytes(desc, T);
 }
 
 int flexmoe_route(const flexmoe_router_desc* desc, int32_t T, const void* logits, const float* bias, const flexmoe_route_out* out,
@@ -503,35 +783,20 @@ int flexmoe_route(const flexmoe_router_desc* desc, int32_t T, const void* logits
     a.logits = logits, a.bias = bias, a.idx = out->topk_idx, a.w = out->topk_w;
     a.counts = out->counts, a.offsets = out->offsets, a.perm = out->perm, a.pos = out->pos;
     a.hist = nullptr, a.ldl = (size_t)ldl;
-    a.T = T, a.E = desc->E, a.k = desc->top_k, a.sigmoid = desc->score == FLEXMOE_SIGMOID, a.normalize = desc->normalize;
+    a.T = T, a.E = desc->E, a.k = desc->top_k, a.bf16 = desc->dtype == FLEXMOE_BF16;
+    a.sigmoid = desc->score == FLEXMOE_SIGMOID, a.normalize = desc->normalize;
     a.groups = desc->groups, a.top_groups = desc->top_groups, a.best = desc->group_best, a.scale = desc->scale;
-    const bool bf16 = desc->dtype == FLEXMOE_BF16;
-    const hipStream_t s = (hipStream_t)stream;
-    if (tables && T <= kOneWorkgroup) {
-        a.chunk = kOneWorkgroup;
-        if (bf16) route_tables_kernel<true, true><<<1, kThreads, 0, s>>>(a);
-        else route_tables_kernel<false, true><<<1, kThreads, 0, s>>>(a);
-        const hipError_t err = hipGetLastError();
-        return err == hipSuccess ? FLEXMOE_OK : hip_fail(err, who);
-    }
-    a.chunk = chunk_tokens(T);
-    if (tables) {
-        const size_t need = route_bytes(desc);
+    a.counted = counted_tokens(T), a.chunk = chunk_tokens(T, a.counted), a.words = hist_words(a.E);
+    if (tables && T > kOneWorkgroup) {
+        const size_t need = route_bytes(desc, T);
         if (!workspace || workspace_bytes < need)
             return fail(FLEXMOE_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace ? workspace_bytes : 0, need);
         if (misaligned(workspace, 255)) return fail(FLEXMOE_EWORKSPACE, "%s: workspace must be 256-byte aligned", who);
-        a.hist = (int32_t*)workspace;
+        a.hist = (uint32_t*)workspace;
     }
-    const int chunks = (T + a.chunk - 1) / a.chunk;
-    if (bf16) route_kernel<true><<<chunks, kThreads, 0, s>>>(a);
-    else route_kernel<false><<<chunks, kThreads, 0, s>>>(a);
-    hipError_t err = hipGetLastError();
+    const hipStream_t s = (hipStream_t)stream;
+    const hipError_t err = a.E <= 64 ? launch_route<1>(a, tables, s) : a.E <= 128 ? launch_route<2>(a, tables, s) : launch_route<4>(a, tables, s);
     if (err != hipSuccess) return hip_fail(err, who);
-    if (tables) {
-        route_tables_kernel<false, false><<<chunks, kThreads, 0, s>>>(a);
-        err = hipGetLastError();
-        if (err != hipSuccess) return hip_fail(err, who);
-    }
     return FLEXMOE_OK;
 }
 

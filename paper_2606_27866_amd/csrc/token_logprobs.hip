@@ -187,10 +187,7 @@ __global__ __launch_bounds__(kVT) void logprob_kernel(const LogprobArgs a) {
     const void* const logits = reinterpret_cast<const char*>(a.logits) + row * a.ld * elem_size<kBf16>();
     const int begin = p * a.length, end = min(a.V, begin + a.length);
     RunningSums sums;
-    for (int at = begin, it = 0; at < end; at += W::step, ++it) {
-        float v[W::units][W::n];
-#pragma unroll
-        for (int u = 0; u < W::units; ++u) load_values<kBf16>(logits, at + u * W::run + t * W::n, end, v[u]);
+    each_step<kBf16>(logits, begin, end, [&](int it, int, const float (&v)[W::units][W::n]) {
         float gm = -INFINITY;
 #pragma unroll
         for (int u = 0; u < W::units; ++u) gm = max_of(v[u], gm);
@@ -200,7 +197,7 @@ __global__ __launch_bounds__(kVT) void logprob_kernel(const LogprobArgs a) {
         for (int u = 0; u < W::units; ++u)
 #pragma unroll
             for (int k = 0; k < W::n; ++k) sums.add(v[u][k], a.c);
-    }
+    });
     const uint32_t own = value_key(sums.t.m);
     Sums all = join_threads(sums.exact(a.c), a.c, part);
     if (!(all.s < 3.0e38f) && all.m > -INFINITY && all.m < INFINITY) {

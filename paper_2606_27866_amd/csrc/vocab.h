@@ -59,6 +59,39 @@ __device__ __forceinline__ void load_values(const void* row, int i, int end, flo
         for (int k = 0; k < n; ++k) v[k] = i + k < end ? v[k] : -INFINITY;
 }
 
+// f(step, its first value's index, the values of this thread's units) for the steps of
+// [begin, end): -inf past the end.  A step's loads have no conditions, so that all of
+// them are in flight together (addresses past the end are those of the last unit); in
+// bf16 those of the next step too, in fp32 they would take too many registers.
+template <bool kBf16, typename F>
+__device__ __forceinline__ void each_step(const void* row, int begin, int end, F&& f) {
+    using W = Vocab<kBf16>;
+    const int t = threadIdx.x, last = (end - 1) / W::n * W::n;
+    u32x4 next[W::units];
+    auto request = [&](int at) {
+#pragma unroll
+        for (int u = 0; u < W::units; ++u) next[u] = load_unit<kBf16>(row, min(at + u * W::run + t * W::n, last));
+    };
+    if (begin < end) request(begin);
+    for (int at = begin, it = 0; at < end; at += W::step, ++it) {
+        float v[W::units][W::n];
+        u32x4 now[W::units];
+#pragma unroll
+        for (int u = 0; u < W::units; ++u) now[u] = next[u];
+        if (kBf16 && at + W::step < end) request(at + W::step);
+#pragma unroll
+        for (int u = 0; u < W::units; ++u) unpack_unit<kBf16>(now[u], v[u]);
+        if (at + W::step > end) {
+#pragma unroll
+            for (int u = 0; u < W::units; ++u)
+#pragma unroll
+                for (int k = 0; k < W::n; ++k) v[u][k] = at + u * W::run + t * W::n + k < end ? v[u][k] : -INFINITY;
+        }
+        f(it, at, v);
+        if (!kBf16 && at + W::step < end) request(at + W::step);
+    }
+}
+
 template <bool kBf16>
 __device__ __forceinline__ float value_at(const void* row, int i) {
     if constexpr (kBf16) return bf16_to_f32(reinterpret_cast<const bf16_t*>(row)[i]);
