@@ -14,9 +14,16 @@
 // the listed tokens are left out of that sum (a map of bits says which) and added
 // to it afterwards, so that q_rest is a sum and not a difference.
 //
-//   distill_sums_kernel   maximum and sums of each part of a row
-//   distill_row_kernel    a wave joins them: losses, factors, gradients of the listed tokens
-//   distill_grad_kernel   factor * exp(x) for a part of a row, then the listed tokens
+// What the teacher's list gives does not hang on the student's maximum m and sum S
+// (S_rest without the listed tokens): with A = sum p log p [+ p_rest log p_rest] and
+// B = sum p (x - y), y the largest listed x,
+//   KL = A - (B - (m - y) sum p) / t + (sum p [+ p_rest]) log S [- p_rest log S_rest].
+//
+// Many rows that fit the registers of a workgroup (distill_whole_kernel): every row is
+// read once; while its gradients leave, the next row's logits come in.  Else:
+//   distill_sums_kernel   maximum and sums of each part of a row, and the lists
+//   distill_grad_kernel   joins a row's parts, then factor * exp(x) for a part of the
+//                         row, then the listed tokens (distill_row_kernel: losses alone)
 #include <algorithm>
 #include <cmath>
 
@@ -28,6 +35,22 @@ using namespace flexmoe;
 
 namespace {
 
+// What a row's list gives: sums over its tokens (see above), what it leaves, the label.
+struct RowList {
+    double a, b, mass, rest;
+    float y, x_label;
+    int label;  // -1: none
+    int pad;
+};
+
+// A token whose gradient is not factor * exp(x): of the list, or the label.
+struct Mark {
+    int id;  // -1: none
+    float p, x;
+    int kind;  // kListed, kLabel or both
+};
+enum { kListed = 1, kLabel = 2 };
+
 struct DistillArgs {
     const void* logits;
     const int32_t *ids, *labels;
@@ -35,10 +58,10 @@ struct DistillArgs {
     float *kl, *ce;
     void* dlogits;
     float* parts;     // [rows][P][4]: m, sum at t, sum at 1
-    float* factors;   // [rows][4]: m, factor at t, factor at 1
-    int2* marks;      // [rows][K + 1]: token (-1: none), bits of its gradient
+    RowList* lists;   // [rows]
+    Mark* marks;      // [rows][K + 1]
     size_t ld, ldd;
-    int V, P, length, K, tail, two;  // two: the labels' sum is not that of t
+    int rows, V, P, length, K, tail, two;  // two: the labels' sum is not that of t
     float c, inv_t, t, kl_weight, ce_weight;
 };
 
@@ -80,15 +103,15 @@ struct TwoSums {
     }
 };
 
-template <bool kTwo>
-__device__ __forceinline__ TwoSums<kTwo> join_threads(TwoSums<kTwo> a, float c, float (*part)[kVT / 64]) {
+template <int kThreads, bool kTwo>
+__device__ __forceinline__ TwoSums<kTwo> join_threads(TwoSums<kTwo> a, float c, float (*part)[kThreads / 64]) {
     const int wave = threadIdx.x >> 6;
     float m = wave_max(a.m);
     if ((threadIdx.x & 63) == 0) part[0][wave] = m;
     __syncthreads();
     m = part[0][0];
 #pragma unroll
-    for (int w = 1; w < kVT / 64; ++w) m = fmaxf(m, part[0][w]);
+    for (int w = 1; w < kThreads / 64; ++w) m = fmaxf(m, part[0][w]);
     a.refer(m, c);
     a.s = wave_total_f(a.s);
     if constexpr (kTwo) a.s1 = wave_total_f(a.s1);
@@ -96,7 +119,7 @@ __device__ __forceinline__ TwoSums<kTwo> join_threads(TwoSums<kTwo> a, float c, 
     __syncthreads();
     a.s = part[1][0], a.s1 = part[2][0];
 #pragma unroll
-    for (int w = 1; w < kVT / 64; ++w) a.s += part[1][w], a.s1 += part[2][w];
+    for (int w = 1; w < kThreads / 64; ++w) a.s += part[1][w], a.s1 += part[2][w];
     return a;
 }
 
@@ -121,11 +144,110 @@ __device__ __forceinline__ void leave_out(const uint32_t* bits, int i, float (&v
         for (int k = 0; k < n; ++k) v[k] = (b >> k) & 1 ? -INFINITY : v[k];
 }
 
+// One wave writes down what a row's list gives, kOwn tokens a lane.  seen: K ints of LDS.
+template <bool kBf16, int kOwn>
+__device__ __forceinline__ void list_row(const DistillArgs& a, size_t row, int* seen) {
+    const int lane = threadIdx.x & 63, K = a.K;
+    const void* const logits = reinterpret_cast<const char*>(a.logits) + row * a.ld * elem_size<kBf16>();
+    const int named = a.labels ? a.labels[row] : -1, label = named < a.V ? max(named, -1) : -1;
+    int id[kOwn];
+    float lp[kOwn], x[kOwn];
+#pragma unroll
+    for (int q = 0; q < kOwn; ++q) {
+        const int k = lane + 64 * q;
+        id[q] = k < K ? a.ids[row * K + k] : -1;
+        lp[q] = k < K ? a.lp[row * K + k] : -INFINITY;
+        if (id[q] < 0 || id[q] >= a.V) id[q] = -1;
+        x[q] = value_at<kBf16>(logits, max(id[q], 0));
+        if (k < K) seen[k] = id[q];
+    }
+    const float x_label = value_at<kBf16>(logits, max(label, 0));
+    __builtin_amdgcn_wave_barrier();
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    // a token that is named again counts with its first place alone
+    bool again[kOwn] = {}, label_listed = false;
+#pragma unroll 8
+    for (int j = 0; j < K; ++j) {
+        const int other = seen[j];
+#pragma unroll
+        for (int q = 0; q < kOwn; ++q) again[q] |= other == id[q] && j < lane + 64 * q;
+        label_listed |= other == label;
+    }
+    __builtin_amdgcn_wave_barrier();
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    float top = 0.f;
+    if (!a.tail) {
+        top = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < kOwn; ++q)
+            if (id[q] >= 0) top = fmaxf(top, lp[q]);
+        top = wave_max(top);
+    }
+    double p[kOwn], logp[kOwn], mass = 0.0;
+#pragma unroll
+    for (int q = 0; q < kOwn; ++q) {
+        if (again[q]) id[q] = -1;
+        logp[q] = id[q] >= 0 && top > -INFINITY ? (double)lp[q] - (double)top : -INFINITY;
+        p[q] = exp(logp[q]);
+        mass += p[q];
+    }
+    mass = wave_total_d(mass);
+    RowList out;
+    out.rest = 0.0;
+    double rest_log = 0.0;
+    if (a.tail) {
+        out.rest = mass != mass ? mass : fmax(0.0, 1.0 - mass);
+        rest_log = out.rest == 0.0 ? 0.0 : out.rest * log(out.rest);
+    } else {
+        const double log_mass = log(mass);
+#pragma unroll
+        for (int q = 0; q < kOwn; ++q) {
+            p[q] = p[q] == 0.0 ? 0.0 : p[q] / mass;
+            logp[q] -= log_mass;
+        }
+        if (mass > 0.0) mass = 1.0;
+    }
+    double sum_a = 0.0, sum_b = 0.0;
+    float y = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < kOwn; ++q)
+        if (id[q] >= 0) y = fmaxf(y, x[q]);
+    y = wave_max(y);
+    if (!(fabsf(y) < INFINITY)) y = 0.f;
+    Mark* const marks = a.marks + row * (K + 1);
+#pragma unroll
+    for (int q = 0; q < kOwn; ++q) {
+        if (p[q] != 0.0) sum_a += p[q] * logp[q], sum_b += p[q] * ((double)x[q] - (double)y);
+        if (id[q] >= 0 && __builtin_isnan(x[q])) sum_b = NAN;
+        if (lane + 64 * q < K) marks[lane + 64 * q] = Mark{id[q], (float)p[q], x[q], kListed | (id[q] == label ? kLabel : 0)};
+    }
+    out.a = wave_total_d(sum_a) + rest_log, out.b = wave_total_d(sum_b), out.mass = mass;
+    out.y = y, out.x_label = x_label, out.label = label;
+    if (lane == 0) {
+        marks[K] = Mark{label_listed ? -1 : label, 0.f, x_label, kLabel};
+        a.lists[row] = out;
+    }
+}
+
+template <bool kBf16>
+__device__ __forceinline__ void list_row(const DistillArgs& a, size_t row, int* seen) {
+    static_assert(kMaxTop == 128, "two tokens a lane");
+    if (a.K <= 64) list_row<kBf16, 1>(a, row, seen);
+    else list_row<kBf16, 2>(a, row, seen);
+}
+
 template <bool kBf16, bool kTail, bool kTwo>
 __global__ __launch_bounds__(kVT) void distill_sums_kernel(const DistillArgs a) {
     using W = Vocab<kBf16>;
     __shared__ uint32_t bits[kTail ? kRange / 32 : 1];
     __shared__ float part[3][kVT / 64];
+    __shared__ int seen[kVT / 64][kMaxTop];
+    const size_t parts = (size_t)a.rows * a.P;
+    if (blockIdx.x >= parts) {  // lists, four rows a workgroup
+        const size_t row = (blockIdx.x - parts) * (kVT / 64) + (threadIdx.x >> 6);
+        if (row < (size_t)a.rows && !(a.row_scale && a.row_scale[row] == 0.f)) list_row<kBf16>(a, row, seen[threadIdx.x >> 6]);
+        return;
+    }
     const size_t row = blockIdx.x / a.P;
     const int p = blockIdx.x % a.P, t = threadIdx.x;
     if (a.row_scale && a.row_scale[row] == 0.f) return;
@@ -148,7 +270,7 @@ __global__ __launch_bounds__(kVT) void distill_sums_kernel(const DistillArgs a) 
         }
     });
     sums.settle(a.c);
-    TwoSums<kTwo> all = join_threads(sums, a.c, part);
+    TwoSums<kTwo> all = join_threads<kVT>(sums, a.c, part);
     if (!(all.s < 3.0e38f && all.s1 < 3.0e38f) && all.m > -INFINITY && all.m < INFINITY) {
         // c m may have left fp32's range (or a value is no number): differences first
         TwoSums<kTwo> again;
@@ -164,7 +286,7 @@ __global__ __launch_bounds__(kVT) void distill_sums_kernel(const DistillArgs a) 
             }
         }
         __syncthreads();
-        all = join_threads(again, a.c, part);
+        all = join_threads<kVT>(again, a.c, part);
     }
     if (t == 0) {
         float* const o = a.parts + 4 * (row * a.P + p);
@@ -172,219 +294,408 @@ __global__ __launch_bounds__(kVT) void distill_sums_kernel(const DistillArgs a) 
     }
 }
 
-__device__ __forceinline__ double wave_sum_d(double v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
+// What a row's tokens are multiplied with.
+struct RowFactors {
+    float m, f, f1;          // all tokens: f 2^(c (x - m)) + f1 2^(log2(e) (x - m))
+    float listed, p, label;  // marked ones: listed 2^(c (x - m)) - p p_k instead of the first; less `label`
+};
+
+// The logarithm of a sum to about 2^-25: its power of two is taken off, whose part is exact in 64 bits.
+__device__ __forceinline__ double log_of(float s) {
+    if (!(s > 0.f && s < INFINITY)) return (double)logf(s);
+    int e;
+    float f = frexpf(s, &e);
+    if (f < 0.70710678f) f *= 2.f, --e;
+    return (double)e * 0.6931471805599453 + (double)logf(f);
 }
 
-constexpr int kOwn = kMaxTop / 64;  // listed tokens of a lane
-
-// One wave ends a row whose largest logit is m and whose sums (with a tail: without
-// the listed tokens) are s and s1.  seen: K + 1 ints of LDS.
-template <bool kBf16>
-__device__ void end_row(const DistillArgs& a, size_t row, const void* logits, float m, float s, float s1, int* seen) {
-    const int lane = threadIdx.x & 63, K = a.K;
-    const double scale = a.row_scale ? (double)a.row_scale[row] : 1.0, inv_t = (double)a.inv_t;
-    const int32_t* const ids = a.ids + row * K;
-    const int label = a.labels ? a.labels[row] : -1;
-    const bool labelled = label >= 0 && label < a.V;
-    int id[kOwn];
-    float lp[kOwn];
-#pragma unroll
-    for (int q = 0; q < kOwn; ++q) {
-        const int k = lane + 64 * q;
-        id[q] = k < K ? ids[k] : -1;
-        lp[q] = k < K ? a.lp[row * K + k] : -INFINITY;
-        if (id[q] < 0 || id[q] >= a.V) id[q] = -1;
-        if (k < K) seen[k] = id[q];
-    }
-    __builtin_amdgcn_wave_barrier();
-    __atomic_signal_fence(__ATOMIC_SEQ_CST);
-    // a token that is named again counts with its first place alone
-    bool again[kOwn] = {}, label_listed = false;
-    for (int j = 0; j < K; ++j) {
-        const int other = seen[j];
-#pragma unroll
-        for (int q = 0; q < kOwn; ++q) again[q] |= other == id[q] && j < lane + 64 * q;
-        label_listed |= other == label;
-    }
-    __builtin_amdgcn_wave_barrier();
-    __atomic_signal_fence(__ATOMIC_SEQ_CST);
-    double e[kOwn], e1[kOwn], logq[kOwn], p[kOwn], logp[kOwn];
-    double listed = 0.0, listed1 = 0.0;
-    bool nan = false;
-#pragma unroll
-    for (int q = 0; q < kOwn; ++q) {
-        if (again[q]) id[q] = -1;
-        const double x = id[q] >= 0 ? (double)value_at<kBf16>(logits, id[q]) - (double)m : -INFINITY;
-        nan |= id[q] >= 0 && __builtin_isnan(value_at<kBf16>(logits, id[q]));
-        logq[q] = x * inv_t;
-        e[q] = id[q] >= 0 ? exp(logq[q]) : 0.0;
-        e1[q] = !a.two ? e[q] : id[q] >= 0 ? exp(x) : 0.0;
-        listed += e[q];
-        listed1 += e1[q];
-    }
-    double S = (double)s, S1 = a.two ? (double)s1 : S;
+// One wave joins a row's maximum and sums (with a tail: without the listed tokens) with
+// its list and marks.  All lanes return the same; lane 0 writes the losses if `writes`.
+__device__ __forceinline__ RowFactors end_row(const DistillArgs& a, size_t row, const RowList& list, const Mark* marks, float m, float s, float s1,
+                                              bool writes) {
+    const int lane = threadIdx.x & 63;
+    const float scale = a.row_scale ? a.row_scale[row] : 1.f;
+    float S = s, S1 = a.two ? s1 : s;
     if (a.tail) {
-        S += wave_sum_d(listed);
-        S1 = a.two ? S1 + wave_sum_d(listed1) : S;
-    }
-    const bool empty = m == -INFINITY && s == 0.f && !__any(nan);
-    // the teacher
-    double mass = 0.0, rest = 0.0, kl = 0.0;
-    if (a.tail) {
-#pragma unroll
-        for (int q = 0; q < kOwn; ++q) {
-            logp[q] = id[q] >= 0 ? (double)lp[q] : -INFINITY;
-            p[q] = exp(logp[q]);
-            mass += p[q];
+        float e = 0.f, e1 = 0.f;
+        for (int k = lane; k < a.K; k += 64) {
+            const Mark mark = marks[k];
+            if (mark.id < 0) continue;
+            e += exp2_fast((mark.x - m) * a.c);
+            e1 += exp2_fast((mark.x - m) * kLog2E);
         }
-        mass = wave_sum_d(mass);
-        rest = mass != mass ? mass : fmax(0.0, 1.0 - mass);
-    } else {
-        float top = -INFINITY;
-#pragma unroll
-        for (int q = 0; q < kOwn; ++q)
-            if (id[q] >= 0) top = fmaxf(top, lp[q]);
-        top = wave_max(top);
-#pragma unroll
-        for (int q = 0; q < kOwn; ++q) {
-            logp[q] = id[q] >= 0 && top > -INFINITY ? (double)lp[q] - (double)top : -INFINITY;
-            p[q] = exp(logp[q]);
-            mass += p[q];
-        }
-        mass = wave_sum_d(mass);
-        const double log_mass = log(mass);
-#pragma unroll
-        for (int q = 0; q < kOwn; ++q) {
-            p[q] = p[q] == 0.0 ? 0.0 : p[q] / mass;
-            logp[q] -= log_mass;
-        }
-        if (mass > 0.0) mass = 1.0;
+        S += wave_total_f(e);
+        S1 = a.two ? S1 + wave_total_f(e1) : S;
     }
-    const double log_s = log(S), total = mass + rest;
-#pragma unroll
-    for (int q = 0; q < kOwn; ++q) {
-        logq[q] -= log_s;
-        if (p[q] != 0.0) kl += p[q] * (logp[q] - logq[q]);
-    }
-    kl = wave_sum_d(kl);
+    const bool empty = m == -INFINITY && s == 0.f && list.b == list.b, labelled = list.label >= 0;
+    const double total = list.mass + list.rest;
     double dense = total;
-    if (a.tail && rest != 0.0) {
-        const double q_rest = (double)s / S;
-        // log probabilities in 32 bits leave about 1e-6 of their own
-        if (s == 0.f) kl += rest <= 1e-5 ? 0.0 : INFINITY;
-        else kl += rest * (log(rest) - log(q_rest));
-        dense = s == 0.f ? 0.0 : total - rest / q_rest;
+    if (writes) {
+        double kl = list.mass == 0.0 ? list.a : list.a - (list.b - ((double)m - (double)list.y) * list.mass) * (double)a.inv_t;
+        kl += total == 0.0 ? 0.0 : total * log_of(S);
+        if (list.rest != 0.0) {
+            // log probabilities in 32 bits leave about 1e-6 of their own
+            if (s == 0.f) kl = list.rest <= 1e-5 ? kl : INFINITY;
+            else kl -= list.rest * log_of(s);
+        }
+        if (empty) kl = list.mass > 0.0 || list.rest > 1e-5 ? INFINITY : 0.0;
+        const double ce = !labelled ? 0.0 : empty ? INFINITY : log_of(S1) - ((double)list.x_label - (double)m);
+        if (lane == 0) {
+            a.kl[row] = (float)kl;
+            a.ce[row] = (float)ce;
+        }
     }
-    if (empty) kl = mass > 0.0 || rest > 1e-5 ? INFINITY : 0.0;
-    const double x_label = labelled ? (double)value_at<kBf16>(logits, label) - (double)m : 0.0;
-    const double ce = !labelled ? 0.0 : empty ? INFINITY : log(S1) - x_label;
-    if (lane == 0) {
-        a.kl[row] = (float)kl;
-        a.ce[row] = (float)ce;
-    }
-    if (!a.dlogits) return;
-    const double by_kl = scale * (double)a.kl_weight * (double)a.t, by_ce = labelled ? scale * (double)a.ce_weight : 0.0;
-    const double f = by_kl * dense / S, f1 = by_ce / S1;
-    if (lane == 0) {
-        float* const o = a.factors + 4 * row;
-        o[0] = m;
-        o[1] = empty ? 0.f : (float)(a.two ? f : f + f1);
-        o[2] = empty || !a.two ? 0.f : (float)f1;
-    }
-    int2* const marks = a.marks + row * (K + 1);
-#pragma unroll
-    for (int q = 0; q < kOwn; ++q) {
-        const int k = lane + 64 * q;
-        if (k >= K) continue;
-        double g = by_kl * (total * e[q] / S - p[q]) + f1 * e1[q];
-        if (id[q] == label) g -= by_ce;
-        marks[k] = make_int2(empty ? -1 : id[q], __float_as_int((float)g));
-    }
-    if (lane == 0) {
-        const double g = f * exp(x_label * inv_t) + f1 * exp(x_label) - by_ce;
-        marks[K] = make_int2(!labelled || label_listed || empty ? -1 : label, __float_as_int((float)g));
-    }
+    if (list.rest != 0.0) dense = s == 0.f ? 0.0 : total - list.rest * ((double)S / (double)s);
+    const float by_kl = scale * a.kl_weight * a.t, by_ce = labelled ? scale * a.ce_weight : 0.f;
+    RowFactors o;
+    o.m = m;
+    o.f = empty ? 0.f : by_kl * (float)dense / S;
+    o.f1 = empty ? 0.f : by_ce / S1;
+    o.listed = empty ? 0.f : by_kl * (float)total / S;
+    o.p = empty ? 0.f : by_kl;
+    o.label = empty ? 0.f : by_ce;
+    return o;
 }
 
-template <bool kBf16>
-__global__ __launch_bounds__(64) void distill_row_kernel(const DistillArgs a) {
-    __shared__ int seen[kMaxTop + 1];
-    const size_t row = blockIdx.x;
-    if (a.row_scale && a.row_scale[row] == 0.f) {
-        if (threadIdx.x == 0) {
-            a.kl[row] = a.ce[row] = 0.f;
-            if (a.dlogits) a.factors[4 * row + 1] = a.factors[4 * row + 2] = 0.f;
-        }
-        if (a.dlogits)
-            for (int k = threadIdx.x; k <= a.K; k += 64) a.marks[row * (a.K + 1) + k] = make_int2(-1, 0);
-        return;
-    }
+__device__ __forceinline__ float marked(const DistillArgs& a, const RowFactors& r, const Mark& k) {
+    const float e = exp2_fast((k.x - r.m) * a.c), e1 = a.two ? exp2_fast((k.x - r.m) * kLog2E) : e;
+    const float of_kl = k.kind & kListed ? r.listed * e - r.p * k.p : r.f * e;
+    return of_kl + r.f1 * e1 - (k.kind & kLabel ? r.label : 0.f);
+}
+
+// A row's sums out of its parts', the same in all lanes.
+__device__ __forceinline__ TwoSums<true> join_parts(const DistillArgs& a, size_t row) {
+    const int lane = threadIdx.x & 63;
     const float* const parts = a.parts + 4 * row * a.P;
     TwoSums<true> all;
-    for (int p = 0; p < a.P; ++p) all.m = fmaxf(all.m, parts[4 * p]);
-    for (int p = 0; p < a.P; ++p) {
+    for (int p = lane; p < a.P; p += 64) all.m = fmaxf(all.m, parts[4 * p]);
+    all.m = wave_max(all.m);
+    for (int p = lane; p < a.P; p += 64) {
         TwoSums<true> one;
         one.m = parts[4 * p], one.s = parts[4 * p + 1], one.s1 = parts[4 * p + 2];
         one.refer(all.m, a.c);
         all.s += one.s;
         all.s1 += one.s1;
     }
-    end_row<kBf16>(a, row, reinterpret_cast<const char*>(a.logits) + row * a.ld * elem_size<kBf16>(), all.m, all.s, all.s1, seen);
+    all.s = wave_total_f(all.s);
+    all.s1 = wave_total_f(all.s1);
+    return all;
+}
+
+// Losses alone: a wave for each row.
+__global__ __launch_bounds__(256) void distill_row_kernel(const DistillArgs a) {
+    const size_t row = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= (size_t)a.rows) return;
+    if (a.row_scale && a.row_scale[row] == 0.f) {
+        if ((threadIdx.x & 63) == 0) a.kl[row] = a.ce[row] = 0.f;
+        return;
+    }
+    const TwoSums<true> all = join_parts(a, row);
+    end_row(a, row, a.lists[row], a.marks + row * (a.K + 1), all.m, all.s, all.s1, true);
+}
+
+// 16 bytes of gradients at value i of a row that ends at `end`.
+template <bool kBf16>
+__device__ __forceinline__ void store_unit(char* out, int i, int end, const u32x4& w) {
+    constexpr int n = Vocab<kBf16>::n;
+    if (i + n <= end) {
+        *reinterpret_cast<u32x4*>(out + (size_t)i * elem_size<kBf16>()) = w;
+    } else {
+#pragma unroll
+        for (int k = 0; k < n - 1; ++k)
+            if (i + k < end) {
+                if constexpr (kBf16) reinterpret_cast<bf16_t*>(out)[i + k] = (bf16_t)(w[k >> 1] >> (16 * (k & 1)));
+                else reinterpret_cast<uint32_t*>(out)[i + k] = w[k];
+            }
+    }
+}
+
+// Gradients of a unit's values; f1 is in f where the temperature is 1.
+template <bool kBf16, bool kTwo>
+__device__ __forceinline__ void gradients(const DistillArgs& a, float m, float f, float f1, float (&v)[Vocab<kBf16>::n]) {
+#pragma unroll
+    for (int k = 0; k < Vocab<kBf16>::n; ++k) {
+        float g = f * exp2_fast((v[k] - m) * a.c);
+        if constexpr (kTwo) g = fmaf(f1, exp2_fast((v[k] - m) * kLog2E), g);
+        v[k] = g;
+    }
+}
+
+template <bool kBf16>
+__device__ __forceinline__ u32x4 pack_unit(const float (&v)[Vocab<kBf16>::n]) {
+    u32x4 w;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if constexpr (kBf16) w[k] = pack_bf16x2(v[2 * k], v[2 * k + 1]);
+        else w[k] = __float_as_uint(v[k]);
+    }
+    return w;
 }
 
 template <bool kBf16, bool kTwo>
 __global__ __launch_bounds__(kVT) void distill_grad_kernel(const DistillArgs a) {
     using W = Vocab<kBf16>;
+    __shared__ RowFactors shared;
     const size_t row = blockIdx.x / a.P;
     const int p = blockIdx.x % a.P, t = threadIdx.x;
     const char* const logits = reinterpret_cast<const char*>(a.logits) + row * a.ld * elem_size<kBf16>();
     char* const out = reinterpret_cast<char*>(a.dlogits) + row * a.ldd * elem_size<kBf16>();
     const int begin = p * a.length, end = min(a.V, begin + a.length);
-    const float m = a.factors[4 * row], f = a.factors[4 * row + 1], f1 = kTwo ? a.factors[4 * row + 2] : 0.f;
-    auto write = [&](int i, const u32x4& w) {
-        if (i + W::n <= end) {
-            *reinterpret_cast<u32x4*>(out + (size_t)i * elem_size<kBf16>()) = w;
-        } else {
-#pragma unroll
-            for (int k = 0; k < W::n - 1; ++k)
-                if (i + k < end) {
-                    if constexpr (kBf16) reinterpret_cast<bf16_t*>(out)[i + k] = (bf16_t)(w[k >> 1] >> (16 * (k & 1)));
-                    else reinterpret_cast<uint32_t*>(out)[i + k] = w[k];
-                }
-        }
-    };
-    const bool zero = f == 0.f && f1 == 0.f;  // padding, which is not read, or nothing off the list
+    if (a.row_scale && a.row_scale[row] == 0.f) {  // padding is not read
+        for (int i = begin + t * W::n; i < end; i += W::run) store_unit<kBf16>(out, i, end, u32x4{0, 0, 0, 0});
+        if (p == 0 && t == 0) a.kl[row] = a.ce[row] = 0.f;
+        return;
+    }
+    if (t < 64) {
+        const TwoSums<true> all = join_parts(a, row);
+        const RowFactors r = end_row(a, row, a.lists[row], a.marks + row * (a.K + 1), all.m, all.s, all.s1, p == 0);
+        if (t == 0) shared = r;
+    }
+    __syncthreads();
+    const RowFactors r = shared;
+    const float f = kTwo ? r.f : r.f + r.f1;
+    const bool zero = f == 0.f && (!kTwo || r.f1 == 0.f);  // nothing off the list
     if (zero)
-        for (int i = begin + t * W::n; i < end; i += W::run) write(i, u32x4{0, 0, 0, 0});
+        for (int i = begin + t * W::n; i < end; i += W::run) store_unit<kBf16>(out, i, end, u32x4{0, 0, 0, 0});
     each_step<kBf16>(logits, begin, zero ? begin : end, [&](int, int at, float (&v)[W::units][W::n]) {
 #pragma unroll
         for (int u = 0; u < W::units; ++u) {
             const int i = at + u * W::run + t * W::n;
-#pragma unroll
-            for (int k = 0; k < W::n; ++k) {
-                float g = f * exp2_fast((v[u][k] - m) * a.c);
-                if constexpr (kTwo) g = fmaf(f1, exp2_fast((v[u][k] - m) * kLog2E), g);
-                v[u][k] = g;
-            }
-            u32x4 w;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if constexpr (kBf16) w[k] = pack_bf16x2(v[u][2 * k], v[u][2 * k + 1]);
-                else w[k] = __float_as_uint(v[u][k]);
-            }
-            if (i < end) write(i, w);
+            gradients<kBf16, kTwo>(a, r.m, f, r.f1, v[u]);
+            if (i < end) store_unit<kBf16>(out, i, end, pack_unit<kBf16>(v[u]));
         }
     });
-    __syncthreads();  // the listed tokens' gradients go over what was written there
+    __syncthreads();  // the marked tokens' gradients go over what was written there
+    if (r.p == 0.f && r.label == 0.f) return;
     for (int k = t; k <= a.K; k += kVT) {
-        const int2 mark = a.marks[row * (a.K + 1) + k];
-        if (mark.x < begin || mark.x >= end) continue;
-        const float g = __int_as_float(mark.y);
-        if constexpr (kBf16) reinterpret_cast<bf16_t*>(out)[mark.x] = f32_to_bf16(g);
-        else reinterpret_cast<float*>(out)[mark.x] = g;
+        const Mark mark = a.marks[row * (a.K + 1) + k];
+        if (mark.id < begin || mark.id >= end) continue;
+        const float g = marked(a, r, mark);
+        if constexpr (kBf16) reinterpret_cast<bf16_t*>(out)[mark.id] = f32_to_bf16(g);
+        else reinterpret_cast<float*>(out)[mark.id] = g;
+    }
+}
+
+// The lists of rows whose gradients distill_whole_kernel makes, a wave each; rows without
+// a loss get their zeros here, each from a workgroup.
+template <bool kBf16>
+__global__ __launch_bounds__(256) void distill_list_kernel(const DistillArgs a) {
+    constexpr int n = Vocab<kBf16>::n;
+    __shared__ int seen[4][kMaxTop];
+    auto live = [&](int row) { return !(a.row_scale && a.row_scale[row] == 0.f); };
+    const int listed = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (listed < a.rows && live(listed)) list_row<kBf16>(a, listed, seen[threadIdx.x >> 6]);
+    const int row = blockIdx.x;
+    if (live(row)) return;
+    char* const out = reinterpret_cast<char*>(a.dlogits) + row * a.ldd * elem_size<kBf16>();
+    for (int i = threadIdx.x * n; i < a.V; i += 256 * n) store_unit<kBf16>(out, i, a.V, u32x4{0, 0, 0, 0});
+    if (threadIdx.x == 0) a.kl[row] = a.ce[row] = 0.f;
+}
+
+// A scalar load of what no kernel writes meanwhile: as a vector load it would be the last
+// of those in flight, and waiting for it would be waiting for the next row.
+template <typename T>
+__device__ __forceinline__ T load_scalar(const T* p) {
+    struct Words {
+        uint32_t w[sizeof(T) / 4];
+    } words;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 4); ++i) words.w[i] = ((const uint32_t __attribute__((address_space(4)))*)(uintptr_t)p)[i];
+    return __builtin_bit_cast(T, words);
+}
+
+// Whole rows in a workgroup's registers, one after another: each is read once.  While the
+// gradients of a row leave unit by unit, the next row's units come into the registers
+// that get free, and kLag units later they are summed: so memory is busy throughout,
+// where it would wait for the first pass of each row.  Unit 0 of a thread is the row's
+// last one, so that only it may be ragged.  A thread knows the marked tokens of its own
+// units from a list in LDS (which is in no order, and need not be).
+// kHeld units a thread: 32 leave registers for two waves of a SIMD, 16 for three.
+constexpr int waves_of(int held) { return held > 16 ? 2 : 3; }
+template <bool kBf16, int kThreads, int kHeld, bool kTail, bool kTwo>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_of(kHeld), waves_of(kHeld)))) void distill_whole_kernel(const DistillArgs a) {
+    constexpr int n = Vocab<kBf16>::n, run = kThreads * n, kLag = kHeld * 3 / 8;
+    __shared__ float part[3][kThreads / 64];
+    __shared__ RowFactors shared;
+    __shared__ Mark marks[2][kMaxTop + 1];  // of this row and of the next
+    __shared__ int after[2][kMaxTop + 1], head[2][kThreads];
+    __shared__ float mark_gradient[kMaxTop + 1];
+    const int t = threadIdx.x, last = (a.V - 1) / n * n, held = (a.V + run - 1) / run;
+    int tn = t * n;
+    u32x4 raw[kHeld];
+    auto logits_of = [&](int row) { return reinterpret_cast<const char*>(a.logits) + row * a.ld * elem_size<kBf16>(); };
+    // unit 0 past the row's end: its last one; units there are none of: the row's first ones, which are in the caches
+    auto request = [&](const char* logits, int i) {
+        const int at = max(held - 1 - i, 0) * run + tn;
+        raw[i] = load_unit<kBf16>(logits, i == 0 ? min(at, last) : at);
+    };
+    auto request_mark = [&](int row) { return a.marks[(size_t)row * (a.K + 1) + min(t, a.K)]; };
+    auto keep_mark = [&](int set, const Mark& mark) {
+        if (t > a.K) return;
+        marks[set][t] = mark;
+        if (mark.id >= 0) after[set][t] = atomicExch(&head[set][mark.id / n % kThreads], t);
+    };
+    auto units_with_marks = [&](int set) {
+        uint32_t has = 0;
+        for (int k = head[set][t]; k >= 0; k = after[set][k]) has |= 1u << (held - 1 - marks[set][k].id / run);
+        return has;
+    };
+    // the next row with a loss from `row` on, or the end
+    auto live = [&](int row) {
+        while (row < a.rows && a.row_scale && load_scalar(a.row_scale + row) == 0.f) row += gridDim.x;
+        return row;
+    };
+    auto leave_out = [&](int set, int i, float (&v)[n]) {
+        for (int k = head[set][t]; k >= 0; k = after[set][k]) {
+            const int at = marks[set][k].kind & kListed ? marks[set][k].id - i : -1;
+#pragma unroll
+            for (int j = 0; j < n; ++j) v[j] = j == at ? -INFINITY : v[j];
+        }
+    };
+    TwoSums<true> sums;
+    auto add_unit = [&](int i, int set, uint32_t has) {
+        if (i >= held) return;
+        const int base = (held - 1 - i) * run + tn;
+        float v[n];
+        unpack_unit<kBf16>(raw[i], v);
+        if (i == 0)
+#pragma unroll
+            for (int k = 0; k < n; ++k) v[k] = base + k < a.V ? v[k] : -INFINITY;
+        sums.raise(max_of(v, -INFINITY), a.c);
+        if (kTail && ((has >> i) & 1)) leave_out(set, base, v);
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < n; ++k) s += exp2_fast(fmaf(v[k], a.c, -sums.r));
+        sums.s += s;
+        if (kTwo)
+#pragma unroll
+            for (int k = 0; k < n; ++k) sums.s1 += exp2_fast(fmaf(v[k], kLog2E, -sums.r1));
+    };
+    int row = live(blockIdx.x), set = 0;
+    if (row >= a.rows) return;
+    Mark mark = request_mark(row);
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) request(logits_of(row), i);
+    head[0][t] = -1;
+    __syncthreads();
+    keep_mark(0, mark);
+    __syncthreads();
+    uint32_t has = units_with_marks(0);
+#pragma unroll
+    for (int i = 0; i < kHeld - kLag; ++i) add_unit(i, 0, has);
+    for (;;) {
+        const int next = live(row + gridDim.x), ahead = next < a.rows ? next : row;
+        const RowList list = load_scalar(a.lists + row);
+        mark = request_mark(ahead);
+        head[set ^ 1][t] = -1;
+#pragma unroll
+        for (int i = kHeld - kLag; i < kHeld; ++i) add_unit(i, set, has);
+        sums.settle(a.c);
+        TwoSums<true> all = join_threads<kThreads>(sums, a.c, part);
+        const bool wide = !(all.s < 3.0e38f && all.s1 < 3.0e38f);  // c m may have left fp32's range, or a value is no number
+        if (wide && all.m > -INFINITY && all.m < INFINITY) {  // differences first
+            TwoSums<true> again;
+            again.m = all.m;
+#pragma unroll 1
+            for (int at = t * n; at < a.V; at += run) {
+                float v[n];
+                load_values<kBf16>(logits_of(row), at, a.V, v);
+                if (kTail) leave_out(set, at, v);
+#pragma unroll
+                for (int k = 0; k < n; ++k) {
+                    again.s += exp2_fast((v[k] - all.m) * a.c);
+                    again.s1 += kTwo ? exp2_fast((v[k] - all.m) * kLog2E) : 0.f;
+                }
+            }
+            __syncthreads();
+            all = join_threads<kThreads>(again, a.c, part);
+        }
+        keep_mark(set ^ 1, mark);  // the heads were cleared before join_threads' barriers
+        if (t < 64) {
+            const RowFactors r = end_row(a, row, list, marks[set], all.m, all.s, all.s1, true);
+            for (int k = t; k <= a.K; k += 64) mark_gradient[k] = marked(a, r, marks[set][k]);
+            if (t == 0) shared = r;
+        }
+        __syncthreads();
+        const RowFactors r = shared;
+        const uint32_t has_next = units_with_marks(set ^ 1);
+        float f = kTwo ? r.f : r.f + r.f1, f1 = kTwo ? r.f1 : 0.f;
+        const bool zero = f == 0.f && f1 == 0.f;  // nothing off the list
+        char* const out = reinterpret_cast<char*>(a.dlogits) + row * a.ldd * elem_size<kBf16>();
+        const char* const logits_ahead = logits_of(ahead);
+        sums = TwoSums<true>();
+        if (wide || zero) {
+#pragma unroll 1
+            for (int at = t * n; at < a.V; at += run) {
+                float v[n];
+                load_values<kBf16>(logits_of(row), at, a.V, v);
+                gradients<kBf16, true>(a, r.m, f, f1, v);
+                u32x4 w = pack_unit<kBf16>(v);
+                if (zero) w = u32x4{0, 0, 0, 0};
+                store_unit<kBf16>(out, at, a.V, w);
+            }
+            __syncthreads();  // the marked tokens' gradients go over what was written there
+            for (int k = t; k <= a.K; k += kThreads) {
+                const int id = r.p == 0.f && r.label == 0.f ? -1 : marks[set][k].id;
+                if (id < 0) continue;
+                if constexpr (kBf16) reinterpret_cast<bf16_t*>(out)[id] = f32_to_bf16(mark_gradient[k]);
+                else reinterpret_cast<float*>(out)[id] = mark_gradient[k];
+            }
+            if (next >= a.rows) return;
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i) request(logits_ahead, i);
+#pragma unroll 1
+            for (int once = 0; once < 1; ++once)
+#pragma unroll
+                for (int i = 0; i < kHeld - kLag; ++i) add_unit(i, set ^ 1, has_next);
+        } else {
+            // exponents against c m rounded, what that is off in the factor
+            const float R = r.m * a.c, R1 = r.m * kLog2E;
+            f *= exp2_fast(-fmaf(r.m, a.c, -R)), f1 *= exp2_fast(-fmaf(r.m, kLog2E, -R1));
+            // without this the compiler keeps what it took apart, and compared, for the sums, which no registers hold
+            asm volatile("" : "+v"(tn));
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i) asm volatile("" : "+v"(raw[i]));
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i) {
+                if (i < held) {
+                    float v[n];
+                    unpack_unit<kBf16>(raw[i], v);
+                    if (kTwo) {
+#pragma unroll
+                        for (int k = 0; k < n; ++k)
+                            v[k] = fmaf(f1, exp2_fast(fmaf(v[k], kLog2E, -R1)), f * exp2_fast(fmaf(v[k], a.c, -R)));
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < n; ++k) v[k] = f * exp2_fast(fmaf(v[k], a.c, -R));
+                    }
+                    u32x4 w = pack_unit<kBf16>(v);
+                    const int base = (held - 1 - i) * run + tn;
+                    if ((has >> i) & 1)
+                        for (int k = head[set][t]; k >= 0; k = after[set][k]) {
+                            const int at = marks[set][k].id - base;
+                            if (at < 0 || at >= n) continue;
+                            const float g = mark_gradient[k];
+                            if constexpr (kBf16) {
+                                const uint32_t bits = (uint32_t)f32_to_bf16(g) << (16 * (at & 1)), mask = 0xffffu << (16 * (at & 1));
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) w[j] = j == at >> 1 ? (w[j] & ~mask) | bits : w[j];
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) w[j] = j == at ? __float_as_uint(g) : w[j];
+                            }
+                        }
+                    if (i > 0) *reinterpret_cast<u32x4*>(out + (size_t)base * elem_size<kBf16>()) = w;
+                    else if (base < a.V) store_unit<kBf16>(out, base, a.V, w);
+                }
+                request(logits_ahead, i);
+                if (i >= kLag) add_unit(i - kLag, set ^ 1, has_next);
+            }
+            if (next >= a.rows) return;
+        }
+        row = next;
+        set ^= 1;
+        has = has_next;
     }
 }
 
@@ -416,34 +727,66 @@ int check_distill(const flexmoe_distill_desc* D, int rows, const char* who, long
 
 int unit_run(int dtype) { return dtype == FLEXMOE_BF16 ? Vocab<true>::run : Vocab<false>::run; }
 
+constexpr int kComputeUnits = 256;
+constexpr int kWanted = 512;  // workgroups of parts of rows
+
 struct DistillLayout {
-    size_t factors, marks, total;
+    size_t lists, marks, total;
 };
 
 DistillLayout distill_layout(const flexmoe_distill_desc* D, int rows) {
     auto up = [](size_t n) { return (n + 255) & ~size_t(255); };
-    const size_t least = (D->V + kRange - 1) / kRange;
-    const size_t parts = std::max<size_t>(rows * least, std::min<size_t>((size_t)std::min(rows, kWantedWorkgroups) * std::max(1, D->V / kLeastRange),
-                                                                         2 * kWantedWorkgroups));
+    const size_t parts = most_parts(rows, D->V, kWanted);
     DistillLayout L;
-    L.factors = up(parts * 16);
-    L.marks = L.factors + up((size_t)rows * 16);
-    L.total = L.marks + up((size_t)rows * (D->top + 1) * 8) + 256;
+    L.lists = up(parts * 16);
+    L.marks = L.lists + up((size_t)rows * sizeof(RowList));
+    L.total = L.marks + up((size_t)rows * (D->top + 1) * sizeof(Mark)) + 256;
     return L;
 }
 
+// Workgroups that are at work together.
+int whole_grid(int threads, int held) { return kComputeUnits * waves_of(held) * 256 / threads; }
+
+template <bool kBf16, int kThreads, int kHeld>
+hipError_t launch_whole(const DistillArgs& a, hipStream_t s) {
+    distill_list_kernel<kBf16><<<a.row_scale ? a.rows : (a.rows + 3) / 4, 256, 0, s>>>(a);
+    const int grid = std::min(a.rows, whole_grid(kThreads, kHeld));
+    if (a.tail && a.two) distill_whole_kernel<kBf16, kThreads, kHeld, true, true><<<grid, kThreads, 0, s>>>(a);
+    else if (a.tail) distill_whole_kernel<kBf16, kThreads, kHeld, true, false><<<grid, kThreads, 0, s>>>(a);
+    else if (a.two) distill_whole_kernel<kBf16, kThreads, kHeld, false, true><<<grid, kThreads, 0, s>>>(a);
+    else distill_whole_kernel<kBf16, kThreads, kHeld, false, false><<<grid, kThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+// Whether rows are held whole by workgroups of `threads` times `held` units.  One read
+// pays where the second one would not find the logits in the last cache: from 96 MB of
+// them on (131072 tokens in bf16, 256, 512, 1024, 4096 rows: 57, 83, 138, 445 us against
+// 38, 86, 173, 644 in parts; 32000 tokens, 1024, 2048, 4096 rows: 42, 68, 133 against 42,
+// 92, 184; 50001 in fp32, 512, 1024, 4096: 61, 113, 368 against 66, 141, 544); of rows
+// that are long beside what is done once for each (5000 tokens in bf16, 4096 rows 51
+// against 42, 16384 tokens 81 against 95, with a tail and labels 115 against 95, 32000
+// tokens 168 against 187); and unless the last round of workgroups leaves many idle.
+bool holds(const DistillArgs& a, int n, int threads, int held) {
+    const size_t row = (size_t)a.V * 16 / n;
+    if (!a.dlogits || a.V > threads * held * n || row * a.rows < (96u << 20) || row < (a.tail || a.two ? 48u << 10 : 24u << 10)) return false;
+    const long long grid = whole_grid(threads, held), rounds = (a.rows + grid - 1) / grid;
+    return 4 * rounds * grid <= 5LL * a.rows;
+}
+
 template <bool kBf16>
-hipError_t launch_distill(const DistillArgs& a, int rows, hipStream_t s) {
-    const unsigned grid = (unsigned)rows * a.P;
+hipError_t launch_distill(const DistillArgs& a, hipStream_t s) {
+    constexpr int n = Vocab<kBf16>::n;
+    if (holds(a, n, 256, 16)) return launch_whole<kBf16, 256, 16>(a, s);
+    if (holds(a, n, 256, 32)) return launch_whole<kBf16, 256, 32>(a, s);
+    if (holds(a, n, 512, 32)) return launch_whole<kBf16, 512, 32>(a, s);
+    const unsigned parts = (unsigned)a.rows * a.P, grid = parts + (a.rows + 3) / 4;
     if (a.tail && a.two) distill_sums_kernel<kBf16, true, true><<<grid, kVT, 0, s>>>(a);
     else if (a.tail) distill_sums_kernel<kBf16, true, false><<<grid, kVT, 0, s>>>(a);
     else if (a.two) distill_sums_kernel<kBf16, false, true><<<grid, kVT, 0, s>>>(a);
     else distill_sums_kernel<kBf16, false, false><<<grid, kVT, 0, s>>>(a);
-    distill_row_kernel<kBf16><<<rows, 64, 0, s>>>(a);
-    if (a.dlogits) {
-        if (a.two) distill_grad_kernel<kBf16, true><<<grid, kVT, 0, s>>>(a);
-        else distill_grad_kernel<kBf16, false><<<grid, kVT, 0, s>>>(a);
-    }
+    if (!a.dlogits) distill_row_kernel<<<(a.rows + 3) / 4, 256, 0, s>>>(a);
+    else if (a.two) distill_grad_kernel<kBf16, true><<<parts, kVT, 0, s>>>(a);
+    else distill_grad_kernel<kBf16, false><<<parts, kVT, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -477,9 +820,9 @@ int flexmoe_distill(const flexmoe_distill_desc* desc, int32_t rows, const void* 
     DistillArgs a;
     a.logits = logits, a.ids = ids, a.labels = labels, a.lp = logprobs, a.row_scale = row_scale, a.kl = kl, a.ce = ce, a.dlogits = dlogits;
     char* const ws = (char*)workspace;
-    a.parts = (float*)ws, a.factors = (float*)(ws + L.factors), a.marks = (int2*)(ws + L.marks);
+    a.parts = (float*)ws, a.lists = (RowList*)(ws + L.lists), a.marks = (Mark*)(ws + L.marks);
     a.ld = (size_t)ld, a.ldd = (size_t)ldd, a.V = desc->V, a.K = desc->top, a.tail = desc->tail;
-    a.P = row_parts(rows, desc->V, unit_run(desc->dtype));
+    a.P = row_parts(rows, desc->V, unit_run(desc->dtype), kWanted);
     a.length = part_length(desc->V, a.P, unit_run(desc->dtype));
     a.two = labels && desc->temperature != 1.f;
     a.t = desc->temperature, a.inv_t = (float)(1.0 / desc->temperature), a.c = (float)(1.4426950408889634 / desc->temperature);
@@ -488,15 +831,15 @@ int flexmoe_distill(const flexmoe_distill_desc* desc, int32_t rows, const void* 
     const size_t es = bf16 ? 2 : 4;
     const int slice = (1 << 23) / a.P;  // a launch's threads are fewer than 2^32
     for (int done = 0; done < rows; done += slice) {
-        const int n = std::min(slice, rows - done);
-        const hipError_t err = bf16 ? launch_distill<true>(a, n, (hipStream_t)stream) : launch_distill<false>(a, n, (hipStream_t)stream);
+        const int n = a.rows = std::min(slice, rows - done);
+        const hipError_t err = bf16 ? launch_distill<true>(a, (hipStream_t)stream) : launch_distill<false>(a, (hipStream_t)stream);
         if (err != hipSuccess) return hip_fail(err, who);
         a.logits = (const char*)a.logits + (size_t)n * ld * es;
         if (a.dlogits) a.dlogits = (char*)a.dlogits + (size_t)n * ldd * es;
         a.ids += (size_t)n * a.K, a.lp += (size_t)n * a.K, a.kl += n, a.ce += n;
         if (labels) a.labels += n;
         if (row_scale) a.row_scale += n;
-        a.parts += (size_t)4 * n * a.P, a.factors += (size_t)4 * n, a.marks += (size_t)n * (a.K + 1);
+        a.parts += (size_t)4 * n * a.P, a.lists += n, a.marks += (size_t)n * (a.K + 1);
     }
     return FLEXMOE_OK;
 }

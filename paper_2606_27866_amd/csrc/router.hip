@@ -78,12 +78,6 @@ __device__ __forceinline__ float wave_max_f(float v) {
     return v;
 }
 
-__device__ __forceinline__ double wave_sum_d(double v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
-}
-
 __device__ __forceinline__ float log_sigmoid(float x) { return fminf(x, 0.f) - log1pf(expf(-fabsf(x))); }
 
 struct RouteScratch {
@@ -128,7 +122,7 @@ __device__ __forceinline__ double exact_sum(const float (&v)[NQ], float top) {
     double z = 0.0;
 #pragma unroll
     for (int q = 0; q < NQ; ++q) z += v[q] == -INFINITY ? 0.0 : exp((double)v[q] - (double)top);
-    return wave_sum_d(z);
+    return wave_total_d(z);
 }
 
 // The choice of one token by one wave, in 64 bits, from its logits v (expert lane NQ + q;

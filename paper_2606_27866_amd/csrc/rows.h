@@ -87,6 +87,30 @@ __device__ __forceinline__ void store8(void* p, size_t i, int left, const float 
     store_raw8<kBf16>(p, i, left, pack8<kBf16>(v));
 }
 
+// Sum of a double over the wave, in every lane: the steps of wave_total_f.
+__device__ __forceinline__ double wave_total_d(double v) {
+    union Halves {
+        double d;
+        int w[2];
+    };
+#define FLEXMOE_DSTEP(C, M)                                            \
+    {                                                                  \
+        Halves h{v};                                                   \
+        h.w[0] = dpp_shift<C, M>(h.w[0]), h.w[1] = dpp_shift<C, M>(h.w[1]); \
+        v += h.d;                                                      \
+    }
+    FLEXMOE_DSTEP(0x111, 0xf);
+    FLEXMOE_DSTEP(0x112, 0xf);
+    FLEXMOE_DSTEP(0x114, 0xf);
+    FLEXMOE_DSTEP(0x118, 0xf);
+    FLEXMOE_DSTEP(0x142, 0xa);
+    FLEXMOE_DSTEP(0x143, 0xc);
+#undef FLEXMOE_DSTEP
+    Halves h{v};
+    h.w[0] = __builtin_amdgcn_readlane(h.w[0], 63), h.w[1] = __builtin_amdgcn_readlane(h.w[1], 63);
+    return h.d;
+}
+
 // Sum over kWaves waves, in every thread: the waves' sums in order.  `part`
 // holds kWaves floats that no other sum uses before the next barrier.
 template <int kWaves>

@@ -26,6 +26,7 @@ using namespace flexmoe;
 namespace {
 
 constexpr int kCandidates = 1024;
+constexpr int kWanted = 512;  // workgroups
 
 struct LogprobArgs {
     const void* logits;
@@ -323,17 +324,10 @@ int check_vocab(const flexmoe_logprob_desc* D, int rows, const char* who, long l
 
 int unit_run(int dtype) { return dtype == FLEXMOE_BF16 ? Vocab<true>::run : Vocab<false>::run; }
 
-// Parts of rows of any call of up to `rows` rows: rows that have to be in parts, or
-// few rows in at most kWantedWorkgroups and one more each.
-size_t most_parts(int rows, int V) {
-    const size_t least = (V + kRange - 1) / kRange, most = V / kLeastRange, few = std::min(rows, kWantedWorkgroups);
-    return std::max(least > 1 ? rows * least : 0, most > 1 ? std::min<size_t>(few * most, 2 * kWantedWorkgroups) : 0);
-}
-
 size_t list_offset(size_t parts) { return (parts * 16 + 255) & ~size_t(255); }
 
 size_t logprob_bytes(const flexmoe_logprob_desc* D, int rows) {
-    const size_t parts = most_parts(rows, D->V);
+    const size_t parts = D->V < 2 * kLeastRange ? 0 : most_parts(rows, D->V, kWanted);  // else rows are whole
     return std::max<size_t>(256, list_offset(parts) + parts * D->top * 8);
 }
 
@@ -372,7 +366,7 @@ int flexmoe_token_logprobs(const flexmoe_logprob_desc* desc, int32_t rows, const
     LogprobArgs a;
     a.logits = logits, a.tokens = tokens, a.logprob = logprob, a.entropy = entropy, a.lse = lse, a.top_ids = top_ids, a.top_logprobs = top_logprobs;
     a.parts = nullptr, a.lists = nullptr, a.ld = (size_t)ld, a.V = desc->V, a.K = desc->top;
-    a.P = row_parts(rows, desc->V, unit_run(desc->dtype));
+    a.P = row_parts(rows, desc->V, unit_run(desc->dtype), kWanted);
     a.length = part_length(desc->V, a.P, unit_run(desc->dtype));
     a.inv_t = (float)(1.0 / desc->temperature), a.c = (float)(1.4426950408889634 / desc->temperature);
     if (a.P > 1) {

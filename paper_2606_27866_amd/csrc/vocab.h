@@ -182,16 +182,20 @@ __device__ __forceinline__ float key_value(uint32_t k) {
 // Larger value first, then lower place first.
 __device__ __forceinline__ uint64_t place_key(float v, int i) { return ((uint64_t)value_key(v) << 32) | (uint32_t)~i; }
 
-// Parts of a row: as few as kRange allows, and while there are few rows as many as
-// fill the compute units.
-constexpr int kWantedWorkgroups = 512;
-inline int row_parts(int rows, int V, int unit_run) {
+// Parts of a row: as few as kRange allows, and while there are few rows as many as make
+// `wanted` workgroups.
+inline int row_parts(int rows, int V, int unit_run, int wanted) {
     const int least = (V + kRange - 1) / kRange;
     const int most = std::max(1, V / kLeastRange);
-    const int wanted = rows > 0 ? (kWantedWorkgroups + rows - 1) / rows : 1;
-    const int parts = std::max(least, std::min(most, wanted));
+    const int parts = std::max(least, std::min(most, rows > 0 ? (wanted + rows - 1) / rows : 1));
     const int length = ((V + parts - 1) / parts + unit_run - 1) / unit_run * unit_run;
     return (V + length - 1) / length;
+}
+// Parts of all rows of any call of up to `rows` rows: rows that have to be in parts, or
+// few rows in at most `wanted` and one more each.
+inline size_t most_parts(int rows, int V, int wanted) {
+    const size_t least = (V + kRange - 1) / kRange, most = std::max(1, V / kLeastRange), few = std::min(rows, wanted);
+    return std::max(rows * least, std::min<size_t>(few * most, 2 * (size_t)wanted));
 }
 inline int part_length(int V, int parts, int unit_run) { return ((V + parts - 1) / parts + unit_run - 1) / unit_run * unit_run; }
 
