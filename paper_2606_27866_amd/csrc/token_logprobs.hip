@@ -7,8 +7,8 @@
 // Every thread keeps the maximum and the sums of its values, and the maximum of
 // each group of 32 of them in LDS.  The K-th largest of the threads' maxima is a
 // bound that at least K values reach; the few groups that reach it are read
-// again (from the caches) for the values that do, and those are ranked by
-// counting.  Where ties or an unlucky order leave more candidates than their
+// again (from the caches, all at once) for the values that do, and those are ranked
+// by counting.  Where ties or an unlucky order leave more candidates than their
 // buffer holds, the K-th largest (value, place) is found digit by digit in
 // further passes over the row, which is exact for any input.
 //
@@ -26,6 +26,9 @@ using namespace flexmoe;
 namespace {
 
 constexpr int kCandidates = 1024;
+constexpr int kJoined = 8;        // keys of a thread that joins the parts' lists
+constexpr int kMostKeys = kJoined * kVT;
+static_assert(kMostKeys >= ((1 << 21) / kRange) * kMaxTop, "the lists of the longest row's parts");
 constexpr int kWanted = 512;  // workgroups
 
 struct LogprobArgs {
@@ -45,19 +48,22 @@ struct TopScratch {
     uint64_t list[kCandidates];
     uint32_t key[kVT];
     uint32_t bound;
-    int count;
+    int count, items;
     int hist[256];
     uint64_t prefix;
     int left;
+    uint16_t item[kCandidates];  // groups that reach the bound
 };
 
-// The K-th largest of the threads' keys (one wave; 0 where there are fewer than K above it).
+// The K-th largest of the threads' keys by their upper halves (one wave): at least K of
+// the keys reach it.
 __device__ __forceinline__ uint32_t kth_key(const uint32_t* key, int K) {
     const int lane = threadIdx.x & 63;
     uint32_t k[kVT / 64], at = 0;
 #pragma unroll
     for (int q = 0; q < kVT / 64; ++q) k[q] = key[lane + 64 * q];
-    for (int bit = 31; bit >= 0; --bit) {
+#pragma unroll 4
+    for (int bit = 31; bit >= 16; --bit) {
         const uint32_t trial = at | (1u << bit);
         int n = 0;
 #pragma unroll
@@ -67,12 +73,13 @@ __device__ __forceinline__ uint32_t kth_key(const uint32_t* key, int K) {
     return at;
 }
 
-// The `want` largest of the candidates each(f) hands out as f(key), in order, to put(rank, key).
-// `own`: the largest value's key of this thread's candidates; near(bound, f) hands out those whose value may reach the bound.
+// The `want` largest of the candidates that each(f) hands out as f(key), in order, to
+// put(rank, key).  `own`: the largest value's key of this thread's candidates;
+// near(bound, f) hands out those whose value may reach the bound, by whichever thread.
 template <typename Each, typename Near, typename Put>
-__device__ void top_of(TopScratch& ts, uint32_t own, int want, Each&& each, Near&& near, Put&& put) {
+__device__ __forceinline__ void top_of(TopScratch& ts, uint32_t own, int want, Each&& each, Near&& near, Put&& put) {
     ts.key[threadIdx.x] = own;
-    if (threadIdx.x == 0) ts.count = 0;
+    if (threadIdx.x == 0) ts.count = ts.items = 0;
     __syncthreads();
     if (threadIdx.x < 64) {
         const uint32_t b = kth_key(ts.key, want);
@@ -107,12 +114,19 @@ __device__ void top_of(TopScratch& ts, uint32_t own, int want, Each&& each, Near
                 }
             });
             __syncthreads();
-            if (threadIdx.x == 0) {
-                int left = ts.left, digit = 255;
-                while (digit > 0 && ts.hist[digit] < left) left -= ts.hist[digit--];
-                ts.left = left;
-                ts.prefix = prefix | ((uint64_t)digit << shift);
-                ts.count = 0;
+            if (threadIdx.x < 64) {  // four digits a lane, the largest first
+                const int lane = threadIdx.x, left = ts.left;
+                int n[4], sum = 0;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) sum += n[q] = ts.hist[255 - 4 * lane - q];
+                const int upto = wave_incl_scan(sum);
+                if (lane == __ffsll((unsigned long long)__ballot(upto >= left)) - 1) {
+                    int rest = left - (upto - sum), q = 0;
+                    while (q < 3 && n[q] < rest) rest -= n[q++];
+                    ts.left = rest;
+                    ts.prefix = prefix | ((uint64_t)(255 - 4 * lane - q) << shift);
+                    ts.count = 0;
+                }
             }
             __syncthreads();
         }
@@ -128,6 +142,7 @@ __device__ void top_of(TopScratch& ts, uint32_t own, int want, Each&& each, Near
     for (int i = threadIdx.x; i < n; i += kVT) {
         const uint64_t k = ts.list[i];
         int rank = 0;
+#pragma unroll 8
         for (int j = 0; j < n; ++j) rank += ts.list[j] > k;
         if (rank < want) put(rank, k);
     }
@@ -239,17 +254,23 @@ __global__ __launch_bounds__(kVT) void logprob_kernel(const LogprobArgs a) {
             }
         };
         auto near = [&](uint32_t bound, auto&& f) {
-            for (int at = begin, it = 0; at < end; at += W::step, ++it) {
-                if (value_key(group[it * kVT + t]) < bound) continue;
-#pragma unroll
-                for (int u = 0; u < W::units; ++u) {
-                    const int i = at + u * W::run + t * W::n;
-                    float v[W::n];
-                    load_values<kBf16>(logits, i, end, v);
-#pragma unroll
-                    for (int k = 0; k < W::n; ++k)
-                        if (i + k < end) f(place_key(v[k], i + k));
+            for (int at = begin, it = 0; at < end; at += W::step, ++it)
+                if (value_key(group[it * kVT + t]) >= bound) {
+                    const int i = atomicAdd(&ts.items, 1);
+                    if (i < kCandidates) ts.item[i] = (uint16_t)(it * kVT + t);
                 }
+            __syncthreads();
+            if (ts.items > kCandidates) {  // digit by digit
+                if (t == 0) ts.count = kCandidates + 1;
+                return;
+            }
+            for (int i = t / W::units; i < ts.items; i += kVT / W::units) {
+                const int item = ts.item[i], at = begin + item / kVT * W::step + t % W::units * W::run + item % kVT * W::n;
+                float v[W::n];
+                load_values<kBf16>(logits, at, end, v);
+#pragma unroll
+                for (int k = 0; k < W::n; ++k)
+                    if (at + k < end) f(place_key(v[k], at + k));
             }
         };
         uint64_t* const list = a.P > 1 ? a.lists + (row * a.P + p) * a.K : nullptr;
@@ -273,26 +294,41 @@ __global__ __launch_bounds__(kVT) void logprob_join_kernel(const LogprobArgs a) 
     const int t = threadIdx.x;
     const void* const logits = reinterpret_cast<const char*>(a.logits) + row * a.ld * elem_size<kBf16>();
     const float* const parts = a.parts + 4 * row * a.P;
+    uint64_t key[kJoined];
+    const int keys = kTop ? a.P * a.K : 0;
+    if constexpr (kTop) {
+        const uint64_t* const lists = a.lists + row * a.P * a.K;
+        // each list turned by some places, else a thread's keys would be of one rank, and the bound a poor one
+#pragma unroll
+        for (int j = 0; j < kJoined; ++j) {
+            const int i = min(t + j * kVT, keys - 1), p = i / a.K;
+            key[j] = lists[p * a.K + (i + 37 * p) % a.K];
+        }
+    }
+    // every wave joins the sums, a part a lane
     Sums all;
-    for (int p = 0; p < a.P; ++p) all.m = fmaxf(all.m, parts[4 * p]);
-    for (int p = 0; p < a.P; ++p) {
+    const int lane = t & 63;
+    for (int p = lane; p < a.P; p += 64) all.m = fmaxf(all.m, parts[4 * p]);
+    all.m = wave_max(all.m);
+    for (int p = lane; p < a.P; p += 64) {
         Sums one;
         one.m = parts[4 * p], one.s = parts[4 * p + 1], one.h = parts[4 * p + 2];
         one.refer(all.m, a.c);
         all.s += one.s;
         all.h += one.h;
     }
+    all.s = wave_total_f(all.s);
+    all.h = wave_total_f(all.h);
     const RowEnd result(all, a.inv_t);
     if (t == 0) write_row(a, row, all, result, token_logit<kBf16>(a, row, logits));
     if constexpr (kTop) {
-        const uint64_t* const lists = a.lists + row * a.P * a.K;
-        const int n = a.P * a.K;
         uint32_t own = 0;
-        for (int i = t; i < n; i += kVT) own = max(own, (uint32_t)(lists[i] >> 32));
         auto each = [&](auto&& f) {
-            for (int i = t; i < n; i += kVT)
-                if (lists[i]) f(lists[i]);
+#pragma unroll
+            for (int j = 0; j < kJoined; ++j)
+                if (t + j * kVT < keys && key[j]) f(key[j]);  // 0: a part of fewer values
         };
+        each([&](uint64_t k) { own = max(own, (uint32_t)(k >> 32)); });
         top_of(ts, own, a.K, each, [&](uint32_t, auto&& f) { each(f); }, [&](int rank, uint64_t k) {
             a.top_ids[row * a.K + rank] = (int32_t)~(uint32_t)k;
             a.top_logprobs[row * a.K + rank] = result.logprob(key_value((uint32_t)(k >> 32)));
@@ -366,7 +402,7 @@ int flexmoe_token_logprobs(const flexmoe_logprob_desc* desc, int32_t rows, const
     LogprobArgs a;
     a.logits = logits, a.tokens = tokens, a.logprob = logprob, a.entropy = entropy, a.lse = lse, a.top_ids = top_ids, a.top_logprobs = top_logprobs;
     a.parts = nullptr, a.lists = nullptr, a.ld = (size_t)ld, a.V = desc->V, a.K = desc->top;
-    a.P = row_parts(rows, desc->V, unit_run(desc->dtype), kWanted);
+    a.P = row_parts(rows, desc->V, unit_run(desc->dtype), kWanted, desc->top ? kMostKeys / desc->top : 1 << 20);
     a.length = part_length(desc->V, a.P, unit_run(desc->dtype));
     a.inv_t = (float)(1.0 / desc->temperature), a.c = (float)(1.4426950408889634 / desc->temperature);
     if (a.P > 1) {

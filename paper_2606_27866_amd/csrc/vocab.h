@@ -183,10 +183,10 @@ __device__ __forceinline__ float key_value(uint32_t k) {
 __device__ __forceinline__ uint64_t place_key(float v, int i) { return ((uint64_t)value_key(v) << 32) | (uint32_t)~i; }
 
 // Parts of a row: as few as kRange allows, and while there are few rows as many as make
-// `wanted` workgroups.
-inline int row_parts(int rows, int V, int unit_run, int wanted) {
+// `wanted` workgroups, `limit` at most.
+inline int row_parts(int rows, int V, int unit_run, int wanted, int limit = 1 << 20) {
     const int least = (V + kRange - 1) / kRange;
-    const int most = std::max(1, V / kLeastRange);
+    const int most = std::max(1, std::min(V / kLeastRange, limit));
     const int parts = std::max(least, std::min(most, rows > 0 ? (wanted + rows - 1) / rows : 1));
     const int length = ((V + parts - 1) / parts + unit_run - 1) / unit_run * unit_run;
     return (V + length - 1) / length;
