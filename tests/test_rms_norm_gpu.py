@@ -12,7 +12,8 @@ from paper_2606_27866_amd import flexmoe as fm  # noqa: E402
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
 BF16, F32 = torch.bfloat16, torch.float32
-SHAPES = [(1, 1), (3, 7), (5, 8), (2, 9), (4, 512), (3, 513), (7, 2048), (1030, 520), (1025, 2047), (2, 2050), (3, 4096), (2, 4097), (1, 16384), (2, 16399)]
+SHAPES = [(1, 1), (3, 7), (5, 8), (2, 9), (4, 512), (3, 513), (7, 2048), (1030, 520), (1025, 2047), (2, 2050), (3, 4096), (2, 4097), (1030, 1000), (2, 8190), (1, 8193),
+          (1, 16384), (2, 16399)]
 
 
 def units(cols):
@@ -165,7 +166,7 @@ def grad_reference(dy, r, w, rstd, dr):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("rows,cols", SHAPES + [(300, 2048), (1100, 64), (2500, 4000)])
+@pytest.mark.parametrize("rows,cols", SHAPES + [(300, 2048), (1100, 64), (2500, 4000), (9000, 1024), (1030, 8192)])
 def test_backward(dtype, rows, cols):
     g, x, _, w = make(rows, cols, dtype)
     dy, dr = matrix(g, rows, cols, dtype, 0.1), matrix(g, rows, cols, dtype, 0.1, 24)
