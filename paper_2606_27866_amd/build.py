@@ -6,8 +6,8 @@ The library is one shared object holding every kernel and the C ABI of
 include/flexmoe.h.  All device code is compiled with packed-fp32 arithmetic
 disabled (-packed-fp32-ops); hipcc's host pass warns that it does not know
 the feature, which is harmless.  _tensors.so (host code, g++ and torch's C++
-headers) reads lists of tensors for the binding's optimizer; without them the
-library is built all the same.
+headers) reads lists of tensors for the binding's optimizer and makes the outputs
+of its operators on rows; without them the library is built all the same.
 """
 from __future__ import annotations
 
@@ -74,7 +74,7 @@ def build(verbose: bool = False) -> str:
     build_library(verbose)
     missing = tensors_missing()
     if missing:
-        sys.stderr.write("without _tensors.so, which the optimizer needs: no %s here\n" % missing)
+        sys.stderr.write("without _tensors.so, which the optimizer and the operators on rows need: no %s here\n" % missing)
     else:
         build_tensors()
     return LIB

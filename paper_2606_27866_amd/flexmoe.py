@@ -247,7 +247,7 @@ def tensors():
     global _tensors
     if _tensors is None:
         if not os.path.exists(TENSORS):
-            raise RuntimeError("_tensors.so, which the optimizer needs, is not built (%s); run `python -m paper_2606_27866_amd.build`" % TENSORS)
+            raise RuntimeError("_tensors.so, which the optimizer and the rows' operators need, is not built (%s); run `python -m paper_2606_27866_amd.build`" % TENSORS)
         import torch  # noqa: F401  (its libraries are loaded first)
         from . import _tensors as module
         _tensors = module
@@ -673,6 +673,26 @@ def _new(shape, dtype, device, stream=None):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+_F32, _BF16, _U8, _I32, _I8 = range(5)  # the native module's types
+
+
+def _make(like, pieces, together, stream=None):
+    """New tensors on like's device, as _new makes them, by the native module: (type, rows) or (type, rows, cols, pitch)
+    each; together: in one allocation, which lives as long as any of them."""
+    import torch
+    if stream is None or not like.is_cuda:
+        return tensors().make(like, pieces, together)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    with torch.cuda.stream(stream):
+        return tensors().make(like, pieces, together)
+
+
+def _row_piece(code, R, cols):
+    """Rows that start on 16-byte boundaries, for _make, of fp32 or bf16 (the C codes) or 8 bits."""
+    return (code, R, cols, _pitch(cols, 4 if code == _F32 else 2 if code == _BF16 else 1))
+
+
 def _padded(shape, dtype, device, stream=None):
     """A new tensor of `shape` whose rows start on 16-byte boundaries (a view of wider rows where they must)."""
     cols = _pitch(shape[-1], dtype.itemsize)
@@ -999,24 +1019,23 @@ class Router:
 
     def route(self, logits, bias=None, tables=True, stream=None) -> Routing:
         """logits [T, E] bf16 or fp32, bias [E] fp32."""
-        T, k, dev = logits.shape[0], self.top_k, logits.device
-        idx, w = _new((T, k), self._i32, dev, stream), _new((T, k), self._f32, dev, stream)
-        more = ()
+        T, k, E = logits.shape[0], self.top_k, self.E
+        out = (_I32, T, k, k), (_F32, T, k, k)
         if tables:
-            t = _new((2 * self.E + 1 + 2 * T * k,), self._i32, dev, stream)
-            more = t.split((self.E, self.E + 1, T * k, T * k))
-        ro = flexmoe_route_out(idx.data_ptr(), w.data_ptr(), *[m.data_ptr() for m in more])
+            out += (_I32, E), (_I32, E + 1), (_I32, T * k), (_I32, T * k)
+        out = _make(logits, out, True, stream)
+        ro = flexmoe_route_out(*[t.data_ptr() for t in out])
         with self._lock:
             self._logits(logits)
             _check(lib().flexmoe_route(self._desc, T, logits.data_ptr(), None if bias is None else _vector(bias, self.E, self._f32, "bias"),
                                        ctypes.byref(ro), *self._ws, _stream(stream)))
-        return Routing(idx, w, *more)
+        return Routing(*out)
 
     def backward(self, logits, topk_idx, dw, dlogits=None, stream=None):
         """The logits' gradient [T, E] from dw [T, top_k], that of the weights."""
         T = logits.shape[0]
         if dlogits is None:
-            dlogits = _new((T, self.E), logits.dtype, logits.device, stream)
+            dlogits, = _make(logits, ((_dtype_code(logits.dtype), T, self.E, self.E),), False, stream)
         with self._lock:
             self._logits(logits)
             _check(lib().flexmoe_route_backward(self._desc, T, logits.data_ptr(), _vector(topk_idx, T * self.top_k, self._i32, "topk_idx"),
@@ -1067,21 +1086,33 @@ class RMSNorm:
 
     def _forward(self, x, residual, r, y, q, scale, want_y, want_q, stream):
         R, dt, shape = self._rows(x, "x")
-        d, dev, w = self.desc, x.device, self.weight
-        if residual is not None and r is None:
-            r = _padded(shape, dt, dev, stream)
-        elif residual is None and r is not None:
+        d, w, code = self.desc, self.weight, _dtype_code(dt)
+        if residual is None and r is not None:
             raise ValueError("r goes with a residual")
-        rstd = None
+        rstd, rows = None, _row_piece(code, R, self.cols)
+        new = (rows,) if residual is not None and r is None else ()
         if want_y:
-            y = _padded(shape, dt, dev, stream) if y is None else y
+            if y is None:
+                new += (rows,)
             if not want_q:
-                rstd = _new((R,), self._f32, dev, stream)
+                new += ((_F32, R),)
         if want_q:
-            q = _padded(shape, self._i8, dev, stream) if q is None else q
-            scale = _new((R,), self._f32, dev, stream) if scale is None else scale
+            if q is None:
+                new += (_row_piece(_I8, R, self.cols),)
+            if scale is None:
+                new += ((_F32, R),)
+        if new:
+            new = iter(_make(x, new, False, stream))
+            if residual is not None and r is None:
+                r = next(new)
+            if want_y:
+                y = next(new) if y is None else y
+                rstd = None if want_q else next(new)
+            if want_q:
+                q = next(new) if q is None else q
+                scale = next(new) if scale is None else scale
         with self._lock:
-            d.dtype, d.ldx = _dtype_code(dt), _matrix(x, shape, dt, "x")
+            d.dtype, d.ldx = code, _matrix(x, shape, dt, "x")
             if residual is not None:
                 d.ldres, d.ldr = _matrix(residual, shape, dt, "residual"), _matrix(r, shape, dt, "r")
             else:
@@ -1100,18 +1131,18 @@ class RMSNorm:
         dw [cols] fp32 is written or, with accumulate, added to; None without weight_grad.
         """
         R, dt, shape = self._rows(dy, "dy")
-        d, dev, w = self.desc, dy.device, self.weight
-        if dx is None:
-            dx = _padded(shape, dt, dev, stream)
-        if not weight_grad:
-            if dw is not None or accumulate:
-                raise ValueError("dw and accumulate go with weight_grad")
-        elif dw is None:
-            if accumulate:
-                raise ValueError("accumulate needs dw")
-            dw = _new((self.cols,), self._f32, dev, stream)
+        d, w, code = self.desc, self.weight, _dtype_code(dt)
+        if not weight_grad and (dw is not None or accumulate):
+            raise ValueError("dw and accumulate go with weight_grad")
+        if weight_grad and dw is None and accumulate:
+            raise ValueError("accumulate needs dw")
+        new = ((_row_piece(code, R, self.cols),) if dx is None else ()) + (((_F32, self.cols),) if weight_grad and dw is None else ())
+        if new:
+            new = iter(_make(dy, new, False, stream))
+            dx = next(new) if dx is None else dx
+            dw = next(new) if weight_grad and dw is None else dw
         with self._lock:
-            d.dtype, d.ldy, d.ldr = _dtype_code(dt), _matrix(dy, shape, dt, "dy"), _matrix(r, shape, dt, "r")
+            d.dtype, d.ldy, d.ldr = code, _matrix(dy, shape, dt, "dy"), _matrix(r, shape, dt, "r")
             d.ldx = _matrix(dx, shape, dt, "dx")
             d.ldres = d.ldx if dr is None else _matrix(dr, shape, dt, "dr")
             _check(lib().flexmoe_rms_norm_backward(self._desc, R, dy.data_ptr(), r.data_ptr(), _vector(w, self.cols, w.dtype, "weight"),
@@ -1150,10 +1181,8 @@ class TokenLogprobs:
     def __call__(self, logits, tokens=None, stream=None) -> Logprobs:
         if logits.dim() != 2:
             raise ValueError("logits must be [R, %d], got %s" % (self.V, tuple(logits.shape)))
-        R, K, dt, d, dev = logits.shape[0], self.top, logits.dtype, self.desc, logits.device
-        values = _new((R * (3 + K),), self._f32, dev, stream)
-        logprob, entropy, lse, top = values.split((R, R, R, R * K))
-        ids, top = _new((R, K), self._i32, dev, stream), top.view(R, K)
+        R, K, dt, d = logits.shape[0], self.top, logits.dtype, self.desc
+        logprob, entropy, lse, ids, top = _make(logits, ((_F32, R), (_F32, R), (_F32, R), (_I32, R, K, K), (_F32, R, K, K)), True, stream)
         with self._lock:
             d.dtype, d.ld = _dtype_code(dt), _matrix(logits, (R, self.V), dt, "logits")
             _check(lib().flexmoe_token_logprobs(self._desc, R, logits.data_ptr(),
@@ -1194,13 +1223,13 @@ class Distillation:
     def _run(self, logits, ids, logprobs, labels, row_scale, grad, dlogits, stream):
         if logits.dim() != 2:
             raise ValueError("logits must be [R, %d], got %s" % (self.V, tuple(logits.shape)))
-        R, K, dt, d, dev = logits.shape[0], self.top, logits.dtype, self.desc, logits.device
+        R, K, dt, d, code = logits.shape[0], self.top, logits.dtype, self.desc, _dtype_code(logits.dtype)
         shape = (R, self.V)
-        kl, ce = _new((2, R), self._f32, dev, stream)
         if grad and dlogits is None:
-            dlogits = _padded(shape, dt, dev, stream)
+            dlogits, = _make(logits, (_row_piece(code, R, self.V),), False, stream)
+        kl, ce = _make(logits, ((_F32, R), (_F32, R)), True, stream)
         with self._lock:
-            d.dtype, d.ld = _dtype_code(dt), _matrix(logits, shape, dt, "logits")
+            d.dtype, d.ld = code, _matrix(logits, shape, dt, "logits")
             d.ldd = _matrix(dlogits, shape, dt, "dlogits") if grad else d.ld
             _check(lib().flexmoe_distill(self._desc, R, logits.data_ptr(), _vector(ids, R * K, self._i32, "ids"),
                                          _vector(logprobs, R * K, self._f32, "logprobs"),

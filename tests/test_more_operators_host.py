@@ -227,3 +227,23 @@ def test_distill_tensors():
     for bad in (x[0], x[:, :32], x.half(), x):  # the last is not on the GPU
         with pytest.raises(ValueError):
             h.forward(bad, ids, lp)
+
+
+def test_outputs_made_together_and_apart():
+    make, like = fm.tensors().make, torch.zeros(1)
+    pieces = ((0, 5), (1, 3, 5, 8), (3, 0), (3, 0, 4, 4), (2, 3), (4, 7, 10, 16))
+    for together in (True, False):
+        made = make(like, pieces, together)
+        assert [tuple(t.shape) for t in made] == [(5,), (3, 5), (0,), (0, 4), (3,), (7, 10)]
+        assert [t.dtype for t in made] == [torch.float32, torch.bfloat16, torch.int32, torch.int32, torch.uint8, torch.int8]
+        assert [t.stride() for t in made] == [(1,), (8, 1), (1,), (4, 1), (1,), (16, 1)]
+        storages = {t.untyped_storage().data_ptr() for t in made if t.numel()}
+        assert len(storages) == (1 if together else 4)
+        for i, t in enumerate(made):
+            t.fill_(i)
+        assert all(bool((t == i).all()) for i, t in enumerate(made))
+    assert make(like, (), True) == ()
+    for bad in [(like,), (like, ((5, 1),), 1), (like, ((0, 1, 3, 2),), 1), (like, ((0, 1, 3),), 1), (None, (), 1), (like, [], 1),
+                (like, ((0, -1),), 1), (like, ((0, "1"),), 1), (like, ((0, 1 << 31, 1 << 31, 1 << 31),), 1), (like, ((0, 1),) * 17, 1)]:
+        with pytest.raises(TypeError):
+            make(*bad)
