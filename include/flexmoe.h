@@ -13,7 +13,12 @@
  * action-learning step (Eqs. 5-8): sampled widths, the masked layer's
  * training forward and backward, and the action-logit gradient.  For training
  * pruned experts back and serving them in fewer bytes: the experts' products
- * with both gradients, products in 8-bit integers, and AdamW.
+ * with both gradients, products in 8-bit integers, and AdamW.  Around the layer:
+ * the root-mean-square norm before it, with its gradients and its rows in 8
+ * bits; routing with other scores, a balance bias and groups, with its
+ * gradient, and the forward that takes it; and over the vocabulary the log
+ * probabilities of tokens and the distillation loss of a pruned model, with its
+ * gradient.
  *
  * General rules for every entry point
  *   - All pointers except the descriptor, the host keep table of
@@ -327,6 +332,21 @@ int flexmoe_layer_forward_noalloc(const flexmoe_layer_desc *desc, int32_t T, con
                                   const void *w_down_r, const int32_t *keep_dev, const void *ws_gate,
                                   const void *ws_up, const void *ws_down, void *y,
                                   const flexmoe_route_out *dbg, void *stream);
+
+/* Forward with the caller's routing (flexmoe_route's, or any): expert topk_idx[t][j]
+ * has the weight topk_w[t][j] (int32 and fp32 [T][top_k], 4-byte aligned) in
+ * token t's sum; norm_topk is not used.  An id that is no expert (-1: a masked
+ * slot, a padding token) goes nowhere, as does one that an earlier slot of the
+ * token has; a token that goes nowhere gets the shared expert alone, or 0.
+ * packed_channels: -1 for the ranked weights of flexmoe_layer_forward, else that
+ * of flexmoe_layer_forward_clipped with its packed weights.  Every other rule and
+ * error is theirs, and so are the bits of y for their own routing. */
+int flexmoe_layer_forward_routed(const flexmoe_layer_desc *desc, int32_t T, const void *x,
+                                 const int32_t *topk_idx, const float *topk_w, const void *w_gate,
+                                 const void *w_up, const void *w_down, const int32_t *keep_dev,
+                                 int64_t packed_channels, const void *ws_gate, const void *ws_up,
+                                 const void *ws_down, void *y, void *workspace,
+                                 size_t workspace_bytes, void *stream);
 
 /* ---- Offline clipping (Sec. 4.4, Table 2): one budget exported as a
  * standalone compact subnetwork, run by the same kernels.

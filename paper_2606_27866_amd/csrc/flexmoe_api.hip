@@ -444,12 +444,18 @@ struct TrainKeep {
     float* dy;
 };
 
+// A caller's routing, in the place of logits.
+struct GivenRouting {
+    const int32_t* ids;
+    const float* weights;
+};
+
 int forward_impl(const flexmoe_layer_desc* desc, int32_t T, const void* x, const float* logits,
                  const void* w_gate_r, const void* w_up_r, const void* w_down_r, const int32_t* keep_dev,
                  int clipped, int packed_limit, const int32_t* bucket_keep, int k_align,
                  const void* ws_gate, const void* ws_up, const void* ws_down, void* y, void* workspace,
                  size_t workspace_bytes, const flexmoe_route_out* dbg, void* stream,
-                 const TrainKeep* tr = nullptr, bool allow_side = true) {
+                 const TrainKeep* tr = nullptr, bool allow_side = true, const GivenRouting* given = nullptr) {
     int rc = check_desc(desc);
     if (rc) return rc;
     const flexmoe_layer_desc& D = *desc;
@@ -464,12 +470,15 @@ int forward_impl(const flexmoe_layer_desc* desc, int32_t T, const void* x, const
     if (T < 0) return fail(FLEXMOE_EINVAL, "T = %d is negative", T);
     if (T > D.max_tokens) return fail(FLEXMOE_ESHAPE, "T = %d exceeds max_tokens = %d", T, D.max_tokens);
     if (T == 0) return FLEXMOE_OK;
-    if (!x || !logits || !w_gate_r || !w_up_r || !w_down_r || (!keep_dev && !bucketed) || (!y && train != 1))
+    if (!x || (given ? !given->ids || !given->weights : !logits) || !w_gate_r || !w_up_r || !w_down_r ||
+        (!keep_dev && !bucketed) || (!y && train != 1))
         return fail(FLEXMOE_EINVAL, "forward: an input/output pointer is NULL");
     for (const void* ptr : {x, w_gate_r, w_up_r, w_down_r, ws_gate, ws_up, ws_down, (const void*)y})
         if (((uintptr_t)ptr) & 15) return fail(FLEXMOE_EINVAL, "x, weights and y must be 16-byte aligned");
     if (((uintptr_t)logits) & 3 || (!bucketed && ((uintptr_t)keep_dev) & 3))
         return fail(FLEXMOE_EINVAL, "logits and keep_dev must be 4-byte aligned");
+    if (given && (((uintptr_t)given->ids | (uintptr_t)given->weights) & 3))
+        return fail(FLEXMOE_EINVAL, "ids and weights must be 4-byte aligned");
     const bool has_shared = D.I_shared > 0;
     if (has_shared != (ws_gate && ws_up && ws_down) || (!has_shared && (ws_gate || ws_up || ws_down)))
         return fail(FLEXMOE_EINVAL, "shared weights must be given iff I_shared > 0");
@@ -481,7 +490,7 @@ int forward_impl(const flexmoe_layer_desc* desc, int32_t T, const void* x, const
     hipStream_t s = (hipStream_t)stream;
     char* ws = (char*)workspace;
     int32_t* idx = (int32_t*)(ws + L.idx);
-    float* wts = (float*)(ws + L.wts);
+    float* wts = given ? const_cast<float*>(given->weights) : (float*)(ws + L.wts);  // not written where given
     int32_t* blockcnt = (int32_t*)(ws + L.blockcnt);
     int32_t* blockbase = (int32_t*)(ws + L.blockbase);
     int32_t* counts = (int32_t*)(ws + L.counts);
@@ -693,8 +702,19 @@ int forward_impl(const flexmoe_layer_desc* desc, int32_t T, const void* x, const
     // is submitted before the shared expert's GEMMs (it then reaches the
     // compute units first); the rest follow them.
     const bool small = (long long)T * D.top_k <= kSmallAssign;
-    const bool pre_routed = small && T > kSmallRouteT;
-    if (small && !pre_routed) {
+    const bool pre_routed = small && T > kSmallRouteT && !given;
+    if (small && given) {
+        KernelTimer kt(FLEXMOE_K_ROUTE, s);
+        err = launch_dispatch_small(nullptr, T, D.E, D.top_k, 0, keep_dev, D.I, D.I_shared, D.d, ts, packed_limit, plan,
+                                    kGivenRouting, const_cast<int32_t*>(given->ids), wts, counts, perm, pos, offsets, seg,
+                                    t1, t2, ord2, s);
+        if (err != hipSuccess) return hip_fail(err, "dispatch launch");
+    } else if (given) {
+        KernelTimer kt(FLEXMOE_K_ROUTE, s);
+        route_given_kernel<<<NB, 64 * kRouteTokens, 0, s>>>(given->ids, T, D.E, D.top_k, idx, blockcnt, NB);
+        err = hipGetLastError();
+        if (err != hipSuccess) return hip_fail(err, "route launch");
+    } else if (small && !pre_routed) {
         // one workgroup routes and dispatches everything (timed as routing)
         KernelTimer kt(FLEXMOE_K_ROUTE, s);
         err = launch_dispatch_small(logits, T, D.E, D.top_k, D.norm_topk, keep_dev, D.I, D.I_shared, D.d, ts,
@@ -731,10 +751,9 @@ int forward_impl(const flexmoe_layer_desc* desc, int32_t T, const void* x, const
         if (err != hipSuccess) return hip_fail(err, "dispatch scan launch");
         {
             KernelTimer kt(FLEXMOE_K_DISPATCH_SCATTER, s);
-            dispatch_scatter_kernel<<<NB, 64, 0, s>>>(idx, keep_dev, counts, blockbase, T, D.E, D.top_k,
-                                                      D.I, D.I_shared, D.d, NB, ts, packed_limit, plan,
-                                                      perm, pos, offsets, seg, t1, t2, ord2);
-            err = hipGetLastError();
+            err = launch_dispatch_scatter(given != nullptr, idx, keep_dev, counts, blockbase, T, D.E, D.top_k, D.I,
+                                          D.I_shared, D.d, NB, ts, packed_limit, plan, perm, pos, offsets, seg, t1, t2,
+                                          ord2, s);
         }
         if (err != hipSuccess) return hip_fail(err, "dispatch scatter launch");
     }
@@ -838,6 +857,20 @@ int flexmoe_layer_forward_noalloc(const flexmoe_layer_desc* desc, int32_t T, con
     return forward_impl(desc, T, x, logits, w_gate_r, w_up_r, w_down_r, keep_dev, 0, 0x7fffffff, nullptr, 0,
                         ws_gate, ws_up, ws_down, y, ws, kNoAllocScratchBytes, dbg, stream, nullptr,
                         /*allow_side=*/false);
+}
+
+int flexmoe_layer_forward_routed(const flexmoe_layer_desc* desc, int32_t T, const void* x, const int32_t* topk_idx,
+                                 const float* topk_w, const void* w_gate, const void* w_up, const void* w_down,
+                                 const int32_t* keep_dev, int64_t packed_channels, const void* ws_gate, const void* ws_up,
+                                 const void* ws_down, void* y, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_desc(desc);
+    if (rc) return rc;
+    if (packed_channels < -1 || packed_channels > (long long)desc->E * packed_width(desc->I))
+        return fail(FLEXMOE_EINVAL, "packed_channels = %lld outside [-1, E * ceil8(I)]", (long long)packed_channels);
+    const bool clipped = packed_channels >= 0;
+    const GivenRouting given{topk_idx, topk_w};
+    return forward_impl(desc, T, x, nullptr, w_gate, w_up, w_down, keep_dev, clipped, clipped ? (int)packed_channels : 0x7fffffff,
+                        nullptr, 0, ws_gate, ws_up, ws_down, y, workspace, workspace_bytes, nullptr, stream, nullptr, true, &given);
 }
 
 int64_t flexmoe_clipped_channels(const flexmoe_layer_desc* desc, const int32_t* keep_host) {

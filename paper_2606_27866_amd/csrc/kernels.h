@@ -254,13 +254,15 @@ __global__ void dispatch_scan_kernel(const int32_t* blockcnt, int NB, int32_t* b
 // (expert ids) and GEMM widths plan[E..2E).
 // keep = NULL: the plan alone
 __global__ void set_plan_kernel(int32_t* keep, int32_t* plan, KeepArgs k, KeepArgs order, KeepArgs kg, int E);
-__global__ void dispatch_scatter_kernel(const int32_t* idx, const int32_t* keep,
-                                        const int32_t* counts, const int32_t* blockbase, int T,
-                                        int E, int k, int I, int I_shared, int d, int NB,
-                                        TileShape ts, int packed_limit, const int32_t* plan,
-                                        int32_t* perm, int32_t* pos,
-                                        int32_t* offsets, SegMeta* seg, int32_t* t1start,
-                                        int32_t* t2start, int32_t* order2);
+// given: idx holds -1 where a caller's routing goes nowhere (route_given_kernel).
+__global__ void route_given_kernel(const int32_t* ids, int T, int E, int k, int32_t* idx, int32_t* blockcnt, int NB);
+hipError_t launch_dispatch_scatter(bool given, const int32_t* idx, const int32_t* keep, const int32_t* counts,
+                                   const int32_t* blockbase, int T, int E, int k, int I, int I_shared, int d, int NB,
+                                   TileShape ts, int packed_limit, const int32_t* plan, int32_t* perm, int32_t* pos,
+                                   int32_t* offsets, SegMeta* seg, int32_t* t1start, int32_t* t2start,
+                                   int32_t* order2, hipStream_t s);
+// pre_routed: 0, 1 (route_kernel wrote idx) or kGivenRouting (idx holds a caller's ids, unchecked).
+constexpr int kGivenRouting = 2;
 hipError_t launch_dispatch_small(const float* logits, int T, int E, int k, int norm_topk, const int32_t* keep, int I,
                                  int I_shared, int d, TileShape ts, int packed_limit, const int32_t* plan,
                                  int pre_routed, int32_t* idx, float* wts, int32_t* counts, int32_t* perm,

@@ -341,8 +341,9 @@ __device__ __forceinline__ int width_rank4(const int* kk_s, int q0, int ks, int 
 // One wave: stable placement of assignments [a0, a1) in rounds of 64.  The
 // match mask of equal expert ids comes from 8 ballots; a lane's rank is the
 // number of matching lower lanes; the lowest matching lane advances run[e].
-// base(e) is where this range's first assignment of expert e goes.
-template <typename BaseFn>
+// base(e) is where this range's first assignment of expert e goes.  kGiven:
+// ids of -1 go nowhere.
+template <bool kGiven, typename BaseFn>
 __device__ __forceinline__ void place(const int32_t* __restrict__ idx, int a0, int a1, const int* kk_s,
                                       int* run, BaseFn base, int32_t* __restrict__ perm,
                                       int32_t* __restrict__ pos) {
@@ -351,27 +352,29 @@ __device__ __forceinline__ void place(const int32_t* __restrict__ idx, int a0, i
     for (int r0 = a0; r0 < a1; r0 += 64) {
         const int a = r0 + lane;
         const bool valid = a < a1;
-        const int e = valid ? idx[a] : 0;
-        uint64_t match = __ballot(valid);
+        const int id = valid ? idx[a] : 0;
+        const bool goes = kGiven ? valid && id >= 0 : valid;
+        const int e = kGiven ? max(id, 0) : id;
+        uint64_t match = __ballot(goes);
 #pragma unroll
         for (int bit = 0; bit < 8; ++bit) {
             const bool b = (e >> bit) & 1;
-            const uint64_t bb = __ballot(valid && b);
+            const uint64_t bb = __ballot(goes && b);
             match &= b ? bb : ~bb;
         }
         const int rank = __popcll(match & lt);
-        const int r = valid ? run[e] : 0;
+        const int r = goes ? run[e] : 0;
         __builtin_amdgcn_wave_barrier();
         __atomic_signal_fence(__ATOMIC_SEQ_CST);
         if (valid) {
-            if (kk_s[e] > 0) {
+            if (goes && kk_s[e] > 0) {
                 const int dst = base(e) + r + rank;
                 perm[dst] = a;
                 pos[a] = dst;
             } else {
                 pos[a] = -1;
             }
-            if ((match & lt) == 0) run[e] = r + __popcll(match);
+            if (goes && (match & lt) == 0) run[e] = r + __popcll(match);
         }
         __builtin_amdgcn_wave_barrier();
         __atomic_signal_fence(__ATOMIC_SEQ_CST);
@@ -398,6 +401,33 @@ __global__ __launch_bounds__(64 * kRouteTokens) void route_kernel(
             wts[(size_t)t * k + lane] = w[0];
             atomicAdd(&hist[id[0]], 1);  // a count: arrival order does not matter
         }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += blockDim.x) blockcnt[(size_t)e * NB + blockIdx.x] = hist[e];
+}
+
+// The expert of assignment a in a caller's routing: -1 (nowhere) for an id
+// that is no expert, and for one that an earlier slot of the token has (an
+// expert has at most T rows, as the tile lists and the decode tiles assume).
+__device__ __forceinline__ int given_expert(const int32_t* __restrict__ ids, int a, int k, int E) {
+    const int e = ids[a];
+    bool ok = (unsigned)e < (unsigned)E;
+    for (int j = a / k * k; j < a; ++j) ok = ok && ids[j] != e;
+    return ok ? e : -1;
+}
+
+// route_kernel's place in a forward with a caller's routing: checks one chunk's
+// ids and counts them.
+__global__ __launch_bounds__(64 * kRouteTokens) void route_given_kernel(
+    const int32_t* __restrict__ ids, int T, int E, int k, int32_t* __restrict__ idx, int32_t* __restrict__ blockcnt, int NB) {
+    __shared__ int hist[kMaxExperts];
+    for (int e = threadIdx.x; e < E; e += blockDim.x) hist[e] = 0;
+    __syncthreads();
+    const int a0 = blockIdx.x * kRouteTokens * k, a1 = min((int)(blockIdx.x + 1) * kRouteTokens, T) * k;
+    for (int a = a0 + (int)threadIdx.x; a < a1; a += blockDim.x) {
+        const int e = given_expert(ids, a, k, E);
+        idx[a] = e;
+        if (e >= 0) atomicAdd(&hist[e], 1);  // a count: arrival order does not matter
     }
     __syncthreads();
     for (int e = threadIdx.x; e < E; e += blockDim.x) blockcnt[(size_t)e * NB + blockIdx.x] = hist[e];
@@ -444,6 +474,7 @@ __global__ __launch_bounds__(256) void dispatch_scan_kernel(const int32_t* __res
     if (threadIdx.x == 0) counts[e] = carry;
 }
 
+template <bool kGiven>
 __global__ __launch_bounds__(64) void dispatch_scatter_kernel(
     const int32_t* __restrict__ idx, const int32_t* __restrict__ keep,
     const int32_t* __restrict__ counts, const int32_t* __restrict__ blockbase, int T, int E, int k,
@@ -475,7 +506,18 @@ __global__ __launch_bounds__(64) void dispatch_scatter_kernel(
     const int a0 = blockIdx.x * kRouteTokens * k;
     const int a1 = min((blockIdx.x + 1) * kRouteTokens, T) * k;
     auto base = [&](int e) { return off[e] + blockbase[(size_t)e * NB + blockIdx.x]; };
-    place(idx, a0, a1, kk_s, run, base, perm, pos);
+    place<kGiven>(idx, a0, a1, kk_s, run, base, perm, pos);
+}
+
+hipError_t launch_dispatch_scatter(bool given, const int32_t* idx, const int32_t* keep, const int32_t* counts,
+                                   const int32_t* blockbase, int T, int E, int k, int I, int I_shared, int d, int NB,
+                                   TileShape ts, int packed_limit, const int32_t* plan, int32_t* perm, int32_t* pos,
+                                   int32_t* offsets, SegMeta* seg, int32_t* t1start, int32_t* t2start,
+                                   int32_t* order2, hipStream_t s) {
+    auto* const kernel = given ? dispatch_scatter_kernel<true> : dispatch_scatter_kernel<false>;
+    kernel<<<NB, 64, 0, s>>>(idx, keep, counts, blockbase, T, E, k, I, I_shared, d, NB, ts, packed_limit, plan, perm, pos,
+                             offsets, seg, t1start, t2start, order2);
+    return hipGetLastError();
 }
 
 // Route, count, scan and place in one workgroup (T * k <= kSmallAssign).
@@ -484,11 +526,12 @@ __global__ __launch_bounds__(64) void dispatch_scatter_kernel(
 // every expert's segment, so the 16 waves place their assignments at once,
 // in the same order as one pass over the tokens would.  With pre_routed the
 // tokens were routed by route_kernel (spread over several compute units):
-// the waves read their tokens' expert ids instead.
+// the waves read their tokens' expert ids instead.  kGiven: the ids in idx are a
+// caller's, checked here.
 // kPairs: the waves route their tokens two at a time and rank them with one
 // compare per pair of experts (launch_dispatch_small: more than one token per
 // wave and more than kRankTwiceExperts experts), else one after another.
-template <bool kPairs>
+template <bool kPairs, bool kGiven>
 __global__ __launch_bounds__(64 * kSmallWaves) void dispatch_small_kernel(
     const float* __restrict__ logits, int T, int E, int k, int norm_topk,
     const int32_t* __restrict__ keep, int I, int I_shared, int d, TileShape ts, int packed_limit,
@@ -518,14 +561,20 @@ __global__ __launch_bounds__(64 * kSmallWaves) void dispatch_small_kernel(
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
     const int per = ceil_div(T, kSmallWaves);
     const int t0 = min(T, wave * per), t1 = min(T, t0 + per);
-    if (pre_routed) {
+    if constexpr (kGiven) {
+        for (int a = t0 * k + lane; a < t1 * k; a += 64) {
+            const int id = given_expert(idx, a, k, E);
+            sidx[a] = id;
+            if (id >= 0) atomicAdd(&hist[wave][id], 1);  // a count: arrival order does not matter
+        }
+    } else if (pre_routed) {
         for (int a = t0 * k + lane; a < t1 * k; a += 64) {
             const int id = min(max(idx[a], 0), E - 1);
             sidx[a] = id;
             atomicAdd(&hist[wave][id], 1);  // a count: arrival order does not matter
         }
     }
-    if (!pre_routed) {
+    if (!kGiven && !pre_routed) {
         auto keep_token = [&](int t, int id, float w) {
             if (lane < k) {
                 idx[(size_t)t * k + lane] = id;
@@ -612,7 +661,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void dispatch_small_kernel(
     __syncthreads();
     // this wave's running position inside each expert starts at its base
     auto base = [&](int e) { return off[e]; };
-    place(sidx, t0 * k, t1 * k, kk_s, hist[wave], base, perm, pos);
+    place<kGiven>(sidx, t0 * k, t1 * k, kk_s, hist[wave], base, perm, pos);
 }
 
 hipError_t launch_dispatch_small(const float* logits, int T, int E, int k, int norm_topk, const int32_t* keep, int I,
@@ -630,12 +679,16 @@ hipError_t launch_dispatch_small(const float* logits, int T, int E, int k, int n
     // small layer 0.5 us, and routing a Qwen2-57B-shaped single token 2 us
     // sooner made its step 2 us longer (121 -> 124): the routed gate/up GEMM
     // then contends with the shared expert's, whose chain ends last.
-    if (T <= kSmallWaves || E <= kRankTwiceExperts || pre_routed)
-        dispatch_small_kernel<false><<<1, 64 * kSmallWaves, 0, s>>>(logits, T, E, k, norm_topk, keep, I, I_shared, d, ts,
+    if (pre_routed == kGivenRouting)
+        dispatch_small_kernel<false, true><<<1, 64 * kSmallWaves, 0, s>>>(nullptr, T, E, k, 0, keep, I, I_shared, d, ts,
+                                                                          packed_limit, plan, 1, idx, wts, counts, perm,
+                                                                          pos, offsets, seg, t1start, t2start, order2);
+    else if (T <= kSmallWaves || E <= kRankTwiceExperts || pre_routed)
+        dispatch_small_kernel<false, false><<<1, 64 * kSmallWaves, 0, s>>>(logits, T, E, k, norm_topk, keep, I, I_shared, d, ts,
                                                                     packed_limit, plan, pre_routed, idx, wts, counts,
                                                                     perm, pos, offsets, seg, t1start, t2start, order2);
     else
-        dispatch_small_kernel<true><<<1, 64 * kSmallWaves, 0, s>>>(logits, T, E, k, norm_topk, keep, I, I_shared, d, ts,
+        dispatch_small_kernel<true, false><<<1, 64 * kSmallWaves, 0, s>>>(logits, T, E, k, norm_topk, keep, I, I_shared, d, ts,
                                                                    packed_limit, plan, 0, idx, wts, counts, perm, pos,
                                                                    offsets, seg, t1start, t2start, order2);
     return hipGetLastError();

@@ -34,7 +34,7 @@ ERRORS = {
 EXPORTED = ("flexmoe_workspace_bytes", "flexmoe_rank_reorder", "flexmoe_set_budget",
             "flexmoe_layer_forward", "flexmoe_keep_from_ratio", "flexmoe_last_error",
             "flexmoe_timing_enable", "flexmoe_timing_read", "flexmoe_clipped_channels",
-            "flexmoe_export_clipped", "flexmoe_layer_forward_clipped",
+            "flexmoe_export_clipped", "flexmoe_layer_forward_clipped", "flexmoe_layer_forward_routed",
             "flexmoe_layer_forward_bucketed", "flexmoe_saliency_workspace_bytes",
             "flexmoe_channel_saliency", "flexmoe_transpose_weights", "flexmoe_sample_actions",
             "flexmoe_train_workspace_bytes", "flexmoe_train_forward", "flexmoe_train_backward",
@@ -163,6 +163,8 @@ def lib():
         L.flexmoe_layer_forward_clipped.argtypes = ([D, i32] + [vp] * 6 + [ctypes.c_int64] + [vp] * 5
                                                     + [sz, ctypes.POINTER(flexmoe_route_out), vp])
         L.flexmoe_layer_forward_clipped.restype = ctypes.c_int
+        L.flexmoe_layer_forward_routed.argtypes = [D, i32] + [vp] * 7 + [ctypes.c_int64] + [vp] * 5 + [sz, vp]
+        L.flexmoe_layer_forward_routed.restype = ctypes.c_int
         L.flexmoe_layer_forward_bucketed.argtypes = ([D, i32] + [vp] * 6 + [i32] + [vp] * 5
                                                      + [sz, ctypes.POINTER(flexmoe_route_out), vp])
         L.flexmoe_layer_forward_bucketed.restype = ctypes.c_int
@@ -383,6 +385,17 @@ def flexmoe_layer_forward_clipped(desc, T, x, logits, w_gate_c, w_up_c, w_down_c
         _p(keep_dev), int(packed_channels), _p(ws_gate), _p(ws_up), _p(ws_down), _p(y),
         _p(workspace), int(workspace_bytes), ctypes.byref(ro) if ro is not None else None,
         _stream(stream)))
+
+
+def flexmoe_layer_forward_routed(desc, T, x, topk_idx, topk_w, w_gate, w_up, w_down, keep_dev, packed_channels, ws_gate,
+                                 ws_up, ws_down, y, workspace, workspace_bytes=None, stream=None):
+    """packed_channels: -1 for ranked weights."""
+    if workspace_bytes is None:
+        workspace_bytes = workspace.numel() * workspace.element_size()
+    _check(lib().flexmoe_layer_forward_routed(
+        ctypes.byref(desc), int(T), _p(x), _p(topk_idx), _p(topk_w), _p(w_gate), _p(w_up), _p(w_down),
+        _p(keep_dev), int(packed_channels), _p(ws_gate), _p(ws_up), _p(ws_down), _p(y),
+        _p(workspace), int(workspace_bytes), _stream(stream)))
 
 
 def flexmoe_layer_forward_bucketed(desc, T, x, logits, w_gate_r, w_up_r, w_down_r, keep_host, k_align,
@@ -1292,11 +1305,16 @@ class Layer:
         keep_dev = torch.from_numpy(np.asarray(keep_host, dtype=np.int32).copy()).to(self.device)
         return ClippedWeights(keep_host, *bufs, P, keep_dev)
 
-    def forward(self, x, logits, y=None, keep=None, dbg=None, stream=None, clipped=None,
-                bucketed=None):
+    def forward(self, x, logits=None, y=None, keep=None, dbg=None, stream=None, clipped=None,
+                bucketed=None, routing=None):
         """clipped: a ClippedWeights of this layer -> the offline-clipped path;
-        bucketed: (keep_host, k_align) -> the bucketed ablation."""
+        bucketed: (keep_host, k_align) -> the bucketed ablation;
+        routing: a Router's Routing in the place of logits (ids of -1 go nowhere)."""
         T = x.shape[0]
+        if (logits is None) == (routing is None):
+            raise ValueError("give either logits or routing")
+        if routing is not None:
+            return self._forward_routed(T, x, routing, y, keep, dbg, stream, clipped, bucketed)
         if y is None:
             y = _new((T, self.desc.d), self.tdtype, self.device, stream)
         D = self.desc
@@ -1317,6 +1335,27 @@ class Layer:
         flexmoe_layer_forward(self.desc, T, x, logits, self.w_gate, self.w_up, self.w_down,
                               self.keep if keep is None else keep, self.ws_gate, self.ws_up,
                               self.ws_down, y, self.workspace, dbg=dbg, stream=stream)
+        return y
+
+
+    def _forward_routed(self, T, x, routing, y, keep, dbg, stream, clipped, bucketed):
+        import torch
+        D = self.desc
+        if dbg is not None or bucketed is not None:
+            raise ValueError("routing goes with neither dbg nor bucketed")
+        n = T * D.top_k
+        idx, w = _vector(routing.topk_idx, n, torch.int32, "topk_idx"), _vector(routing.topk_w, n, torch.float32, "topk_w")
+        if y is None:
+            y = _new((T, D.d), self.tdtype, self.device, stream)
+        _packed(x, T * D.d, "x")
+        _packed(y, T * D.d, "y")
+        if clipped is None:
+            weights, packed = (self.w_gate, self.w_up, self.w_down, self.keep if keep is None else keep), -1
+        else:
+            weights = clipped.w_gate_c, clipped.w_up_c, clipped.w_down_c, clipped.keep_dev if keep is None else keep
+            packed = clipped.packed_channels
+        flexmoe_layer_forward_routed(D, T, x, idx, w, *weights, packed, self.ws_gate, self.ws_up, self.ws_down, y,
+                                     self.workspace, stream=stream)
         return y
 
 

@@ -247,3 +247,27 @@ def test_outputs_made_together_and_apart():
                 (like, ((0, -1),), 1), (like, ((0, "1"),), 1), (like, ((0, 1 << 31, 1 << 31, 1 << 31),), 1), (like, ((0, 1),) * 17, 1)]:
         with pytest.raises(TypeError):
             make(*bad)
+
+
+# ---- the forward with a caller's routing ---------------------------------------
+def test_routed_forward_arguments():
+    D = fm.make_desc(64, 8, 40, 2, 0, fm.FLEXMOE_BF16, 1, 100)
+
+    def call(T=10, x=FAKE, ids=FAKE, w=FAKE, keep=FAKE, packed=-1, y=FAKE, ws=FAKE, nbytes=1 << 30, shared=None):
+        fm.flexmoe_layer_forward_routed(D, T, x, ids, w, FAKE, FAKE, FAKE, keep, packed, shared, shared, shared, y, ws, nbytes, 0)
+
+    for kw, code in [(dict(T=-1), -1), (dict(T=101), -2), (dict(x=None), -1), (dict(ids=None), -1), (dict(w=None), -1), (dict(keep=None), -1),
+                     (dict(y=None), -1), (dict(packed=-2), -1), (dict(packed=8 * 40 + 8), -1), (dict(ids=FAKE + 2), -1), (dict(w=FAKE + 1), -1),
+                     (dict(x=FAKE + 8), -1), (dict(keep=FAKE + 2), -1), (dict(ws=None), -4), (dict(nbytes=64), -4), (dict(ws=FAKE + 8), -4),
+                     (dict(shared=FAKE), -1)]:
+        assert code_of(call, **kw) == code, kw
+    call(T=0, x=None, ids=None, w=None)  # nothing to do
+
+
+def test_layer_takes_logits_or_routing():
+    layer = fm.Layer(64, 8, 40, 2, device="cpu")
+    x, logits, r = torch.zeros(1, 64, dtype=torch.bfloat16), torch.zeros(1, 8), fm.Routing(torch.zeros(1, 2, dtype=torch.int32), torch.zeros(1, 2))
+    for kw in [dict(), dict(logits=logits, routing=r), dict(routing=r, dbg={}), dict(routing=r, bucketed=([40] * 8, 8)),
+               dict(routing=r), dict(routing=r._replace(topk_idx=torch.zeros(1, 2, dtype=torch.int64)))]:
+        with pytest.raises(ValueError):
+            layer.forward(x, **kw)
