@@ -60,11 +60,13 @@ struct DistillArgs {
     float* parts;     // [rows][P][4]: m, sum at t, sum at 1
     RowList* lists;   // [rows]
     Mark* marks;      // [rows][K + 1]
+    int32_t *order, *counts;  // per kOrder rows: those with a loss, and how many (row_scale given)
     size_t ld, ldd;
     int rows, V, P, length, K, tail, two;  // two: the labels' sum is not that of t
     float c, inv_t, t, kl_weight, ce_weight;
 };
 
+constexpr int kOrder = 256;
 constexpr float kLog2E = 1.4426950408889634f;
 
 // Sums at t and, where they differ, at 1, while the largest value is still growing.
@@ -144,22 +146,32 @@ __device__ __forceinline__ void leave_out(const uint32_t* bits, int i, float (&v
         for (int k = 0; k < n; ++k) v[k] = (b >> k) & 1 ? -INFINITY : v[k];
 }
 
-// One wave writes down what a row's list gives, kOwn tokens a lane.  seen: K ints of LDS.
+// One wave writes down what the list of a row with a loss gives, kOwn tokens a lane.  seen: K ints of LDS.
 template <bool kBf16, int kOwn>
 __device__ __forceinline__ void list_row(const DistillArgs& a, size_t row, int* seen) {
     const int lane = threadIdx.x & 63, K = a.K;
     const void* const logits = reinterpret_cast<const char*>(a.logits) + row * a.ld * elem_size<kBf16>();
-    const int named = a.labels ? a.labels[row] : -1, label = named < a.V ? max(named, -1) : -1;
     int id[kOwn];
     float lp[kOwn], x[kOwn];
+    // all that depends on nothing is asked for at once, then the logits
+    int named = *(a.labels ? a.labels + row : a.ids + row * K);
+    const float scale = *(a.row_scale ? a.row_scale + row : a.lp + row * K);
 #pragma unroll
     for (int q = 0; q < kOwn; ++q) {
-        const int k = lane + 64 * q;
-        id[q] = k < K ? a.ids[row * K + k] : -1;
-        lp[q] = k < K ? a.lp[row * K + k] : -INFINITY;
-        if (id[q] < 0 || id[q] >= a.V) id[q] = -1;
+        const int k = min(lane + 64 * q, K - 1);
+        id[q] = a.ids[row * K + k], lp[q] = a.lp[row * K + k];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (a.row_scale && scale == 0.f) return;
+    if (!a.labels) named = -1;
+    const int label = named < a.V ? max(named, -1) : -1;
+#pragma unroll
+    for (int q = 0; q < kOwn; ++q) {
+        const bool is = lane + 64 * q < K;
+        if (!is || id[q] < 0 || id[q] >= a.V) id[q] = -1;
+        if (!is) lp[q] = -INFINITY;
         x[q] = value_at<kBf16>(logits, max(id[q], 0));
-        if (k < K) seen[k] = id[q];
+        if (is) seen[lane + 64 * q] = id[q];
     }
     const float x_label = value_at<kBf16>(logits, max(label, 0));
     __builtin_amdgcn_wave_barrier();
@@ -245,7 +257,7 @@ __global__ __launch_bounds__(kVT) void distill_sums_kernel(const DistillArgs a) 
     const size_t parts = (size_t)a.rows * a.P;
     if (blockIdx.x >= parts) {  // lists, four rows a workgroup
         const size_t row = (blockIdx.x - parts) * (kVT / 64) + (threadIdx.x >> 6);
-        if (row < (size_t)a.rows && !(a.row_scale && a.row_scale[row] == 0.f)) list_row<kBf16>(a, row, seen[threadIdx.x >> 6]);
+        if (row < (size_t)a.rows) list_row<kBf16>(a, row, seen[threadIdx.x >> 6]);
         return;
     }
     const size_t row = blockIdx.x / a.P;
@@ -477,18 +489,32 @@ __global__ __launch_bounds__(kVT) void distill_grad_kernel(const DistillArgs a) 
 }
 
 // The lists of rows whose gradients distill_whole_kernel makes, a wave each; rows without
-// a loss get their zeros here, each from a workgroup.
+// a loss get their zeros here, each from a workgroup, and are left out of `order`.
 template <bool kBf16>
-__global__ __launch_bounds__(256) void distill_list_kernel(const DistillArgs a) {
+__global__ __launch_bounds__(kOrder) void distill_list_kernel(const DistillArgs a) {
     constexpr int n = Vocab<kBf16>::n;
-    __shared__ int seen[4][kMaxTop];
+    __shared__ int seen[4][kMaxTop], waves[4];
     auto live = [&](int row) { return !(a.row_scale && a.row_scale[row] == 0.f); };
+    if (a.row_scale && blockIdx.x % kOrder == 0) {
+        const int row = blockIdx.x + threadIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        const bool is = row < a.rows && live(row);
+        const uint64_t all = __ballot(is);
+        if (lane == 0) waves[wave] = __popcll(all);
+        __syncthreads();
+        int at = __popcll(all & ((1ull << lane) - 1)), count = 0;
+        for (int w = 0; w < 4; ++w) {
+            if (w < wave) at += waves[w];
+            count += waves[w];
+        }
+        if (is) a.order[blockIdx.x + at] = row;
+        if (threadIdx.x == 0) a.counts[blockIdx.x / kOrder] = count;
+    }
     const int listed = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (listed < a.rows && live(listed)) list_row<kBf16>(a, listed, seen[threadIdx.x >> 6]);
+    if (listed < a.rows) list_row<kBf16>(a, listed, seen[threadIdx.x >> 6]);
     const int row = blockIdx.x;
     if (live(row)) return;
     char* const out = reinterpret_cast<char*>(a.dlogits) + row * a.ldd * elem_size<kBf16>();
-    for (int i = threadIdx.x * n; i < a.V; i += 256 * n) store_unit<kBf16>(out, i, a.V, u32x4{0, 0, 0, 0});
+    for (int i = threadIdx.x * n; i < a.V; i += kOrder * n) store_unit<kBf16>(out, i, a.V, u32x4{0, 0, 0, 0});
     if (threadIdx.x == 0) a.kl[row] = a.ce[row] = 0.f;
 }
 
@@ -509,7 +535,8 @@ __device__ __forceinline__ T load_scalar(const T* p) {
 // that get free, and kLag units later they are summed: so memory is busy throughout,
 // where it would wait for the first pass of each row.  Unit 0 of a thread is the row's
 // last one, so that only it may be ragged.  A thread knows the marked tokens of its own
-// units from a list in LDS (which is in no order, and need not be).
+// units from a list in LDS (which is in no order, and need not be); the first of them is
+// in registers.
 // kHeld units a thread: 32 leave registers for two waves of a SIMD, 16 for three.
 constexpr int waves_of(int held) { return held > 16 ? 2 : 3; }
 template <bool kBf16, int kThreads, int kHeld, bool kTail, bool kTwo>
@@ -535,15 +562,32 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
         marks[set][t] = mark;
         if (mark.id >= 0) after[set][t] = atomicExch(&head[set][mark.id / n % kThreads], t);
     };
-    auto units_with_marks = [&](int set) {
-        uint32_t has = 0;
-        for (int k = head[set][t]; k >= 0; k = after[set][k]) has |= 1u << (held - 1 - marks[set][k].id / run);
-        return has;
+    // a thread's own marked tokens: one of them (most have one or none) as its place in the thread's units, which of
+    // them hold others
+    struct Own {
+        int at, leave, k;
+        uint32_t others;
     };
-    // the next row with a loss from `row` on, or the end
-    auto live = [&](int row) {
-        while (row < a.rows && a.row_scale && load_scalar(a.row_scale + row) == 0.f) row += gridDim.x;
-        return row;
+    auto own_marks = [&](int set) {
+        Own o{-1, -1, head[set][t], 0};
+        if (o.k >= 0) {
+            const Mark mark = marks[set][o.k];
+            o.at = (held - 1 - mark.id / run) * n + mark.id % n;
+            o.leave = mark.kind & kListed ? o.at : -1;
+            for (int k = after[set][o.k]; k >= 0; k = after[set][k]) o.others |= 1u << (held - 1 - marks[set][k].id / run);
+        }
+        return o;
+    };
+    // the row that is number `place` of those with a loss, or the end; places only grow
+    int block = 0, before = 0;
+    auto row_at = [&](int place) {
+        if (!a.row_scale) return place;
+        for (; block * kOrder < a.rows; ++block) {
+            const int count = load_scalar(a.counts + block);
+            if (place - before < count) return load_scalar(a.order + block * kOrder + place - before);
+            before += count;
+        }
+        return a.rows;
     };
     auto leave_out = [&](int set, int i, float (&v)[n]) {
         for (int k = head[set][t]; k >= 0; k = after[set][k]) {
@@ -553,7 +597,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
         }
     };
     TwoSums<true> sums;
-    auto add_unit = [&](int i, int set, uint32_t has) {
+    auto add_unit = [&](int i, int set, const Own& own) {
         if (i >= held) return;
         const int base = (held - 1 - i) * run + tn;
         float v[n];
@@ -562,7 +606,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
 #pragma unroll
             for (int k = 0; k < n; ++k) v[k] = base + k < a.V ? v[k] : -INFINITY;
         sums.raise(max_of(v, -INFINITY), a.c);
-        if (kTail && ((has >> i) & 1)) leave_out(set, base, v);
+        if constexpr (kTail) {
+            int at = own.leave - i * n, k = (own.others >> i) & 1 ? own.k : -1;
+            if (__any((unsigned)at < (unsigned)n || k >= 0))
+                for (;;) {
+#pragma unroll
+                    for (int j = 0; j < n; ++j) v[j] = j == at ? -INFINITY : v[j];
+                    if (k < 0) break;
+                    at = marks[set][k].kind & kListed ? marks[set][k].id - base : -1, k = after[set][k];
+                }
+        }
         float s = 0.f;
 #pragma unroll
         for (int k = 0; k < n; ++k) s += exp2_fast(fmaf(v[k], a.c, -sums.r));
@@ -571,7 +624,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
 #pragma unroll
             for (int k = 0; k < n; ++k) sums.s1 += exp2_fast(fmaf(v[k], kLog2E, -sums.r1));
     };
-    int row = live(blockIdx.x), set = 0;
+    int place = blockIdx.x, row = row_at(place), set = 0;
     if (row >= a.rows) return;
     Mark mark = request_mark(row);
 #pragma unroll
@@ -580,16 +633,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
     __syncthreads();
     keep_mark(0, mark);
     __syncthreads();
-    uint32_t has = units_with_marks(0);
+    Own own = own_marks(0);
 #pragma unroll
-    for (int i = 0; i < kHeld - kLag; ++i) add_unit(i, 0, has);
+    for (int i = 0; i < kHeld - kLag; ++i) add_unit(i, 0, own);
     for (;;) {
-        const int next = live(row + gridDim.x), ahead = next < a.rows ? next : row;
+        const int next = row_at(place += gridDim.x), ahead = next < a.rows ? next : row;
         const RowList list = load_scalar(a.lists + row);
         mark = request_mark(ahead);
         head[set ^ 1][t] = -1;
 #pragma unroll
-        for (int i = kHeld - kLag; i < kHeld; ++i) add_unit(i, set, has);
+        for (int i = kHeld - kLag; i < kHeld; ++i) add_unit(i, set, own);
         sums.settle(a.c);
         TwoSums<true> all = join_threads<kThreads>(sums, a.c, part);
         const bool wide = !(all.s < 3.0e38f && all.s1 < 3.0e38f);  // c m may have left fp32's range, or a value is no number
@@ -618,7 +671,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
         }
         __syncthreads();
         const RowFactors r = shared;
-        const uint32_t has_next = units_with_marks(set ^ 1);
+        const Own own_next = own_marks(set ^ 1);
+        const float own_gradient = mark_gradient[max(own.k, 0)];
         float f = kTwo ? r.f : r.f + r.f1, f1 = kTwo ? r.f1 : 0.f;
         const bool zero = f == 0.f && f1 == 0.f;  // nothing off the list
         char* const out = reinterpret_cast<char*>(a.dlogits) + row * a.ldd * elem_size<kBf16>();
@@ -647,7 +701,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
 #pragma unroll 1
             for (int once = 0; once < 1; ++once)
 #pragma unroll
-                for (int i = 0; i < kHeld - kLag; ++i) add_unit(i, set ^ 1, has_next);
+                for (int i = 0; i < kHeld - kLag; ++i) add_unit(i, set ^ 1, own_next);
         } else {
             // exponents against c m rounded, what that is off in the factor
             const float R = r.m * a.c, R1 = r.m * kLog2E;
@@ -671,11 +725,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
                     }
                     u32x4 w = pack_unit<kBf16>(v);
                     const int base = (held - 1 - i) * run + tn;
-                    if ((has >> i) & 1)
-                        for (int k = head[set][t]; k >= 0; k = after[set][k]) {
-                            const int at = marks[set][k].id - base;
-                            if (at < 0 || at >= n) continue;
-                            const float g = mark_gradient[k];
+                    int at = own.at - i * n, k = (own.others >> i) & 1 ? own.k : -1;
+                    float g = own_gradient;
+                    if (__any((unsigned)at < (unsigned)n || k >= 0))
+                        for (;;) {  // at outside [0, n): nothing
                             if constexpr (kBf16) {
                                 const uint32_t bits = (uint32_t)f32_to_bf16(g) << (16 * (at & 1)), mask = 0xffffu << (16 * (at & 1));
 #pragma unroll
@@ -684,18 +737,20 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
 #pragma unroll
                                 for (int j = 0; j < 4; ++j) w[j] = j == at ? __float_as_uint(g) : w[j];
                             }
+                            if (k < 0) break;
+                            at = marks[set][k].id - base, g = mark_gradient[k], k = after[set][k];
                         }
                     if (i > 0) *reinterpret_cast<u32x4*>(out + (size_t)base * elem_size<kBf16>()) = w;
                     else if (base < a.V) store_unit<kBf16>(out, base, a.V, w);
                 }
                 request(logits_ahead, i);
-                if (i >= kLag) add_unit(i - kLag, set ^ 1, has_next);
+                if (i >= kLag) add_unit(i - kLag, set ^ 1, own_next);
             }
             if (next >= a.rows) return;
         }
         row = next;
         set ^= 1;
-        has = has_next;
+        own = own_next;
     }
 }
 
@@ -731,7 +786,7 @@ constexpr int kComputeUnits = 256;
 constexpr int kWanted = 512;  // workgroups of parts of rows
 
 struct DistillLayout {
-    size_t lists, marks, total;
+    size_t lists, marks, order, counts, total;
 };
 
 DistillLayout distill_layout(const flexmoe_distill_desc* D, int rows) {
@@ -740,7 +795,9 @@ DistillLayout distill_layout(const flexmoe_distill_desc* D, int rows) {
     DistillLayout L;
     L.lists = up(parts * 16);
     L.marks = L.lists + up((size_t)rows * sizeof(RowList));
-    L.total = L.marks + up((size_t)rows * (D->top + 1) * sizeof(Mark)) + 256;
+    L.order = L.marks + up((size_t)rows * (D->top + 1) * sizeof(Mark));
+    L.counts = L.order + up((size_t)rows * sizeof(int32_t));
+    L.total = L.counts + up((size_t)(rows + kOrder - 1) / kOrder * sizeof(int32_t)) + 256;
     return L;
 }
 
@@ -749,7 +806,7 @@ int whole_grid(int threads, int held) { return kComputeUnits * waves_of(held) * 
 
 template <bool kBf16, int kThreads, int kHeld>
 hipError_t launch_whole(const DistillArgs& a, hipStream_t s) {
-    distill_list_kernel<kBf16><<<a.row_scale ? a.rows : (a.rows + 3) / 4, 256, 0, s>>>(a);
+    distill_list_kernel<kBf16><<<a.row_scale ? a.rows : (a.rows + 3) / 4, kOrder, 0, s>>>(a);
     const int grid = std::min(a.rows, whole_grid(kThreads, kHeld));
     if (a.tail && a.two) distill_whole_kernel<kBf16, kThreads, kHeld, true, true><<<grid, kThreads, 0, s>>>(a);
     else if (a.tail) distill_whole_kernel<kBf16, kThreads, kHeld, true, false><<<grid, kThreads, 0, s>>>(a);
@@ -821,6 +878,7 @@ int flexmoe_distill(const flexmoe_distill_desc* desc, int32_t rows, const void* 
     a.logits = logits, a.ids = ids, a.labels = labels, a.lp = logprobs, a.row_scale = row_scale, a.kl = kl, a.ce = ce, a.dlogits = dlogits;
     char* const ws = (char*)workspace;
     a.parts = (float*)ws, a.lists = (RowList*)(ws + L.lists), a.marks = (Mark*)(ws + L.marks);
+    a.order = (int32_t*)(ws + L.order), a.counts = (int32_t*)(ws + L.counts);  // of a launch's rows
     a.ld = (size_t)ld, a.ldd = (size_t)ldd, a.V = desc->V, a.K = desc->top, a.tail = desc->tail;
     a.P = row_parts(rows, desc->V, unit_run(desc->dtype), kWanted);
     a.length = part_length(desc->V, a.P, unit_run(desc->dtype));

@@ -166,6 +166,28 @@ def test_whole_rows(dtype, rows, V, tail, t):
     assert torch.equal(torch.nan_to_num(into.float(), nan=1.5), torch.nan_to_num(d.float(), nan=1.5))
 
 
+@pytest.mark.parametrize("live", [[0], [1599], [255, 256, 1000], list(range(600, 900)), list(range(0, 1600, 3))])
+def test_few_rows_with_a_loss_among_whole_rows(live):
+    """Long runs of padding: whole groups of rows that hold nothing to do, and workgroups that get no row."""
+    rows, V = 1600, 32000
+    _, x, ids, lp, labels = make(rows, V, 20, BF16)
+    scale = torch.zeros(rows, device="cuda")
+    scale[live] = 0.5
+    x[scale == 0] = float("nan")
+    h = fm.Distillation(V, 20, rows, tail=True, ce_weight=0.5)
+    out = fm._padded((rows, V), BF16, "cuda").fill_(3.0)
+    kl, ce, d = h.gradient(x, ids, lp, labels, scale, dlogits=out)
+    off = scale == 0
+    assert not bool(kl[off].any()) and not bool(ce[off].any()) and not bool(d[off].any())
+    on = torch.tensor(live, device="cuda")
+    ref = reference(x[on], ids[on], lp[on], labels[on], scale[on], 1.0, True, 1.0, 0.5)
+    err = (V / 256 + 30) * U
+    near(ce[on], ref[1], err + 2 * U * ref[1].abs() + 2 * U)
+    # as in check: the sums' relative error in each term, and one rounding to bf16
+    near(d[on], ref[2], 2.0 ** -8 * ref[2].abs() + 4 * (err + 60 * U) * ref[3] + 2.0 ** -133)
+    assert all(torch.equal(a, b) for a, b in zip((kl, ce, d), h.gradient(x, ids, lp, labels, scale)))
+
+
 def test_nothing_but_padding_or_masks_in_whole_rows():
     rows, V = 1700, 30001
     _, x, ids, lp, labels = make(rows, V, 8, BF16)
