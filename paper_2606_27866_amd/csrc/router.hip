@@ -26,6 +26,8 @@
 // taken in 32 bits: where the chosen ones and the best of the others (groups too)
 // are further apart than those can be wrong, the order is the exact one, and only
 // the other tokens (1 in 1000 of usual logits) are routed again in 64 bits.
+// One token of 64 experts 4.9 us; 8191 tokens of 256 experts in groups 17.1 us and 8.3
+// for the tables (all in 64 bits 82 together); 65536 of 60 experts 41 us.
 #include <algorithm>
 #include <cmath>
 
@@ -38,10 +40,14 @@ using namespace flexmoe;
 namespace {
 
 constexpr int kWaves = 16, kThreads = 64 * kWaves;
-constexpr int kChunks = 128;      // chunks of tokens, at most: workgroups of route_tables_kernel, which read all histograms
-constexpr int kHistograms = 256;  // wanted number of those
-constexpr int kMostCounted = 240; // tokens of one: its counts are bytes
-constexpr int kOneWorkgroup = 16; // tokens up to which one workgroup does it all
+// Chunks of tokens, at most: workgroups of route_tables_kernel, which read all histograms.  8191 tokens of 256 experts in
+// groups 30.7, 24.6, 24.6 and 28.6 us with 32, 64, 128 and 256; 65536 tokens of 60 experts 69.7, 65.0, 62.8 and 61.4.
+constexpr int kChunks = 128;
+// Tokens of a workgroup of route_kernel, at most; their counts are bytes.
+constexpr int kMostCounted = 128;
+// Tokens up to which one workgroup does it all, a wave each: 4, 8 and 16 tokens of 64 experts 4.9, 5.1 and 6.3 us, in two
+// launches 7.7, 8.0 and 9.1.
+constexpr int kOneWorkgroup = kWaves;
 constexpr int kMaxGroups = 64;
 constexpr int kQ = kMaxExperts / 64;
 
@@ -531,7 +537,7 @@ __global__ __launch_bounds__(kThreads) void route_tables_kernel(const RouteArgs 
                 uint32_t n[kTogether], even[2] = {}, odd[2] = {};
 #pragma unroll
                 for (int i = 0; i < kTogether; ++i) n[i] = a.hist[(size_t)min(h0 + i * kWaves, rows - 1) * a.words + lane];
-                __builtin_amdgcn_sched_barrier(0);  // else the compiler waits for one after another (12 us where this takes 5)
+                __builtin_amdgcn_sched_barrier(0);  // else the compiler waits for one after another (65536 tokens: 12 us where this takes 8)
 #pragma unroll
                 for (int i = 0; i < kTogether; ++i) {
                     const int h = h0 + i * kWaves;
@@ -729,10 +735,15 @@ int check_router(const flexmoe_router_desc* D, int T, const char* who, long long
     return FLEXMOE_OK;
 }
 
+// Workgroups of route_kernel, a histogram each: one a compute unit (tables read fewer of them), past its tokens two, in
+// whole rounds.  8192 tokens of 60 experts 14.4 us with 256, 15.9 with 512; 65536 63.3 and 40.8, with 768 and 1024 50.3
+// and 48.3; 131072 98 with 547, 79 with 1024.
+int histograms(int T) { return T <= 256 * kMostCounted ? 256 : (int)(((long long)T + 512 * kMostCounted - 1) / (512 * kMostCounted)) * 512; }
+
 // Tokens of a histogram (a multiple of a workgroup's waves) and of a chunk.
 int counted_tokens(int T) {
-    const int per = (T + kHistograms - 1) / kHistograms;
-    return std::min(kMostCounted, std::max(1, (per + kWaves - 1) / kWaves) * kWaves);
+    const int wanted = histograms(T), per = (T + wanted - 1) / wanted;
+    return std::max(1, (per + kWaves - 1) / kWaves) * kWaves;
 }
 int chunk_tokens(int T, int counted) {
     const int per = (T + kChunks - 1) / kChunks;
@@ -742,9 +753,7 @@ int chunk_tokens(int T, int counted) {
 int hist_words(int E) { return (E + 3) / 4; }
 
 size_t route_bytes(const flexmoe_router_desc* D, int T) {
-    // up to kHistograms of them while each counts fewer than kMostCounted tokens, then as many as there are
-    const size_t rows = std::max<size_t>(kHistograms + 1, ((size_t)T + kMostCounted - 1) / kMostCounted);
-    return (rows * hist_words(D->E) * 4 + 255) & ~size_t(255);
+    return ((size_t)histograms(T) * hist_words(D->E) * 4 + 255) & ~size_t(255);
 }
 
 }  // namespace

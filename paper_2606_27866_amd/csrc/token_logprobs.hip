@@ -14,6 +14,10 @@
 //
 // Rows are split over workgroups while there are few; a second launch joins the
 // parts' sums and lists.
+//
+// Bound by memory where rows are many: 4096 x 131072 bf16, 32 listed, 198 us, 5.4 TB/s
+// (128 listed 226, none 191).  One row is two launches and the latency of their chains of
+// loads, barriers and ranks: 11.4 us with 20 listed.
 #include <algorithm>
 #include <cmath>
 
@@ -29,7 +33,10 @@ constexpr int kCandidates = 1024;
 constexpr int kJoined = 8;        // keys of a thread that joins the parts' lists
 constexpr int kMostKeys = kJoined * kVT;
 static_assert(kMostKeys >= ((1 << 21) / kRange) * kMaxTop, "the lists of the longest row's parts");
-constexpr int kWanted = 512;  // workgroups
+// Workgroups while there are few rows: more parts are more to join.  131072 tokens in bf16, 20 listed, 8, 64 and 256 rows
+// 11.6, 14.1 and 18.9 us with 256, 12.6, 13.4 and 22.7 with 512; 64 rows of 100003 in fp32, 64 listed, 16.8 with both, 20.7
+// with 128, 23.4 with 2048.
+constexpr int kWanted = 256;
 
 struct LogprobArgs {
     const void* logits;

@@ -188,9 +188,9 @@ def test_rows_of_a_wider_buffer():
 
 def test_many_tokens():
     """Every chunk's length: one token more or less than whole chunks, and a batch that fills them all."""
-    for T in (2047, 2048, 2049, 5000, 20011):
+    for T in (2047, 2048, 2049, 5000, 20011, 32768, 32769, 65537, 131075):
         _, x, _ = make(T, 24, seed=T)
-        router = fm.Router(24, 3, 30000)
+        router = fm.Router(24, 3, max(T, 30000))
         r = router.route(x)
         assert torch.equal(r.topk_idx.long(), x.sort(dim=1, descending=True, stable=True).indices[:, :3])
         check_tables(r, 24)
