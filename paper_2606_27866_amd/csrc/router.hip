@@ -209,18 +209,24 @@ __device__ __forceinline__ int choose_exact(const RouteArgs& a, const float (&v)
     return my_id;
 }
 
-// Whether two scores of 32 bits, a >= b, may stand in another order than the exact
-// ones.  A score is off by at most 16 units of 2^-24 of itself (difference, exp, a sum
-// of 256, quotient), with its bias by one of the sum more; `bias` is the sum of both
-// values' largest possible biases, so that the scores are at most |a| + |b| + bias.
-__device__ __forceinline__ bool too_near(float a, float b, float bias) { return a - b <= 20.f * 0x1p-24f * (fabsf(a) + fabsf(b) + bias); }
-
-__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
-// x's relative error in the exponent weighs s (1 - s) |x| < 0.3 in s: 4 units of 2^-24 with exp, sum and reciprocal
-__device__ __forceinline__ float sigmoid_fast(float x) { return __builtin_amdgcn_rcpf(1.f + exp_fast(-x)); }
-
 // What decides: the logits themselves, or scores, with a bias or in sums of a group's two best.
 enum { kByLogits = 0, kBySigmoid = 1, kBySoftmax = 2 };
+
+// Whether two scores of 32 bits, a >= b, may stand in another order than the exact
+// ones.  A score s is off by so many units of 2^-24 of itself: softmax 16 (exp, a sum of 256,
+// quotient), sigmoid 5 (exp, a sum, reciprocal), and |ln s| more, the size of the exponent
+// that was rounded; with its bias and in a group's sum by one each of what they are.  That
+// is below 26 and 15 from 2^-10 on, below 106 down to where fp32 ends.  `bias` is the sum of
+// both values' largest possible biases, so that the scores are at most |a| + |b| + bias,
+// and s |ln s| falls with s.
+template <int kBy>
+__device__ __forceinline__ bool too_near(float a, float b, float bias) {
+    const float size = fabsf(a) + fabsf(b) + bias;
+    return a - b <= (size < 0x1p-10f ? 128.f : kBy == kBySigmoid ? 15.f : 26.f) * 0x1p-24f * size + 0x1p-100f;
+}
+
+__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
+__device__ __forceinline__ float sigmoid_fast(float x) { return __builtin_amdgcn_rcpf(1.f + exp_fast(-x)); }
 
 // The choice of one token, whose logits are in v (expert lane NQ + q; -inf past E), also
 // in rs.v, from values of 32 bits; `unsure`: they do not tell.
@@ -304,7 +310,7 @@ __device__ __forceinline__ int choose_fast(const RouteArgs& a, const float (&v)[
         }
         if constexpr (kBy != kByLogits) {
             const uint32_t next = wave_max_u(group);
-            if (next) unsure |= too_near(key32_value(last), key32_value(next), 2.f * bias);
+            if (next) unsure |= too_near<kBy>(key32_value(last), key32_value(next), 2.f * bias);
         }
         // lane NQ + q is in group (lane NQ + q) / members: the product is exact below 2^16
         const uint32_t inv = (65536 + members - 1) / members;
@@ -336,7 +342,7 @@ __device__ __forceinline__ int choose_fast(const RouteArgs& a, const float (&v)[
     for (int j = 0; j < 64; ++j) {
         const uint32_t m = wave_max_u(key[0]);
         if (m == 0) break;
-        if (j >= a.k && (kBy == kByLogits || !too_near(key32_value(last), key32_value(m), bias))) break;
+        if (j >= a.k && (kBy == kByLogits || !too_near<kBy>(key32_value(last), key32_value(m), bias))) break;
         const int from = __ffsll((unsigned long long)__ballot(key[0] == m)) - 1;
         const int id = __builtin_amdgcn_readlane((int)place[0], from);
         if (lane == j) mine = m, my_id = id;
@@ -352,7 +358,7 @@ __device__ __forceinline__ int choose_fast(const RouteArgs& a, const float (&v)[
     }
     if constexpr (kBy != kByLogits) {
         const uint32_t after = (uint32_t)__shfl_down((int)mine, 1, 64);
-        const uint64_t close = __ballot(lane + 1 < listed && too_near(key32_value(mine), key32_value(after), bias));
+        const uint64_t close = __ballot(lane + 1 < listed && too_near<kBy>(key32_value(mine), key32_value(after), bias));
         unsure |= listed == 64;  // more of them than lanes
         if (close && !unsure) {  // the listed ones' scores in 64 bits, ranked by counting
             const double z = kBy == kBySoftmax ? exact_sum<NQ>(v, top) : 1.0;
@@ -411,12 +417,12 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int t, int lane,
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
     float w;
     if (a.normalize) {
-        const float m = wave_max_f(my_logit);
         if (!a.sigmoid) {
+            const float m = wave_max_f(my_logit);
             w = my_id < 0 ? 0.f : exp_fast(my_logit - m);
-        } else if (m > -60.f) {
+        } else if (!__any(my_id >= 0 && my_logit < -60.f)) {
             w = my_id < 0 ? 0.f : sigmoid_fast(my_logit);
-        } else {  // scores near the end of fp32's range, or past it: differences of their logarithms
+        } else {  // a score near the end of fp32's range, or past it: differences of their logarithms
             const float ls = my_id < 0 ? -INFINITY : log_sigmoid(my_logit);
             const float most = wave_max_f(ls);
             w = my_id < 0 ? 0.f : expf(ls - most);
@@ -530,7 +536,7 @@ __global__ __launch_bounds__(kThreads) void route_tables_kernel(const RouteArgs 
         // every 16th histogram a wave; sums of whole numbers
         const int rows = (a.T + a.counted - 1) / a.counted, mine = t0 / a.counted;
         if (lane < a.words) {
-            // 32 of them requested together; two experts' counts in the halves of a word (32 times 240 at most)
+            // 32 of them requested together; two experts' counts in the halves of a word (32 times 128 at most)
             constexpr int kTogether = 32;
             int all[4] = {}, before[4] = {};
             for (int h0 = wave; h0 < rows; h0 += kTogether * kWaves) {

@@ -140,6 +140,23 @@ def test_scores_next_to_each_other():
 
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("level", [20.0, 60.0, 86.0, 100.0])
+def test_scores_far_down(score, level):
+    """Small scores are less exact in 32 bits, and past e^-87 they are none: sums of a group's two best that depend on it."""
+    g, x, _ = make(300, 64)
+    x = -level + x * 1e-6 * level
+    x[:, 63] = 0.0
+    check(x, None, 8, score, groups=16, top_groups=4, best=2)
+    check(x, torch.full((64,), 2.0 ** -80, device="cuda"), 8, score)
+    x = torch.full((4, 16), -300.0, device="cuda")
+    x[:, 14] = 0.0
+    x[:, 0], x[:, 1], x[:, 6] = -86.5, -88.0, -86.4
+    x[1, :2], x[1, 6] = -86.45, -86.4
+    x[2, 1] = -89.5
+    check(x, None, 4, score, groups=8, top_groups=2, best=2)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("groups,best", [(1, 1), (4, 1), (4, 2)])
 def test_masks(score, groups, best):
     """-inf in some places, in all but a few, everywhere; the lowest finite value; a bias of -inf."""
