@@ -78,7 +78,7 @@ constexpr float kLog2E = 1.4426950408889634f;
 // Sums at t and, where they differ, at 1, while the largest value is still growing.
 template <bool kTwo>
 struct TwoSums {
-    float m = -INFINITY, s = 0.f, r = 0.f, s1 = 0.f, r1 = 0.f;
+    float m = -INFINITY, s = 0.f, r = 0.f, s1 = 0.f, r1 = 0.f, limit = -INFINITY;
 
     __device__ __forceinline__ void raise(float largest, float c) {
         if (!__any(largest > m)) return;
@@ -89,6 +89,20 @@ struct TwoSums {
                 if constexpr (kTwo) s1 *= exp2_fast(r1 - to1);
             }
             m = largest, r = to, r1 = to1;
+        }
+    }
+    // The same for the largest value so far, but that the references stay while values are at most 2^16 times what
+    // they stand for: nearly every step has a lane with a new largest one, few have one that is so much larger.
+    __device__ __forceinline__ void raise_past(float largest, float c, float margin) {
+        m = largest;
+        if (!__any(largest > limit)) return;
+        if (largest > limit) {
+            const float to = largest * c, to1 = largest * kLog2E;
+            if (limit > -INFINITY) {
+                s *= exp2_fast(r - to);
+                if constexpr (kTwo) s1 *= exp2_fast(r1 - to1);
+            }
+            limit = largest + margin, r = to, r1 = to1;
         }
     }
     __device__ __forceinline__ void add(float v, float c) {
@@ -110,6 +124,19 @@ struct TwoSums {
         m = to;
     }
 };
+
+// The wave's bits, in every lane.
+__device__ __forceinline__ uint32_t wave_or(uint32_t v) {
+#define FLEXMOE_OSTEP(C, M) v |= (uint32_t)dpp_shift<C, M>((int)v)
+    FLEXMOE_OSTEP(0x111, 0xf);
+    FLEXMOE_OSTEP(0x112, 0xf);
+    FLEXMOE_OSTEP(0x114, 0xf);
+    FLEXMOE_OSTEP(0x118, 0xf);
+    FLEXMOE_OSTEP(0x142, 0xa);
+    FLEXMOE_OSTEP(0x143, 0xc);
+#undef FLEXMOE_OSTEP
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
 
 template <int kThreads, bool kTwo>
 __device__ __forceinline__ TwoSums<kTwo> join_threads(TwoSums<kTwo> a, float c, float (*part)[kThreads / 64]) {
@@ -312,6 +339,8 @@ __global__ __launch_bounds__(kVT) void distill_sums_kernel(const DistillArgs a) 
     }
 }
 
+__device__ __forceinline__ float scale_of(const DistillArgs& a, size_t row) { return a.row_scale ? a.row_scale[row] : 1.f; }
+
 // What a row's tokens are multiplied with.
 struct RowFactors {
     float m, f, f1;          // all tokens: f 2^(c (x - m)) + f1 2^(log2(e) (x - m))
@@ -330,9 +359,8 @@ __device__ __forceinline__ double log_of(float s) {
 // One wave joins a row's maximum and sums (with a tail: without the listed tokens) with
 // its list and marks.  All lanes return the same; lane 0 writes the losses if `writes`.
 __device__ __forceinline__ RowFactors end_row(const DistillArgs& a, size_t row, const RowList& list, const Mark* marks, float m, float s, float s1,
-                                              bool writes) {
+                                              float scale, bool writes) {
     const int lane = threadIdx.x & 63;
-    const float scale = a.row_scale ? a.row_scale[row] : 1.f;
     float S = s, S1 = a.two ? s1 : s;
     if (a.tail) {
         float e = 0.f, e1 = 0.f;
@@ -409,7 +437,7 @@ __global__ __launch_bounds__(256) void distill_row_kernel(const DistillArgs a) {
         return;
     }
     const TwoSums<true> all = join_parts(a, row);
-    end_row(a, row, a.lists[row], a.marks + row * (a.K + 1), all.m, all.s, all.s1, true);
+    end_row(a, row, a.lists[row], a.marks + row * (a.K + 1), all.m, all.s, all.s1, scale_of(a, row), true);
 }
 
 // 16 bytes of gradients at value i of a row that ends at `end`.
@@ -466,7 +494,7 @@ __global__ __launch_bounds__(kVT) void distill_grad_kernel(const DistillArgs a) 
     }
     if (t < 64) {
         const TwoSums<true> all = join_parts(a, row);
-        const RowFactors r = end_row(a, row, a.lists[row], a.marks + row * (a.K + 1), all.m, all.s, all.s1, p == 0);
+        const RowFactors r = end_row(a, row, a.lists[row], a.marks + row * (a.K + 1), all.m, all.s, all.s1, scale_of(a, row), p == 0);
         if (t == 0) shared = r;
     }
     __syncthreads();
@@ -553,35 +581,40 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
     __shared__ Mark marks[2][kMaxTop + 1];  // of this row and of the next
     __shared__ int after[2][kMaxTop + 1], head[2][kThreads];
     __shared__ float mark_gradient[kMaxTop + 1];
-    const int t = threadIdx.x, last = (a.V - 1) / n * n, held = (a.V + run - 1) / run;
+    const int t = threadIdx.x, whole = a.V / n, held = (a.V + run - 1) / run;
     int tn = t * n;
     u32x4 raw[kHeld];
+    // Rows as buffers: the units that a row does not have are read as zeros and not written, so that every unit is one
+    // request and one store, which the compiler counts; under a condition it would wait for half of those in flight.
+    auto buffer = [&](const char* row, int units) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(row), (short)0, units * 16, 0x00020000); };
+    auto offset = [&](int i) { return (uint32_t)((held - 1 - i) * (run * 16 / n) + tn * (16 / n)); };
     auto logits_of = [&](int row) { return reinterpret_cast<const char*>(a.logits) + row * a.ld * elem_size<kBf16>(); };
-    // unit 0 past the row's end: its last one; units there are none of: the row's first ones, which are in the caches
-    auto request = [&](const char* logits, int i) {
-        const int at = max(held - 1 - i, 0) * run + tn;
-        raw[i] = load_unit<kBf16>(logits, i == 0 ? min(at, last) : at);
+    auto request = [&](__amdgpu_buffer_rsrc_t logits, int i) {
+        raw[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(logits, offset(i), 0, 0));
     };
+    const int units = (a.V + n - 1) / n;
     auto request_mark = [&](int row) { return a.marks[(size_t)row * (a.K + 1) + min(t, a.K)]; };
     auto keep_mark = [&](int set, const Mark& mark) {
         if (t > a.K) return;
         marks[set][t] = mark;
         if (mark.id >= 0) after[set][t] = atomicExch(&head[set][mark.id / n % kThreads], t);
     };
-    // a thread's own marked tokens: one of them (most have one or none) as its place in the thread's units, which of
-    // them hold others
+    // a thread's own marked tokens: one of them (most have one or none) as its place in the thread's units, and which of
+    // those hold others
     struct Own {
         int at, leave, k;
-        uint32_t others;
+        uint32_t units, others;  // units: of all threads of the wave
     };
     auto own_marks = [&](int set) {
-        Own o{-1, -1, head[set][t], 0};
+        Own o{-1, -1, head[set][t], 0, 0};
         if (o.k >= 0) {
             const Mark mark = marks[set][o.k];
             o.at = (held - 1 - mark.id / run) * n + mark.id % n;
             o.leave = mark.kind & kListed ? o.at : -1;
             for (int k = after[set][o.k]; k >= 0; k = after[set][k]) o.others |= 1u << (held - 1 - marks[set][k].id / run);
+            o.units = o.others | 1u << (o.at / n);
         }
+        o.units = wave_or(o.units);
         return o;
     };
     // the row that is number `place` of those with a loss, or the end; places only grow
@@ -603,6 +636,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
         }
     };
     TwoSums<true> sums;
+    const float margin = 16.f / fmaxf(a.c, kLog2E);
     auto add_unit = [&](int i, int set, const Own& own) {
         if (i >= held) return;
         const int base = (held - 1 - i) * run + tn;
@@ -611,30 +645,40 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
         if (i == 0)
 #pragma unroll
             for (int k = 0; k < n; ++k) v[k] = base + k < a.V ? v[k] : -INFINITY;
-        sums.raise(max_of(v, -INFINITY), a.c);
-        if constexpr (kTail) {
-            int at = own.leave - i * n, k = (own.others >> i) & 1 ? own.k : -1;
-            if (__any((unsigned)at < (unsigned)n || k >= 0))
-                for (;;) {
+        sums.raise_past(max_of(v, sums.m), a.c, margin);
+        float e[n], e1[n];
 #pragma unroll
-                    for (int j = 0; j < n; ++j) v[j] = j == at ? -INFINITY : v[j];
-                    if (k < 0) break;
-                    at = marks[set][k].kind & kListed ? marks[set][k].id - base : -1, k = after[set][k];
-                }
+        for (int k = 0; k < n; ++k) {
+            e[k] = exp2_fast(fmaf(v[k], a.c, -sums.r));
+            if constexpr (kTwo) e1[k] = exp2_fast(fmaf(v[k], kLog2E, -sums.r1));
         }
-        float s = 0.f;
+        if (kTail && ((own.units >> i) & 1)) {  // the listed ones are left out
+            int at = own.leave - i * n, k = (own.others >> i) & 1 ? own.k : -1;
+            for (;;) {
 #pragma unroll
-        for (int k = 0; k < n; ++k) s += exp2_fast(fmaf(v[k], a.c, -sums.r));
+                for (int j = 0; j < n; ++j) {
+                    e[j] = j == at ? 0.f : e[j];
+                    if constexpr (kTwo) e1[j] = j == at ? 0.f : e1[j];
+                }
+                if (k < 0) break;
+                at = marks[set][k].kind & kListed ? marks[set][k].id - base : -1, k = after[set][k];
+            }
+        }
+        float s = e[0], s1 = kTwo ? e1[0] : 0.f;
+#pragma unroll
+        for (int k = 1; k < n; ++k) {
+            s += e[k];
+            if constexpr (kTwo) s1 += e1[k];
+        }
         sums.s += s;
-        if (kTwo)
-#pragma unroll
-            for (int k = 0; k < n; ++k) sums.s1 += exp2_fast(fmaf(v[k], kLog2E, -sums.r1));
+        if constexpr (kTwo) sums.s1 += s1;
     };
-    int place = blockIdx.x, row = row_at(place), set = 0;
+    int place = blockIdx.x, row = row_at(place), next = row_at(place += gridDim.x), set = 0;
     if (row >= a.rows) return;
-    Mark mark = request_mark(row);
+    auto or_last = [&](int r) { return r < a.rows ? r : row; };
+    Mark mark = request_mark(row), mark_ahead = request_mark(or_last(next));
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) request(logits_of(row), i);
+    for (int i = 0; i < kHeld; ++i) request(buffer(logits_of(row), units), i);
     head[0][t] = -1;
     __syncthreads();
     keep_mark(0, mark);
@@ -643,9 +687,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
 #pragma unroll
     for (int i = 0; i < kHeld - kLag; ++i) add_unit(i, 0, own);
     for (;;) {
-        const int next = row_at(place += gridDim.x), ahead = next < a.rows ? next : row;
+        const int ahead = or_last(next), after_next = row_at(place += gridDim.x);
         const RowList list = load_scalar(a.lists + row);
-        mark = request_mark(ahead);
+        const float scale = a.row_scale ? load_scalar(a.row_scale + row) : 1.f;
         head[set ^ 1][t] = -1;
 #pragma unroll
         for (int i = kHeld - kLag; i < kHeld; ++i) add_unit(i, set, own);
@@ -669,9 +713,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
             __syncthreads();
             all = join_threads<kThreads>(again, a.c, part);
         }
-        keep_mark(set ^ 1, mark);  // the heads were cleared before join_threads' barriers
+        keep_mark(set ^ 1, mark_ahead);  // the heads were cleared before join_threads' barriers
         if (t < 64) {
-            const RowFactors r = end_row(a, row, list, marks[set], all.m, all.s, all.s1, true);
+            const RowFactors r = end_row(a, row, list, marks[set], all.m, all.s, all.s1, scale, true);
             for (int k = t; k <= a.K; k += 64) mark_gradient[k] = marked(a, r, marks[set][k]);
             if (t == 0) shared = r;
         }
@@ -682,8 +726,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
         float f = kTwo ? r.f : r.f + r.f1, f1 = kTwo ? r.f1 : 0.f;
         const bool zero = f == 0.f && f1 == 0.f;  // nothing off the list
         char* const out = reinterpret_cast<char*>(a.dlogits) + row * a.ldd * elem_size<kBf16>();
-        const char* const logits_ahead = logits_of(ahead);
+        const __amdgpu_buffer_rsrc_t logits_ahead = buffer(logits_of(ahead), units), gradients_of = buffer(out, whole);
         sums = TwoSums<true>();
+        mark_ahead = request_mark(or_last(after_next));  // before the stores: waiting for it is waiting for what was asked before
         if (wide || zero) {
 #pragma unroll 1
             for (int at = t * n; at < a.V; at += run) {
@@ -718,6 +763,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
             for (int i = 0; i < kHeld; ++i) asm volatile("" : "+v"(raw[i]));
 #pragma unroll
             for (int i = 0; i < kHeld; ++i) {
+                u32x4 w{};
+                const int base = (held - 1 - i) * run + tn;
                 if (i < held) {
                     float v[n];
                     unpack_unit<kBf16>(raw[i], v);
@@ -729,11 +776,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
 #pragma unroll
                         for (int k = 0; k < n; ++k) v[k] = f * exp2_fast(fmaf(v[k], a.c, -R));
                     }
-                    u32x4 w = pack_unit<kBf16>(v);
-                    const int base = (held - 1 - i) * run + tn;
-                    int at = own.at - i * n, k = (own.others >> i) & 1 ? own.k : -1;
-                    float g = own_gradient;
-                    if (__any((unsigned)at < (unsigned)n || k >= 0))
+                    w = pack_unit<kBf16>(v);
+                    if ((own.units >> i) & 1) {
+                        int at = own.at - i * n, k = (own.others >> i) & 1 ? own.k : -1;
+                        float g = own_gradient;
                         for (;;) {  // at outside [0, n): nothing
                             if constexpr (kBf16) {
                                 const uint32_t bits = (uint32_t)f32_to_bf16(g) << (16 * (at & 1)), mask = 0xffffu << (16 * (at & 1));
@@ -746,15 +792,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
                             if (k < 0) break;
                             at = marks[set][k].id - base, g = mark_gradient[k], k = after[set][k];
                         }
-                    if (i > 0) *reinterpret_cast<u32x4*>(out + (size_t)base * elem_size<kBf16>()) = w;
-                    else if (base < a.V) store_unit<kBf16>(out, base, a.V, w);
+                    }
                 }
+                if (i == 0 && base / n == whole && base < a.V) store_unit<kBf16>(out, base, a.V, w);
+                __builtin_amdgcn_raw_buffer_store_b128(w, gradients_of, offset(i), 0, 0);
                 request(logits_ahead, i);
                 if (i >= kLag) add_unit(i - kLag, set ^ 1, own_next);
             }
             if (next >= a.rows) return;
         }
-        row = next;
+        row = next, next = after_next;
         set ^= 1;
         own = own_next;
     }
