@@ -571,11 +571,13 @@ __device__ __forceinline__ T load_scalar(const T* p) {
 // last one, so that only it may be ragged.  A thread knows the marked tokens of its own
 // units from a list in LDS (which is in no order, and need not be); the first of them is
 // in registers.
-// kHeld units a thread: 32 leave registers for two waves of a SIMD, 16 for three.
+// kHeld units a thread: 32 leave registers for two waves of a SIMD, 16 for three.  kLag: what comes sooner is waited for,
+// what comes later is summed when no store is left to hide it (4096 x 131072 bf16, with tail, labels and a temperature
+// 485, 483, 489, 499 and 537 us with 4, 6, 8, 12 and 16; plain 430, 427, 429, 431, 436).
 constexpr int waves_of(int held) { return held > 16 ? 2 : 3; }
 template <bool kBf16, int kThreads, int kHeld, bool kTail, bool kTwo>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_of(kHeld), waves_of(kHeld)))) void distill_whole_kernel(const DistillArgs a) {
-    constexpr int n = Vocab<kBf16>::n, run = kThreads * n, kLag = kHeld * 3 / 8;
+    constexpr int n = Vocab<kBf16>::n, run = kThreads * n, kLag = kHeld * 3 / 16;
     __shared__ float part[3][kThreads / 64];
     __shared__ RowFactors shared;
     __shared__ Mark marks[2][kMaxTop + 1];  // of this row and of the next
