@@ -25,10 +25,11 @@
 //   distill_grad_kernel   joins a row's parts, then factor * exp(x) for a part of the
 //                         row, then the listed tokens (distill_row_kernel: losses alone)
 //
-// Bound by memory where rows are many: 4096 x 131072 bf16, 64 listed, 440 us, 4.9 TB/s
-// (424 of them whole rows, 16 the lists, whose 64-bit logarithms are bound by
-// instructions); 1021 x 50001 fp32 with tail, labels and 20 % padding 127 us, 2.9 TB/s: four
-// rows a workgroup, in step, so that the sums' joins between them stay uncovered.
+// Bound by memory where rows are many: 4096 x 131072 bf16, 64 listed, 430 us, 5.0 TB/s
+// (418 of them whole rows, 16 the lists, whose 64-bit logarithms are bound by instructions
+// and their tokens' logits by latency); with tail, labels and t = 2 483, 20 % padding 402. 1021 x
+// 50001 fp32 with tail, labels and 20 % padding 121 us, 3.0 TB/s: three or four rows a workgroup, all
+// in step, and four exponentials a value, whose instructions take half the time.
 // Losses alone of 48 x 131072: 8 us.
 #include <algorithm>
 #include <cmath>
@@ -874,12 +875,13 @@ hipError_t launch_whole(const DistillArgs& a, hipStream_t s) {
 
 // Whether rows are held whole by workgroups of `threads` times `held` units.  One read
 // pays where the second one would not find the logits in the last cache: from 96 MB of
-// them on (131072 tokens in bf16, 256, 512, 1024, 4096 rows: 57, 83, 138, 445 us against
-// 38, 86, 173, 644 in parts; 32000 tokens, 1024, 2048, 4096 rows: 42, 68, 133 against 42,
-// 92, 184; 50001 in fp32, 512, 1024, 4096: 61, 113, 368 against 66, 141, 544); of rows
-// that are long beside what is done once for each (5000 tokens in bf16, 4096 rows 51
-// against 42, 16384 tokens 81 against 95, with a tail and labels 115 against 95, 32000
-// tokens 168 against 187); and unless the last round of workgroups leaves many idle.
+// them on (131072 tokens in bf16, 256, 512, 1024, 4096 rows: 52, 73, 129, 429 us against
+// 37, 66, 167, 638 in parts; 32000 tokens, 1024, 2048, 4096 rows: 36, 60, 121 against 38,
+// 71, 176; 50001 in fp32, 512, 1024, 4096: 52, 103, 353 against 53, 119, 537); of rows
+// that are long beside what is done once for each (16384 rows in bf16 of 5000 tokens 162
+// against 129, of 12800 227 against 300; with a tail, labels and a temperature 12800 tokens
+// 329 against 287, 32000 tokens 528 against 682); and unless the last round of workgroups
+// leaves many idle.
 bool holds(const DistillArgs& a, int n, int threads, int held) {
     const size_t row = (size_t)a.V * 16 / n;
     if (!a.dlogits || a.V > threads * held * n || row * a.rows < (96u << 20) || row < (a.tail || a.two ? 48u << 10 : 24u << 10)) return false;
