@@ -27,7 +27,7 @@
 // are further apart than those can be wrong, the order is the exact one, and only
 // the other tokens (1 in 1000 of usual logits) are routed again in 64 bits.
 // One token of 64 experts 4.9 us; 8191 tokens of 256 experts in groups 17.1 us and 8.3
-// for the tables (all in 64 bits 82 together); 65536 of 60 experts 41 us.
+// for the tables (all in 64 bits 82 together); 65536 of 60 experts 38 us.
 #include <algorithm>
 #include <cmath>
 
@@ -78,31 +78,12 @@ __device__ __forceinline__ uint64_t score_key(double c) {
     return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
 }
 
-__device__ __forceinline__ float wave_max_f(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    return v;
-}
-
 __device__ __forceinline__ float log_sigmoid(float x) { return fminf(x, 0.f) - log1pf(expf(-fabsf(x))); }
 
 struct RouteScratch {
     double c[kMaxExperts];  // scores in 64 bits, or the first half in 32
     float v[kMaxExperts];   // logits
 };
-
-// Largest of the wave's keys, in every lane.
-__device__ __forceinline__ uint32_t wave_max_u(uint32_t v) {
-#define FLEXMOE_USTEP(C, M) v = max(v, (uint32_t)dpp_shift<C, M>((int)v))
-    FLEXMOE_USTEP(0x111, 0xf);
-    FLEXMOE_USTEP(0x112, 0xf);
-    FLEXMOE_USTEP(0x114, 0xf);
-    FLEXMOE_USTEP(0x118, 0xf);
-    FLEXMOE_USTEP(0x142, 0xa);
-    FLEXMOE_USTEP(0x143, 0xc);
-#undef FLEXMOE_USTEP
-    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
-}
 
 // Order of values that are no NaN as whole numbers: -inf (masked) 0.
 __device__ __forceinline__ uint32_t key32(float c) {
@@ -112,7 +93,7 @@ __device__ __forceinline__ uint32_t key32(float c) {
 __device__ __forceinline__ float key32_value(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
 
 // Largest of the wave's keys, in every lane: upper halves first.
-__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
+__device__ __forceinline__ uint64_t wave_max_key(uint64_t v) {
     const uint32_t hi = wave_max_u((uint32_t)(v >> 32));
     const uint32_t lo = wave_max_u((uint32_t)(v >> 32) == hi ? (uint32_t)v : 0u);
     return ((uint64_t)hi << 32) | lo;
@@ -142,7 +123,7 @@ __device__ __forceinline__ int choose_exact(const RouteArgs& a, const float (&v)
         top = v[0];
 #pragma unroll
         for (int q = 1; q < NQ; ++q) top = fmaxf(top, v[q]);
-        top = wave_max_f(top);
+        top = wave_max(top);
         z = exact_sum<NQ>(v, top);
     }
 #pragma unroll
@@ -177,7 +158,7 @@ __device__ __forceinline__ int choose_exact(const RouteArgs& a, const float (&v)
         __atomic_signal_fence(__ATOMIC_SEQ_CST);
         kept = 0;
         for (int j = 0; j < a.top_groups; ++j) {
-            const uint64_t m = wave_max(group);
+            const uint64_t m = wave_max_key(group);
             if (m == 0) break;
             const uint64_t all = __ballot(group == m), first = all & -all;
             kept |= first;
@@ -197,7 +178,7 @@ __device__ __forceinline__ int choose_exact(const RouteArgs& a, const float (&v)
 #pragma unroll
         for (int q = 1; q < NQ; ++q)
             if (key[q] > best) best = key[q], at = lane * NQ + q;  // the lower place of equal ones
-        const uint64_t m = wave_max(best);
+        const uint64_t m = wave_max_key(best);
         if (m == 0) break;
         const int from = __ffsll((unsigned long long)__ballot(best == m)) - 1;
         const int id = __builtin_amdgcn_readlane(at, from);
@@ -408,7 +389,7 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int t, int lane,
     __builtin_amdgcn_wave_barrier();
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
     const bool whole = !a.sigmoid && !a.normalize;  // weights out of a softmax over all experts
-    if (kBy == kBySoftmax || whole) top = wave_max_f(top);
+    if (kBy == kBySoftmax || whole) top = wave_max(top);
     bool unsure;
     my_id = choose_fast<NQ, kBy, kGroups>(a, v, lane, rs, top, unsure);
     if (unsure) my_id = choose_exact<NQ>(a, v, lane, rs);
@@ -418,13 +399,13 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int t, int lane,
     float w;
     if (a.normalize) {
         if (!a.sigmoid) {
-            const float m = wave_max_f(my_logit);
+            const float m = wave_max(my_logit);
             w = my_id < 0 ? 0.f : exp_fast(my_logit - m);
         } else if (!__any(my_id >= 0 && my_logit < -60.f)) {
             w = my_id < 0 ? 0.f : sigmoid_fast(my_logit);
         } else {  // a score near the end of fp32's range, or past it: differences of their logarithms
             const float ls = my_id < 0 ? -INFINITY : log_sigmoid(my_logit);
-            const float most = wave_max_f(ls);
+            const float most = wave_max(ls);
             w = my_id < 0 ? 0.f : expf(ls - most);
         }
         w /= wave_total_f(w);
@@ -684,7 +665,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const RouteGradArgs a) 
             ls[q] = !in ? -INFINITY : a.sigmoid ? log_sigmoid(v[q]) : v[q];
             top = fmaxf(top, ls[q]);
         }
-        top = wave_max_f(top);
+        top = wave_max(top);
 #pragma unroll
         for (int q = 0; q < kQ; ++q) {
             const float p = ls[q] == -INFINITY ? 0.f : expf(ls[q] - top);

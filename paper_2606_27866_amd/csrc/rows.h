@@ -87,6 +87,31 @@ __device__ __forceinline__ void store8(void* p, size_t i, int left, const float 
     store_raw8<kBf16>(p, i, left, pack8<kBf16>(v));
 }
 
+// Largest of the wave's whole numbers, and of its values (NaN left out), in every lane: the steps of wave_total_f.
+__device__ __forceinline__ uint32_t wave_max_u(uint32_t v) {
+#define FLEXMOE_USTEP(C, M) v = max(v, (uint32_t)dpp_shift<C, M>((int)v))
+    FLEXMOE_USTEP(0x111, 0xf);
+    FLEXMOE_USTEP(0x112, 0xf);
+    FLEXMOE_USTEP(0x114, 0xf);
+    FLEXMOE_USTEP(0x118, 0xf);
+    FLEXMOE_USTEP(0x142, 0xa);
+    FLEXMOE_USTEP(0x143, 0xc);
+#undef FLEXMOE_USTEP
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ __forceinline__ float wave_max(float v) {
+    // a lane without a source keeps its own
+#define FLEXMOE_MSTEP(C, M) v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), C, M, 0xf, false)))
+    FLEXMOE_MSTEP(0x111, 0xf);
+    FLEXMOE_MSTEP(0x112, 0xf);
+    FLEXMOE_MSTEP(0x114, 0xf);
+    FLEXMOE_MSTEP(0x118, 0xf);
+    FLEXMOE_MSTEP(0x142, 0xa);
+    FLEXMOE_MSTEP(0x143, 0xc);
+#undef FLEXMOE_MSTEP
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
 // Sum of a double over the wave, in every lane: the steps of wave_total_f.
 __device__ __forceinline__ double wave_total_d(double v) {
     union Halves {
@@ -128,8 +153,7 @@ __device__ __forceinline__ float sum_over_waves(float v, float* part) {
 
 template <int kWaves>
 __device__ __forceinline__ uint32_t max_over_waves(uint32_t m, uint32_t* part) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+    m = wave_max_u(m);
     if constexpr (kWaves > 1) {
         if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
         __syncthreads();

@@ -209,6 +209,7 @@ __global__ __launch_bounds__(kVT) void logprob_kernel(const LogprobArgs a) {
     const int p = blockIdx.x % a.P, t = threadIdx.x;
     const void* const logits = reinterpret_cast<const char*>(a.logits) + row * a.ld * elem_size<kBf16>();
     const int begin = p * a.length, end = min(a.V, begin + a.length);
+    const float of_token = a.P == 1 ? token_logit<kBf16>(a, row, logits) : 0.f;  // on its way early
     RunningSums sums;
     each_step<kBf16>(logits, begin, end, [&](int it, int, const float (&v)[W::units][W::n]) {
         float gm = -INFINITY;
@@ -243,7 +244,7 @@ __global__ __launch_bounds__(kVT) void logprob_kernel(const LogprobArgs a) {
     const RowEnd result(all, a.inv_t);
     if (t == 0) {
         if (a.P == 1) {
-            write_row(a, row, all, result, token_logit<kBf16>(a, row, logits));
+            write_row(a, row, all, result, of_token);
         } else {
             float* const o = a.parts + 4 * (row * a.P + p);
             o[0] = all.m, o[1] = all.s, o[2] = all.h;
@@ -301,6 +302,7 @@ __global__ __launch_bounds__(kVT) void logprob_join_kernel(const LogprobArgs a) 
     const int t = threadIdx.x;
     const void* const logits = reinterpret_cast<const char*>(a.logits) + row * a.ld * elem_size<kBf16>();
     const float* const parts = a.parts + 4 * row * a.P;
+    const float of_token = token_logit<kBf16>(a, row, logits);  // on its way early
     uint64_t key[kJoined];
     const int keys = kTop ? a.P * a.K : 0;
     if constexpr (kTop) {
@@ -327,7 +329,7 @@ __global__ __launch_bounds__(kVT) void logprob_join_kernel(const LogprobArgs a) 
     all.s = wave_total_f(all.s);
     all.h = wave_total_f(all.h);
     const RowEnd result(all, a.inv_t);
-    if (t == 0) write_row(a, row, all, result, token_logit<kBf16>(a, row, logits));
+    if (t == 0) write_row(a, row, all, result, of_token);
     if constexpr (kTop) {
         uint32_t own = 0;
         auto each = [&](auto&& f) {

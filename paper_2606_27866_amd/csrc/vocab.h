@@ -108,12 +108,6 @@ __device__ __forceinline__ float max_of(const float (&v)[N], float m) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    return v;
-}
-
 // sum of 2^(c (x - m)) and, weighted by it, of c (x - m): of values whose largest is m.
 struct Sums {
     float m = -INFINITY, s = 0.f, h = 0.f;
