@@ -95,15 +95,17 @@ bool piece_of(PyObject* o, Piece* p) {
     return p->bytes < (int64_t)1 << 60;
 }
 
-// make(like, ((code, rows) or (code, rows, cols, pitch), ...), together) -> the tensors, on like's device, rows
-// `pitch` values apart: in one allocation (each on a 256-byte boundary) or in one each.
+// make(like, ((code, rows) or (code, rows, cols, pitch), ...), together[, dst]) -> the tensors, on like's device, rows
+// `pitch` values apart: in one allocation (each on a 256-byte boundary) or in one each; their addresses to dst.
 PyObject* make(PyObject*, PyObject* const* args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     constexpr Py_ssize_t kMost = 16;
     Piece pieces[kMost];
-    bool ok = n == 3 && THPVariable_Check(args[0]) && PyTuple_Check(args[1]) && PyTuple_GET_SIZE(args[1]) <= kMost;
+    bool ok = (n == 3 || n == 4) && THPVariable_Check(args[0]) && PyTuple_Check(args[1]) && PyTuple_GET_SIZE(args[1]) <= kMost;
     const Py_ssize_t count = ok ? PyTuple_GET_SIZE(args[1]) : 0;
     const int together = ok ? PyObject_IsTrue(args[2]) : 0;
+    void** const dst = ok && n == 4 ? pointer<void*>(args[3]) : nullptr;
+    if (PyErr_Occurred()) return nullptr;
     int64_t all = 0;
     for (Py_ssize_t i = 0; ok && i < count; ++i) {
         ok = piece_of(PyTuple_GET_ITEM(args[1], i), &pieces[i]);
@@ -112,7 +114,7 @@ PyObject* make(PyObject*, PyObject* const* args, Py_ssize_t n) {
         ok = !__builtin_add_overflow(all, (pieces[i].bytes + 255) / 256 * 256, &all);
     }
     if (!ok || together < 0) {
-        if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "make(like, ((code, rows) or (code, rows, cols, pitch), ...), together)");
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "make(like, ((code, rows) or (code, rows, cols, pitch), ...), together[, dst])");
         return nullptr;
     }
     const at::TensorOptions options = at::TensorOptions().device(THPVariable_Unpack(args[0]).device()).dtype(at::kByte);
@@ -128,6 +130,7 @@ PyObject* make(PyObject*, PyObject* const* args, Py_ssize_t n) {
         if (together) impl->set_storage_offset(p.at / (int64_t)p.type.itemsize());
         const int64_t sizes[] = {p.rows, p.cols}, strides[] = {p.pitch, 1}, dims = p.cols < 0 ? 1 : 2;
         impl->set_sizes_and_strides(at::IntArrayRef(sizes, dims), at::IntArrayRef(dims == 2 ? strides : strides + 1, dims));
+        if (dst) dst[i] = t.data_ptr();
         PyObject* o = THPVariable_Wrap(std::move(t));
         if (!o) return nullptr;
         PyTuple_SET_ITEM(out.get(), i, o);

@@ -689,16 +689,16 @@ def _new(shape, dtype, device, stream=None):
 _F32, _BF16, _U8, _I32, _I8 = range(5)  # the native module's types
 
 
-def _make(like, pieces, together, stream=None):
+def _make(like, pieces, together, stream=None, *dst):
     """New tensors on like's device, as _new makes them, by the native module: (type, rows) or (type, rows, cols, pitch)
-    each; together: in one allocation, which lives as long as any of them."""
-    import torch
+    each; together: in one allocation, which lives as long as any of them; dst: where their addresses go."""
     if stream is None or not like.is_cuda:
-        return tensors().make(like, pieces, together)
+        return tensors().make(like, pieces, together, *dst)
+    import torch
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
     with torch.cuda.stream(stream):
-        return tensors().make(like, pieces, together)
+        return tensors().make(like, pieces, together, *dst)
 
 
 def _row_piece(code, R, cols):
@@ -1021,7 +1021,9 @@ class Router:
         self._desc = ctypes.byref(self.desc)
         self.workspace = torch.empty(flexmoe_route_workspace_bytes(self.desc, max_tokens), dtype=torch.uint8, device=device)
         self._ws = (self.workspace.data_ptr(), self.workspace.numel())
-        self._lock = threading.Lock()  # holds the descriptor's type and stride
+        self._out = flexmoe_route_out()
+        self._out_ref, self._out_at = ctypes.byref(self._out), ctypes.addressof(self._out)
+        self._lock = threading.Lock()  # holds the descriptor's type and stride, and the outputs' addresses
 
     def _logits(self, logits):
         if logits.dim() != 2:
@@ -1036,12 +1038,14 @@ class Router:
         out = (_I32, T, k, k), (_F32, T, k, k)
         if tables:
             out += (_I32, E), (_I32, E + 1), (_I32, T * k), (_I32, T * k)
-        out = _make(logits, out, True, stream)
-        ro = flexmoe_route_out(*[t.data_ptr() for t in out])
+        ro = self._out
         with self._lock:
             self._logits(logits)
-            _check(lib().flexmoe_route(self._desc, T, logits.data_ptr(), None if bias is None else _vector(bias, self.E, self._f32, "bias"),
-                                       ctypes.byref(ro), *self._ws, _stream(stream)))
+            if not tables:
+                ro.counts = ro.offsets = ro.perm = ro.pos = None
+            out = _make(logits, out, True, stream, self._out_at)
+            _check(lib().flexmoe_route(self._desc, T, logits.data_ptr(), None if bias is None else _vector(bias, E, self._f32, "bias"),
+                                       self._out_ref, *self._ws, _stream(stream)))
         return Routing(*out)
 
     def backward(self, logits, topk_idx, dw, dlogits=None, stream=None):

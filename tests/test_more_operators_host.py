@@ -243,6 +243,10 @@ def test_outputs_made_together_and_apart():
             t.fill_(i)
         assert all(bool((t == i).all()) for i, t in enumerate(made))
     assert make(like, (), True) == ()
+    for together in (True, False):
+        at = (fm.ctypes.c_void_p * 3)(7, 7, 7)
+        made = make(like, ((3, 2, 4, 4), (0, 5)), together, fm.ctypes.addressof(at))
+        assert [at[i] for i in range(3)] == [made[0].data_ptr(), made[1].data_ptr(), 7]
     for bad in [(like,), (like, ((5, 1),), 1), (like, ((0, 1, 3, 2),), 1), (like, ((0, 1, 3),), 1), (None, (), 1), (like, [], 1),
                 (like, ((0, -1),), 1), (like, ((0, "1"),), 1), (like, ((0, 1 << 31, 1 << 31, 1 << 31),), 1), (like, ((0, 1),) * 17, 1)]:
         with pytest.raises(TypeError):
