@@ -11,13 +11,15 @@
 //
 // A divergence is a small difference of large logarithms: what concerns the
 // listed tokens is in 64 bits, a row's sum of exponentials in 32.  With a tail
-// the listed tokens are left out of that sum (a map of bits says which) and added
-// to it afterwards, so that q_rest is a sum and not a difference.
+// the listed tokens are left out of the row's maximum and sum (a map of bits says
+// which) and joined with them afterwards, so that q_rest is a sum, not a difference,
+// and of terms up to 1, however far the listed tokens lie above.
 //
-// What the teacher's list gives does not hang on the student's maximum m and sum S
-// (S_rest without the listed tokens): with A = sum p log p [+ p_rest log p_rest] and
+// What the teacher's list gives does not hang on the student's maximum M and sum S
+// (m and s without the listed tokens): with A = sum p log p [+ p_rest log p_rest] and
 // B = sum p (x - y), y the largest listed x,
-//   KL = A - (B - (m - y) sum p) / t + (sum p [+ p_rest]) log S [- p_rest log S_rest].
+//   KL = A - (B - (M - y) sum p) / t + (sum p [+ p_rest]) log S [- p_rest (log s + (m - M) / t)]
+// and off the list p_rest / q_rest q_v = p_rest e^((x - m) / t) / s.
 //
 // Many rows that fit the registers of a workgroup (distill_whole_kernel): every row is
 // read once; while its gradients leave, the next row's logits come in.  Else:
@@ -27,7 +29,7 @@
 //
 // Bound by memory where rows are many: 4096 x 131072 bf16, 64 listed, 430 us, 5.0 TB/s
 // (418 of them whole rows, 16 the lists, whose 64-bit logarithms are bound by instructions
-// and their tokens' logits by latency); with tail, labels and t = 2 483, 20 % padding 402. 1021 x
+// and their tokens' logits by latency); with tail, labels and t = 2 486, 20 % padding 402. 1021 x
 // 50001 fp32 with tail, labels and 20 % padding 121 us, 3.0 TB/s: three or four rows a workgroup, all
 // in step, and four exponentials a value, whose instructions take half the time.
 // Losses alone of 48 x 131072: 8 us.
@@ -304,16 +306,17 @@ __global__ __launch_bounds__(kVT) void distill_sums_kernel(const DistillArgs a) 
     each_step<kBf16>(logits, begin, end, [&](int, int at, float (&v)[W::units][W::n]) {
         float gm = -INFINITY;
 #pragma unroll
-        for (int u = 0; u < W::units; ++u) gm = max_of(v[u], gm);
-        sums.raise(gm, a.c);
-#pragma unroll
         for (int u = 0; u < W::units; ++u) {
             const int i = at + u * W::run + t * W::n;
             if constexpr (kTail)
                 if (i < end) leave_out<kBf16>(bits, i - begin, v[u]);
+            gm = max_of(v[u], gm);
+        }
+        sums.raise(gm, a.c);
+#pragma unroll
+        for (int u = 0; u < W::units; ++u)
 #pragma unroll
             for (int k = 0; k < W::n; ++k) sums.add(v[u][k], a.c);
-        }
     });
     sums.settle(a.c);
     TwoSums<kTwo> all = join_threads<kVT>(sums, a.c, part);
@@ -344,8 +347,9 @@ __device__ __forceinline__ float scale_of(const DistillArgs& a, size_t row) { re
 
 // What a row's tokens are multiplied with.
 struct RowFactors {
-    float m, f, f1;          // all tokens: f 2^(c (x - m)) + f1 2^(log2(e) (x - m))
-    float listed, p, label;  // marked ones: listed 2^(c (x - m)) - p p_k instead of the first; less `label`
+    float m, f, f1;              // tokens off the list: f 2^(c (x - m)) + f1 2^(log2(e) (x - m))
+    float M, listed, listed1;    // listed ones: listed 2^(c (x - M)) - p p_k + listed1 2^(log2(e) (x - M))
+    float p, label;              // the label: less `label`
 };
 
 // The logarithm of a sum to about 2^-25: its power of two is taken off, whose part is exact in 64 bits.
@@ -362,52 +366,65 @@ __device__ __forceinline__ double log_of(float s) {
 __device__ __forceinline__ RowFactors end_row(const DistillArgs& a, size_t row, const RowList& list, const Mark* marks, float m, float s, float s1,
                                               float scale, bool writes) {
     const int lane = threadIdx.x & 63;
-    float S = s, S1 = a.two ? s1 : s;
+    float M = m, S = s, S1 = a.two ? s1 : s, down = 1.f, down1 = 1.f;  // down: e^((m - M) / t)
     if (a.tail) {
+        for (int k = lane; k < a.K; k += 64)
+            if (marks[k].id >= 0) M = fmaxf(M, marks[k].x);
+        M = wave_max(M);
         float e = 0.f, e1 = 0.f;
         for (int k = lane; k < a.K; k += 64) {
             const Mark mark = marks[k];
-            if (mark.id < 0) continue;
-            e += exp2_fast((mark.x - m) * a.c);
-            e1 += exp2_fast((mark.x - m) * kLog2E);
+            if (mark.id < 0 || mark.x == -INFINITY) continue;
+            e += exp2_fast((mark.x - M) * a.c);
+            e1 += exp2_fast((mark.x - M) * kLog2E);
         }
-        S += wave_total_f(e);
-        S1 = a.two ? S1 + wave_total_f(e1) : S;
+        down = m == -INFINITY ? 0.f : exp2_fast((m - M) * a.c);
+        down1 = !a.two ? down : m == -INFINITY ? 0.f : exp2_fast((m - M) * kLog2E);
+        S = S * down + wave_total_f(e);
+        S1 = a.two ? S1 * down1 + wave_total_f(e1) : S;
     }
-    const bool empty = m == -INFINITY && s == 0.f && list.b == list.b, labelled = list.label >= 0;
+    const bool empty = M == -INFINITY && S == 0.f && list.b == list.b, labelled = list.label >= 0;
+    const bool none = s == 0.f && S == S;  // no token off the list has a probability
     const double total = list.mass + list.rest;
-    double dense = total;
     if (writes) {
-        double kl = list.mass == 0.0 ? list.a : list.a - (list.b - ((double)m - (double)list.y) * list.mass) * (double)a.inv_t;
-        kl += total == 0.0 ? 0.0 : total * log_of(S);
+        double kl = list.mass == 0.0 ? list.a : list.a - (list.b - ((double)M - (double)list.y) * list.mass) * (double)a.inv_t;
+        const double log_S = total == 0.0 ? 0.0 : log_of(S);
+        kl += total * log_S;
         if (list.rest != 0.0) {
-            // log probabilities in 32 bits leave about 1e-6 of their own
-            if (s == 0.f) kl = list.rest <= 1e-5 ? kl : INFINITY;
-            else kl -= list.rest * log_of(s);
+            // log probabilities in 32 bits leave about 1e-6 of their own: nothing, where there is no token for it
+            if (none) kl = list.rest <= 1e-5 ? kl - list.rest * (log(list.rest) + log_S) : INFINITY;
+            else kl -= list.rest * (log_of(s) + ((double)m - (double)M) * (double)a.inv_t);
         }
         if (empty) kl = list.mass > 0.0 || list.rest > 1e-5 ? INFINITY : 0.0;
-        const double ce = !labelled ? 0.0 : empty ? INFINITY : log_of(S1) - ((double)list.x_label - (double)m);
+        const double ce = !labelled ? 0.0 : empty ? INFINITY : log_of(S1) - ((double)list.x_label - (double)M);
         if (lane == 0) {
             a.kl[row] = (float)kl;
             a.ce[row] = (float)ce;
         }
     }
-    if (list.rest != 0.0) dense = s == 0.f ? 0.0 : total - list.rest * ((double)S / (double)s);
+    // s is at least about 1: neither quotient leaves fp32's range
+    double dense = total;
+    if (a.tail) dense = total * (double)down - (list.rest != 0.0 ? list.rest * ((double)S / (double)s) : 0.0);
     const float by_kl = scale * a.kl_weight * a.t, by_ce = labelled ? scale * a.ce_weight : 0.f;
+    const bool no_dense = empty || (a.tail && none);
     RowFactors o;
     o.m = m;
-    o.f = empty ? 0.f : by_kl * (float)dense / S;
-    o.f1 = empty ? 0.f : by_ce / S1;
+    o.f = no_dense ? 0.f : by_kl * (float)dense / S;
+    o.f1 = no_dense ? 0.f : by_ce * down1 / S1;
+    o.M = M;
     o.listed = empty ? 0.f : by_kl * (float)total / S;
+    o.listed1 = empty ? 0.f : by_ce / S1;
     o.p = empty ? 0.f : by_kl;
     o.label = empty ? 0.f : by_ce;
     return o;
 }
 
 __device__ __forceinline__ float marked(const DistillArgs& a, const RowFactors& r, const Mark& k) {
-    const float e = exp2_fast((k.x - r.m) * a.c), e1 = a.two ? exp2_fast((k.x - r.m) * kLog2E) : e;
-    const float of_kl = k.kind & kListed ? r.listed * e - r.p * k.p : r.f * e;
-    return of_kl + r.f1 * e1 - (k.kind & kLabel ? r.label : 0.f);
+    const bool listed = k.kind & kListed;
+    const float d = k.x == -INFINITY ? -INFINITY : k.x - (listed ? r.M : r.m);
+    const float e = exp2_fast(d * a.c), e1 = a.two ? exp2_fast(d * kLog2E) : e;
+    const float of_kl = listed ? r.listed * e - r.p * k.p : r.f * e;
+    return of_kl + (listed ? r.listed1 : r.f1) * e1 - (k.kind & kLabel ? r.label : 0.f);
 }
 
 // A row's sums out of its parts', the same in all lanes.
@@ -648,24 +665,21 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
         if (i == 0)
 #pragma unroll
             for (int k = 0; k < n; ++k) v[k] = base + k < a.V ? v[k] : -INFINITY;
+        if (kTail && ((own.units >> i) & 1)) {  // the listed ones are left out, of the maximum too
+            int at = own.leave - i * n, k = (own.others >> i) & 1 ? own.k : -1;
+            for (;;) {
+#pragma unroll
+                for (int j = 0; j < n; ++j) v[j] = j == at ? -INFINITY : v[j];
+                if (k < 0) break;
+                at = marks[set][k].kind & kListed ? marks[set][k].id - base : -1, k = after[set][k];
+            }
+        }
         sums.raise_past(max_of(v, sums.m), a.c, margin);
         float e[n], e1[n];
 #pragma unroll
         for (int k = 0; k < n; ++k) {
             e[k] = exp2_fast(fmaf(v[k], a.c, -sums.r));
             if constexpr (kTwo) e1[k] = exp2_fast(fmaf(v[k], kLog2E, -sums.r1));
-        }
-        if (kTail && ((own.units >> i) & 1)) {  // the listed ones are left out
-            int at = own.leave - i * n, k = (own.others >> i) & 1 ? own.k : -1;
-            for (;;) {
-#pragma unroll
-                for (int j = 0; j < n; ++j) {
-                    e[j] = j == at ? 0.f : e[j];
-                    if constexpr (kTwo) e1[j] = j == at ? 0.f : e1[j];
-                }
-                if (k < 0) break;
-                at = marks[set][k].kind & kListed ? marks[set][k].id - base : -1, k = after[set][k];
-            }
         }
         float s = e[0], s1 = kTwo ? e1[0] : 0.f;
 #pragma unroll
