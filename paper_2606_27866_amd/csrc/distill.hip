@@ -72,7 +72,8 @@ struct DistillArgs {
     int32_t *order, *counts;  // per kOrder rows: those with a loss, and how many (row_scale given)
     size_t ld, ldd;
     int rows, V, P, length, K, tail, two;  // two: the labels' sum is not that of t
-    float c, inv_t, t, kl_weight, ce_weight;
+    float c, t, kl_weight, ce_weight;
+    double inv_t;
 };
 
 constexpr int kOrder = 256;
@@ -387,13 +388,13 @@ __device__ __forceinline__ RowFactors end_row(const DistillArgs& a, size_t row, 
     const bool none = s == 0.f && S == S;  // no token off the list has a probability
     const double total = list.mass + list.rest;
     if (writes) {
-        double kl = list.mass == 0.0 ? list.a : list.a - (list.b - ((double)M - (double)list.y) * list.mass) * (double)a.inv_t;
+        double kl = list.mass == 0.0 ? list.a : list.a - (list.b - ((double)M - (double)list.y) * list.mass) * a.inv_t;
         const double log_S = total == 0.0 ? 0.0 : log_of(S);
         kl += total * log_S;
         if (list.rest != 0.0) {
             // log probabilities in 32 bits leave about 1e-6 of their own: nothing, where there is no token for it
             if (none) kl = list.rest <= 1e-5 ? kl - list.rest * (log(list.rest) + log_S) : INFINITY;
-            else kl -= list.rest * (log_of(s) + ((double)m - (double)M) * (double)a.inv_t);
+            else kl -= list.rest * (log_of(s) + ((double)m - (double)M) * a.inv_t);
         }
         if (empty) kl = list.mass > 0.0 || list.rest > 1e-5 ? INFINITY : 0.0;
         const double ce = !labelled ? 0.0 : empty ? INFINITY : log_of(S1) - ((double)list.x_label - (double)M);
@@ -956,7 +957,7 @@ int flexmoe_distill(const flexmoe_distill_desc* desc, int32_t rows, const void* 
     a.P = row_parts(rows, desc->V, unit_run(desc->dtype), kWanted);
     a.length = part_length(desc->V, a.P, unit_run(desc->dtype));
     a.two = labels && desc->temperature != 1.f;
-    a.t = desc->temperature, a.inv_t = (float)(1.0 / desc->temperature), a.c = (float)(1.4426950408889634 / desc->temperature);
+    a.t = desc->temperature, a.inv_t = 1.0 / desc->temperature, a.c = (float)(1.4426950408889634 / desc->temperature);
     a.kl_weight = desc->kl_weight, a.ce_weight = desc->ce_weight;
     const bool bf16 = desc->dtype == FLEXMOE_BF16;
     const size_t es = bf16 ? 2 : 4;
