@@ -60,6 +60,7 @@ struct RouteArgs {
     size_t ldl;
     int T, E, k, bf16, sigmoid, normalize, groups, top_groups, best;
     int counted, chunk;  // tokens of a histogram, and of a workgroup of the tables (a multiple)
+    int first;           // histogram of a launch's first workgroup
     int words;
     float scale;
 };
@@ -443,13 +444,13 @@ __global__ __launch_bounds__(kThreads) void route_kernel(const RouteArgs a) {
     if (threadIdx.x < kMaxExperts) hist[threadIdx.x] = 0;
     __syncthreads();
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int t0 = blockIdx.x * a.counted, t1 = min(a.T, t0 + a.counted);
+    const int block = a.first + blockIdx.x, t0 = block * a.counted, t1 = min(a.T, t0 + a.counted);
     route_range<NQ, kBy, kGroups>(a, t0 + wave, t1, kWaves, lane, rs[wave], hist);
     if (!a.hist) return;
     __syncthreads();
     const int e = 4 * threadIdx.x;
     if ((int)threadIdx.x < a.words)
-        a.hist[(size_t)blockIdx.x * a.words + threadIdx.x] =
+        a.hist[(size_t)block * a.words + threadIdx.x] =
             (uint32_t)hist[e] | (uint32_t)hist[e + 1] << 8 | (uint32_t)hist[e + 2] << 16 | (uint32_t)hist[e + 3] << 24;
 }
 
@@ -603,7 +604,14 @@ hipError_t launch_route(const RouteArgs& a, bool tables, hipStream_t s) {
         route_tables_kernel<true, NQ, kBy, kGroups><<<1, kThreads, 0, s>>>(a);
         return hipGetLastError();
     }
-    route_kernel<NQ, kBy, kGroups><<<(a.T + a.counted - 1) / a.counted, kThreads, 0, s>>>(a);
+    RouteArgs b = a;
+    constexpr int kSlice = 1 << 21;  // a launch's threads are fewer than 2^32
+    const int blocks = (a.T + a.counted - 1) / a.counted;
+    for (b.first = 0; b.first < blocks; b.first += kSlice) {
+        route_kernel<NQ, kBy, kGroups><<<std::min(kSlice, blocks - b.first), kThreads, 0, s>>>(b);
+        const hipError_t err = hipGetLastError();
+        if (err != hipSuccess) return err;
+    }
     if (tables) route_tables_kernel<false, 1, 0, false><<<(a.T + a.chunk - 1) / a.chunk, kThreads, 0, s>>>(a);
     return hipGetLastError();
 }
@@ -772,7 +780,7 @@ int flexmoe_route(const flexmoe_router_desc* desc, int32_t T, const void* logits
     RouteArgs a;
     a.logits = logits, a.bias = bias, a.idx = out->topk_idx, a.w = out->topk_w;
     a.counts = out->counts, a.offsets = out->offsets, a.perm = out->perm, a.pos = out->pos;
-    a.hist = nullptr, a.ldl = (size_t)ldl;
+    a.hist = nullptr, a.ldl = (size_t)ldl, a.first = 0;
     a.T = T, a.E = desc->E, a.k = desc->top_k, a.bf16 = desc->dtype == FLEXMOE_BF16;
     a.sigmoid = desc->score == FLEXMOE_SIGMOID, a.normalize = desc->normalize;
     a.groups = desc->groups, a.top_groups = desc->top_groups, a.best = desc->group_best, a.scale = desc->scale;
