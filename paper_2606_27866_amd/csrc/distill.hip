@@ -29,7 +29,7 @@
 //
 // Bound by memory where rows are many: 4096 x 131072 bf16, 64 listed, 430 us, 5.0 TB/s
 // (418 of them whole rows, 16 the lists, whose 64-bit logarithms are bound by instructions
-// and their tokens' logits by latency); with tail, labels and t = 2 486, 20 % padding 402. 1021 x
+// and their tokens' logits by latency); with tail, labels and t = 2 482, 20 % padding 402. 1021 x
 // 50001 fp32 with tail, labels and 20 % padding 121 us, 3.0 TB/s: three or four rows a workgroup, all
 // in step, and four exponentials a value, whose instructions take half the time.
 // Losses alone of 48 x 131072: 8 us.
@@ -47,7 +47,8 @@ namespace {
 // What a row's list gives: sums over its tokens (see above), what it leaves, the label.
 struct RowList {
     double a, b, mass, rest;
-    float y, x_label;
+    float y, e, e1;  // with a tail: sums of 2^(c (x - y)) and 2^(log2(e) (x - y)); 0 where all x are -inf
+    float x_label;
     int label;  // -1: none
     int pad;
 };
@@ -242,7 +243,7 @@ __device__ __forceinline__ void list_row(const DistillArgs& a, size_t row, int* 
     }
     mass = wave_total_d(mass);
     RowList out;
-    out.rest = 0.0;
+    out.rest = 0.0, out.e = out.e1 = 0.f;
     double rest_log = 0.0;
     if (a.tail) {
         out.rest = mass != mass ? mass : fmax(0.0, 1.0 - mass);
@@ -263,6 +264,17 @@ __device__ __forceinline__ void list_row(const DistillArgs& a, size_t row, int* 
         if (id[q] >= 0) y = fmaxf(y, x[q]);
     y = wave_max(y);
     if (!(fabsf(y) < INFINITY)) y = 0.f;
+    if (a.tail) {  // NaN for one of NaN or +inf
+        float e = 0.f, e1 = 0.f;
+#pragma unroll
+        for (int q = 0; q < kOwn; ++q)
+            if (id[q] >= 0 && x[q] != -INFINITY) {
+                const float d = __builtin_isinf(x[q]) ? NAN : x[q] - y;
+                e += exp2_fast(d * a.c);
+                e1 += exp2_fast(d * kLog2E);
+            }
+        out.e = wave_total_f(e), out.e1 = wave_total_f(e1);
+    }
     Mark* const marks = a.marks + row * (K + 1);
 #pragma unroll
     for (int q = 0; q < kOwn; ++q) {
@@ -362,27 +374,31 @@ __device__ __forceinline__ double log_of(float s) {
     return (double)e * 0.6931471805599453 + (double)logf(f);
 }
 
+// e^x for x <= 0 to about 2^-32 of itself (an error here is one of all that lies on one side of a gap): its power of two,
+// and the exponential series up to u^8 / 8! for what is left, |u| <= 0.35; 0 below 2^-200.
+__device__ __forceinline__ double exp_down(double x) {
+    const double z = fmax(x * 1.4426950408889634, -200.0), whole = rint(z), u = (z - whole) * 0.6931471805599453;
+    double e = 1.0 / 40320;
+    for (double c : {1.0 / 5040, 1.0 / 720, 1.0 / 120, 1.0 / 24, 1.0 / 6, 0.5, 1.0, 1.0}) e = fma(e, u, c);
+    return x > -138.0 ? ldexp(e, (int)whole) : 0.0;
+}
+
 // One wave joins a row's maximum and sums (with a tail: without the listed tokens) with
 // its list and marks.  All lanes return the same; lane 0 writes the losses if `writes`.
 __device__ __forceinline__ RowFactors end_row(const DistillArgs& a, size_t row, const RowList& list, const Mark* marks, float m, float s, float s1,
                                               float scale, bool writes) {
     const int lane = threadIdx.x & 63;
-    float M = m, S = s, S1 = a.two ? s1 : s, down = 1.f, down1 = 1.f;  // down: e^((m - M) / t)
-    if (a.tail) {
-        for (int k = lane; k < a.K; k += 64)
-            if (marks[k].id >= 0) M = fmaxf(M, marks[k].x);
-        M = wave_max(M);
-        float e = 0.f, e1 = 0.f;
-        for (int k = lane; k < a.K; k += 64) {
-            const Mark mark = marks[k];
-            if (mark.id < 0 || mark.x == -INFINITY) continue;
-            e += exp2_fast((mark.x - M) * a.c);
-            e1 += exp2_fast((mark.x - M) * kLog2E);
+    float M = m, S = s, S1 = a.two ? s1 : s;
+    double down = 1.0, down1 = 1.0;  // e^((m - M) / t), e^(m - M)
+    if (a.tail && list.e != 0.f) {
+        const double gap = m == -INFINITY ? -INFINITY : -fabs((double)m - (double)list.y);
+        const double far = exp_down(gap * a.inv_t), far1 = a.two ? exp_down(gap) : far;
+        if (m >= list.y) {
+            S = (float)(s + far * list.e), S1 = a.two ? (float)(s1 + far1 * list.e1) : S;
+        } else {
+            M = list.y, down = far, down1 = far1;
+            S = (float)(far * s + list.e), S1 = a.two ? (float)(far1 * s1 + list.e1) : S;
         }
-        down = m == -INFINITY ? 0.f : exp2_fast((m - M) * a.c);
-        down1 = !a.two ? down : m == -INFINITY ? 0.f : exp2_fast((m - M) * kLog2E);
-        S = S * down + wave_total_f(e);
-        S1 = a.two ? S1 * down1 + wave_total_f(e1) : S;
     }
     const bool empty = M == -INFINITY && S == 0.f && list.b == list.b, labelled = list.label >= 0;
     const bool none = s == 0.f && S == S;  // no token off the list has a probability
@@ -405,13 +421,13 @@ __device__ __forceinline__ RowFactors end_row(const DistillArgs& a, size_t row, 
     }
     // s is at least about 1: neither quotient leaves fp32's range
     double dense = total;
-    if (a.tail) dense = total * (double)down - (list.rest != 0.0 ? list.rest * ((double)S / (double)s) : 0.0);
+    if (a.tail) dense = total * down - (list.rest != 0.0 ? list.rest * ((double)S / (double)s) : 0.0);
     const float by_kl = scale * a.kl_weight * a.t, by_ce = labelled ? scale * a.ce_weight : 0.f;
     const bool no_dense = empty || (a.tail && none);
     RowFactors o;
     o.m = m;
     o.f = no_dense ? 0.f : by_kl * (float)dense / S;
-    o.f1 = no_dense ? 0.f : by_ce * down1 / S1;
+    o.f1 = no_dense ? 0.f : by_ce * (float)down1 / S1;
     o.M = M;
     o.listed = empty ? 0.f : by_kl * (float)total / S;
     o.listed1 = empty ? 0.f : by_ce / S1;

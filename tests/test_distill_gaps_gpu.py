@@ -184,3 +184,25 @@ def test_gradient_against_differences():
             loss.append(float(h.forward(y, ids, lp)[0].double()) * t * t)
         # third derivative of t^2 KL: below 1 / t; roundings of the loss over 2 step
         assert abs((loss[0] - loss[1]) / (2 * step) - float(d[0, v])) <= step ** 2 / 6 / t + 2 * t * t * 40 * U * 30 / (2 * step)
+
+
+@pytest.mark.parametrize("t", [0.7, 1.0, 2.0, 0.03])
+def test_the_join_across_a_gap_keeps_small_divergences(t):
+    """All others are 0, so that their sum is exact, and one listed token has about as much as they together: KL, a few hundredths at most, is off by
+    the rounding of S (u), the logarithms of S and s (half a step of up to 0.35 each, u / 2 together) and its own, within 3 u."""
+    t, rows, V = float(np.float32(t)), 48, 1 << 20
+    g = torch.Generator(device="cuda")
+    g.manual_seed(9)
+    x = torch.zeros(rows, V, device="cuda")
+    x[:, 77] = (math.log(V) + torch.empty(rows, device="cuda").uniform_(-0.3, 0.3, generator=g)) * t
+    ids = torch.full((rows, 1), 77, dtype=torch.int32, device="cuda")
+    lp = torch.log(torch.empty(rows, 1, device="cuda").uniform_(0.45, 0.55, generator=g))
+    h = fm.Distillation(V, 1, rows, temperature=t, tail=True)
+    p, others = lp.double().exp(), math.log(V - 1)
+    top = x[:, 77:78].double() / t
+    log_s = torch.logaddexp(top, torch.full_like(top, others))
+    want = (p * (lp.double() - (top - log_s)) + (1 - p) * (torch.log1p(-p) - (others - log_s))).squeeze(1)
+    for kl in (h.forward(x, ids, lp)[0], h.gradient(x, ids, lp)[0]):
+        assert bool((want < 0.1).all())
+        off = (kl.double() - want).abs() / U
+        assert bool((off <= 3).all()), float(off.max())
