@@ -1348,11 +1348,11 @@ class Layer:
         if dbg is not None or bucketed is not None:
             raise ValueError("routing goes with neither dbg nor bucketed")
         n = T * D.top_k
+        _vector(x, T * D.d, self.tdtype, "x")  # rows of another type may be shorter than what is read
         idx, w = _vector(routing.topk_idx, n, torch.int32, "topk_idx"), _vector(routing.topk_w, n, torch.float32, "topk_w")
         if y is None:
             y = _new((T, D.d), self.tdtype, self.device, stream)
-        _packed(x, T * D.d, "x")
-        _packed(y, T * D.d, "y")
+        _vector(y, T * D.d, self.tdtype, "y")
         if clipped is None:
             weights, packed = (self.w_gate, self.w_up, self.w_down, self.keep if keep is None else keep), -1
         else:
