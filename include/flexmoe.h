@@ -620,7 +620,9 @@ int flexmoe_route_backward(const flexmoe_router_desc *desc, int32_t T, const voi
  * holds parts of dw; one for max_rows serves every call.
  * Shapes (FLEXMOE_ESHAPE otherwise): cols from 1 to 2^21; strides (elements, 0 =
  * packed) at least cols, at most 2^21 and whole 16-byte units, as for the
- * grouped products; 0 <= rows <= max_rows <= 2^30.  eps from 1e-30 to 1.
+ * grouped products; rows and w start on 16-byte boundaries and may be read up to
+ * the unit that their last element lies in; 0 <= rows <= max_rows <= 2^30.  eps
+ * from 1e-30 to 1.
  * rows = 0 is a no-op; the backward then writes a dw of zeros. */
 typedef struct flexmoe_norm_desc {
     int32_t cols;
@@ -695,7 +697,9 @@ int flexmoe_token_logprobs(const flexmoe_logprob_desc *desc, int32_t rows, const
  * label is on one, or where the teacher leaves more than 1e-5 and no token but
  * the listed ones has a probability.  Rows with a NaN or +inf give NaN; a row of
  * nothing but -inf gets gradients of 0.  Deterministic.
- * The listed tokens' logarithms and p are in 64 bits, sums over V in fp32.
+ * The listed tokens' logarithms and p are in 64 bits, sums over V in fp32, with a
+ * tail those of the other tokens against their own largest: finite logits may lie
+ * any distance apart.
  * dlogits may be logits itself (with ldd = ld).  Shapes (FLEXMOE_ESHAPE
  * otherwise): 1 <= V <= 2^21, 1 <= top <= 128; ld and ldd as
  * flexmoe_token_logprobs' ld; nothing past V is written; 0 <= rows <= max_rows <=

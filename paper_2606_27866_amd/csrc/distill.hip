@@ -28,9 +28,9 @@
 //                         row, then the listed tokens (distill_row_kernel: losses alone)
 //
 // Bound by memory where rows are many: 4096 x 131072 bf16, 64 listed, 430 us, 5.0 TB/s
-// (418 of them whole rows, 16 the lists, whose 64-bit logarithms are bound by instructions
+// (414 of them whole rows, 16 the lists, whose 64-bit logarithms are bound by instructions
 // and their tokens' logits by latency); with tail, labels and t = 2 482, 20 % padding 402. 1021 x
-// 50001 fp32 with tail, labels and 20 % padding 121 us, 3.0 TB/s: three or four rows a workgroup, all
+// 50001 fp32 with tail, labels and 20 % padding 120 us, 3.0 TB/s: three or four rows a workgroup, all
 // in step, and four exponentials a value, whose instructions take half the time.
 // Losses alone of 48 x 131072: 8 us.
 #include <algorithm>
@@ -606,7 +606,8 @@ __device__ __forceinline__ T load_scalar(const T* p) {
 // last one, so that only it may be ragged.  A thread knows the marked tokens of its own
 // units from a list in LDS (which is in no order, and need not be); the first of them is
 // in registers.
-// kHeld units a thread: 32 leave registers for two waves of a SIMD, 16 for three.  kLag: what comes sooner is waited for,
+// kHeld units a thread: 32 leave registers for two waves of a SIMD (207 to 216 of 256 are in use, and 145 to 193 scalar ones are
+// spilled to lanes of vector registers), 16 for three.  kLag: what comes sooner is waited for,
 // what comes later is summed when no store is left to hide it (4096 x 131072 bf16, with tail, labels and a temperature
 // 485, 483, 489, 499 and 537 us with 4, 6, 8, 12 and 16; plain 430, 427, 429, 431, 436).
 constexpr int waves_of(int held) { return held > 16 ? 2 : 3; }

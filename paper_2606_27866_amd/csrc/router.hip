@@ -26,7 +26,7 @@
 // taken in 32 bits: where the chosen ones and the best of the others (groups too)
 // are further apart than those can be wrong, the order is the exact one, and only
 // the other tokens (1 in 1000 of usual logits) are routed again in 64 bits.
-// One token of 64 experts 4.9 us; 8191 tokens of 256 experts in groups 17.1 us and 8.3
+// One token of 64 experts 4.7 us; 8191 tokens of 256 experts in groups 16.6 us and 8.2
 // for the tables (all in 64 bits 82 together); 65536 of 60 experts 38 us.
 #include <algorithm>
 #include <cmath>
@@ -41,7 +41,8 @@ namespace {
 
 constexpr int kWaves = 16, kThreads = 64 * kWaves;
 // Chunks of tokens, at most: workgroups of route_tables_kernel, which read all histograms.  8191 tokens of 256 experts in
-// groups 30.7, 24.6, 24.6 and 28.6 us with 32, 64, 128 and 256; 65536 tokens of 60 experts 69.7, 65.0, 62.8 and 61.4.
+// groups, all of a call, 30.3, 29.1, 29.1 and 29.2 us with 32, 64, 128 and 256; 65536 tokens of 60 experts 44.9, 40.1, 37.8 and
+// 36.9, of 256 experts with 64, 128 and 256 68.4, 63.9 and 62.5.
 constexpr int kChunks = 128;
 // Tokens of a workgroup of route_kernel, at most; their counts are bytes.
 constexpr int kMostCounted = 128;
@@ -731,8 +732,8 @@ int check_router(const flexmoe_router_desc* D, int T, const char* who, long long
 }
 
 // Workgroups of route_kernel, a histogram each: one a compute unit (tables read fewer of them), past its tokens two, in
-// whole rounds.  8192 tokens of 60 experts 14.4 us with 256, 15.9 with 512; 65536 63.3 and 40.8, with 768 and 1024 50.3
-// and 48.3; 131072 98 with 547, 79 with 1024.
+// whole rounds.  8192 tokens of 60 experts 14.2 us with 256, 15.6 with 512; 65536 37.8 with 512, 47.3 and 45.2 with 768 and
+// 1024; 131072 98 with 547, 79 with 1024 (of an earlier form of the kernel).
 int histograms(int T) { return T <= 256 * kMostCounted ? 256 : (int)(((long long)T + 512 * kMostCounted - 1) / (512 * kMostCounted)) * 512; }
 
 // Tokens of a histogram (a multiple of a workgroup's waves) and of a chunk.
